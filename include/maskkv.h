@@ -20,6 +20,10 @@
  *   maskkv_layer_importance, maskkv_layer_budgets   Stage 2, layer level: I^(l) = 1 - mean
  *                   cosine similarity of the attention sub-layer's input and output states, and
  *                   the boundary-aware split of the total budget over the layers.
+ *   maskkv_compact_mx, maskkv_expand_mx, maskkv_attend_mx   the cache in 4 bits: eviction that stores the kept
+ *                   rows so, the values that they stand for, and the attention that reads them.
+ *   maskkv_accumulate, maskkv_evict (and _mx)   further eviction from the cache: the attention that each cached row has
+ *                   got over the denoising steps, and the rows of each head that got most.
  *   maskkv_value_shift   Section 3.1 (feature-cache background): response tokens whose value
  *                   vector turned by more than a threshold between two denoising steps.
  *
@@ -241,6 +245,92 @@ int maskkv_attend_full(const maskkv_desc* desc, const maskkv_tensor* Q_resp,
                        const maskkv_tensor* K_full, const maskkv_tensor* V_full, float scale,
                        const maskkv_tensor* O, float* lse,
                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A cache in 4 bits (microscaling: one power of two for 32 neighbours along the head dimension).  All DEVICE, rows contiguous:
+ * codes [capacity, d/2] bytes, scales [capacity, d/32] bytes.  Byte i of a row's codes holds element 2i in its low and element
+ * 2i+1 in its high four bits: bit 3 is the sign, bits 0-2 number the sizes 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Scale byte s of a row
+ * belongs to its elements 32s .. 32s+31, which stand for size * 2^(byte - 127); 255: for NaN, all of them.  maskkv_compact_mx
+ * writes the bytes 3 .. 252 and 255 (above 252 the largest sizes would pass the range of fp32).
+ * Pointers are multiples of 16 bytes.  A row takes 17/64 of what it takes in bf16.
+ */
+typedef struct maskkv_mx_cache {
+  void* k_codes;
+  void* k_scales;
+  void* v_codes;
+  void* v_scales;
+} maskkv_mx_cache;
+
+/*
+ * Eviction as a gather into 4 bits: as maskkv_compact, but row r of the cache receives prompt row idx[r] of its head rounded to
+ * 4 bits.  Of 32 neighbours x the scale is the smallest 2^e with max |x| <= 6 * 2^e, -124 <= e <= 125, and every x becomes the
+ * nearest of the sizes times 2^e, a tie the one with the even number; what is beyond 6 * 2^125 becomes that.  32 neighbours with a NaN
+ * or an infinity among them stand for NaN.  The result does not depend on anything but the row: equal rows give equal bytes.
+ * Rows >= min(capacity, cu_budget[B*H]) are left untouched.
+ */
+int maskkv_compact_mx(const maskkv_desc* desc, const maskkv_tensor* K, const maskkv_tensor* V,
+                      const int32_t* idx, const int32_t* cu_budget, int64_t capacity,
+                      const maskkv_mx_cache* cache, void* stream);
+
+/*
+ * The values that a cache in 4 bits stands for, as packed rows Kc, Vc (DEVICE [capacity, d] in desc->dtype, exact in both
+ * dtypes): what maskkv_attend and maskkv_accumulate read.  Rows >= min(capacity, cu_budget[B*H]) are left untouched.
+ */
+int maskkv_expand_mx(const maskkv_desc* desc, const maskkv_mx_cache* cache, const int32_t* cu_budget, int64_t capacity,
+                     void* Kc, void* Vc, void* stream);
+
+/* Workspace (DEVICE bytes) for maskkv_attend_mx with this description and capacity: partial results where few query rows
+ * attend to many rows and the key axis is dealt to several workgroups; 0 where it is not.  256-byte alignment. */
+int maskkv_attend_mx_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes);
+
+/*
+ * maskkv_attend over a cache in 4 bits: the cached rows are the values that they stand for, the response rows K_resp/V_resp and the
+ * queries are in desc->dtype, and everything else is as there (fp32 accumulation, probabilities rounded to desc->dtype only as
+ * the operand of the P.V product, lse optional).  n_resp may be 1.
+ */
+int maskkv_attend_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const maskkv_mx_cache* cache,
+                     const int32_t* cu_budget, int64_t capacity, const maskkv_tensor* K_resp,
+                     const maskkv_tensor* V_resp, float scale, const maskkv_tensor* O, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The attention that each cached row gets, added up over the denoising steps.  For row r of the cache of (b, h):
+ *   weights_out[r] = decay * weights_in[r] + sum_i exp(q_i . k_r * scale - row_lse[i])
+ * over all g * n_resp query rows i of the head's group (numbered as in Q_resp: query head first, then query), with the natural-log
+ * normalisers that maskkv_attend or maskkv_attend_mx returned for the same queries, cache, response rows and scale
+ * (row_lse[(b*H + h)*g*n_resp + i]).  A query row whose row_lse is +infinity adds nothing.  Kc: DEVICE [capacity, d] in
+ * desc->dtype; weights: DEVICE float [capacity]; weights_in may be weights_out.  0 <= decay <= 1; with decay 0 weights_in is not
+ * read and may be NULL.  fp32 accumulation in a fixed order: equal calls give equal bits.  Rows >= min(capacity,
+ * cu_budget[B*H]) are left untouched.  _mx: the same over a cache in 4 bits, of which only the keys are read (v_codes and
+ * v_scales may be NULL).
+ */
+int maskkv_accumulate(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc, const int32_t* cu_budget,
+                      int64_t capacity, float scale, const float* row_lse, float decay, const float* weights_in,
+                      float* weights_out, void* stream);
+int maskkv_accumulate_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const maskkv_mx_cache* cache,
+                         const int32_t* cu_budget, int64_t capacity, float scale, const float* row_lse, float decay,
+                         const float* weights_in, float* weights_out, void* stream);
+
+/*
+ * Further eviction from the cache.  Of the n_h rows [cu_budget[bh], cu_budget[bh+1]) of every head (row numbers clipped to
+ * capacity) the min(max(budgets[bh], 0), n_h) with the largest weights stay, ties to the lower row (a NaN counts as less than
+ * every number, and -0 as 0), in their order:
+ *   rows[r']   = the packed row that row r' of the smaller cache was,  r' in [cu_out[bh], cu_out[bh+1])
+ *   Kc_out[r'] = Kc[rows[r']], and V, weights_out[r'] = weights[rows[r']] and idx_out[r'] = idx[rows[r']] likewise
+ *   cu_out     = exclusive prefix sum of the rows that stay, B*H+1 entries.
+ * rows, idx, idx_out: DEVICE int32 [capacity_out], [capacity], [capacity_out]; idx and idx_out (the rows' prompt positions)
+ * may both be NULL, and so may weights_out.  Where more than capacity_out rows stay, those beyond it are not written while
+ * cu_out holds the unclipped sums; sum_h budgets[bh] and capacity are always enough.  The smaller cache has buffers
+ * of its own: an output that overlaps an input is MASKKV_EINVAL.  rows is written and read by the call.  _mx: the same for a cache in 4
+ * bits, whose bytes are moved as they are.
+ */
+int maskkv_evict(const maskkv_desc* desc, const float* weights, const int32_t* cu_budget, int64_t capacity,
+                 const int32_t* budgets, const void* Kc, const void* Vc, const int32_t* idx, void* Kc_out, void* Vc_out,
+                 int32_t* idx_out, int32_t* rows, float* weights_out, int32_t* cu_out, int64_t capacity_out, void* stream);
+int maskkv_evict_mx(const maskkv_desc* desc, const float* weights, const int32_t* cu_budget, int64_t capacity,
+                    const int32_t* budgets, const maskkv_mx_cache* cache, const int32_t* idx,
+                    const maskkv_mx_cache* cache_out, int32_t* idx_out, int32_t* rows, float* weights_out,
+                    int32_t* cu_out, int64_t capacity_out, void* stream);
 
 /*
  * Stage 2, head level, on the device.  For every b:

@@ -29,6 +29,8 @@ SYMBOLS = [
     "maskkv_select_workspace_bytes", "maskkv_select",
     "maskkv_compact",
     "maskkv_attend_workspace_bytes", "maskkv_attend", "maskkv_attend_full",
+    "maskkv_compact_mx", "maskkv_expand_mx", "maskkv_attend_mx_workspace_bytes", "maskkv_attend_mx",
+    "maskkv_accumulate", "maskkv_accumulate_mx", "maskkv_evict", "maskkv_evict_mx",
     "maskkv_head_budgets",
     "maskkv_layer_importance_workspace_bytes", "maskkv_layer_importance", "maskkv_layer_budgets",
     "maskkv_value_shift",
@@ -102,6 +104,21 @@ class Desc:
             c._keep = arr
             c.prompt_len = ct.cast(arr, ct.POINTER(ct.c_int32))
         return c
+
+
+@dataclass
+class MxCache:
+    """Python mirror of maskkv_mx_cache: uint8 device tensors, codes [capacity, d/2] and scales [capacity, d/32]."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: Optional[torch.Tensor] = None    # (maskkv_accumulate_mx reads the keys only)
+    v_scales: Optional[torch.Tensor] = None
+
+    @classmethod
+    def empty(cls, capacity: int, d: int, device="cuda") -> "MxCache":
+        """Uninitialised room for `capacity` rows of head_dim d."""
+        room = lambda width: torch.empty((capacity, width), dtype=torch.uint8, device=device)
+        return cls(room(d // 2), room(d // 32), room(d // 2), room(d // 32))
 
 
 def tensor_view(t: torch.Tensor, seq_start: Optional[Sequence[int]] = None) -> _CTensor:
@@ -216,6 +233,74 @@ def maskkv_attend_full(desc: Desc, Q_resp, K_full, V_full, scale: float, O, lse:
     status = _native.attend_full(desc, Q_resp, K_full, V_full, scale, O, lse, workspace, stream)
     if status:
         _check(status, "maskkv_attend_full")
+
+
+def maskkv_compact_mx(desc: Desc, K, V, idx: torch.Tensor, cu_budget: torch.Tensor, capacity: int, cache: MxCache,
+                      stream=None) -> None:
+    """maskkv_compact into a cache in 4 bits."""
+    status = _native.compact_mx(desc, K, V, idx, cu_budget, capacity, cache, stream)
+    if status:
+        _check(status, "maskkv_compact_mx")
+
+
+def maskkv_expand_mx(desc: Desc, cache: MxCache, cu_budget: torch.Tensor, capacity: int, Kc: torch.Tensor, Vc: torch.Tensor,
+                     stream=None) -> None:
+    """The values that a cache in 4 bits stands for, as packed rows in the description's dtype."""
+    status = _native.expand_mx(desc, cache, cu_budget, capacity, Kc, Vc, stream)
+    if status:
+        _check(status, "maskkv_expand_mx")
+
+
+def maskkv_attend_mx_workspace_bytes(desc: Desc, capacity: int) -> int:
+    return _size(_native.attend_mx_ws(desc, capacity), "maskkv_attend_mx_workspace_bytes")
+
+
+def maskkv_attend_mx(desc: Desc, Q_resp, cache: MxCache, cu_budget: torch.Tensor, capacity: int, K_resp, V_resp, scale: float,
+                     O, lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None) -> None:
+    """maskkv_attend over a cache in 4 bits."""
+    status = _native.attend_mx(desc, Q_resp, cache, cu_budget, capacity, K_resp, V_resp, scale, O, lse, workspace, stream)
+    if status:
+        _check(status, "maskkv_attend_mx")
+
+
+def maskkv_accumulate(desc: Desc, Q_resp, Kc: torch.Tensor, cu_budget: torch.Tensor, capacity: int, scale: float,
+                      row_lse: torch.Tensor, decay: float, weights_in: Optional[torch.Tensor], weights_out: torch.Tensor,
+                      stream=None) -> None:
+    """decay * weights_in + the attention that each cached row gets; weights_in may be weights_out, or None with decay 0."""
+    status = _native.accumulate(desc, Q_resp, Kc, cu_budget, capacity, scale, row_lse, decay, weights_in, weights_out, stream)
+    if status:
+        _check(status, "maskkv_accumulate")
+
+
+def maskkv_accumulate_mx(desc: Desc, Q_resp, cache: MxCache, cu_budget: torch.Tensor, capacity: int, scale: float,
+                         row_lse: torch.Tensor, decay: float, weights_in: Optional[torch.Tensor], weights_out: torch.Tensor,
+                         stream=None) -> None:
+    """maskkv_accumulate over the keys of a cache in 4 bits."""
+    status = _native.accumulate_mx(desc, Q_resp, cache, cu_budget, capacity, scale, row_lse, decay, weights_in, weights_out, stream)
+    if status:
+        _check(status, "maskkv_accumulate_mx")
+
+
+def maskkv_evict(desc: Desc, weights: torch.Tensor, cu_budget: torch.Tensor, capacity: int, budgets: torch.Tensor,
+                 Kc: torch.Tensor, Vc: torch.Tensor, idx: Optional[torch.Tensor], Kc_out: torch.Tensor, Vc_out: torch.Tensor,
+                 idx_out: Optional[torch.Tensor], rows: torch.Tensor, weights_out: Optional[torch.Tensor],
+                 cu_out: torch.Tensor, capacity_out: int, stream=None) -> None:
+    """The rows of largest weight of every head, into a smaller cache; idx and idx_out (prompt positions) go together or are None."""
+    status = _native.evict(desc, weights, cu_budget, capacity, budgets, Kc, Vc, idx, Kc_out, Vc_out, idx_out, rows, weights_out,
+                           cu_out, capacity_out, stream)
+    if status:
+        _check(status, "maskkv_evict")
+
+
+def maskkv_evict_mx(desc: Desc, weights: torch.Tensor, cu_budget: torch.Tensor, capacity: int, budgets: torch.Tensor,
+                    cache: MxCache, idx: Optional[torch.Tensor], cache_out: MxCache, idx_out: Optional[torch.Tensor],
+                    rows: torch.Tensor, weights_out: Optional[torch.Tensor], cu_out: torch.Tensor, capacity_out: int,
+                    stream=None) -> None:
+    """maskkv_evict of a cache in 4 bits."""
+    status = _native.evict_mx(desc, weights, cu_budget, capacity, budgets, cache, idx, cache_out, idx_out, rows, weights_out,
+                              cu_out, capacity_out, stream)
+    if status:
+        _check(status, "maskkv_evict_mx")
 
 
 def maskkv_head_budgets(desc: Desc, prompt_mass: torch.Tensor, k_l: int, alpha: float, budgets: torch.Tensor,

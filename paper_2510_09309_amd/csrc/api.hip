@@ -123,6 +123,43 @@ int check_workspace(const char* what, void* ws, size_t have, size_t need) {
   return MASKKV_OK;
 }
 
+// A packed array of `rows` rows: its pointer is there (unless there are no rows) and a multiple of 16 bytes.
+int check_packed(const char* what, const char* name, const void* p, int64_t rows) {
+  if (rows > 0 && !p) {
+    set_error("%s: %s is NULL", what, name);
+    return MASKKV_EINVAL;
+  }
+  if ((uintptr_t)p & 15) {
+    set_error("%s: %s must be 16-byte aligned", what, name);
+    return MASKKV_EINVAL;
+  }
+  return MASKKV_OK;
+}
+
+int check_capacity(const char* what, const char* name, int64_t capacity) {
+  if (capacity >= 0 && capacity <= 0x7FFFFFFF) return MASKKV_OK;
+  set_error("%s: %s %lld outside 0..2^31-1", what, name, (long long)capacity);
+  return MASKKV_EINVAL;
+}
+
+int check_mx(const char* what, const char* name, const maskkv_mx_cache* c, int64_t rows, bool keys_only, MxCache* out) {
+  *out = MxCache{};
+  if (!c) {
+    set_error("%s: %s is NULL", what, name);
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_packed(what, "k_codes", c->k_codes, rows)) return e;
+  if (int e = check_packed(what, "k_scales", c->k_scales, rows)) return e;
+  out->k_codes = reinterpret_cast<char*>(c->k_codes);
+  out->k_scales = reinterpret_cast<char*>(c->k_scales);
+  if (keys_only) return MASKKV_OK;
+  if (int e = check_packed(what, "v_codes", c->v_codes, rows)) return e;
+  if (int e = check_packed(what, "v_scales", c->v_scales, rows)) return e;
+  out->v_codes = reinterpret_cast<char*>(c->v_codes);
+  out->v_scales = reinterpret_cast<char*>(c->v_scales);
+  return MASKKV_OK;
+}
+
 float pick_scale(const maskkv_desc* d, float scale) { return scale > 0.f ? scale : 1.0f / sqrtf((float)d->d); }
 
 // ---- static scratch of maskkv_score_static: one copy per GPU for the life of the process
@@ -416,6 +453,180 @@ int maskkv_attend_full(const maskkv_desc* desc, const maskkv_tensor* Q_resp, con
   if (int e = check_workspace("attend_full", workspace, workspace_bytes, attend_workspace_bytes(desc, true))) return e;
   return launch_attend(desc, lens, true, q, nullptr, nullptr, nullptr, 0, k2, v2, pick_scale(desc, scale), o, lse,
                        workspace, reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_compact_mx(const maskkv_desc* desc, const maskkv_tensor* K, const maskkv_tensor* V, const int32_t* idx,
+                      const int32_t* cu_budget, int64_t capacity, const maskkv_mx_cache* cache, void* stream) {
+  Lens lens;
+  View k, v;
+  MxCache mx;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = make_view(desc, K, "K", &k)) return e;
+  if (int e = make_view(desc, V, "V", &v)) return e;
+  if (int e = check_capacity("compact_mx", "capacity", capacity)) return e;
+  if (!cu_budget || (capacity > 0 && !idx)) {
+    set_error("compact_mx: cu_budget or idx is NULL");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_mx("compact_mx", "cache", cache, capacity, false, &mx)) return e;
+  return launch_compact_mx(desc, lens, k, v, idx, cu_budget, capacity, mx, reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_expand_mx(const maskkv_desc* desc, const maskkv_mx_cache* cache, const int32_t* cu_budget, int64_t capacity,
+                     void* Kc, void* Vc, void* stream) {
+  Lens lens;
+  MxCache mx;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("expand_mx", "capacity", capacity)) return e;
+  if (!cu_budget) {
+    set_error("expand_mx: cu_budget is NULL");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_mx("expand_mx", "cache", cache, capacity, false, &mx)) return e;
+  if (int e = check_packed("expand_mx", "Kc", Kc, capacity)) return e;
+  if (int e = check_packed("expand_mx", "Vc", Vc, capacity)) return e;
+  return launch_expand_mx(desc, mx, cu_budget, capacity, Kc, Vc, reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_attend_mx_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes) {
+  Lens lens;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("attend_mx", "capacity", capacity)) return e;
+  if (!bytes) {
+    set_error("bytes is NULL");
+    return MASKKV_EINVAL;
+  }
+  *bytes = attend_mx_workspace_bytes(desc, capacity);
+  return MASKKV_OK;
+}
+
+int maskkv_attend_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const maskkv_mx_cache* cache,
+                     const int32_t* cu_budget, int64_t capacity, const maskkv_tensor* K_resp, const maskkv_tensor* V_resp,
+                     float scale, const maskkv_tensor* O, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  Lens lens;
+  View q, k2, v2, o;
+  MxCache mx;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = make_view(desc, Q_resp, "Q_resp", &q)) return e;
+  if (int e = make_view(desc, K_resp, "K_resp", &k2)) return e;
+  if (int e = make_view(desc, V_resp, "V_resp", &v2)) return e;
+  if (int e = make_view(desc, O, "O", &o)) return e;
+  if (int e = check_capacity("attend_mx", "capacity", capacity)) return e;
+  if (!cu_budget) {
+    set_error("attend_mx: cu_budget is NULL");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_mx("attend_mx", "cache", cache, capacity, false, &mx)) return e;
+  if (int e = check_workspace("attend_mx", workspace, workspace_bytes, attend_mx_workspace_bytes(desc, capacity))) return e;
+  return launch_attend_mx(desc, q, mx, cu_budget, capacity, k2, v2, pick_scale(desc, scale), o, lse, workspace,
+                          reinterpret_cast<hipStream_t>(stream));
+}
+
+// Both forms of maskkv_accumulate: over Kc, or over the keys of `cache`.
+static int accumulate_entry(const char* what, const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc,
+                            const maskkv_mx_cache* cache, bool mx, const int32_t* cu_budget, int64_t capacity, float scale,
+                            const float* row_lse, float decay, const float* weights_in, float* weights_out, void* stream) {
+  Lens lens;
+  View q;
+  MxCache keys{};
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = make_view(desc, Q_resp, "Q_resp", &q)) return e;
+  if (int e = check_capacity(what, "capacity", capacity)) return e;
+  if (int e = mx ? check_mx(what, "cache", cache, capacity, true, &keys) : check_packed(what, "Kc", Kc, capacity)) return e;
+  if (!(decay >= 0.f && decay <= 1.f)) {
+    set_error("%s: decay %g outside [0, 1]", what, (double)decay);
+    return MASKKV_EINVAL;
+  }
+  if (!cu_budget || !row_lse || (capacity > 0 && (!weights_out || (decay > 0.f && !weights_in)))) {
+    set_error("%s: cu_budget, row_lse, weights_out or (with a decay above 0) weights_in is NULL", what);
+    return MASKKV_EINVAL;
+  }
+  return launch_accumulate(desc, q, mx ? nullptr : Kc, keys, cu_budget, capacity, pick_scale(desc, scale), row_lse, decay,
+                           weights_in, weights_out, reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_accumulate(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc, const int32_t* cu_budget,
+                      int64_t capacity, float scale, const float* row_lse, float decay, const float* weights_in,
+                      float* weights_out, void* stream) {
+  return accumulate_entry("accumulate", desc, Q_resp, Kc, nullptr, false, cu_budget, capacity, scale, row_lse, decay,
+                          weights_in, weights_out, stream);
+}
+
+int maskkv_accumulate_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const maskkv_mx_cache* cache,
+                         const int32_t* cu_budget, int64_t capacity, float scale, const float* row_lse, float decay,
+                         const float* weights_in, float* weights_out, void* stream) {
+  return accumulate_entry("accumulate_mx", desc, Q_resp, nullptr, cache, true, cu_budget, capacity, scale, row_lse, decay,
+                          weights_in, weights_out, stream);
+}
+
+// Both forms of maskkv_evict; `moved` says which rows move with the ones that stay.
+static int evict_entry(const char* what, const maskkv_desc* desc, const float* weights, const int32_t* cu_budget,
+                       int64_t capacity, const int32_t* budgets, const MovedRows& moved, const int32_t* idx, int32_t* idx_out,
+                       int32_t* rows, float* weights_out, int32_t* cu_out, int64_t capacity_out, void* stream) {
+  if (!cu_budget || !budgets || !cu_out || (capacity > 0 && !weights) || (capacity_out > 0 && !rows) || !idx != !idx_out) {
+    set_error("%s: cu_budget, budgets, cu_out, weights or rows is NULL, or only one of idx and idx_out is", what);
+    return MASKKV_EINVAL;
+  }
+  const int64_t heads = (int64_t)desc->B * desc->H;
+  struct Span {
+    const void* p;
+    int64_t bytes;
+  };
+  Span in[kMoved + 4] = {{weights, capacity * 4}, {idx, capacity * 4}, {cu_budget, (heads + 1) * 4}, {budgets, heads * 4}};
+  Span out[kMoved + 4] = {{weights_out, capacity_out * 4}, {idx_out, capacity_out * 4}, {rows, capacity_out * 4},
+                          {cu_out, (heads + 1) * 4}};
+  for (int i = 0; i < kMoved; ++i) {
+    in[4 + i] = {moved.from[i], moved.bytes[i] * capacity};
+    out[4 + i] = {moved.to[i], moved.bytes[i] * capacity_out};
+  }
+  auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && a.bytes > 0 && b.bytes > 0 && x < y + (uint64_t)b.bytes && y < x + (uint64_t)a.bytes;
+  };
+  for (int o = 0; o < kMoved + 4; ++o) {
+    for (int i = 0; i < kMoved + 4; ++i)
+      if (meet(out[o], in[i]) || (i < o && meet(out[o], out[i]))) {
+        set_error("%s: an output overlaps an input or another output (the smaller cache needs buffers of its own)", what);
+        return MASKKV_EINVAL;
+      }
+  }
+  return launch_evict(desc, weights, cu_budget, capacity, budgets, moved, idx, idx_out, rows, weights_out, cu_out, capacity_out,
+                      reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_evict(const maskkv_desc* desc, const float* weights, const int32_t* cu_budget, int64_t capacity,
+                 const int32_t* budgets, const void* Kc, const void* Vc, const int32_t* idx, void* Kc_out, void* Vc_out,
+                 int32_t* idx_out, int32_t* rows, float* weights_out, int32_t* cu_out, int64_t capacity_out, void* stream) {
+  Lens lens;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("evict", "capacity", capacity)) return e;
+  if (int e = check_capacity("evict", "capacity_out", capacity_out)) return e;
+  if (int e = check_packed("evict", "Kc", Kc, capacity)) return e;
+  if (int e = check_packed("evict", "Vc", Vc, capacity)) return e;
+  if (int e = check_packed("evict", "Kc_out", Kc_out, capacity_out)) return e;
+  if (int e = check_packed("evict", "Vc_out", Vc_out, capacity_out)) return e;
+  const int row = desc->d * elem_bytes(desc);
+  const MovedRows moved = {{(const char*)Kc, (const char*)Vc}, {(char*)Kc_out, (char*)Vc_out}, {row, row}};
+  return evict_entry("evict", desc, weights, cu_budget, capacity, budgets, moved, idx, idx_out, rows, weights_out, cu_out,
+                     capacity_out, stream);
+}
+
+int maskkv_evict_mx(const maskkv_desc* desc, const float* weights, const int32_t* cu_budget, int64_t capacity,
+                    const int32_t* budgets, const maskkv_mx_cache* cache, const int32_t* idx,
+                    const maskkv_mx_cache* cache_out, int32_t* idx_out, int32_t* rows, float* weights_out,
+                    int32_t* cu_out, int64_t capacity_out, void* stream) {
+  Lens lens;
+  MxCache from, to;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("evict_mx", "capacity", capacity)) return e;
+  if (int e = check_capacity("evict_mx", "capacity_out", capacity_out)) return e;
+  if (int e = check_mx("evict_mx", "cache", cache, capacity, false, &from)) return e;
+  if (int e = check_mx("evict_mx", "cache_out", cache_out, capacity_out, false, &to)) return e;
+  const MovedRows moved = {{from.k_codes, from.v_codes, from.k_scales, from.v_scales},
+                           {to.k_codes, to.v_codes, to.k_scales, to.v_scales},
+                           {desc->d / 2, desc->d / 2, desc->d / 32, desc->d / 32}};
+  return evict_entry("evict_mx", desc, weights, cu_budget, capacity, budgets, moved, idx, idx_out, rows, weights_out, cu_out,
+                     capacity_out, stream);
 }
 
 int maskkv_head_budgets(const maskkv_desc* desc, const float* prompt_mass, int32_t k_l, float alpha, int32_t* budgets,

@@ -93,6 +93,35 @@ int launch_attend(const maskkv_desc* d, const Lens& lens, bool full, const View&
                   const int32_t* cu_budget, int64_t capacity, const View& K2, const View& V2, float scale,
                   const View& O, float* lse, void* workspace, hipStream_t stream);
 
+// mx.hip: the cache in 4 bits (device pointers; scales one byte per 32 elements)
+struct MxCache {
+  char *k_codes, *k_scales, *v_codes, *v_scales;
+};
+int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, const View& V, const int32_t* idx, const int32_t* cu_budget,
+                      int64_t capacity, const MxCache& cache, hipStream_t stream);
+int launch_expand_mx(const maskkv_desc* d, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, void* Kc, void* Vc,
+                     hipStream_t stream);
+
+// attend_mx.hip
+size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity);
+int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,
+                     const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream);
+
+// accumulate.hip.  Kc or, where that is null, the keys of `cache`.
+int launch_accumulate(const maskkv_desc* d, const View& Q, const void* Kc, const MxCache& cache, const int32_t* cu_budget, int64_t capacity,
+                      float scale, const float* row_lse, float decay, const float* weights_in, float* weights_out, hipStream_t stream);
+
+// evict.hip.  What is moved with a row that stays: up to four arrays of rows of a multiple of 2 bytes each.
+constexpr int kMoved = 4;
+struct MovedRows {
+  const char* from[kMoved];
+  char* to[kMoved];
+  int bytes[kMoved];  // of a row; 0: not there
+};
+int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_budget, int64_t capacity, const int32_t* budgets,
+                 const MovedRows& moved, const int32_t* idx, int32_t* idx_out, int32_t* rows, float* weights_out, int32_t* cu_out,
+                 int64_t capacity_out, hipStream_t stream);
+
 // layer.hip
 size_t layer_importance_workspace_bytes();
 int launch_layer_importance(const void* h_in, const void* h_out, int64_t n, int hidden, int dtype, int64_t row_bytes,

@@ -1,0 +1,155 @@
+// The cache in 4 bits: eviction that stores the kept rows so, and the values that such rows stand for.
+//
+// Both are streams: 2 d eb bytes of K and V in and 2 (d/2 + d/32) out for a row that is stored, the reverse for one that is expanded.
+// A lane takes 16 bytes of a row of K and the same of V, so that loads are whole rows and the lanes of a group of 32 elements are
+// four (bf16) or eight (fp32) neighbours, which find the group's largest magnitude by exchanges inside a row of lanes, without the LDS.
+#include "mx.hpp"
+
+namespace maskkv {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct CompactMxParams {
+  View K, V;
+  Lens lens;
+  int H, BH;
+  int d;
+  const int32_t* idx;
+  const int32_t* cu;
+  int64_t capacity;
+  MxCache out;
+};
+
+// The largest magnitude of a group, as the bits of an fp32, in all of its lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_with(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t group_most(const u32x4& x) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = x[i];
+    if (sizeof(T) == 2)
+      m = max(m, max(w << 16 & 0x7FFF0000u, w & 0x7FFF0000u));
+    else
+      m = max(m, w & 0x7FFFFFFFu);
+  }
+  m = max_with<0xB1>(m);                       // neighbours
+  m = max_with<0x4E>(m);                       // pairs
+  if (sizeof(T) == 4) m = max_with<0x141>(m);  // the other four of eight
+  return m;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_group(const u32x4& x, char* codes, char* scales, int piece) {
+  const uint32_t scale = mx_scale(group_most<T>(x));
+  const uint32_t c = mx_encode<T>(x, scale);
+  if (sizeof(T) == 2)
+    reinterpret_cast<uint32_t*>(codes)[piece] = c;
+  else
+    reinterpret_cast<uint16_t*>(codes)[piece] = (uint16_t)c;
+  constexpr int kLanes = kMxGroup * sizeof(T) / 16;
+  if (piece % kLanes == 0) scales[piece / kLanes] = (char)scale;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxParams prm) {
+  const int pieces = prm.d * (int)sizeof(T) / 16;  // of a row: 8, 16 or 32
+  const int64_t total = min((int64_t)prm.cu[prm.BH], prm.capacity);
+  const int lane = threadIdx.x & 63;
+  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * (64 / pieces);  // of this wave
+  if (first >= total) return;
+  const int64_t row = first + lane / pieces;
+  const int64_t at = min(row, total - 1);  // (lanes behind the last row do it again, and store nothing)
+  int bh = head_of_row(prm.cu, prm.BH, (int)first);
+  while (bh + 1 < prm.BH && prm.cu[bh + 1] <= at) ++bh;
+  const int b = bh / prm.H, h = bh % prm.H, piece = lane % pieces;
+  // a position outside the prompt is clamped rather than read out of bounds
+  const int src = min(max(prm.idx[at], 0), max(prm.lens.P[b] - 1, 0));
+  const u32x4 k = *reinterpret_cast<const u32x4*>(prm.K.row(b, h, src) + piece * 16);
+  const u32x4 v = *reinterpret_cast<const u32x4*>(prm.V.row(b, h, src) + piece * 16);
+  if (row >= total) return;  // (all lanes of a row at once: the exchanges below stay inside a row)
+  store_group<T>(k, prm.out.k_codes + row * (prm.d / 2), prm.out.k_scales + row * (prm.d / kMxGroup), piece);
+  store_group<T>(v, prm.out.v_codes + row * (prm.d / 2), prm.out.v_scales + row * (prm.d / kMxGroup), piece);
+}
+
+struct ExpandParams {
+  MxCache in;
+  const int32_t* total;  // cu[BH]
+  int64_t capacity;
+  int d;
+  char *Kc, *Vc;
+};
+
+// Eight elements a thread, of K and of V.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void expand_mx_kernel(const ExpandParams prm) {
+  const int pieces = prm.d / 8;
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= min((int64_t)prm.total[0], prm.capacity) * pieces) return;
+  const char* codes[2] = {prm.in.k_codes, prm.in.v_codes};
+  const char* scales[2] = {prm.in.k_scales, prm.in.v_scales};
+  char* to[2] = {prm.Kc, prm.Vc};
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const uint32_t c = reinterpret_cast<const uint32_t*>(codes[n])[i];
+    const float unit = mx_unit(reinterpret_cast<const uint8_t*>(scales[n])[i / 4]);
+    if (sizeof(T) == 2) {
+      reinterpret_cast<u32x4*>(to[n])[i] = mx_decode_bf16(c, unit);
+    } else {
+      float x[8];
+      mx_decode_f32(c, unit, x);
+      reinterpret_cast<float4*>(to[n])[2 * i] = make_float4(x[0], x[1], x[2], x[3]);
+      reinterpret_cast<float4*>(to[n])[2 * i + 1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+  }
+}
+
+}  // namespace
+
+int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, const View& V, const int32_t* idx, const int32_t* cu_budget,
+                      int64_t capacity, const MxCache& cache, hipStream_t stream) {
+  if (capacity == 0) return MASKKV_OK;
+  CompactMxParams prm;
+  prm.K = K;
+  prm.V = V;
+  prm.lens = lens;
+  prm.H = d->H;
+  prm.BH = d->B * d->H;
+  prm.d = d->d;
+  prm.idx = idx;
+  prm.cu = cu_budget;
+  prm.capacity = capacity;
+  prm.out = cache;
+  const int rows = kThreads / (d->d * (d->dtype == MASKKV_BF16 ? 2 : 4) / 16);  // of a workgroup
+  const dim3 grid((unsigned)((capacity + rows - 1) / rows));
+  if (d->dtype == MASKKV_BF16)
+    hipLaunchKernelGGL(compact_mx_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, prm);
+  else
+    hipLaunchKernelGGL(compact_mx_kernel<float>, grid, dim3(kThreads), 0, stream, prm);
+  return check_launch("compact_mx");
+}
+
+int launch_expand_mx(const maskkv_desc* d, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, void* Kc, void* Vc,
+                     hipStream_t stream) {
+  if (capacity == 0) return MASKKV_OK;
+  ExpandParams prm;
+  prm.in = cache;
+  prm.total = cu_budget + (int64_t)d->B * d->H;
+  prm.capacity = capacity;
+  prm.d = d->d;
+  prm.Kc = reinterpret_cast<char*>(Kc);
+  prm.Vc = reinterpret_cast<char*>(Vc);
+  const dim3 grid((unsigned)((capacity * (d->d / 8) + kThreads - 1) / kThreads));
+  if (d->dtype == MASKKV_BF16)
+    hipLaunchKernelGGL(expand_mx_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, prm);
+  else
+    hipLaunchKernelGGL(expand_mx_kernel<float>, grid, dim3(kThreads), 0, stream, prm);
+  return check_launch("expand_mx");
+}
+
+}  // namespace maskkv

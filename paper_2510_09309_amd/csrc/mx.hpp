@@ -1,0 +1,85 @@
+// The cache in 4 bits: a group of 32 neighbours along the head dimension has one power of two 2^e (byte e + 127) and a code of
+// four bits each, sign and one of the sizes 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+//
+// gfx950 converts two elements an instruction, both ways, with the scale as an fp32 of which the exponent counts: over every code, scale
+// byte, bf16 and four million fp32 values the instructions give the nearest size times 2^e with ties to the even code, what is
+// beyond the largest size as that, and NaN for the scale byte 255.
+#pragma once
+
+#include "kernels.hpp"
+
+namespace maskkv {
+
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kMxGroup = 32;
+constexpr uint32_t kMxLeast = 3, kMxMost = 252, kMxNan = 255;
+
+// The scale byte of a group from the largest of its elements' magnitudes (their bits as fp32): the smallest 2^e with most <= 6 * 2^e.
+// 6 * 2^e has the mantissa 1.5 and an exponent of e + 2: a mantissa above 1.5 carries into the next one.  Below 2^-124 even the smallest size
+// would be no normal bf16, and above 2^125 the largest none at all.
+__device__ __forceinline__ uint32_t mx_scale(uint32_t most) {
+  if (most >= 0x7F800000u) return kMxNan;
+  const uint32_t up = (most + 0x003FFFFFu) >> 23;
+  return min(max(up, kMxLeast + 2) - 2, kMxMost);
+}
+
+__device__ __forceinline__ float mx_unit(uint32_t scale) { return as_f32(scale << 23); }
+
+// Eight (four) codes of a lane's 16 bytes of bf16 (fp32).  (A group of NaN has codes of 0.)
+template <typename T>
+__device__ __forceinline__ uint32_t mx_encode(const u32x4& x, uint32_t scale);
+template <>
+__device__ __forceinline__ uint32_t mx_encode<bf16_t>(const u32x4& x, uint32_t scale) {
+  const float unit = mx_unit(scale);
+  const uint32_t w0 = x[0], w1 = x[1], w2 = x[2], w3 = x[3];
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w0), unit, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w1), unit, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w2), unit, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w3), unit, 3);
+  return scale == kMxNan ? 0u : c;
+}
+template <>
+__device__ __forceinline__ uint32_t mx_encode<float>(const u32x4& x, uint32_t scale) {
+  const float unit = mx_unit(scale);
+  const uint32_t w0 = x[0], w1 = x[1], w2 = x[2], w3 = x[3];
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, as_f32(w0), as_f32(w1), unit, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, as_f32(w2), as_f32(w3), unit, 1);
+  return scale == kMxNan ? 0u : c;
+}
+
+// The values of eight codes: as four words of bf16, or as floats.
+__device__ __forceinline__ u32x4 mx_decode_bf16(uint32_t codes, float unit) {
+  u32x4 x;
+  x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0));
+  x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1));
+  x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2));
+  x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3));
+  return x;
+}
+__device__ __forceinline__ void mx_decode_f32(uint32_t codes, float unit, float (&x)[8]) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 1),
+              c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, unit, 3);
+  x[0] = a[0], x[1] = a[1], x[2] = b[0], x[3] = b[1], x[4] = c[0], x[5] = c[1], x[6] = d[0], x[7] = d[1];
+}
+
+// The head that a packed row belongs to, the largest with cu[head] <= row (row < cu[BH]); found by a wave for a row that its lanes
+// share, 64 ways at a time.
+__device__ __forceinline__ int head_of_row(const int32_t* cu, int BH, int row) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = BH;
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64;
+    const int probe = min(lo + (lane + 1) * step, hi);
+    const int n = __popcll(__ballot(cu[probe] <= row));  // true for a prefix of the lanes
+    const int from = n == 0 ? lo : min(lo + n * step, hi);
+    hi = n == 64 ? hi : min(lo + (n + 1) * step, hi);
+    lo = from;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+}  // namespace maskkv

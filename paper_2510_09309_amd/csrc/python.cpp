@@ -30,12 +30,20 @@ struct Fns {
   decltype(&maskkv_compact) compact;
   decltype(&maskkv_attend) attend;
   decltype(&maskkv_attend_full) attend_full;
+  decltype(&maskkv_compact_mx) compact_mx;
+  decltype(&maskkv_expand_mx) expand_mx;
+  decltype(&maskkv_attend_mx_workspace_bytes) attend_mx_ws;
+  decltype(&maskkv_attend_mx) attend_mx;
+  decltype(&maskkv_accumulate) accumulate;
+  decltype(&maskkv_accumulate_mx) accumulate_mx;
+  decltype(&maskkv_evict) evict;
+  decltype(&maskkv_evict_mx) evict_mx;
   decltype(&maskkv_head_budgets) head_budgets;
   decltype(&maskkv_layer_importance) layer_importance;
   decltype(&maskkv_value_shift) value_shift;
 } fn;
 
-PyObject *kB, *kH, *kd, *kdtype, *kn_resp, *kn_query, *kP_max, *kq_per_kv, *kprompt_len, *kcuda_stream, *kdata_ptr;
+PyObject *kB, *kH, *kd, *kdtype, *kn_resp, *kn_query, *kP_max, *kq_per_kv, *kprompt_len, *kcuda_stream, *kdata_ptr, *kk_codes, *kk_scales, *kv_codes, *kv_scales;
 
 struct Error {};  // a Python exception has been set
 
@@ -394,6 +402,194 @@ PyObject* value_shift(PyObject*, Args a, Py_ssize_t n) {  // V_now, V_prev, delt
   });
 }
 
+// ---- the cache in 4 bits and further eviction: these calls look at what they are given as far as Python knows it, before the
+// library does (it sees pointers): type, size, device.
+
+void on_this_device(const at::Tensor& t, const char* what) {
+  if (t.is_cuda() && t.get_device() == c10::hip::getCurrentHIPStream().device_index()) return;
+  PyErr_Format(PyExc_AssertionError, "%s: need a tensor on the current device", what);
+  throw Error{};
+}
+
+// A contiguous tensor of `type` with at least `least` elements on the current device, or None where `optional`.
+template <typename T>
+T* buffer(PyObject* o, at::ScalarType type, int64_t least, const char* what, bool optional = false) {
+  if (o == Py_None && (optional || least <= 0)) return nullptr;
+  if (!THPVariable_Check(o)) {
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor", what);
+    throw Error{};
+  }
+  const at::Tensor& t = THPVariable_Unpack(o);
+  on_this_device(t, what);
+  if (t.scalar_type() != type || !t.is_contiguous() || t.numel() < least) {
+    PyErr_Format(PyExc_AssertionError, "%s: need a contiguous tensor of %s with at least %lld elements", what, c10::toString(type),
+                 (long long)least);
+    throw Error{};
+  }
+  return static_cast<T*>(t.data_ptr());
+}
+
+at::ScalarType element_type(const maskkv_desc& d) { return d.dtype == MASKKV_BF16 ? at::kBFloat16 : at::kFloat; }
+
+int64_t heads_of(const maskkv_desc& d) { return (int64_t)d.B * d.H; }
+int64_t group_of(const maskkv_desc& d) { return d.q_per_kv > 1 ? d.q_per_kv : 1; }
+
+// A view as ViewArg takes it; a plain tensor is also held against the description: [>= B, >= heads, >= rows, d] of its dtype.
+struct CheckedView : ViewArg {
+  CheckedView(PyObject* o, const maskkv_desc& d, int64_t heads, int64_t rows, const char* what) : ViewArg(o) {
+    if (!THPVariable_Check(o)) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    on_this_device(t, what);
+    if (t.scalar_type() != element_type(d) || t.size(0) < d.B || t.size(1) < heads || t.size(2) < rows || t.size(3) != d.d) {
+      PyErr_Format(PyExc_AssertionError, "%s: need [%d, %lld, %lld, %d] of the description's dtype", what, (int)d.B, (long long)heads,
+                   (long long)rows, (int)d.d);
+      throw Error{};
+    }
+  }
+};
+
+int64_t longest_prompt(const maskkv_desc& d) {
+  if (!d.prompt_len || d.B > MASKKV_MAX_BATCH) return d.P_max;
+  int64_t most = 0;
+  for (int b = 0; b < d.B; ++b) most = d.prompt_len[b] > most ? d.prompt_len[b] : most;
+  return most;
+}
+
+struct MxArg {
+  maskkv_mx_cache c;
+  MxArg(PyObject* o, const maskkv_desc& d, int64_t rows, bool keys_only = false) {
+    const struct {
+      PyObject* name;
+      void** to;
+      int64_t row;
+      bool optional;
+      const char* what;
+    } all[] = {{kk_codes, &c.k_codes, d.d / 2, false, "k_codes"}, {kk_scales, &c.k_scales, d.d / 32, false, "k_scales"},
+               {kv_codes, &c.v_codes, d.d / 2, keys_only, "v_codes"}, {kv_scales, &c.v_scales, d.d / 32, keys_only, "v_scales"}};
+    for (const auto& e : all) {
+      Ref v(PyObject_GetAttr(o, e.name));
+      *e.to = buffer<void>(v.o, at::kByte, rows * e.row, e.what, e.optional);
+    }
+  }
+};
+
+PyObject* compact_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, K, V, idx, cu, capacity, cache, stream
+  return call<8>(n, [&] {
+    DescArg d(a[0]);
+    const int64_t cap = as_i64(a[5]);
+    CheckedView k(a[1], d.d, d.d.H, longest_prompt(d.d), "K"), v(a[2], d.d, d.d.H, longest_prompt(d.d), "V");
+    const int32_t *idx = buffer<int32_t>(a[3], at::kInt, cap, "idx"), *cu = buffer<int32_t>(a[4], at::kInt, heads_of(d.d) + 1, "cu_budget");
+    MxArg mx(a[6], d.d, cap);
+    void* st = as_stream(a[7]);
+    return without_gil([&] { return fn.compact_mx(&d.d, &k.v, &v.v, idx, cu, cap, &mx.c, st); });
+  });
+}
+PyObject* expand_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, cache, cu, capacity, Kc, Vc, stream
+  return call<7>(n, [&] {
+    DescArg d(a[0]);
+    const int64_t cap = as_i64(a[3]);
+    MxArg mx(a[1], d.d, cap);
+    const int32_t* cu = buffer<int32_t>(a[2], at::kInt, heads_of(d.d) + 1, "cu_budget");
+    void *kc = buffer<void>(a[4], element_type(d.d), cap * d.d.d, "Kc"), *vc = buffer<void>(a[5], element_type(d.d), cap * d.d.d, "Vc");
+    void* st = as_stream(a[6]);
+    return without_gil([&] { return fn.expand_mx(&d.d, &mx.c, cu, cap, kc, vc, st); });
+  });
+}
+PyObject* attend_mx_ws(PyObject*, Args a, Py_ssize_t n) {
+  return call<2>(n, [&]() -> long long {
+    DescArg d(a[0]);
+    size_t bytes = 0;
+    const int s = fn.attend_mx_ws(&d.d, as_i64(a[1]), &bytes);
+    return s ? -s : (long long)bytes;
+  });
+}
+PyObject* attend_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, Q, cache, cu, capacity, Kr, Vr, scale, O, lse, workspace, stream
+  return call<12>(n, [&] {
+    DescArg d(a[0]);
+    const int64_t cap = as_i64(a[4]), g = group_of(d.d);
+    CheckedView q(a[1], d.d, d.d.H * g, d.d.n_resp, "Q_resp"), k2(a[5], d.d, d.d.H, d.d.n_resp, "K_resp"),
+        v2(a[6], d.d, d.d.H, d.d.n_resp, "V_resp"), o(a[8], d.d, d.d.H * g, d.d.n_resp, "O");
+    MxArg mx(a[2], d.d, cap);
+    const int32_t* cu = buffer<int32_t>(a[3], at::kInt, heads_of(d.d) + 1, "cu_budget");
+    const float scale = (float)as_f64(a[7]);
+    float* lse = buffer<float>(a[9], at::kFloat, heads_of(d.d) * g * d.d.n_resp, "lse", true);
+    const size_t wn = nbytes(a[10]);
+    void *ws = wn ? buffer<void>(a[10], THPVariable_Unpack(a[10]).scalar_type(), 0, "workspace") : nullptr, *st = as_stream(a[11]);
+    return without_gil([&] { return fn.attend_mx(&d.d, &q.v, &mx.c, cu, cap, &k2.v, &v2.v, scale, &o.v, lse, ws, wn, st); });
+  });
+}
+// desc, Q, Kc or cache, cu, capacity, scale, lse, decay, weights_in, weights_out, stream
+PyObject* accumulate_any(Args a, Py_ssize_t n, bool mx) {
+  return call<11>(n, [&] {
+    DescArg d(a[0]);
+    const int64_t cap = as_i64(a[4]), g = group_of(d.d);
+    CheckedView q(a[1], d.d, d.d.H * g, d.d.n_resp, "Q_resp");
+    const int32_t* cu = buffer<int32_t>(a[3], at::kInt, heads_of(d.d) + 1, "cu_budget");
+    const float scale = (float)as_f64(a[5]), decay = (float)as_f64(a[7]);
+    const float* lse = buffer<float>(a[6], at::kFloat, heads_of(d.d) * g * d.d.n_resp, "row_lse");
+    const float* in = buffer<float>(a[8], at::kFloat, cap, "weights_in", true);
+    float* out = buffer<float>(a[9], at::kFloat, cap, "weights_out");
+    void* st = as_stream(a[10]);
+    if (mx) {
+      MxArg c(a[2], d.d, cap, true);
+      return without_gil([&] { return fn.accumulate_mx(&d.d, &q.v, &c.c, cu, cap, scale, lse, decay, in, out, st); });
+    }
+    const void* kc = buffer<void>(a[2], element_type(d.d), cap * d.d.d, "Kc");
+    return without_gil([&] { return fn.accumulate(&d.d, &q.v, kc, cu, cap, scale, lse, decay, in, out, st); });
+  });
+}
+PyObject* accumulate(PyObject*, Args a, Py_ssize_t n) { return accumulate_any(a, n, false); }
+PyObject* accumulate_mx(PyObject*, Args a, Py_ssize_t n) { return accumulate_any(a, n, true); }
+
+struct EvictArgs {  // weights, cu, capacity, budgets ... idx ... idx_out, rows, weights_out, cu_out, capacity_out, stream
+  int64_t cap, cap_out;
+  const float* weights;
+  const int32_t *cu, *budgets, *idx;
+  int32_t *idx_out, *rows, *cu_out;
+  float* weights_out;
+  void* st;
+  EvictArgs(const maskkv_desc& d, Args a, PyObject* from, Args out) {
+    cap = as_i64(a[3]);
+    cap_out = as_i64(out[4]);
+    weights = buffer<float>(a[1], at::kFloat, cap, "weights");
+    cu = buffer<int32_t>(a[2], at::kInt, heads_of(d) + 1, "cu_budget");
+    budgets = buffer<int32_t>(a[4], at::kInt, heads_of(d), "budgets");
+    idx = buffer<int32_t>(from, at::kInt, cap, "idx", true);
+    idx_out = buffer<int32_t>(out[0], at::kInt, cap_out, "idx_out", true);
+    rows = buffer<int32_t>(out[1], at::kInt, cap_out, "rows");
+    weights_out = buffer<float>(out[2], at::kFloat, cap_out, "weights_out", true);
+    cu_out = buffer<int32_t>(out[3], at::kInt, heads_of(d) + 1, "cu_out");
+    st = as_stream(out[5]);
+  }
+};
+// desc, weights, cu, capacity, budgets, Kc, Vc, idx, Kc_out, Vc_out, idx_out, rows, weights_out, cu_out, capacity_out, stream
+PyObject* evict(PyObject*, Args a, Py_ssize_t n) {
+  return call<16>(n, [&] {
+    DescArg d(a[0]);
+    EvictArgs e(d.d, a, a[7], a + 10);
+    const at::ScalarType t = element_type(d.d);
+    const int64_t in = e.cap * d.d.d, out = e.cap_out * d.d.d;
+    const void *kc = buffer<void>(a[5], t, in, "Kc"), *vc = buffer<void>(a[6], t, in, "Vc");
+    void *ko = buffer<void>(a[8], t, out, "Kc_out"), *vo = buffer<void>(a[9], t, out, "Vc_out");
+    return without_gil([&] {
+      return fn.evict(&d.d, e.weights, e.cu, e.cap, e.budgets, kc, vc, e.idx, ko, vo, e.idx_out, e.rows, e.weights_out, e.cu_out,
+                      e.cap_out, e.st);
+    });
+  });
+}
+// desc, weights, cu, capacity, budgets, cache, idx, cache_out, idx_out, rows, weights_out, cu_out, capacity_out, stream
+PyObject* evict_mx(PyObject*, Args a, Py_ssize_t n) {
+  return call<14>(n, [&] {
+    DescArg d(a[0]);
+    EvictArgs e(d.d, a, a[6], a + 8);
+    MxArg from(a[5], d.d, e.cap), to(a[7], d.d, e.cap_out);
+    return without_gil([&] {
+      return fn.evict_mx(&d.d, e.weights, e.cu, e.cap, e.budgets, &from.c, e.idx, &to.c, e.idx_out, e.rows, e.weights_out, e.cu_out,
+                         e.cap_out, e.st);
+    });
+  });
+}
+
 // bind({name: address}): the loaded library's entry points.
 PyObject* bind(PyObject*, PyObject* table) {
   const struct {
@@ -404,7 +600,10 @@ PyObject* bind(PyObject*, PyObject* table) {
       {"maskkv_attend_workspace_bytes", &fn.attend_ws}, {"maskkv_score", &fn.score},
       {"maskkv_score_given_lse", &fn.score_given_lse}, {"maskkv_score_static", &fn.score_static},
       {"maskkv_select", &fn.select}, {"maskkv_compact", &fn.compact}, {"maskkv_attend", &fn.attend},
-      {"maskkv_attend_full", &fn.attend_full}, {"maskkv_head_budgets", &fn.head_budgets},
+      {"maskkv_attend_full", &fn.attend_full}, {"maskkv_compact_mx", &fn.compact_mx}, {"maskkv_expand_mx", &fn.expand_mx},
+      {"maskkv_attend_mx_workspace_bytes", &fn.attend_mx_ws}, {"maskkv_attend_mx", &fn.attend_mx},
+      {"maskkv_accumulate", &fn.accumulate}, {"maskkv_accumulate_mx", &fn.accumulate_mx}, {"maskkv_evict", &fn.evict},
+      {"maskkv_evict_mx", &fn.evict_mx}, {"maskkv_head_budgets", &fn.head_budgets},
       {"maskkv_layer_importance", &fn.layer_importance}, {"maskkv_value_shift", &fn.value_shift}};
   for (const auto& e : all) {
     PyObject* v = PyDict_GetItemString(table, e.name);
@@ -418,7 +617,8 @@ PyObject* bind(PyObject*, PyObject* table) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(score_ws), FAST(select_ws), FAST(attend_ws), FAST(score), FAST(score_given_lse),
                          FAST(score_static), FAST(select), FAST(compact), FAST(attend), FAST(attend_full),
-                         FAST(head_budgets), FAST(layer_importance), FAST(value_shift),
+                         FAST(compact_mx), FAST(expand_mx), FAST(attend_mx_ws), FAST(attend_mx), FAST(accumulate),
+                         FAST(accumulate_mx), FAST(evict), FAST(evict_mx), FAST(head_budgets), FAST(layer_importance), FAST(value_shift),
                          {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -430,7 +630,8 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     const char* text;
   } names[] = {{&kB, "B"}, {&kH, "H"}, {&kd, "d"}, {&kdtype, "dtype"}, {&kn_resp, "n_resp"}, {&kn_query, "n_query"},
                {&kP_max, "P_max"}, {&kq_per_kv, "q_per_kv"}, {&kprompt_len, "prompt_len"},
-               {&kcuda_stream, "cuda_stream"}, {&kdata_ptr, "data_ptr"}};
+               {&kcuda_stream, "cuda_stream"}, {&kdata_ptr, "data_ptr"}, {&kk_codes, "k_codes"}, {&kk_scales, "k_scales"},
+               {&kv_codes, "v_codes"}, {&kv_scales, "v_scales"}};
   for (const auto& n : names) {
     *n.to = PyUnicode_InternFromString(n.text);
     if (!*n.to) return nullptr;
