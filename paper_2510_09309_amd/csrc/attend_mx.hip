@@ -1,120 +1,489 @@
 // Attention of the response span over a cache in 4 bits and the response's own rows.
 //
-// A workgroup per query row: 256 keys at a time, a logit a thread, the running maximum and sum of the softmax, then the
-// values, an element of the head dimension a thread.
+// A workgroup of four waves serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row
+// axis), so that a lane owns one query and its probabilities are the B operand of O^T = V^T P^T as they stand.  The waves take
+// tiles of 32 keys in turn, each through registers and LDS of its own, without a barrier, and are merged at the end.  A
+// row's two halves along the head dimension belong to the two halves of a wave: a lane's codes of a key are 16 (8) whole words
+// in a row, its scales two bytes (one), and the conversion of a word is an operand of a matrix instruction.  Values are converted on
+// their way into LDS, from where a transposing read brings them as V^T.  The response's tiles come first: what is read of the
+// cache for the first of its tiles is under way meanwhile.
+//
+// Where heads x query tiles are fewer than the compute units, or a head may be far longer than the others, the tiles are dealt to
+// several workgroups, and a second kernel joins their partial results.
+#include <type_traits>
+
+#include "attend.hpp"
 #include "mx.hpp"
 
 namespace maskkv {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kUnits = 256;  // compute units
+constexpr int kTile = 32;    // keys of a tile, and query rows of a workgroup
+constexpr int kWaves = 4;
 
 struct AttendMxParams {
   View Q, K2, V2, O;
   MxCache cache;
   const int32_t* cu;
   int64_t capacity;
-  int H, q_per_kv, n_resp, n_q;
-  float c;  // scale * log2(e)
+  int H, BH, q_per_kv, n_resp, n_q, qtiles;
+  int chunk;      // tiles of a workgroup, or 0: all of its head
+  int part_rows;  // query rows of a partial result
+  float c;        // scale * log2(e)
   float* lse;
+  float* part_o;    // [units * qtiles][part_rows][D]
+  float2* part_ml;  // [units * qtiles][part_rows]
+  int2* parts;      // [BH] a head's first unit, and how many it has
 };
 
-template <typename T>
-__device__ __forceinline__ float element(const char* p, int i) {
-  if (sizeof(T) == 2) return as_f32((uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << 16);
-  return reinterpret_cast<const float*>(p)[i];
+template <typename T, int D>
+struct MxCfg {
+  static constexpr int kRowB = D * (int)sizeof(T);
+  static constexpr int kPPR = kRowB / 16;        // pieces of 16 bytes in a row
+  static constexpr int kLoads = kPPR / 2;        // of 16 bytes a lane, of a tile's K (and V)
+  static constexpr int kRPL = 64 / kPPR;         // rows of such a load
+  static constexpr int kWords = D / 16;          // code words of a lane's half row
+  static constexpr int kDB = D / 32;
+  static constexpr int kTileB = kTile * kRowB;
+  static constexpr int kWaveB = 2 * kTileB;      // K (of the response) and V
+  static constexpr int kSumP = D + 4;            // floats from one query's sums to the next while the waves are merged
+  static constexpr int kSumB = kTile * kSumP * 4;
+  static constexpr int kLds = kWaves * (kWaveB > kSumB ? kWaveB : kSumB) + kWaves * kTile * 8;
+  // K: piece p of a row in slot p ^ swz_k(row).
+  __device__ static uint32_t swz_k(uint32_t row) { return sizeof(T) == 2 && D == 64 ? (row >> 1) & 7 : row & 15; }
+  // V: bf16 see v_swizzle; fp32: blocks of 32 columns, exchanged in every other four rows.
+  __device__ static uint32_t v_slot(uint32_t row, uint32_t p) {
+    return sizeof(T) == 2 ? (p ^ v_swizzle<D>(row) << 1) : p ^ ((row >> 2) & 1) << 3;
+  }
+};
+
+// Tiles of a head: those of the response first.
+struct Head {
+  int first, cached;  // its rows of the cache
+  int tiles;
+};
+__device__ __forceinline__ Head head_at(const AttendMxParams& prm, int bh) {
+  const int capacity = (int)prm.capacity;
+  Head x;
+  x.first = min(prm.cu[bh], capacity);
+  x.cached = max(min(prm.cu[bh + 1], capacity) - x.first, 0);
+  x.tiles = (x.cached + kTile - 1) / kTile + (prm.n_resp + kTile - 1) / kTile;
+  return x;
 }
 
-template <bool MAX>
-__device__ __forceinline__ float over_all(float v, float* part) {
+// The head of a unit when every head has as many units as its tiles ask for, and the number of its first; -1 behind the last.
+__device__ __forceinline__ int head_of_unit(const AttendMxParams& prm, int unit, int& first_unit, int& units) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base < prm.BH; base += 64) {
+    const int bh = base + lane;
+    const int own = bh < prm.BH ? (head_at(prm, min(bh, prm.BH - 1)).tiles + prm.chunk - 1) / prm.chunk : 0;
+    int upto = own;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float w = __shfl_xor(v, o, 64);
-    v = MAX ? fmaxf(v, w) : v + w;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      upto += lane >= o ? v : 0;
+    }
+    const uint64_t over = __ballot(before + upto > unit);
+    if (over) {
+      const int at = __builtin_ctzll(over);
+      units = __builtin_amdgcn_readlane(own, at);
+      first_unit = before + __builtin_amdgcn_readlane(upto, at) - units;
+      return base + at;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return MAX ? fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) : (part[0] + part[1]) + (part[2] + part[3]);
+  return -1;
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void attend_mx_kernel(const AttendMxParams prm) {
-  __shared__ float q[D], p[kThreads], part[4], half[2][D];
-  const int bh = blockIdx.y, i = blockIdx.x, t = threadIdx.x;
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx_kernel(const AttendMxParams prm) {
+  using C = MxCfg<T, D>;
+  constexpr bool F32 = sizeof(T) == 4;
+  extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
+  // Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there.
+  const int slot = blockIdx.x / 8;
+  const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
+  int bh = unit, first_unit = unit, units = 1;
+  if (prm.chunk)
+    bh = head_of_unit(prm, unit, first_unit, units);
+  else if (bh >= prm.BH)
+    bh = -1;
+  if (bh < 0) return;
+  bh = __builtin_amdgcn_readfirstlane(bh);
   const int b = bh / prm.H, h = bh % prm.H;
-  const int64_t c0 = min((int64_t)prm.cu[bh], prm.capacity), c1 = min((int64_t)prm.cu[bh + 1], prm.capacity);
-  const int cached = max((int)(c1 - c0), 0), n = cached + prm.n_resp;
-  const char* qrow = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, i);
-  if (t < D) q[t] = element<T>(qrow, t);
-  float m = kNegBig, l = 0.f, o = 0.f;
-  for (int base = 0; base < n; base += kThreads) {
-    __syncthreads();
-    const int j = base + t;
-    float s = 0.f;
-    if (j < cached) {
-      for (int e = 0; e < D / 8; ++e) {
-        float x[8];
-        mx_decode_f32(reinterpret_cast<const uint32_t*>(prm.cache.k_codes + (c0 + j) * (D / 2))[e],
-                      mx_unit(reinterpret_cast<const uint8_t*>(prm.cache.k_scales)[(c0 + j) * (D / 32) + e / 4]), x);
-        for (int u = 0; u < 8; ++u) s = fmaf(q[8 * e + u], x[u], s);
-      }
-    } else if (j < n) {
-      const char* k = prm.K2.row(b, h, j - cached);
-      for (int e = 0; e < D; ++e) s = fmaf(q[e], element<T>(k, e), s);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  const Head head = head_at(prm, bh);
+  if (prm.chunk && unit == first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(first_unit, units);
+  const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
+  const int t0 = prm.chunk ? (unit - first_unit) * prm.chunk : 0;
+  const int t1 = prm.chunk ? min(head.tiles, t0 + prm.chunk) : head.tiles;
+
+  char* const k_lds = mx_lds + wave * C::kWaveB;
+  char* const v_lds = k_lds + C::kTileB;
+  const uint32_t v_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)v_lds;
+
+  // ---- what is under way: a tile of the cache, or of the response
+  u32x4 kc[D / 64], vc[D / 64];
+  uint32_t ks = 0, vs = 0;
+  auto load_cached = [&](int t) {  // tile t of the cache; rows behind the last one are the last one
+    const int64_t row = head.first + min(t * kTile + r, head.cached - 1);
+    const int64_t at = row * (D / 2) + g * (D / 4);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      kc[j] = *reinterpret_cast<const u32x4*>(prm.cache.k_codes + at + 16 * j);
+      vc[j] = *reinterpret_cast<const u32x4*>(prm.cache.v_codes + at + 16 * j);
     }
-    s *= prm.c;
-    const float m_new = fmaxf(m, over_all<true>(j < n ? s : kNegBig, part));
-    const float x = j < n ? fast_exp2(s - m_new) : 0.f, alpha = fast_exp2(m - m_new);
-    l = l * alpha + over_all<false>(x, part);
-    o *= alpha;
-    m = m_new;
-    p[t] = x;
-    __syncthreads();
-    const int e = t % D, g = t / D;
-    const int many = min(n - base, kThreads);
-    for (int u = g; u < many; u += kThreads / D) {
-      const int r = base + u;
-      float v;
-      if (r < cached) {
-        float x8[8];
-        mx_decode_f32(reinterpret_cast<const uint32_t*>(prm.cache.v_codes + (c0 + r) * (D / 2))[e / 8],
-                      mx_unit(reinterpret_cast<const uint8_t*>(prm.cache.v_scales)[(c0 + r) * (D / 32) + e / 32]), x8);
-        v = x8[0];
-        for (int w = 1; w < 8; ++w) v = e % 8 == w ? x8[w] : v;
+    const int64_t s = row * (D / 32) + g * (D / 64);
+    if (D == 128) {
+      ks = *reinterpret_cast<const uint16_t*>(prm.cache.k_scales + s);
+      vs = *reinterpret_cast<const uint16_t*>(prm.cache.v_scales + s);
+    } else {
+      ks = *reinterpret_cast<const uint8_t*>(prm.cache.k_scales + s);
+      vs = *reinterpret_cast<const uint8_t*>(prm.cache.v_scales + s);
+    }
+  };
+  u32x4 kr[C::kLoads], vr[C::kLoads];
+  auto load_resp = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
+      kr[j] = *reinterpret_cast<const u32x4*>(prm.K2.row(b, h, row) + lane % C::kPPR * 16);
+      vr[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, row) + lane % C::kPPR * 16);
+    }
+  };
+
+  // This wave's tiles: t0 + wave, and every fourth from there; those of the response are the first `resp` of them.
+  const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
+  const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
+  auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
+  if (resp > 0) load_resp(tile_of(0));
+  if (mine > resp) load_cached(tile_of(resp) - resp_tiles);
+
+  // ---- this lane's query: half of its row, as the B operand of the first product
+  u32x4 qf[C::kPPR / 2];
+  {
+    const char* q = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, min(qtile * kTile + r, prm.n_q - 1)) + g * (C::kRowB / 2);
+#pragma unroll
+    for (int i = 0; i < C::kPPR / 2; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
+  }
+
+  f32x16 o[C::kDB], s;
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
+  float m = kNegBig, l = 0.f;
+
+  auto logits_step = [&](int i, const u32x4& x) {  // bf16: word i of the lane's half row
+    mfma_step<bf16_t>(x, qf[i], s);
+  };
+  auto logits_step_f32 = [&](int i, const float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t q = qf[2 * i + e / 4][e % 4];
+      s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], as_f32(q), s, 0, 0, 0);
+    }
+  };
+
+  // ---- softmax of a tile with `left` rows, and the output update.  Lanes l and l ^ 32 have the same query.
+  auto update = [&](int left) {
+    if (left < kTile) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i / 4) + 4 * g + i % 4 >= left) s[i] = -INFINITY;
+    }
+    float bm = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) bm = fmaxf(bm, s[i]);
+    const float cand = max_halves(bm) * prm.c;
+    const bool bump = cand > m + kLazyBump;  // (see attend.hip)
+    if (__any(bump)) {
+      const float m_new = bump ? cand : m;
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = fast_exp2(fmaf(s[i], prm.c, -m));
+      s[i] = p;
+      l += p;
+    }
+    if constexpr (!F32) {
+#pragma unroll
+      for (int tp = 0; tp < 2; ++tp) {
+        u32x4 pf;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(s[8 * tp + 2 * w], s[8 * tp + 2 * w + 1]);
+#pragma unroll
+        for (int db = 0; db < C::kDB; ++db) {
+          const uint32_t from = v_at + v_read_offset<D>(lane, db);
+          const u32x2 lo = read_transposed(from, 16 * tp * C::kRowB), hi = read_transposed(from, (16 * tp + 8) * C::kRowB);
+          mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[db]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = 8 * (i / 4) + 4 * g + i % 4;
+#pragma unroll
+        for (int db = 0; db < C::kDB; ++db) {
+          const float v = *reinterpret_cast<const float*>(v_lds + row * C::kRowB + ((db ^ ((row >> 2) & 1)) * 32 + r) * 4);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[i], o[db], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  for (int i = 0; i < resp; ++i) {
+    const int t = tile_of(i);
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const uint32_t row = j * C::kRPL + lane / C::kPPR, p = lane % C::kPPR;
+      *reinterpret_cast<u32x4*>(k_lds + row * C::kRowB + ((p ^ C::swz_k(row)) << 4)) = kr[j];
+      *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + (C::v_slot(row, p) << 4)) = vr[j];
+    }
+    if (i + 1 < resp) load_resp(tile_of(i + 1));
+    asm volatile("" ::: "memory");
+    s = f32x16{};
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) {
+      auto piece = [&](int p) { return *reinterpret_cast<const u32x4*>(k_lds + r * C::kRowB + ((p ^ C::swz_k(r)) << 4)); };
+      if constexpr (F32) {
+        const u32x4 a = piece(g * (C::kPPR / 2) + 2 * w), c = piece(g * (C::kPPR / 2) + 2 * w + 1);
+        const uint32_t a0 = a[0], a1 = a[1], a2 = a[2], a3 = a[3], c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+        const float x[8] = {as_f32(a0), as_f32(a1), as_f32(a2), as_f32(a3), as_f32(c0), as_f32(c1), as_f32(c2), as_f32(c3)};
+        logits_step_f32(w, x);
       } else {
-        v = element<T>(prm.V2.row(b, h, r - cached), e);
+        logits_step(w, piece(g * (C::kPPR / 2) + w));
       }
-      o = fmaf(p[u], v, o);
+    }
+    update(prm.n_resp - t * kTile);
+    asm volatile("" ::: "memory");
+  }
+  for (int i = resp; i < mine; ++i) {
+    const int t = tile_of(i) - resp_tiles;
+    // V on its way into LDS, K into the first product
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) {
+      const uint32_t word = vc[w / 4][w % 4];
+      const float unit = mx_unit(vs >> (8 * (w / 4)) & 255);
+      if constexpr (F32) {
+        float x[8];
+        mx_decode_f32(word, unit, x);
+        const uint32_t p = g * (C::kPPR / 2) + 2 * w;
+        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p + 1) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+      } else {
+        *reinterpret_cast<u32x4*>(v_lds + r * C::kRowB + (C::v_slot(r, g * (C::kPPR / 2) + w) << 4)) = mx_decode_bf16(word, unit);
+      }
+    }
+    u32x4 k_now[D / 64];
+    const uint32_t s_now = ks;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) k_now[j] = kc[j];
+    if (i + 1 < mine) load_cached(t + kWaves);
+    asm volatile("" ::: "memory");
+    s = f32x16{};
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) {
+      const uint32_t word = k_now[w / 4][w % 4];
+      const float unit = mx_unit(s_now >> (8 * (w / 4)) & 255);
+      if constexpr (F32) {
+        float x[8];
+        mx_decode_f32(word, unit, x);
+        logits_step_f32(w, x);
+      } else {
+        logits_step(w, mx_decode_bf16(word, unit));
+      }
+    }
+    update(head.cached - t * kTile);
+    asm volatile("" ::: "memory");
+  }
+
+  // ---- the waves' results become one: sums of each wave, in units of the largest reference, through LDS
+  l = sum_halves(l);
+  float2* const ml = reinterpret_cast<float2*>(mx_lds + C::kLds - kWaves * kTile * 8);
+  if (g == 0) ml[wave * kTile + r] = make_float2(m, l);
+  __syncthreads();
+  float top = kNegBig;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kTile + r].x);
+  const float mine_by = fast_exp2(m - top);
+  float* const sums = reinterpret_cast<float*>(mx_lds);
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = make_float4(o[db][4 * i] * mine_by, o[db][4 * i + 1] * mine_by, o[db][4 * i + 2] * mine_by, o[db][4 * i + 3] * mine_by);
+      *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * db + 8 * i + 4 * g) = x;
+    }
+  __syncthreads();
+  constexpr int kEach = 8;               // elements of a row that a thread writes
+  constexpr int kPerRow = D / kEach;     // threads of a row
+  for (int row = threadIdx.x / kPerRow; row < kTile; row += kWaves * 64 / kPerRow) {
+    const int q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;
+    if (q >= prm.n_q) break;
+    float mq = kNegBig, lq = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mq = fmaxf(mq, ml[w * kTile + row].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) lq += ml[w * kTile + row].y * fast_exp2(ml[w * kTile + row].x - mq);
+    float x[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; e += 4) {
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float4 z = *reinterpret_cast<const float4*>(sums + (w * kTile + row) * C::kSumP + at + e);
+        y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+      }
+      x[e] = y.x, x[e + 1] = y.y, x[e + 2] = y.z, x[e + 3] = y.w;
+    }
+    if (units > 1) {
+      const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + row;
+      float4* to = reinterpret_cast<float4*>(prm.part_o + part * D + at);
+      to[0] = make_float4(x[0], x[1], x[2], x[3]);
+      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+      if (at == 0) prm.part_ml[part] = make_float2(mq, lq);
+      continue;
+    }
+    const float by = 1.f / lq;
+    char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + at * (int)sizeof(T);
+    if constexpr (F32) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
+      reinterpret_cast<float4*>(to)[1] = make_float4(x[4] * by, x[5] * by, x[6] * by, x[7] * by);
+    } else {
+      *reinterpret_cast<u32x4*>(to) = u32x4{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by),
+                                            pack_bf16x2(x[4] * by, x[5] * by), pack_bf16x2(x[6] * by, x[7] * by)};
+    }
+    if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
+  }
+}
+
+// A workgroup per query row of a head that has several units: their sums in units of the largest reference, dealt to groups of
+// D/4 threads.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_mx_join_kernel(const AttendMxParams prm) {
+  constexpr int kPer = D / 4, kGroups = 256 / kPer;
+  __shared__ float4 sums[kGroups][kPer];
+  __shared__ float2 tops[kGroups];
+  const int bh = blockIdx.y, q = blockIdx.x;
+  const int first = prm.parts[bh].x, units = prm.parts[bh].y;
+  if (units <= 1) return;
+  const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer;
+  const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
+  const int64_t part0 = first * step + (int64_t)(q / kTile) * prm.part_rows + q % kTile;
+  float m = kNegBig, l = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int u = grp; u < units; u += kGroups) {
+    const float2 ml = prm.part_ml[part0 + u * step];
+    const float4 y = *reinterpret_cast<const float4*>(prm.part_o + (part0 + u * step) * D + at * 4);
+    const float m_new = fmaxf(m, ml.x);
+    const float old = fast_exp2(m - m_new), now = fast_exp2(ml.x - m_new);
+    m = m_new;
+    l = l * old + ml.y * now;
+    x = make_float4(x.x * old + y.x * now, x.y * old + y.y * now, x.z * old + y.z * now, x.w * old + y.w * now);
+  }
+  sums[grp][at] = x;
+  if (at == 0) tops[grp] = make_float2(m, l);
+  __syncthreads();
+  if (grp > 0) return;
+  float top = kNegBig;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, tops[i].x);
+  l = 0.f;
+  x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const float by = fast_exp2(tops[i].x - top);
+    const float4 y = sums[i][at];
+    l += tops[i].y * by;
+    x = make_float4(x.x + y.x * by, x.y + y.y * by, x.z + y.z * by, x.w + y.w * by);
+  }
+  const float by = 1.f / l;
+  char* to = prm.O.group_row(bh / prm.H, bh % prm.H, prm.q_per_kv, prm.n_resp, q) + at * 4 * (int)sizeof(T);
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<float4*>(to) = make_float4(x.x * by, x.y * by, x.z * by, x.w * by);
+  else
+    *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(x.x * by, x.y * by), pack_bf16x2(x.z * by, x.w * by)};
+  if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// How the tiles are dealt out.
+struct Deal {
+  int qtiles, part_rows;
+  int chunk;      // tiles of a unit, or 0: a unit per head
+  int64_t units;  // at most
+};
+constexpr int kLeastChunk = 8;      // tiles of a unit: two of each wave
+constexpr int kLongHead = 1 << 14;  // keys up to which the heads of a launch that fills the chip are left whole
+
+Deal deal_of(const maskkv_desc* d, int64_t capacity) {
+  const int n_q = query_heads_per_kv(d) * d->n_resp;
+  const int64_t BH = (int64_t)d->B * d->H;
+  Deal x;
+  x.qtiles = (n_q + kTile - 1) / kTile;
+  x.part_rows = n_q < kTile ? n_q : kTile;
+  x.chunk = 0;
+  x.units = BH;
+  // what the host knows of the heads' lengths: no head has more rows than the longest prompt, and all of them as many as there is room for
+  const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
+  if (BH * x.qtiles >= kUnits && most <= kLongHead) return x;
+  const int64_t tiles = capacity / kTile + BH * (1 + (d->n_resp + kTile - 1) / kTile);
+  int64_t chunk = (tiles * x.qtiles + 2 * kUnits - 1) / (2 * kUnits);
+  if (chunk < kLeastChunk) chunk = kLeastChunk;
+  if (chunk * kTile >= most + 2 * kTile) return x;  // (a head's last tiles of both kinds may be short)
+  x.chunk = (int)chunk;
+  x.units = tiles / chunk + BH;
+  return x;
+}
+
+size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
+
+template <typename T, int D>
+int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) {
+  using C = MxCfg<T, D>;
+  static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
+  const int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
+  if (groups > 0x7FFFFFFF) {
+    set_error("attend_mx: %lld workgroups are more than a launch can have", (long long)groups);
+    return MASKKV_ESHAPE;
+  }
+  const auto kernel = attend_mx_kernel<T, D>;
+  if (C::kLds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+    if (e != hipSuccess) {
+      set_error("attend_mx: hipFuncSetAttribute: %s", hipGetErrorString(e));
+      return MASKKV_EHIP;
     }
   }
-  __syncthreads();
-  if (kThreads / D == 4) {
-    if (t >= 2 * D) half[t / D - 2][t % D] = o;
-    __syncthreads();
-    if (t < 2 * D) o += half[t / D][t % D];
-    __syncthreads();
-  }
-  if (t >= D && t < 2 * D) half[0][t - D] = o;
-  __syncthreads();
-  if (t < D) {
-    o = (o + half[0][t]) / l;
-    char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, i);
-    if (sizeof(T) == 2)
-      reinterpret_cast<uint16_t*>(to)[t] = (uint16_t)pack_bf16x2(o, o);
-    else
-      reinterpret_cast<float*>(to)[t] = o;
-  }
-  if (t == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + i] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), C::kLds, stream, prm);
+  if (int e = check_launch("attend_mx")) return e;
+  if (!deal.chunk) return MASKKV_OK;
+  hipLaunchKernelGGL((attend_mx_join_kernel<T, D>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(256), 0, stream, prm);
+  return check_launch("attend_mx (join)");
 }
 
 }  // namespace
 
-size_t attend_mx_workspace_bytes(const maskkv_desc*, int64_t) { return 0; }
+size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
+  const Deal x = deal_of(d, capacity);
+  if (!x.chunk) return 0;
+  const size_t rows = (size_t)x.units * x.qtiles * x.part_rows;
+  return pad256(rows * d->d * 4) + pad256(rows * 8) + pad256((size_t)d->B * d->H * 8);
+}
 
 int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,
-                     const View& V2, float scale, const View& O, float* lse, void*, hipStream_t stream) {
+                     const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream) {
+  const Deal deal = deal_of(d, capacity);
   AttendMxParams prm;
   prm.Q = Q;
   prm.K2 = K2;
@@ -124,24 +493,23 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
   prm.cu = cu_budget;
   prm.capacity = capacity;
   prm.H = d->H;
+  prm.BH = d->B * d->H;
   prm.q_per_kv = query_heads_per_kv(d);
   prm.n_resp = d->n_resp;
   prm.n_q = prm.q_per_kv * d->n_resp;
+  prm.qtiles = deal.qtiles;
+  prm.chunk = deal.chunk;
+  prm.part_rows = deal.part_rows;
   prm.c = scale * kLog2e;
   prm.lse = lse;
-  const dim3 grid((unsigned)prm.n_q, (unsigned)(d->B * d->H));
-  if (d->dtype == MASKKV_BF16) {
-    if (d->d == 128)
-      hipLaunchKernelGGL((attend_mx_kernel<bf16_t, 128>), grid, dim3(kThreads), 0, stream, prm);
-    else
-      hipLaunchKernelGGL((attend_mx_kernel<bf16_t, 64>), grid, dim3(kThreads), 0, stream, prm);
-  } else {
-    if (d->d == 128)
-      hipLaunchKernelGGL((attend_mx_kernel<float, 128>), grid, dim3(kThreads), 0, stream, prm);
-    else
-      hipLaunchKernelGGL((attend_mx_kernel<float, 64>), grid, dim3(kThreads), 0, stream, prm);
-  }
-  return check_launch("attend_mx");
+  const size_t rows = (size_t)deal.units * deal.qtiles * deal.part_rows;
+  char* ws = reinterpret_cast<char*>(workspace);
+  prm.part_o = reinterpret_cast<float*>(ws);
+  prm.part_ml = reinterpret_cast<float2*>(ws + pad256(rows * d->d * 4));
+  prm.parts = reinterpret_cast<int2*>(ws + pad256(rows * d->d * 4) + pad256(rows * 8));
+  if (d->dtype == MASKKV_BF16)
+    return d->d == 128 ? launch_one<bf16_t, 128>(prm, deal, stream) : launch_one<bf16_t, 64>(prm, deal, stream);
+  return d->d == 128 ? launch_one<float, 128>(prm, deal, stream) : launch_one<float, 64>(prm, deal, stream);
 }
 
 }  // namespace maskkv
