@@ -67,8 +67,9 @@ def attend(Q, K, V, scale=None):
 def accumulate(Q, K, lse, decay=0.0, before=None, scale=None):
     """What each row of K gets from the queries with the given normalisers, on top of decay * before."""
     Q, K, lse = (np.asarray(a, dtype=np.float64) for a in (Q, K, lse))
-    s = Q @ K.T * (1.0 / math.sqrt(Q.shape[1]) if scale is None else scale)
-    got = np.exp(s - lse[:, None]).sum(axis=0)
+    voting = lse != np.inf                              # the others add nothing, whatever they hold
+    s = Q[voting] @ K.T * (1.0 / math.sqrt(Q.shape[1]) if scale is None else scale)
+    got = np.exp(s - lse[voting, None]).sum(axis=0)
     return got if decay == 0.0 else decay * np.asarray(before, dtype=np.float64) + got
 
 

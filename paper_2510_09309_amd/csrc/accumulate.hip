@@ -1,12 +1,20 @@
 // The attention that each cached row gets, added up over the denoising steps: for a cached row k of a head
 //   out = decay * in + sum_i exp(q_i . k * scale - lse_i)    over the query rows i of the head's group.
 //
-// A thread per cached row, the query rows in order.
+// A wave holds 32 rows of the cache as the A operand of its matrix instructions for as long as it takes all query rows past
+// them, 32 at a step: a lane then owns one query, whose normaliser is one number, and adds up what that query gives to 16 of the
+// rows; the lanes' sums meet once, at the end.  The queries come through LDS, moved as whole rows.
+//
+// Where there are many cached rows the four waves of a workgroup hold 32 each and share the queries (SHARE); where there
+// are few, all waves hold the same 32 and take the steps in turn.  Sums have a fixed order either way.
 #include "mx.hpp"
 
 namespace maskkv {
 
 namespace {
+
+constexpr int kUnits = 256;  // compute units
+constexpr int kTile = 32;    // cached rows of a wave, query rows of a step
 
 struct AccumulateParams {
   View Q;
@@ -21,52 +29,189 @@ struct AccumulateParams {
   float* out;
 };
 
-template <typename T>
-__device__ __forceinline__ float element(const char* p, int i) {
-  if (sizeof(T) == 2) return as_f32((uint32_t) reinterpret_cast<const uint16_t*>(p)[i] << 16);
-  return reinterpret_cast<const float*>(p)[i];
-}
+template <typename T, int D, int WAVES, bool SHARE>
+struct AccCfg {
+  static constexpr int kRowB = D * (int)sizeof(T);
+  static constexpr int kPPR = kRowB / 16;             // pieces of 16 bytes in a row
+  static constexpr int kMovers = SHARE ? WAVES : 1;   // waves that move a step's queries
+  static constexpr int kRPL = kMovers * 64 / kPPR;    // rows of a load of theirs
+  static constexpr int kLoads = kTile / kRPL;
+  static constexpr int kStepB = kTile * kRowB;
+  static constexpr int kLds = (SHARE ? 2 : WAVES) * kStepB;  // two steps, or one of each wave
+  __device__ static uint32_t swz(uint32_t row) { return sizeof(T) == 2 && D == 64 ? (row >> 1) & 7 : row & 15; }
+};
 
-template <typename T, int D, bool MX>
-__global__ __launch_bounds__(256) void accumulate_kernel(const AccumulateParams prm) {
-  const int64_t total = min((int64_t)prm.cu[prm.BH], prm.capacity);
-  const int64_t first = (int64_t)blockIdx.x * 256 + (threadIdx.x & ~63);
-  if (first >= total) return;
-  const int64_t row = min(first + (threadIdx.x & 63), total - 1);
-  int bh = head_of_row(prm.cu, prm.BH, (int)first);
-  while (bh + 1 < prm.BH && prm.cu[bh + 1] <= row) ++bh;
-  float k[D];
-  if (MX) {
+template <typename T, int D, bool MX, int WAVES, bool SHARE>
+__global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const AccumulateParams prm) {
+  using C = AccCfg<T, D, WAVES, SHARE>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int kRows = SHARE ? WAVES * kTile : kTile;  // cached rows of a workgroup
+  extern __shared__ __attribute__((aligned(16))) char acc_lds[];
+  __shared__ float part[WAVES][kTile];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  // Each XCD (workgroups whose numbers are congruent modulo 8) takes a run of units: a head's queries stay in one L2.
+  const int unit = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  const int capacity = (int)prm.capacity;
+  int first_unit = 0, units = 0;
+  const int bh = head_of_unit(prm.BH, unit, [&](int i) {
+    const int a = min(prm.cu[i], capacity), z = min(prm.cu[i + 1], capacity);
+    return max(z - a + kRows - 1, 0) / kRows;
+  }, first_unit, units);
+  if (bh < 0) return;
+  const int b = bh / prm.H, h = bh % prm.H;
+  const int last = min(prm.cu[bh + 1], capacity) - 1;
+  const int row0 = min(prm.cu[bh], capacity) + (unit - first_unit) * kRows + (SHARE ? wave * kTile : 0);  // of this wave
+  const int64_t row = min(row0 + r, last);
+
+  const int steps = (prm.n_q + kTile - 1) / kTile;
+  constexpr int kEvery = SHARE ? 1 : WAVES;  // a wave's steps: every so many
+  const int mover = SHARE ? threadIdx.x : lane;
+  u32x4 moved[C::kLoads];
+  float lse = 0.f;
+  auto load_step = [&](int s) {
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      float x[8];
-      mx_decode_f32(reinterpret_cast<const uint32_t*>(prm.cache.k_codes + row * (D / 2))[i],
-                    mx_unit(reinterpret_cast<const uint8_t*>(prm.cache.k_scales)[row * (D / 32) + i / 4]), x);
+    for (int j = 0; j < C::kLoads; ++j) {
+      const int i = min(s * kTile + j * C::kRPL + mover / C::kPPR, prm.n_q - 1);
+      moved[j] = *reinterpret_cast<const u32x4*>(prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, i) + mover % C::kPPR * 16);
+    }
+    lse = s * kTile + r < prm.n_q ? prm.lse[(int64_t)bh * prm.n_q + s * kTile + r] : INFINITY;
+  };
+  auto store_step = [&](char* to) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) k[8 * i + j] = x[j];
+    for (int j = 0; j < C::kLoads; ++j) {
+      const uint32_t i = j * C::kRPL + mover / C::kPPR, p = mover % C::kPPR;
+      *reinterpret_cast<u32x4*>(to + i * C::kRowB + ((p ^ C::swz(i)) << 4)) = moved[j];
+    }
+  };
+  const int s0 = SHARE ? 0 : wave;
+  if (s0 < steps) load_step(s0);
+
+  // ---- this lane's half of a cached row
+  u32x4 kf[C::kPPR / 2];
+  if constexpr (MX) {
+    const char* codes = prm.cache.k_codes + row * (D / 2) + g * (D / 4);
+    const uint8_t* scales = reinterpret_cast<const uint8_t*>(prm.cache.k_scales) + row * (D / 32) + g * (D / 64);
+    u32x4 c[D / 64];
+    float unit_of[D / 64];
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) {
+      c[j] = reinterpret_cast<const u32x4*>(codes)[j];
+      unit_of[j] = mx_unit(scales[j]);
+    }
+#pragma unroll
+    for (int w = 0; w < D / 16; ++w) {
+      const uint32_t word = c[w / 4][w % 4];
+      if constexpr (F32) {
+        float x[8];
+        mx_decode_f32(word, unit_of[w / 4], x);
+        kf[2 * w] = u32x4{as_u32(x[0]), as_u32(x[1]), as_u32(x[2]), as_u32(x[3])};
+        kf[2 * w + 1] = u32x4{as_u32(x[4]), as_u32(x[5]), as_u32(x[6]), as_u32(x[7])};
+      } else {
+        kf[w] = mx_decode_bf16(word, unit_of[w / 4]);
+      }
     }
   } else {
+    const u32x4* k = reinterpret_cast<const u32x4*>(prm.Kc + row * C::kRowB + g * (C::kRowB / 2));
 #pragma unroll
-    for (int i = 0; i < D; ++i) k[i] = element<T>(prm.Kc + row * (D * (int)sizeof(T)), i);
+    for (int i = 0; i < C::kPPR / 2; ++i) kf[i] = k[i];
   }
-  float sum = 0.f;
-  for (int i = 0; i < prm.n_q; ++i) {
-    const char* q = prm.Q.group_row(bh / prm.H, bh % prm.H, prm.q_per_kv, prm.n_resp, i);
-    float s = 0.f;
+
+  float sum[16];
 #pragma unroll
-    for (int j = 0; j < D; ++j) s = fmaf(element<T>(q, j), k[j], s);
-    sum += fast_exp2(fmaf(s, prm.c, -prm.lse[(int64_t)bh * prm.n_q + i] * kLog2e));
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  auto take = [&](const char* from, float lse_now) {
+    f32x16 x = {};
+#pragma unroll
+    for (int i = 0; i < C::kPPR / 2; ++i)
+      mfma_step<T>(kf[i], *reinterpret_cast<const u32x4*>(from + r * C::kRowB + (((g * (C::kPPR / 2) + i) ^ C::swz(r)) << 4)), x);
+    const float by = -lse_now * kLog2e;
+    const bool none = lse_now == INFINITY;  // (adds nothing, whatever the query holds)
+    if (__any(none)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] += none ? 0.f : fast_exp2(fmaf(x[i], prm.c, by));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(x[i], prm.c, by));
+    }
+  };
+  if constexpr (SHARE) {
+    store_step(acc_lds);
+    __syncthreads();
+    for (int s = 0; s < steps; ++s) {
+      const float lse_now = lse;
+      if (s + 1 < steps) load_step(s + 1);
+      take(acc_lds + (s & 1) * C::kStepB, lse_now);
+      if (s + 1 < steps) store_step(acc_lds + ((s + 1) & 1) * C::kStepB);
+      __syncthreads();
+    }
+  } else {
+    char* own = acc_lds + wave * C::kStepB;
+    for (int s = s0; s < steps; s += kEvery) {
+      store_step(own);
+      const float lse_now = lse;
+      if (s + kEvery < steps) load_step(s + kEvery);
+      asm volatile("" ::: "memory");
+      take(own, lse_now);
+      asm volatile("" ::: "memory");
+    }
   }
-  if (first + (threadIdx.x & 63) < total) prm.out[row] = prm.decay > 0.f ? fmaf(prm.decay, prm.in[row], sum) : sum;
+
+  // ---- a row's sum over the 32 lanes of its half: each exchange leaves a lane half of the rows
+#pragma unroll
+  for (int half = 8; half > 0; half >>= 1) {
+    const bool upper = lane & 2 * half;
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const float keep = upper ? sum[half + i] : sum[i], give = upper ? sum[i] : sum[half + i];
+      sum[i] = keep + __shfl_xor(give, 2 * half, 64);
+    }
+  }
+  float total = sum[0] + __shfl_xor(sum[0], 1, 64);
+  const int i = (lane >> 1) & 15, at = 8 * (i / 4) + 4 * g + i % 4;
+  const bool mine = !(lane & 1);
+  if constexpr (!SHARE) {
+    if (mine) part[wave][at] = total;
+    __syncthreads();
+    if (wave > 0) return;
+    total = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) total += part[w][at];
+  }
+  if (mine && row0 + at <= last) prm.out[row0 + at] = prm.decay > 0.f ? fmaf(prm.decay, prm.in[row0 + at], total) : total;
+}
+
+template <typename T, int D, bool MX, int WAVES, bool SHARE>
+int launch_form(const AccumulateParams& prm, hipStream_t stream) {
+  using C = AccCfg<T, D, WAVES, SHARE>;
+  static_assert(C::kLds + WAVES * kTile * 4 <= 160 * 1024, "a workgroup's LDS");
+  const int rows = SHARE ? WAVES * kTile : kTile;
+  const int64_t groups = (prm.capacity / rows + prm.BH + 7) / 8 * 8;  // (each head's last ones may be short)
+  const auto kernel = accumulate_kernel<T, D, MX, WAVES, SHARE>;
+  if (C::kLds > 48 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+    if (e != hipSuccess) {
+      set_error("accumulate: cannot raise dynamic LDS limit: %s", hipGetErrorString(e));
+      (void)hipGetLastError();
+      return MASKKV_EHIP;
+    }
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(WAVES * 64), C::kLds, stream, prm);
+  return check_launch("accumulate");
+}
+
+// Few: there are fewer tiles of cached rows than waves that fill the chip, and more than one step of queries to deal to waves instead.
+template <typename T, int D, bool MX>
+int launch_rows(const AccumulateParams& prm, hipStream_t stream) {
+  const int64_t tiles = prm.capacity / kTile + prm.BH;
+  const int steps = (prm.n_q + kTile - 1) / kTile;
+  if (steps > 1 && tiles < 4 * kUnits) return launch_form<T, D, MX, 4, false>(prm, stream);
+  return launch_form<T, D, MX, 4, true>(prm, stream);
 }
 
 template <typename T, int D>
-void launch_one(const AccumulateParams& prm, hipStream_t stream) {
-  const dim3 grid((unsigned)((prm.capacity + 255) / 256));
-  if (prm.Kc)
-    hipLaunchKernelGGL((accumulate_kernel<T, D, false>), grid, dim3(256), 0, stream, prm);
-  else
-    hipLaunchKernelGGL((accumulate_kernel<T, D, true>), grid, dim3(256), 0, stream, prm);
+int launch_one(const AccumulateParams& prm, hipStream_t stream) {
+  return prm.Kc ? launch_rows<T, D, false>(prm, stream) : launch_rows<T, D, true>(prm, stream);
 }
 
 }  // namespace
@@ -91,10 +236,8 @@ int launch_accumulate(const maskkv_desc* d, const View& Q, const void* Kc, const
   prm.in = weights_in;
   prm.out = weights_out;
   if (d->dtype == MASKKV_BF16)
-    d->d == 128 ? launch_one<bf16_t, 128>(prm, stream) : launch_one<bf16_t, 64>(prm, stream);
-  else
-    d->d == 128 ? launch_one<float, 128>(prm, stream) : launch_one<float, 64>(prm, stream);
-  return check_launch("accumulate");
+    return d->d == 128 ? launch_one<bf16_t, 128>(prm, stream) : launch_one<bf16_t, 64>(prm, stream);
+  return d->d == 128 ? launch_one<float, 128>(prm, stream) : launch_one<float, 64>(prm, stream);
 }
 
 }  // namespace maskkv

@@ -73,31 +73,6 @@ __device__ __forceinline__ Head head_at(const AttendMxParams& prm, int bh) {
   return x;
 }
 
-// The head of a unit when every head has as many units as its tiles ask for, and the number of its first; -1 behind the last.
-__device__ __forceinline__ int head_of_unit(const AttendMxParams& prm, int unit, int& first_unit, int& units) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int base = 0; base < prm.BH; base += 64) {
-    const int bh = base + lane;
-    const int own = bh < prm.BH ? (head_at(prm, min(bh, prm.BH - 1)).tiles + prm.chunk - 1) / prm.chunk : 0;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      upto += lane >= o ? v : 0;
-    }
-    const uint64_t over = __ballot(before + upto > unit);
-    if (over) {
-      const int at = __builtin_ctzll(over);
-      units = __builtin_amdgcn_readlane(own, at);
-      first_unit = before + __builtin_amdgcn_readlane(upto, at) - units;
-      return base + at;
-    }
-    before += __builtin_amdgcn_readlane(upto, 63);
-  }
-  return -1;
-}
-
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx_kernel(const AttendMxParams prm) {
   using C = MxCfg<T, D>;
@@ -108,11 +83,10 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
   int bh = unit, first_unit = unit, units = 1;
   if (prm.chunk)
-    bh = head_of_unit(prm, unit, first_unit, units);
+    bh = head_of_unit(prm.BH, unit, [&](int i) { return (head_at(prm, i).tiles + prm.chunk - 1) / prm.chunk; }, first_unit, units);
   else if (bh >= prm.BH)
     bh = -1;
   if (bh < 0) return;
-  bh = __builtin_amdgcn_readfirstlane(bh);
   const int b = bh / prm.H, h = bh % prm.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;

@@ -82,4 +82,30 @@ __device__ __forceinline__ int head_of_row(const int32_t* cu, int BH, int row) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The head of a unit of work when head bh has count(bh) units, -1 behind the last; what it is the first of, and how many the head
+// has.  Found by a wave, which counts 64 heads at a time.
+template <typename F>
+__device__ __forceinline__ int head_of_unit(int BH, int unit, F count, int& first, int& units) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base < BH; base += 64) {
+    const int own = base + lane < BH ? count(base + lane) : 0;
+    int upto = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(upto, o, 64);
+      upto += lane >= o ? v : 0;
+    }
+    const uint64_t over = __ballot(before + upto > unit);
+    if (over) {
+      const int at = __builtin_ctzll(over);
+      units = __builtin_amdgcn_readlane(own, at);
+      first = before + __builtin_amdgcn_readlane(upto, at) - units;
+      return __builtin_amdgcn_readfirstlane(base + at);
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return -1;
+}
+
 }  // namespace maskkv

@@ -48,7 +48,7 @@ HALF = {"bf16": 2.0 ** -8, "f32": U}
 
 
 def logit_error(Q, K, scale, *more):
-    Q, K = np.abs(np.asarray(Q, np.float64)), np.abs(np.asarray(K, np.float64))
+    Q, K = np.abs(np.nan_to_num(np.asarray(Q, np.float64))), np.abs(np.asarray(K, np.float64))    # (NaN: of rows that do not count)
     S = Q @ K.T * scale
     top = max([S.max() if S.size else 0.0] + [np.abs(x).max() for x in more if np.size(x)])
     return U * ((Q.shape[1] + 4) * (S.max() if S.size else 0.0) + 8 * top + 64)

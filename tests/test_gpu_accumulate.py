@@ -94,6 +94,11 @@ def test_rows_without_a_weight(mx, n):
         lse[:, ::2] = np.inf
     check(11, 1, 2, 64, "bf16", n, [50, 40], mx, edit=some)
 
+    def not_even_numbers(Q, K, lse):
+        lse[:, 1::2], Q[:, :, 1::2] = np.inf, np.nan
+    check(15, 1, 2, 64, "bf16", n, [50, 40], mx, edit=not_even_numbers)
+    check(16, 1, 2, 128, "f32", n, [50, 40], mx, edit=not_even_numbers)
+
     def all_of_them(Q, K, lse):
         lse[:] = np.inf
     got = check(12, 1, 2, 64, "bf16", n, [50, 40], mx, edit=all_of_them)
