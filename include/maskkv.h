@@ -321,8 +321,8 @@ int maskkv_accumulate_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, c
  * rows, idx, idx_out: DEVICE int32 [capacity_out], [capacity], [capacity_out]; idx and idx_out (the rows' prompt positions)
  * may both be NULL, and so may weights_out.  Where more than capacity_out rows stay, those beyond it are not written while
  * cu_out holds the unclipped sums; sum_h budgets[bh] and capacity are always enough.  The smaller cache has buffers
- * of its own: an output that overlaps an input is MASKKV_EINVAL.  rows is written and read by the call.  _mx: the same for a cache in 4
- * bits, whose bytes are moved as they are.
+ * of its own: an output that overlaps an input is MASKKV_EINVAL.  P_max may not exceed 4 Mi tokens, as in maskkv_select.  _mx: the same
+ * for a cache in 4 bits, whose bytes are moved as they are.
  */
 int maskkv_evict(const maskkv_desc* desc, const float* weights, const int32_t* cu_budget, int64_t capacity,
                  const int32_t* budgets, const void* Kc, const void* Vc, const int32_t* idx, void* Kc_out, void* Vc_out,

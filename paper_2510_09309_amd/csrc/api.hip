@@ -567,6 +567,10 @@ static int evict_entry(const char* what, const maskkv_desc* desc, const float* w
     set_error("%s: cu_budget, budgets, cu_out, weights or rows is NULL, or only one of idx and idx_out is", what);
     return MASKKV_EINVAL;
   }
+  if (desc->P_max > select_max_prompt()) {
+    set_error("%s: heads of more than %lld rows are not supported (P_max = %d)", what, (long long)select_max_prompt(), desc->P_max);
+    return MASKKV_ESHAPE;
+  }
   const int64_t heads = (int64_t)desc->B * desc->H;
   struct Span {
     const void* p;

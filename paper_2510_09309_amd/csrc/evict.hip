@@ -1,22 +1,25 @@
 // Further eviction from a packed cache: of each head the rows of largest weight stay.
 //
-// Two launches.  The first, a workgroup per head, finds the smallest weight that stays by a search over the bits of the
-// weights' order, and lists the rows that stay, ascending.  The second moves them: a packed row's number is all it needs, so
-// no search for heads comes before its loads.
-#include "kernels.hpp"
+// One launch.  A workgroup moves up to `per` rows of the smaller cache that belong to one head.  It finds that head from the
+// budgets, and which of the head's rows they are by itself, from all of the head's weights: several workgroups of a head do
+// the same search, which costs the latency of one, where a list made by one of them would cost a launch between the two.
+//
+// The search is for the smallest weight that stays, two bits of the weights' order a round: every wave counts its rows at or above
+// three candidates by ballots and the waves' counts meet in LDS, one barrier a round; it ends when a candidate has as many rows as
+// stay.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again every round.
+#include "mx.hpp"
 
 namespace maskkv {
 
 namespace {
-
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 
 struct EvictParams {
   const float* weights;
   const int32_t *cu, *budgets, *idx;
   int64_t capacity, capacity_out;
   int BH;
+  int per;        // rows of a workgroup at most
+  int row_shift;  // 16-byte pieces of a row, both large arrays together: 1 << row_shift
   int32_t *rows, *idx_out, *cu_out;
   float* weights_out;
   MovedRows moved;
@@ -30,96 +33,215 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int length_of(const EvictParams& prm, int bh, int& first) {
+struct HeadRows {
+  int first, n, stay;
+};
+__device__ __forceinline__ HeadRows rows_of(const EvictParams& prm, int bh) {
   const int capacity = (int)prm.capacity;
-  first = min(prm.cu[bh], capacity);
-  return max(min(prm.cu[bh + 1], capacity) - first, 0);
-}
-__device__ __forceinline__ int stay_of(const EvictParams& prm, int bh) {
-  int first;
-  const int n = length_of(prm, bh, first);
-  return min(max(prm.budgets[bh], 0), n);
-}
-
-// The sum of a value over the workgroup.
-__device__ __forceinline__ int sum_all(int v, int* part) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  int s = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) s += part[w];
-  return s;
+  const int budget = prm.budgets[bh], a = min(prm.cu[bh], capacity), z = min(prm.cu[bh + 1], capacity);
+  HeadRows x;
+  x.first = a;
+  x.n = max(z - a, 0);
+  x.stay = min(max(budget, 0), x.n);
+  return x;
 }
 
-__global__ __launch_bounds__(kThreads) void evict_rows_kernel(const EvictParams prm) {
-  __shared__ int part[kWaves], ties_of[kWaves];
-  const int bh = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  int before = 0;
-  for (int i = t; i < bh; i += kThreads) before += stay_of(prm, i);
-  before = sum_all(before, part);
-  int first;
-  const int n = length_of(prm, bh, first), k = stay_of(prm, bh);
-  if (t == 0) {
-    prm.cu_out[bh] = before;
-    if (bh == prm.BH - 1) prm.cu_out[prm.BH] = before + k;
-  }
-  if (k == 0) return;
-  const float* w = prm.weights + first;
-  uint32_t least = 0;  // the largest order that k rows have at least
-  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
-    int c = 0;
-    for (int i = t; i < n; i += kThreads) c += order_of(w[i]) >= (least | bit);
-    if (sum_all(c, part) >= k) least |= bit;
-  }
-  int above = 0;
-  for (int i = t; i < n; i += kThreads) above += order_of(w[i]) > least;
-  int ties = k - sum_all(above, part);  // so many of the rows at `least` stay, the first ones
-  int at = before;
-  for (int base = 0; base < n; base += kThreads) {
-    const int i = base + t;
-    const uint32_t o = i < n ? order_of(w[i]) : 0u;
-    const uint64_t over = __ballot(i < n && o > least), same = __ballot(i < n && o == least);
-    __syncthreads();
-    if (lane == 0) {
-      part[wave] = __popcll(over);
-      ties_of[wave] = __popcll(same);
-    }
-    __syncthreads();
-    int overs = 0, sames = 0, all_overs = 0, all_sames = 0;  // before this wave, and of all waves
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      overs += v < wave ? part[v] : 0;
-      sames += v < wave ? ties_of[v] : 0;
-      all_overs += part[v];
-      all_sames += ties_of[v];
-    }
-    const uint64_t below = (1ull << lane) - 1;
-    overs += __popcll(over & below);
-    sames += __popcll(same & below);
-    const bool stays = (over >> lane & 1) || ((same >> lane & 1) && sames < ties);
-    const int to = at + overs + min(sames, ties);
-    if (stays && to < prm.capacity_out) prm.rows[to] = first + i;
-    at += all_overs + min(all_sames, ties);
-    ties -= min(all_sames, ties);
-  }
-}
-
-// A wave moves one row's bytes of every array, 2 a lane and step.
-__global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams prm) {
+// How many rows stay of the heads before each, by one wave.
+__device__ __forceinline__ void write_prefix(const EvictParams& prm) {
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= min((int64_t)prm.cu_out[prm.BH], prm.capacity_out)) return;
-  const int64_t from = prm.rows[row];
+  int before = 0;
+  for (int base = 0; base < prm.BH; base += 64) {
+    const int bh = base + lane;
+    const int stay = bh < prm.BH ? rows_of(prm, bh).stay : 0;
+    const int upto = wave_prefix(stay);
+    if (bh < prm.BH) prm.cu_out[bh] = before + upto - stay;
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (lane == 0) prm.cu_out[prm.BH] = before;
+}
+
+// The numbers of the rows that stay with ranks lo .. hi-1 among the head's, into `list`.  VALUES: rows of a thread, in registers, or 0.
+template <int THREADS, int VALUES>
+__device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int32_t* list, int (*counts)[THREADS / 64][4]) {
+  constexpr int kWaves = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int each = VALUES ? VALUES : (n + THREADS - 1) / THREADS;
+  const int row0 = wave * each * 64 + lane;  // a wave's rows lie side by side, 64 a step
+  uint32_t held[VALUES ? VALUES : 1];
+  auto read = [&](int v) {
+    const int row = row0 + v * 64;
+    const float x = w[min(row, n - 1)];
+    return row < n ? order_of(x) : 0u;
+  };
+  if constexpr (VALUES > 0) {
 #pragma unroll
-  for (int m = 0; m < kMoved; ++m)
-    for (int i = lane * 2; i < prm.moved.bytes[m]; i += 128)
-      *reinterpret_cast<uint16_t*>(prm.moved.to[m] + row * prm.moved.bytes[m] + i) =
-          *reinterpret_cast<const uint16_t*>(prm.moved.from[m] + from * prm.moved.bytes[m] + i);
-  if (lane == 0 && prm.idx) prm.idx_out[row] = prm.idx[from];
-  if (lane == 0 && prm.weights_out) prm.weights_out[row] = prm.weights[from];
+    for (int v = 0; v < VALUES; ++v) held[v] = read(v);
+  }
+  auto over_rows = [&](auto f) {
+    if constexpr (VALUES > 0) {
+#pragma unroll
+      for (int v = 0; v < VALUES; ++v) f(held[v], v);
+    } else {
+#pragma unroll 8
+      for (int v = 0; v < each; ++v) f(read(v), v);
+    }
+  };
+
+  uint32_t least = 0;     // a row at or above it stays, or may
+  bool exact = k == n;    // just those stay
+  for (int shift = 30, round = 0; shift >= 0 && !exact; shift -= 2, ++round) {
+    int c[3] = {0, 0, 0};
+    over_rows([&](uint32_t o, int) {
+#pragma unroll
+      for (int j = 0; j < 3; ++j) c[j] += __popcll(__ballot(o >= (least | (uint32_t)(j + 1) << shift)));
+    });
+    int* mine = counts[round & 1][wave];
+    if (lane == 0) {
+      mine[0] = c[0];
+      mine[1] = c[1];
+      mine[2] = c[2];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+      int s;
+      if (kWaves == 4) {
+        s = counts[round & 1][0][j] + counts[round & 1][1][j] + counts[round & 1][2][j] + counts[round & 1][3][j];
+      } else {
+        s = counts[round & 1][lane % kWaves][j];  // (16 waves: the sum over a row of 16 lanes)
+        s = plus_dpp<0x121, 0xf>(s);
+        s = plus_dpp<0x122, 0xf>(s);
+        s = plus_dpp<0x124, 0xf>(s);
+        s = plus_dpp<0x128, 0xf>(s);
+      }
+      c[j] = __builtin_amdgcn_readfirstlane(s);
+    }
+    uint32_t digit = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (c[j] >= k) {
+        digit = j + 1;
+        exact = c[j] == k;
+      }
+    least |= digit << shift;
+  }
+  const auto over = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && (exact ? o >= least : o > least)); };
+  const auto same = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && !exact && o == least); };
+  int overs = 0, sames = 0;
+  over_rows([&](uint32_t o, int v) {
+    overs += __popcll(over(o, v));
+    sames += __popcll(same(o, v));
+  });
+  if constexpr (VALUES > 0) {  // (the ballots are formed again below: kept from here to there they would take all registers)
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) asm volatile("" : "+v"(held[v]));
+  }
+  __syncthreads();
+  if (lane == 0) {
+    counts[0][wave][0] = overs;
+    counts[0][wave][1] = sames;
+  }
+  __syncthreads();
+  int ties = k;  // so many of the rows at `least` stay, the first ones
+  overs = sames = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    const int a = counts[0][i][0], b = counts[0][i][1];
+    ties -= a;
+    overs += i < wave ? a : 0;
+    sames += i < wave ? b : 0;
+  }
+  ties = __builtin_amdgcn_readfirstlane(ties);
+  overs = __builtin_amdgcn_readfirstlane(overs);
+  sames = __builtin_amdgcn_readfirstlane(sames);
+  const uint64_t below = (1ull << lane) - 1;
+  over_rows([&](uint32_t o, int v) {
+    const uint64_t a = over(o, v), b = same(o, v);
+    const int before = sames + __popcll(b & below);
+    const int rank = overs + __popcll(a & below) + min(before, ties);
+    const bool stays = (a >> lane & 1) || ((b >> lane & 1) && before < ties);
+    if (stays && rank >= lo && rank < hi) list[rank - lo] = row0 + v * 64;
+    overs += __popcll(a);
+    sames += __popcll(b);
+  });
+}
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams prm) {
+  extern __shared__ int32_t list[];  // [per]
+  __shared__ int counts[2][THREADS / 64][4];
+  const int lane = threadIdx.x & 63;
+  if (blockIdx.x == 0 && threadIdx.x < 64) write_prefix(prm);
+
+  // ---- the head of this workgroup's rows, how many rows stay of the heads before it, and which of its own these are
+  const int unit = blockIdx.x;
+  int before = 0, units_before = 0, bh = -1, part = 0;
+  for (int base = 0; base < prm.BH && bh < 0; base += 64) {
+    const int stay = base + lane < prm.BH ? rows_of(prm, base + lane).stay : 0;
+    const int units = (int)(((uint32_t)stay + prm.per - 1) / prm.per);
+    const int rows_upto = wave_prefix(stay), upto = wave_prefix(units);
+    const uint64_t found = __ballot(units_before + upto > unit);
+    if (found) {
+      const int at = __builtin_ctzll(found);
+      bh = base + at;
+      part = unit - units_before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
+      before += __builtin_amdgcn_readlane(rows_upto, at) - __builtin_amdgcn_readlane(stay, at);
+    } else {
+      units_before += __builtin_amdgcn_readlane(upto, 63);
+      before += __builtin_amdgcn_readlane(rows_upto, 63);
+    }
+  }
+  if (bh < 0) return;
+  const HeadRows x = rows_of(prm, bh);
+  const int lo = part * prm.per;
+  const int64_t to = (int64_t)before + lo;
+  const int rows = (int)min((int64_t)min(x.stay - lo, prm.per), prm.capacity_out - to);
+  if (rows <= 0) return;
+
+  const float* w = prm.weights + x.first;
+  if (x.n <= THREADS)
+    list_rows<THREADS, 1>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  else if (x.n <= THREADS * 4)
+    list_rows<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  else if (x.n <= THREADS * 16)
+    list_rows<THREADS, 16>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  else if (x.n <= THREADS * 32)
+    list_rows<THREADS, 32>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  else
+    list_rows<THREADS, 0>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  __syncthreads();
+
+  // ---- the rows, 16 bytes a thread and step
+  const int pieces = 1 << prm.row_shift, half = pieces / 2;
+  constexpr int kAtOnce = 4;
+  for (int i0 = threadIdx.x; i0 < rows << prm.row_shift; i0 += kAtOnce * THREADS) {
+    u32x4 x4[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = min(i0 + u * THREADS, (rows << prm.row_shift) - 1), piece = i & (pieces - 1), m = piece >= half;
+      const int64_t from = x.first + list[i >> prm.row_shift];
+      x4[u] = *reinterpret_cast<const u32x4*>(prm.moved.from[m] + (from * half + (piece - m * half)) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + u * THREADS, piece = i & (pieces - 1), m = piece >= half;
+      if (i < rows << prm.row_shift)
+        *reinterpret_cast<u32x4*>(prm.moved.to[m] + ((to + (i >> prm.row_shift)) * half + (piece - m * half)) * 16) = x4[u];
+    }
+  }
+  for (int i = threadIdx.x; i < rows; i += THREADS) {
+    const int64_t from = x.first + list[i];
+    prm.rows[to + i] = (int32_t)from;
+    if (prm.idx) prm.idx_out[to + i] = prm.idx[from];
+    if (prm.weights_out) prm.weights_out[to + i] = prm.weights[from];
+    if (prm.moved.bytes[2] == 4) {
+      reinterpret_cast<uint32_t*>(prm.moved.to[2])[to + i] = reinterpret_cast<const uint32_t*>(prm.moved.from[2])[from];
+      reinterpret_cast<uint32_t*>(prm.moved.to[3])[to + i] = reinterpret_cast<const uint32_t*>(prm.moved.from[3])[from];
+    } else if (prm.moved.bytes[2] == 2) {
+      reinterpret_cast<uint16_t*>(prm.moved.to[2])[to + i] = reinterpret_cast<const uint16_t*>(prm.moved.from[2])[from];
+      reinterpret_cast<uint16_t*>(prm.moved.to[3])[to + i] = reinterpret_cast<const uint16_t*>(prm.moved.from[3])[from];
+    }
+  }
 }
 
 }  // namespace
@@ -140,12 +262,19 @@ int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_b
   prm.cu_out = cu_out;
   prm.weights_out = weights_out;
   prm.moved = moved;
-  hipLaunchKernelGGL(evict_rows_kernel, dim3(prm.BH), dim3(kThreads), 0, stream, prm);
-  if (int e = check_launch("evict (rows)")) return e;
+  prm.row_shift = 0;
+  while (16 << prm.row_shift < 2 * moved.bytes[0]) ++prm.row_shift;
+  // Workgroups for two of every compute unit, of 16 rows at least and of no more than the list has room for.
   const int64_t most = capacity_out < capacity ? capacity_out : capacity;  // (no more rows stay than there are)
-  if (most == 0) return MASKKV_OK;
-  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)((most + 3) / 4)), dim3(256), 0, stream, prm);
-  return check_launch("evict (move)");
+  int64_t per = (most + 511) / 512;
+  per = per < 16 ? 16 : per > 8192 ? 8192 : per;
+  prm.per = (int)per;
+  const int64_t groups = most / per + prm.BH;  // (each head's last one may have fewer)
+  if (capacity / prm.BH <= 2048)
+    hipLaunchKernelGGL(evict_kernel<256>, dim3((unsigned)groups), dim3(256), per * 4, stream, prm);
+  else
+    hipLaunchKernelGGL(evict_kernel<1024>, dim3((unsigned)groups), dim3(1024), per * 4, stream, prm);
+  return check_launch("evict");
 }
 
 }  // namespace maskkv

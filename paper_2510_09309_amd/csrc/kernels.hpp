@@ -111,12 +111,12 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
 int launch_accumulate(const maskkv_desc* d, const View& Q, const void* Kc, const MxCache& cache, const int32_t* cu_budget, int64_t capacity,
                       float scale, const float* row_lse, float decay, const float* weights_in, float* weights_out, hipStream_t stream);
 
-// evict.hip.  What is moved with a row that stays: up to four arrays of rows of a multiple of 2 bytes each.
+// evict.hip.  What is moved with a row that stays: two arrays of rows of the same multiple of 16 bytes, and two of rows of 4, 2 or no bytes.
 constexpr int kMoved = 4;
 struct MovedRows {
   const char* from[kMoved];
   char* to[kMoved];
-  int bytes[kMoved];  // of a row; 0: not there
+  int bytes[kMoved];  // of a row
 };
 int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_budget, int64_t capacity, const int32_t* budgets,
                  const MovedRows& moved, const int32_t* idx, int32_t* idx_out, int32_t* rows, float* weights_out, int32_t* cu_out,

@@ -82,6 +82,20 @@ __device__ __forceinline__ int head_of_row(const int32_t* cu, int BH, int row) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// The sum of a value over the lanes up to this one (rows of 16 lanes by shifts, then row ends into the rows behind).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_dpp(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_prefix(int v) {
+  v = plus_dpp<0x111, 0xf>(v);
+  v = plus_dpp<0x112, 0xf>(v);
+  v = plus_dpp<0x114, 0xf>(v);
+  v = plus_dpp<0x118, 0xf>(v);
+  v = plus_dpp<0x142, 0xa>(v);
+  return plus_dpp<0x143, 0xc>(v);
+}
+
 // The head of a unit of work when head bh has count(bh) units, -1 behind the last; what it is the first of, and how many the head
 // has.  Found by a wave, which counts 64 heads at a time.
 template <typename F>
@@ -90,12 +104,7 @@ __device__ __forceinline__ int head_of_unit(int BH, int unit, F count, int& firs
   int before = 0;
   for (int base = 0; base < BH; base += 64) {
     const int own = base + lane < BH ? count(base + lane) : 0;
-    int upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(upto, o, 64);
-      upto += lane >= o ? v : 0;
-    }
+    const int upto = wave_prefix(own);
     const uint64_t over = __ballot(before + upto > unit);
     if (over) {
       const int at = __builtin_ctzll(over);

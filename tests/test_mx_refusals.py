@@ -132,6 +132,11 @@ def test_a_smaller_cache_that_overlaps_the_old_one_is_refused(mk):
         assert c.evict_mx(out=out) == 1 and "overlaps" in c.error()
 
 
+def test_heads_beyond_what_select_keeps_are_refused(mk):
+    c = Calls(mk, P_max=(1 << 22) + 1)
+    assert c.evict() == 2 and c.evict_mx() == 2 and "rows" in c.error()
+
+
 def test_workspace_query(mk):
     d = mk.Desc(B=1, H=2, d=64, dtype=mk.MASKKV_BF16, n_resp=8, P_max=100)
     assert mk.maskkv_attend_mx_workspace_bytes(d, 0) >= 0
