@@ -341,6 +341,219 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   }
 }
 
+// ---- many query rows of bf16: a workgroup of four waves serves 128 of a head, 32 a wave, over tiles of 64 keys that all of them read
+// from LDS as bf16.  Two workgroups share a compute unit, so that one's softmax runs beside the other's products, and within a
+// wave the logits of the next tile are formed beside the softmax of this one.
+//
+// Iteration t reads K(t+1) and V(t), and brings K(t+2) and V(t+1) into the other two of four buffers, which iteration t-1 has
+// read: one barrier an iteration.  Tiles of the cache come through registers, read an iteration ahead and converted on their way
+// into LDS; those of the response by direct transfers.
+constexpr int kWideTile = 64;
+constexpr int kWideQueries = 128;
+
+template <int D>
+struct WideCfg {
+  static constexpr int kRowB = 2 * D;
+  static constexpr int kPPR = kRowB / 16;
+  static constexpr int kSteps = D / 16;
+  static constexpr int kDB = D / 32;
+  static constexpr int kTileB = kWideTile * kRowB;
+  static constexpr int kLds = 4 * kTileB;                  // K(t), K(t+1), V(t), V(t+1)
+  static constexpr int kMoves = kWideTile * kRowB / 4096;  // direct transfers of 1 KiB a wave and tile
+  static constexpr int kMoveRows = 1024 / kRowB;
+  static constexpr int kWords = D / 32;                    // code words of a thread: a quarter of a row
+  __device__ static uint32_t swz_k(uint32_t row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxParams prm) {
+  using C = WideCfg<D>;
+  extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
+  const int slot = blockIdx.x / 8;
+  const int bh = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
+  if (bh >= prm.BH) return;
+  const int b = bh / prm.H, h = bh % prm.H;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  const int first = min(prm.cu[bh], (int)prm.capacity);
+  const int cached = max(min(prm.cu[bh + 1], (int)prm.capacity) - first, 0);
+  const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
+  const int tiles = resp_tiles + (cached + kWideTile - 1) / kWideTile;  // those of the response first
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mx_lds;
+  const uint32_t k_at = lds0, v_at = lds0 + 2 * C::kTileB;
+
+  // ---- tiles on their way
+  const int my_row = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+  uint32_t kc[C::kWords], vc[C::kWords], ks = 0, vs = 0;
+  auto read = [&](int t, const char* codes, const char* scales, uint32_t (&c)[C::kWords], uint32_t& s) {
+    if (t < resp_tiles || t >= tiles) return;
+    const int64_t row = first + min((t - resp_tiles) * kWideTile + my_row, cached - 1);
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(codes + row * (D / 2) + quarter * (D / 8));
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) c[w] = from[w];
+    s = reinterpret_cast<const uint8_t*>(scales)[row * (D / 32) + quarter * (D / 32) / 4];
+  };
+  auto transfer = [&](int t, const View& from, uint32_t to, bool k) {
+#pragma unroll
+    for (int j = 0; j < C::kMoves; ++j) {
+      const uint32_t row = (wave * C::kMoves + j) * C::kMoveRows + (uint32_t)lane / C::kPPR, p = (uint32_t)lane % C::kPPR;
+      const uint32_t piece = k ? p ^ C::swz_k(row) : p ^ v_swizzle<D>(row) << 1;
+      dma16_from(from.row(b, h, min(t * kWideTile + (int)row, prm.n_resp - 1)) + piece * 16, to + (wave * C::kMoves + j) * 1024);
+    }
+  };
+  auto convert = [&](const uint32_t (&c)[C::kWords], uint32_t s, uint32_t to, bool k) {
+    const float unit = mx_unit(s);
+    const uint32_t row = my_row;
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) {
+      const uint32_t p = quarter * C::kWords + w;
+      *in_lds<u32x4>(to + row * C::kRowB + ((k ? p ^ C::swz_k(row) : p ^ v_swizzle<D>(row) << 1) << 4)) = mx_decode_bf16(c[w], unit);
+    }
+  };
+  auto bring_k = [&](int t) {  // K(t) into its buffer
+    if (t >= tiles) return;
+    if (t < resp_tiles)
+      transfer(t, prm.K2, k_at + (t & 1) * C::kTileB, true);
+    else
+      convert(kc, ks, k_at + (t & 1) * C::kTileB, true);
+  };
+  auto bring_v = [&](int t) {
+    if (t >= tiles) return;
+    if (t < resp_tiles)
+      transfer(t, prm.V2, v_at + (t & 1) * C::kTileB, false);
+    else
+      convert(vc, vs, v_at + (t & 1) * C::kTileB, false);
+  };
+  auto read_k = [&](int t) { read(t, prm.cache.k_codes, prm.cache.k_scales, kc, ks); };
+  auto read_v = [&](int t) { read(t, prm.cache.v_codes, prm.cache.v_scales, vc, vs); };
+  auto arrive = [] {  // what this wave has moved and written is there, and so is everyone's behind the barrier
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  read_k(0);
+  read_v(0);
+  const int q0 = qtile * kWideQueries + wave * 32;
+  u32x4 qf[C::kSteps];
+  {
+    const char* q = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, min(q0 + r, prm.n_q - 1)) + g * D;
+#pragma unroll
+    for (int i = 0; i < C::kSteps; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
+  }
+  bring_k(0);
+  read_k(1);
+  bring_k(1);
+  bring_v(0);
+  read_k(2);
+  read_v(1);
+  arrive();
+
+  f32x16 o[C::kDB], s[2], next[2];
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
+  float m = kNegBig, l = 0.f;
+  const float c = prm.c;
+  // fragments of K: of steps [from, to) of the logits of tile t, both blocks of 32 keys
+  auto logits = [&](int t, int from, int to, f32x16 (&x)[2]) {
+    const uint32_t at = k_at + (t & 1) * C::kTileB + r * C::kRowB;
+#pragma unroll
+    for (int i = from; i < to; ++i)
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const u32x4 k = *in_lds<const u32x4>(at + (((C::kPPR / 2 * g + i) ^ C::swz_k(r)) << 4), kb * 32 * C::kRowB);
+        mfma_step<bf16_t>(k, qf[i], x[kb]);
+      }
+  };
+  s[0] = s[1] = f32x16{};
+  logits(0, 0, C::kSteps, s);
+  arrive();  // (K(2) takes the place of K(0))
+
+  for (int t = 0; t < tiles; ++t) {
+    bring_k(t + 2);
+    bring_v(t + 1);
+    read_k(t + 3);
+    read_v(t + 2);
+    next[0] = next[1] = f32x16{};
+    const bool more = t + 1 < tiles;
+    if (more) logits(t + 1, 0, C::kSteps / 2, next);
+    const int left = (t < resp_tiles ? prm.n_resp - t * kWideTile : cached - (t - resp_tiles) * kWideTile);
+    if (left < kWideTile) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (kb * 32 + 8 * (i / 4) + 4 * g + i % 4 >= left) s[kb][i] = -INFINITY;
+    }
+    float bm = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bm = fmaxf(bm, s[kb][i]);
+    const float cand = max_halves(bm) * c;
+    const bool bump = cand > m + kLazyBump;  // (see attend.hip)
+    if (__any(bump)) {
+      const float m_new = bump ? cand : m;
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+    if (more) logits(t + 1, C::kSteps / 2, C::kSteps, next);
+    u32x4 pf[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = fast_exp2(fmaf(s[kb][i], c, -m));
+        s[kb][i] = p;
+        sum += p;
+      }
+#pragma unroll
+      for (int tp = 0; tp < 2; ++tp)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) pf[2 * kb + tp][w] = pack_bf16x2(s[kb][8 * tp + 2 * w], s[kb][8 * tp + 2 * w + 1]);
+    }
+    l += sum;
+    const uint32_t at = v_at + (t & 1) * C::kTileB;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db) {
+        const uint32_t from = at + v_read_offset<D>(lane, db);
+        const u32x2 lo = read_transposed(from, 16 * n * C::kRowB), hi = read_transposed(from, (16 * n + 8) * C::kRowB);
+        mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[n], o[db]);
+      }
+    s[0] = next[0];
+    s[1] = next[1];
+    arrive();
+  }
+
+  // ---- out, by way of LDS: whole rows
+  l = sum_halves(l);
+  const float by = 1.f / l;
+  char* own = mx_lds + wave * 32 * (C::kRowB + 16);
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x2*>(own + r * (C::kRowB + 16) + (32 * db + 8 * i + 4 * g) * 2) =
+          u32x2{pack_bf16x2(o[db][4 * i] * by, o[db][4 * i + 1] * by), pack_bf16x2(o[db][4 * i + 2] * by, o[db][4 * i + 3] * by)};
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 32 * C::kPPR / 64; ++j) {
+    const int row = (j * 64 + lane) / C::kPPR, p = lane % C::kPPR;
+    if (q0 + row < prm.n_q)
+      *reinterpret_cast<u32x4*>(prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q0 + row) + p * 16) =
+          *reinterpret_cast<const u32x4*>(own + row * (C::kRowB + 16) + p * 16);
+  }
+  if (prm.lse && g == 0 && q0 + r < prm.n_q) prm.lse[(int64_t)bh * prm.n_q + q0 + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // A workgroup per query row of a head that has several units: their sums in units of the largest reference, dealt to groups of
 // D/4 threads.
 template <typename T, int D>
@@ -393,6 +606,7 @@ __global__ __launch_bounds__(256) void attend_mx_join_kernel(const AttendMxParam
 
 // How the tiles are dealt out.
 struct Deal {
+  bool wide;      // 128 query rows a workgroup, heads whole
   int qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
@@ -404,10 +618,15 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
   Deal x;
+  x.wide = d->dtype == MASKKV_BF16 && n_q > kWideQueries / 2 && BH * ((n_q + kWideQueries - 1) / kWideQueries) >= kUnits / 2;
   x.qtiles = (n_q + kTile - 1) / kTile;
   x.part_rows = n_q < kTile ? n_q : kTile;
   x.chunk = 0;
   x.units = BH;
+  if (x.wide) {
+    x.qtiles = (n_q + kWideQueries - 1) / kWideQueries;
+    return x;
+  }
   // what the host knows of the heads' lengths: no head has more rows than the longest prompt, and all of them as many as there is room for
   const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
   if (BH * x.qtiles >= kUnits && most <= kLongHead) return x;
@@ -422,8 +641,25 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
+template <int D>
+int launch_wide(const AttendMxParams& prm, hipStream_t stream) {
+  using C = WideCfg<D>;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_mx_wide_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+  if (e != hipSuccess) {
+    set_error("attend_mx: hipFuncSetAttribute: %s", hipGetErrorString(e));
+    (void)hipGetLastError();
+    return MASKKV_EHIP;
+  }
+  const int64_t groups = (int64_t)(prm.BH + 7) / 8 * 8 * prm.qtiles;  // (no more than 2^16 heads of 2^20 / 128 tiles: 2^29)
+  hipLaunchKernelGGL(attend_mx_wide_kernel<D>, dim3((unsigned)groups), dim3(256), C::kLds, stream, prm);
+  return check_launch("attend_mx (wide)");
+}
+
 template <typename T, int D>
 int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) {
+  if constexpr (sizeof(T) == 2) {
+    if (deal.wide) return launch_wide<D>(prm, stream);
+  }
   using C = MxCfg<T, D>;
   static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
   const int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
@@ -436,6 +672,7 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
     if (e != hipSuccess) {
       set_error("attend_mx: hipFuncSetAttribute: %s", hipGetErrorString(e));
+      (void)hipGetLastError();
       return MASKKV_EHIP;
     }
   }
