@@ -365,67 +365,114 @@ struct WideCfg {
   __device__ static uint32_t swz_k(uint32_t row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
 };
 
+// The head of a given rank by descending number of tiles, equal ones by ascending number: the lanes of a wave hold all heads'
+// counts, a bit of the wanted count takes a ballot per 64 heads.
+constexpr int kRanked = 256;  // heads up to which their order is found so
+template <typename F>
+__device__ __forceinline__ int head_of_rank(int BH, int rank, F tiles_of) {
+  constexpr int N = kRanked / 64;
+  const int lane = threadIdx.x & 63;
+  int tiles[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) tiles[i] = i * 64 + lane < BH ? min(tiles_of(i * 64 + lane), 0xFFFF) : 0;
+  int found = 0, above = 0;  // the count, and how many heads have more tiles
+  for (int bit = 1 << 15; bit > 0; bit >>= 1) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(tiles[i] >= (found | bit)));
+    if (n > rank)
+      found |= bit;
+    else
+      above = n;
+  }
+  int left = rank - above, head = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint64_t same = __ballot(tiles[i] == found);
+    const int n = __popcll(same);
+    if (left >= 0 && left < n) {
+      const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+      head = i * 64 + __builtin_ctzll(__ballot(tiles[i] == found && before == left));
+    }
+    left -= n;
+  }
+  return head;
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxParams prm) {
   using C = WideCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
   const int slot = blockIdx.x / 8;
-  const int bh = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
+  int bh = slot / prm.qtiles * 8 + blockIdx.x % 8;
+  const int qtile = slot % prm.qtiles;
   if (bh >= prm.BH) return;
+  const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
+  const int capacity = (int)prm.capacity;
+  auto cached_of = [&](int i) { return max(min(prm.cu[i + 1], capacity) - min(prm.cu[i], capacity), 0); };
+  if (prm.BH <= kRanked) bh = head_of_rank(prm.BH, bh, [&](int i) { return (cached_of(i) + kWideTile - 1) / kWideTile + resp_tiles; });
+  bh = __builtin_amdgcn_readfirstlane(bh);
   const int b = bh / prm.H, h = bh % prm.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
-  const int first = min(prm.cu[bh], (int)prm.capacity);
-  const int cached = max(min(prm.cu[bh + 1], (int)prm.capacity) - first, 0);
-  const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
+  const int first = min(prm.cu[bh], capacity), cached = cached_of(bh);
   const int tiles = resp_tiles + (cached + kWideTile - 1) / kWideTile;  // those of the response first
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mx_lds;
-  const uint32_t k_at = lds0, v_at = lds0 + 2 * C::kTileB;
 
-  // ---- tiles on their way
+  // ---- tiles on their way.  Of the cache a thread takes a quarter of a row; of the response a wave takes a quarter of the rows.
   const int my_row = threadIdx.x >> 2, quarter = threadIdx.x & 3;
+  const char* const codes_k = prm.cache.k_codes + (int64_t)first * (D / 2);
+  const char* const codes_v = prm.cache.v_codes + (int64_t)first * (D / 2);
+  const char* const scales_k = prm.cache.k_scales + (int64_t)first * (D / 32);
+  const char* const scales_v = prm.cache.v_scales + (int64_t)first * (D / 32);
   uint32_t kc[C::kWords], vc[C::kWords], ks = 0, vs = 0;
   auto read = [&](int t, const char* codes, const char* scales, uint32_t (&c)[C::kWords], uint32_t& s) {
-    if (t < resp_tiles || t >= tiles) return;
-    const int64_t row = first + min((t - resp_tiles) * kWideTile + my_row, cached - 1);
-    const uint32_t* from = reinterpret_cast<const uint32_t*>(codes + row * (D / 2) + quarter * (D / 8));
+    const int base = (t - resp_tiles) * kWideTile;
+    if (base < 0 || base >= cached) return;
+    const uint32_t row = min(my_row, cached - base - 1);
+    const char* from = codes + (int64_t)base * (D / 2);
 #pragma unroll
-    for (int w = 0; w < C::kWords; ++w) c[w] = from[w];
-    s = reinterpret_cast<const uint8_t*>(scales)[row * (D / 32) + quarter * (D / 32) / 4];
+    for (int w = 0; w < C::kWords; ++w) c[w] = *reinterpret_cast<const uint32_t*>(from + (row * (D / 2) + quarter * (D / 8) + 4 * w));
+    s = *reinterpret_cast<const uint8_t*>(scales + (int64_t)base * (D / 32) + (row * (D / 32) + quarter * (D / 32) / 4));
   };
-  auto transfer = [&](int t, const View& from, uint32_t to, bool k) {
+  const char* const resp_k = prm.K2.row(b, h, 0);
+  const char* const resp_v = prm.V2.row(b, h, 0);
+  const uint32_t moved = wave * (kWideTile / 4) + (uint32_t)lane / C::kPPR;  // this lane's row of the wave's first transfer
+  const uint32_t piece_k = ((uint32_t)lane % C::kPPR ^ C::swz_k(moved)) << 4, piece_v = ((uint32_t)lane % C::kPPR ^ v_swizzle<D>(moved) << 1) << 4;
+  auto transfer = [&](int t, const char* from, int64_t stride, uint32_t piece, uint32_t step, uint32_t to) {
+    const int left = prm.n_resp - t * kWideTile;
+    from += (int64_t)t * kWideTile * stride;
 #pragma unroll
-    for (int j = 0; j < C::kMoves; ++j) {
-      const uint32_t row = (wave * C::kMoves + j) * C::kMoveRows + (uint32_t)lane / C::kPPR, p = (uint32_t)lane % C::kPPR;
-      const uint32_t piece = k ? p ^ C::swz_k(row) : p ^ v_swizzle<D>(row) << 1;
-      dma16_from(from.row(b, h, min(t * kWideTile + (int)row, prm.n_resp - 1)) + piece * 16, to + (wave * C::kMoves + j) * 1024);
+    for (int j = 0; j < C::kMoves; ++j) {  // (a row's permutation changes from a transfer to the next by an exclusive-or of its own)
+      const uint32_t row = min((int)moved + j * C::kMoveRows, left - 1);
+      dma16(from, row * (uint32_t)stride + (piece ^ (j * step & (C::kRowB - 1))), to + (wave * C::kMoves + j) * 1024);
     }
   };
-  auto convert = [&](const uint32_t (&c)[C::kWords], uint32_t s, uint32_t to, bool k) {
+  // where this thread's quarter of a row goes, as the byte to which a word's number is added by an exclusive-or
+  const uint32_t to_k = my_row * C::kRowB + ((quarter * C::kWords ^ C::swz_k(my_row)) << 4);
+  const uint32_t to_v = my_row * C::kRowB + ((quarter * C::kWords ^ v_swizzle<D>(my_row) << 1) << 4);
+  auto convert = [&](const uint32_t (&c)[C::kWords], uint32_t s, uint32_t to) {
     const float unit = mx_unit(s);
-    const uint32_t row = my_row;
 #pragma unroll
-    for (int w = 0; w < C::kWords; ++w) {
-      const uint32_t p = quarter * C::kWords + w;
-      *in_lds<u32x4>(to + row * C::kRowB + ((k ? p ^ C::swz_k(row) : p ^ v_swizzle<D>(row) << 1) << 4)) = mx_decode_bf16(c[w], unit);
-    }
+    for (int w = 0; w < C::kWords; ++w) *in_lds<u32x4>(lds0 + (to ^ w << 4)) = mx_decode_bf16(c[w], unit);
   };
-  auto bring_k = [&](int t) {  // K(t) into its buffer
+  // K(t), V(t) into the buffer of an even or odd tile
+  auto bring_k = [&](int t, uint32_t odd) {
     if (t >= tiles) return;
     if (t < resp_tiles)
-      transfer(t, prm.K2, k_at + (t & 1) * C::kTileB, true);
+      transfer(t, resp_k, prm.K2.stride_t, piece_k, C::swz_k(C::kMoveRows) << 4, lds0 + odd * C::kTileB);
     else
-      convert(kc, ks, k_at + (t & 1) * C::kTileB, true);
+      convert(kc, ks, to_k + odd * C::kTileB);
   };
-  auto bring_v = [&](int t) {
+  auto bring_v = [&](int t, uint32_t odd) {
     if (t >= tiles) return;
     if (t < resp_tiles)
-      transfer(t, prm.V2, v_at + (t & 1) * C::kTileB, false);
+      transfer(t, resp_v, prm.V2.stride_t, piece_v, 0, lds0 + (2 + odd) * C::kTileB);
     else
-      convert(vc, vs, v_at + (t & 1) * C::kTileB, false);
+      convert(vc, vs, to_v + (2 + odd) * C::kTileB);
   };
-  auto read_k = [&](int t) { read(t, prm.cache.k_codes, prm.cache.k_scales, kc, ks); };
-  auto read_v = [&](int t) { read(t, prm.cache.v_codes, prm.cache.v_scales, vc, vs); };
+  auto read_k = [&](int t) { read(t, codes_k, scales_k, kc, ks); };
+  auto read_v = [&](int t) { read(t, codes_v, scales_v, vc, vs); };
   auto arrive = [] {  // what this wave has moved and written is there, and so is everyone's behind the barrier
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -441,42 +488,49 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
     for (int i = 0; i < C::kSteps; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
   }
-  bring_k(0);
+  bring_k(0, 0);
   read_k(1);
-  bring_k(1);
-  bring_v(0);
-  read_k(2);
+  bring_v(0, 0);
   read_v(1);
+  bring_k(1, 1);
+  read_k(2);
   arrive();
 
-  f32x16 o[C::kDB], s[2], next[2];
+  f32x16 o[C::kDB], even[2], odd[2];
 #pragma unroll
   for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
   float m = kNegBig, l = 0.f;
   const float c = prm.c;
-  // fragments of K: of steps [from, to) of the logits of tile t, both blocks of 32 keys
-  auto logits = [&](int t, int from, int to, f32x16 (&x)[2]) {
-    const uint32_t at = k_at + (t & 1) * C::kTileB + r * C::kRowB;
+  uint32_t k_at[C::kSteps], v_at[C::kDB];
+#pragma unroll
+  for (int i = 0; i < C::kSteps; ++i) k_at[i] = lds0 + r * C::kRowB + (((C::kPPR / 2 * g + i) ^ C::swz_k(r)) << 4);
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) v_at[db] = lds0 + 2 * C::kTileB + v_read_offset<D>(lane, db);
+  // steps [from, to) of the logits of an even or odd tile, both blocks of 32 keys
+  auto logits = [&](uint32_t is_odd, int from, int to, f32x16 (&x)[2]) {
+    if (from == 0) x[0] = x[1] = f32x16{};
 #pragma unroll
     for (int i = from; i < to; ++i)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
-        const u32x4 k = *in_lds<const u32x4>(at + (((C::kPPR / 2 * g + i) ^ C::swz_k(r)) << 4), kb * 32 * C::kRowB);
+        const u32x4 k = *in_lds<const u32x4>(k_at[i], is_odd * C::kTileB + kb * 32 * C::kRowB);
         mfma_step<bf16_t>(k, qf[i], x[kb]);
       }
   };
-  s[0] = s[1] = f32x16{};
-  logits(0, 0, C::kSteps, s);
+  logits(0, 0, C::kSteps, even);
   arrive();  // (K(2) takes the place of K(0))
 
-  for (int t = 0; t < tiles; ++t) {
-    bring_k(t + 2);
-    bring_v(t + 1);
-    read_k(t + 3);
-    read_v(t + 2);
-    next[0] = next[1] = f32x16{};
-    const bool more = t + 1 < tiles;
-    if (more) logits(t + 1, 0, C::kSteps / 2, next);
+  // Tile t (odd or not) with its logits in `s`; with MORE those of the next into `next`.
+  auto step = [&](int t, auto odd_tile, auto more, f32x16 (&s)[2], f32x16 (&next)[2]) {
+    constexpr uint32_t kOdd = decltype(odd_tile)::value;
+    constexpr bool kMore = decltype(more)::value;
+    if constexpr (kMore) {
+      bring_k(t + 2, kOdd);
+      bring_v(t + 1, 1 - kOdd);
+      read_k(t + 3);
+      read_v(t + 2);
+      logits(1 - kOdd, 0, C::kSteps / 2, next);
+    }
     const int left = (t < resp_tiles ? prm.n_resp - t * kWideTile : cached - (t - resp_tiles) * kWideTile);
     if (left < kWideTile) {
 #pragma unroll
@@ -502,7 +556,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
-    if (more) logits(t + 1, C::kSteps / 2, C::kSteps, next);
+    if constexpr (kMore) logits(1 - kOdd, C::kSteps / 2, C::kSteps, next);
     u32x4 pf[4];
     float sum = 0.f;
 #pragma unroll
@@ -519,18 +573,28 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
         for (int w = 0; w < 4; ++w) pf[2 * kb + tp][w] = pack_bf16x2(s[kb][8 * tp + 2 * w], s[kb][8 * tp + 2 * w + 1]);
     }
     l += sum;
-    const uint32_t at = v_at + (t & 1) * C::kTileB;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int db = 0; db < C::kDB; ++db) {
-        const uint32_t from = at + v_read_offset<D>(lane, db);
-        const u32x2 lo = read_transposed(from, 16 * n * C::kRowB), hi = read_transposed(from, (16 * n + 8) * C::kRowB);
+        const int imm = kOdd * C::kTileB + 16 * n * C::kRowB;
+        const u32x2 lo = read_transposed(v_at[db], imm), hi = read_transposed(v_at[db], imm + 8 * C::kRowB);
         mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[n], o[db]);
       }
-    s[0] = next[0];
-    s[1] = next[1];
     arrive();
+  };
+  using Yes = std::true_type;
+  using No = std::false_type;
+  int t = 0;
+  for (; t + 2 < tiles; t += 2) {
+    step(t, No(), Yes(), even, odd);
+    step(t + 1, Yes(), Yes(), odd, even);
+  }
+  if (t + 1 < tiles) {
+    step(t, No(), Yes(), even, odd);
+    step(t + 1, Yes(), No(), odd, even);
+  } else {
+    step(t, No(), No(), even, odd);
   }
 
   // ---- out, by way of LDS: whole rows
