@@ -499,52 +499,60 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   f32x16 o[C::kDB], even[2], odd[2];
 #pragma unroll
   for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
-  float m = kNegBig, l = 0.f;
+  float m = kNegBig, l = 0.f, top = 0.f;  // top: the largest logit of the tile whose turn comes next
   const float c = prm.c;
   uint32_t k_at[C::kSteps], v_at[C::kDB];
 #pragma unroll
   for (int i = 0; i < C::kSteps; ++i) k_at[i] = lds0 + r * C::kRowB + (((C::kPPR / 2 * g + i) ^ C::swz_k(r)) << 4);
 #pragma unroll
   for (int db = 0; db < C::kDB; ++db) v_at[db] = lds0 + 2 * C::kTileB + v_read_offset<D>(lane, db);
-  // steps [from, to) of the logits of an even or odd tile, both blocks of 32 keys
-  auto logits = [&](uint32_t is_odd, int from, int to, f32x16 (&x)[2]) {
-    if (from == 0) x[0] = x[1] = f32x16{};
-#pragma unroll
-    for (int i = from; i < to; ++i)
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const u32x4 k = *in_lds<const u32x4>(k_at[i], is_odd * C::kTileB + kb * 32 * C::kRowB);
-        mfma_step<bf16_t>(k, qf[i], x[kb]);
-      }
+  // Fragment n of a tile: 0 .. kQK-1 of its keys (two chains of products, one for 32 keys each), from kQK on of the values of the tile before.
+  constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 3;
+  u32x4 fr[kAhead + 1];
+  auto fetch = [&](int n, uint32_t odd_k) {
+    u32x4& f = fr[n % (kAhead + 1)];
+    if (n < kQK) {
+      f = *in_lds<const u32x4>(k_at[n / 2], odd_k * C::kTileB + n % 2 * 32 * C::kRowB);
+    } else {
+      const int i = n - kQK, imm = (1 - odd_k) * C::kTileB + i / C::kDB * 16 * C::kRowB;
+      const u32x2 lo = read_transposed(v_at[i % C::kDB], imm), hi = read_transposed(v_at[i % C::kDB], imm + 8 * C::kRowB);
+      f = u32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
   };
-  logits(0, 0, C::kSteps, even);
+  auto mask = [&](int t, f32x16 (&s)[2]) {  // keys behind the last one of the response, or of the cache
+    const int left = t < resp_tiles ? prm.n_resp - t * kWideTile : cached - (t - resp_tiles) * kWideTile;
+    if (left >= kWideTile) return;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (kb * 32 + 8 * (i / 4) + 4 * g + i % 4 >= left) s[kb][i] = -INFINITY;
+  };
+#pragma unroll
+  for (int n = 0; n < kQK; ++n) {
+    fetch(n, 0);
+    if (n < 2) even[n] = f32x16{};
+    mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], even[n % 2]);
+  }
+  mask(0, even);
+  top = even[0][0];
+#pragma unroll
+  for (int i = 0; i < 32; ++i) top = fmaxf(top, even[i / 16][i % 16]);
   arrive();  // (K(2) takes the place of K(0))
 
-  // Tile t (odd or not) with its logits in `s`; with MORE those of the next into `next`.
+  // Tile t (odd or not) with its logits in `s`; with MORE those of the next into `next`.  The next tile's logits are formed beside
+  // this one's exponentials, this one's part of the output beside the search for the next one's largest logit.
   auto step = [&](int t, auto odd_tile, auto more, f32x16 (&s)[2], f32x16 (&next)[2]) {
     constexpr uint32_t kOdd = decltype(odd_tile)::value;
     constexpr bool kMore = decltype(more)::value;
+    constexpr int kFrom = kMore ? 0 : kQK;
     if constexpr (kMore) {
       bring_k(t + 2, kOdd);
       bring_v(t + 1, 1 - kOdd);
       read_k(t + 3);
       read_v(t + 2);
-      logits(1 - kOdd, 0, C::kSteps / 2, next);
     }
-    const int left = (t < resp_tiles ? prm.n_resp - t * kWideTile : cached - (t - resp_tiles) * kWideTile);
-    if (left < kWideTile) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (kb * 32 + 8 * (i / 4) + 4 * g + i % 4 >= left) s[kb][i] = -INFINITY;
-    }
-    float bm = s[0][0];
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) bm = fmaxf(bm, s[kb][i]);
-    const float cand = max_halves(bm) * c;
+    const float cand = max_halves(top) * c;
     const bool bump = cand > m + kLazyBump;  // (see attend.hip)
     if (__any(bump)) {
       const float m_new = bump ? cand : m;
@@ -556,31 +564,46 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
-    if constexpr (kMore) logits(1 - kOdd, C::kSteps / 2, C::kSteps, next);
     u32x4 pf[4];
-    float sum = 0.f;
+    auto probabilities = [&](int i) {  // values i and i + 1 of the 32
+      const float p0 = fast_exp2(fmaf(s[i / 16][i % 16], c, -m)), p1 = fast_exp2(fmaf(s[i / 16][i % 16 + 1], c, -m));
+      l += p0 + p1;
+      uint32_t both = pack_bf16x2(p0, p1);
+      asm volatile("" : "+v"(both), "+v"(l));  // (formed here, beside the products, and not where it is first needed)
+      pf[i / 8][i % 8 / 2] = both;
+    };
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int n = 0; n < kAhead; ++n) fetch(kFrom + n, 1 - kOdd);
+    if constexpr (kMore) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = fast_exp2(fmaf(s[kb][i], c, -m));
-        s[kb][i] = p;
-        sum += p;
+      for (int n = 0; n < kQK; ++n) {
+        fetch(n + kAhead, 1 - kOdd);
+        if (n < 2) next[n] = f32x16{};
+        mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], next[n % 2]);
+#pragma unroll
+        for (int i = n * 32 / kQK; i < (n + 1) * 32 / kQK; i += 2) probabilities(i);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      mask(t + 1, next);
+    } else {
 #pragma unroll
-      for (int tp = 0; tp < 2; ++tp)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) pf[2 * kb + tp][w] = pack_bf16x2(s[kb][8 * tp + 2 * w], s[kb][8 * tp + 2 * w + 1]);
+      for (int i = 0; i < 32; i += 2) probabilities(i);
     }
-    l += sum;
+    float high = -INFINITY;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int n = kQK; n < kQK + kPV; ++n) {
+      if (n + kAhead < kQK + kPV) fetch(n + kAhead, 1 - kOdd);
+      mfma_step<bf16_t>(fr[n % (kAhead + 1)], pf[(n - kQK) / C::kDB], o[(n - kQK) % C::kDB]);
+      if constexpr (kMore) {
 #pragma unroll
-      for (int db = 0; db < C::kDB; ++db) {
-        const int imm = kOdd * C::kTileB + 16 * n * C::kRowB;
-        const u32x2 lo = read_transposed(v_at[db], imm), hi = read_transposed(v_at[db], imm + 8 * C::kRowB);
-        mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf[n], o[db]);
+        for (int i = (n - kQK) * 32 / kPV; i < (n + 1 - kQK) * 32 / kPV; ++i) high = fmaxf(high, next[i / 16][i % 16]);
+        asm volatile("" : "+v"(high));
       }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    top = high;
     arrive();
   };
   using Yes = std::true_type;
