@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     if (left < kTile) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (8 * (i / 4) + 4 * g + i % 4 >= left) s[i] = -INFINITY;
+        if (8 * (i / 4) + i % 4 >= left - 4 * g) s[i] = -INFINITY;
     }
     float bm = s[0];
 #pragma unroll
@@ -522,11 +522,12 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   auto mask = [&](int t, f32x16 (&s)[2]) {  // keys behind the last one of the response, or of the cache
     const int left = t < resp_tiles ? prm.n_resp - t * kWideTile : cached - (t - resp_tiles) * kWideTile;
     if (left >= kWideTile) return;
+    const int mine = left - 4 * g;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (kb * 32 + 8 * (i / 4) + 4 * g + i % 4 >= left) s[kb][i] = -INFINITY;
+        if (kb * 32 + 8 * (i / 4) + i % 4 >= mine) s[kb][i] = -INFINITY;
   };
 #pragma unroll
   for (int n = 0; n < kQK; ++n) {
