@@ -53,15 +53,12 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   // Each XCD (workgroups whose numbers are congruent modulo 8) takes a run of units: a head's queries stay in one L2.
   const int unit = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
   const int capacity = (int)prm.capacity;
-  int first_unit = 0, units = 0;
-  const int bh = head_of_unit(prm.BH, unit, [&](int i) {
-    const int a = min(prm.cu[i], capacity), z = min(prm.cu[i + 1], capacity);
-    return max(z - a + kRows - 1, 0) / kRows;
-  }, first_unit, units);
+  const UnitHead head = head_of_unit(prm.cu, prm.BH, capacity, unit, [](int n) { return (int)(((uint32_t)n + kRows - 1) / kRows); });
+  const int bh = head.bh;
   if (bh < 0) return;
   const int b = bh / prm.H, h = bh % prm.H;
-  const int last = min(prm.cu[bh + 1], capacity) - 1;
-  const int row0 = min(prm.cu[bh], capacity) + (unit - first_unit) * kRows + (SHARE ? wave * kTile : 0);  // of this wave
+  const int last = head.first + head.rows - 1;
+  const int row0 = head.first + (unit - head.first_unit) * kRows + (SHARE ? wave * kTile : 0);  // of this wave
   const int64_t row = min(row0 + r, last);
 
   const int steps = (prm.n_q + kTile - 1) / kTile;

@@ -38,6 +38,12 @@ struct AttendMxParams {
   int2* parts;      // [BH] a head's first unit, and how many it has
 };
 
+__device__ __forceinline__ void fetch_attend_mx_arguments() {
+  typedef AttendMxParams A;
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_VIEW_ARGUMENTS(A, K2), MASKKV_VIEW_ARGUMENTS(A, V2), MASKKV_VIEW_ARGUMENTS(A, O),
+                   MASKKV_ARGUMENT(A, cache), MASKKV_ARGUMENT(A, H), (uint32_t)(offsetof(A, parts) + 4)});
+}
+
 template <typename T, int D>
 struct MxCfg {
   static constexpr int kRowB = D * (int)sizeof(T);
@@ -59,69 +65,63 @@ struct MxCfg {
   }
 };
 
-// Tiles of a head: those of the response first.
-struct Head {
-  int first, cached;  // its rows of the cache
-  int tiles;
-};
-__device__ __forceinline__ Head head_at(const AttendMxParams& prm, int bh) {
-  const int capacity = (int)prm.capacity;
-  Head x;
-  x.first = min(prm.cu[bh], capacity);
-  x.cached = max(min(prm.cu[bh + 1], capacity) - x.first, 0);
-  x.tiles = (x.cached + kTile - 1) / kTile + (prm.n_resp + kTile - 1) / kTile;
-  return x;
-}
-
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx_kernel(const AttendMxParams prm) {
   using C = MxCfg<T, D>;
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
+  fetch_attend_mx_arguments();
   // Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there.
   const int slot = blockIdx.x / 8;
   const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
-  int bh = unit, first_unit = unit, units = 1;
-  if (prm.chunk)
-    bh = head_of_unit(prm.BH, unit, [&](int i) { return (head_at(prm, i).tiles + prm.chunk - 1) / prm.chunk; }, first_unit, units);
-  else if (bh >= prm.BH)
-    bh = -1;
-  if (bh < 0) return;
+  const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
+  auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kTile - 1) / kTile) + resp_tiles; };  // those of the response first
+  const int capacity = (int)prm.capacity;
+  UnitHead head;
+  if (prm.chunk) {
+    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
+    if (head.bh < 0) return;
+  } else {
+    if (unit >= prm.BH) return;
+    const int first = min(prm.cu[unit], capacity);
+    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
+  }
+  const int bh = head.bh, units = head.units, cached = head.rows, tiles = tiles_of(cached);
   const int b = bh / prm.H, h = bh % prm.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
-  const Head head = head_at(prm, bh);
-  if (prm.chunk && unit == first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(first_unit, units);
-  const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
-  const int t0 = prm.chunk ? (unit - first_unit) * prm.chunk : 0;
-  const int t1 = prm.chunk ? min(head.tiles, t0 + prm.chunk) : head.tiles;
+  if (prm.chunk && unit == head.first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, units);
+  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
+  const int t1 = prm.chunk ? min(tiles, t0 + prm.chunk) : tiles;
 
   char* const k_lds = mx_lds + wave * C::kWaveB;
   char* const v_lds = k_lds + C::kTileB;
   const uint32_t v_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)v_lds;
 
-  // ---- what is under way: a tile of the cache, or of the response
-  u32x4 kc[D / 64], vc[D / 64];
-  uint32_t ks = 0, vs = 0;
-  auto load_cached = [&](int t) {  // tile t of the cache; rows behind the last one are the last one
-    const int64_t row = head.first + min(t * kTile + r, head.cached - 1);
+  // ---- what is under way: two tiles of the cache, and one of the response
+  struct Cached {
+    u32x4 k[D / 64], v[D / 64];
+    uint32_t ks, vs;
+  } one, two;
+  auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {  // tile t of the cache; rows behind the last one are the last one
+    const int64_t row = head.first + min(t * kTile + r, cached - 1);
     const int64_t at = row * (D / 2) + g * (D / 4);
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      kc[j] = *reinterpret_cast<const u32x4*>(prm.cache.k_codes + at + 16 * j);
-      vc[j] = *reinterpret_cast<const u32x4*>(prm.cache.v_codes + at + 16 * j);
+      x.k[j] = *reinterpret_cast<const u32x4*>(prm.cache.k_codes + at + 16 * j);
+      x.v[j] = *reinterpret_cast<const u32x4*>(prm.cache.v_codes + at + 16 * j);
     }
     const int64_t s = row * (D / 32) + g * (D / 64);
     if (D == 128) {
-      ks = *reinterpret_cast<const uint16_t*>(prm.cache.k_scales + s);
-      vs = *reinterpret_cast<const uint16_t*>(prm.cache.v_scales + s);
+      x.ks = *reinterpret_cast<const uint16_t*>(prm.cache.k_scales + s);
+      x.vs = *reinterpret_cast<const uint16_t*>(prm.cache.v_scales + s);
     } else {
-      ks = *reinterpret_cast<const uint8_t*>(prm.cache.k_scales + s);
-      vs = *reinterpret_cast<const uint8_t*>(prm.cache.v_scales + s);
+      x.ks = *reinterpret_cast<const uint8_t*>(prm.cache.k_scales + s);
+      x.vs = *reinterpret_cast<const uint8_t*>(prm.cache.v_scales + s);
     }
   };
   u32x4 kr[C::kLoads], vr[C::kLoads];
-  auto load_resp = [&](int t) {
+  auto load_resp = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < C::kLoads; ++j) {
       const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
   auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
   if (resp > 0) load_resp(tile_of(0));
-  if (mine > resp) load_cached(tile_of(resp) - resp_tiles);
+  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, one);
+  if (mine > resp + 1) load_cached(tile_of(resp + 1) - resp_tiles, two);
 
   // ---- this lane's query: half of its row, as the B operand of the first product
   u32x4 qf[C::kPPR / 2];
@@ -150,10 +151,10 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
   float m = kNegBig, l = 0.f;
 
-  auto logits_step = [&](int i, const u32x4& x) {  // bf16: word i of the lane's half row
+  auto logits_step = [&](int i, const u32x4& x) __attribute__((always_inline)) {  // bf16: word i of the lane's half row
     mfma_step<bf16_t>(x, qf[i], s);
   };
-  auto logits_step_f32 = [&](int i, const float (&x)[8]) {
+  auto logits_step_f32 = [&](int i, const float (&x)[8]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t q = qf[2 * i + e / 4][e % 4];
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   };
 
   // ---- softmax of a tile with `left` rows, and the output update.  Lanes l and l ^ 32 have the same query.
-  auto update = [&](int left) {
+  auto update = [&](int left) __attribute__((always_inline)) {
     if (left < kTile) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -241,44 +242,44 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     update(prm.n_resp - t * kTile);
     asm volatile("" ::: "memory");
   }
-  for (int i = resp; i < mine; ++i) {
+  auto take = [&](int i, Cached& x) __attribute__((always_inline)) {
     const int t = tile_of(i) - resp_tiles;
     // V on its way into LDS, K into the first product
 #pragma unroll
     for (int w = 0; w < C::kWords; ++w) {
-      const uint32_t word = vc[w / 4][w % 4];
-      const float unit = mx_unit(vs >> (8 * (w / 4)) & 255);
+      const uint32_t word = x.v[w / 4][w % 4];
+      const float unit = mx_unit(x.vs >> (8 * (w / 4)) & 255);
       if constexpr (F32) {
-        float x[8];
-        mx_decode_f32(word, unit, x);
+        float y[8];
+        mx_decode_f32(word, unit, y);
         const uint32_t p = g * (C::kPPR / 2) + 2 * w;
-        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p) << 4)) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p + 1) << 4)) = make_float4(x[4], x[5], x[6], x[7]);
+        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p) << 4)) = make_float4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p + 1) << 4)) = make_float4(y[4], y[5], y[6], y[7]);
       } else {
         *reinterpret_cast<u32x4*>(v_lds + r * C::kRowB + (C::v_slot(r, g * (C::kPPR / 2) + w) << 4)) = mx_decode_bf16(word, unit);
       }
     }
-    u32x4 k_now[D / 64];
-    const uint32_t s_now = ks;
-#pragma unroll
-    for (int j = 0; j < D / 64; ++j) k_now[j] = kc[j];
-    if (i + 1 < mine) load_cached(t + kWaves);
     asm volatile("" ::: "memory");
     s = f32x16{};
 #pragma unroll
     for (int w = 0; w < C::kWords; ++w) {
-      const uint32_t word = k_now[w / 4][w % 4];
-      const float unit = mx_unit(s_now >> (8 * (w / 4)) & 255);
+      const uint32_t word = x.k[w / 4][w % 4];
+      const float unit = mx_unit(x.ks >> (8 * (w / 4)) & 255);
       if constexpr (F32) {
-        float x[8];
-        mx_decode_f32(word, unit, x);
-        logits_step_f32(w, x);
+        float y[8];
+        mx_decode_f32(word, unit, y);
+        logits_step_f32(w, y);
       } else {
         logits_step(w, mx_decode_bf16(word, unit));
       }
     }
-    update(head.cached - t * kTile);
+    if (i + 2 < mine) load_cached(t + 2 * kWaves, x);
+    update(cached - t * kTile);
     asm volatile("" ::: "memory");
+  };
+  for (int i = resp; i < mine; i += 2) {
+    take(i, one);
+    if (i + 1 < mine) take(i + 1, two);
   }
 
   // ---- the waves' results become one: sums of each wave, in units of the largest reference, through LDS
@@ -291,13 +292,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kTile + r].x);
   const float mine_by = fast_exp2(m - top);
   float* const sums = reinterpret_cast<float*>(mx_lds);
+  if (qtile * kTile + r < prm.n_q)
 #pragma unroll
-  for (int db = 0; db < C::kDB; ++db)
+    for (int db = 0; db < C::kDB; ++db)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 x = make_float4(o[db][4 * i] * mine_by, o[db][4 * i + 1] * mine_by, o[db][4 * i + 2] * mine_by, o[db][4 * i + 3] * mine_by);
-      *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * db + 8 * i + 4 * g) = x;
-    }
+      for (int i = 0; i < 4; ++i) {
+        const float4 x = make_float4(o[db][4 * i] * mine_by, o[db][4 * i + 1] * mine_by, o[db][4 * i + 2] * mine_by, o[db][4 * i + 3] * mine_by);
+        *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * db + 8 * i + 4 * g) = x;
+      }
   __syncthreads();
   constexpr int kEach = 8;               // elements of a row that a thread writes
   constexpr int kPerRow = D / kEach;     // threads of a row
@@ -403,6 +405,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxParams prm) {
   using C = WideCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
+  fetch_attend_mx_arguments();
   const int slot = blockIdx.x / 8;
   int bh = slot / prm.qtiles * 8 + blockIdx.x % 8;
   const int qtile = slot % prm.qtiles;
@@ -426,13 +429,16 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   const char* const scales_k = prm.cache.k_scales + (int64_t)first * (D / 32);
   const char* const scales_v = prm.cache.v_scales + (int64_t)first * (D / 32);
   uint32_t kc[C::kWords], vc[C::kWords], ks = 0, vs = 0;
-  auto read = [&](int t, const char* codes, const char* scales, uint32_t (&c)[C::kWords], uint32_t& s) {
+  // (An LDS write of 16 bytes a lane takes eight lanes at a time, here two rows: the words of a thread are read, and written, in another order
+  // in every other row, or half of a row, so that the eight fall on different banks.)
+  const uint32_t turn_k = D == 128 ? quarter & 2 : my_row & 1, turn_v = (D == 128 ? quarter & 2 : 0) ^ (my_row & 1);
+  auto read = [&](int t, const char* codes, const char* scales, uint32_t turn, uint32_t (&c)[C::kWords], uint32_t& s) {
     const int base = (t - resp_tiles) * kWideTile;
     if (base < 0 || base >= cached) return;
     const uint32_t row = min(my_row, cached - base - 1);
     const char* from = codes + (int64_t)base * (D / 2);
 #pragma unroll
-    for (int w = 0; w < C::kWords; ++w) c[w] = *reinterpret_cast<const uint32_t*>(from + (row * (D / 2) + quarter * (D / 8) + 4 * w));
+    for (int w = 0; w < C::kWords; ++w) c[w] = *reinterpret_cast<const uint32_t*>(from + (row * (D / 2) + quarter * (D / 8) + 4 * (w ^ turn)));
     s = *reinterpret_cast<const uint8_t*>(scales + (int64_t)base * (D / 32) + (row * (D / 32) + quarter * (D / 32) / 4));
   };
   const char* const resp_k = prm.K2.row(b, h, 0);
@@ -449,8 +455,8 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
     }
   };
   // where this thread's quarter of a row goes, as the byte to which a word's number is added by an exclusive-or
-  const uint32_t to_k = my_row * C::kRowB + ((quarter * C::kWords ^ C::swz_k(my_row)) << 4);
-  const uint32_t to_v = my_row * C::kRowB + ((quarter * C::kWords ^ v_swizzle<D>(my_row) << 1) << 4);
+  const uint32_t to_k = my_row * C::kRowB + ((quarter * C::kWords ^ C::swz_k(my_row) ^ turn_k) << 4);
+  const uint32_t to_v = my_row * C::kRowB + ((quarter * C::kWords ^ v_swizzle<D>(my_row) << 1 ^ turn_v) << 4);
   auto convert = [&](const uint32_t (&c)[C::kWords], uint32_t s, uint32_t to) {
     const float unit = mx_unit(s);
 #pragma unroll
@@ -471,8 +477,8 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
     else
       convert(vc, vs, to_v + (2 + odd) * C::kTileB);
   };
-  auto read_k = [&](int t) { read(t, codes_k, scales_k, kc, ks); };
-  auto read_v = [&](int t) { read(t, codes_v, scales_v, vc, vs); };
+  auto read_k = [&](int t) { read(t, codes_k, scales_k, turn_k, kc, ks); };
+  auto read_v = [&](int t) { read(t, codes_v, scales_v, turn_v, vc, vs); };
   auto arrive = [] {  // what this wave has moved and written is there, and so is everyone's behind the barrier
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -507,7 +513,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
   for (int db = 0; db < C::kDB; ++db) v_at[db] = lds0 + 2 * C::kTileB + v_read_offset<D>(lane, db);
   // Fragment n of a tile: 0 .. kQK-1 of its keys (two chains of products, one for 32 keys each), from kQK on of the values of the tile before.
-  constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 3;
+  constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 2;
   u32x4 fr[kAhead + 1];
   auto fetch = [&](int n, uint32_t odd_k) {
     u32x4& f = fr[n % (kAhead + 1)];
@@ -642,30 +648,47 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   if (prm.lse && g == 0 && q0 + r < prm.n_q) prm.lse[(int64_t)bh * prm.n_q + q0 + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// A workgroup per query row of a head that has several units: their sums in units of the largest reference, dealt to groups of
-// D/4 threads.
+// The partial results of the heads that have several units, a query row at a time: sums in units of the largest reference, dealt
+// to groups of D/4 threads, each of which asks for kAtOnce partial results before it uses the first.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_mx_join_kernel(const AttendMxParams prm) {
-  constexpr int kPer = D / 4, kGroups = 256 / kPer;
+__global__ __launch_bounds__(512) void attend_mx_join_kernel(const AttendMxParams prm) {
+  constexpr int kPer = D / 4, kGroups = 512 / kPer, kAtOnce = 8;
   __shared__ float4 sums[kGroups][kPer];
   __shared__ float2 tops[kGroups];
+  const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer;
+  const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
   const int bh = blockIdx.y, q = blockIdx.x;
   const int first = prm.parts[bh].x, units = prm.parts[bh].y;
   if (units <= 1) return;
-  const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer;
-  const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
   const int64_t part0 = first * step + (int64_t)(q / kTile) * prm.part_rows + q % kTile;
   float m = kNegBig, l = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int u = grp; u < units; u += kGroups) {
-    const float2 ml = prm.part_ml[part0 + u * step];
-    const float4 y = *reinterpret_cast<const float4*>(prm.part_o + (part0 + u * step) * D + at * 4);
-    const float m_new = fmaxf(m, ml.x);
-    const float old = fast_exp2(m - m_new), now = fast_exp2(ml.x - m_new);
-    m = m_new;
-    l = l * old + ml.y * now;
-    x = make_float4(x.x * old + y.x * now, x.y * old + y.y * now, x.z * old + y.z * now, x.w * old + y.w * now);
+  for (int u0 = grp; u0 < units; u0 += kAtOnce * kGroups) {
+    float2 ml[kAtOnce];
+    float4 y[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      ml[i] = make_float2(kNegBig, 0.f);
+      y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (u0 + i * kGroups < units) {
+        const int64_t part = part0 + (u0 + i * kGroups) * step;
+        ml[i] = prm.part_ml[part];
+        y[i] = *reinterpret_cast<const float4*>(prm.part_o + part * D + at * 4);
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+    const float old = fast_exp2(m - top);
+    m = top;
+    l *= old;
+    x = make_float4(x.x * old, x.y * old, x.z * old, x.w * old);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float by = fast_exp2(ml[i].x - m);
+      l = fmaf(ml[i].y, by, l);
+      x = make_float4(fmaf(y[i].x, by, x.x), fmaf(y[i].y, by, x.y), fmaf(y[i].z, by, x.z), fmaf(y[i].w, by, x.w));
+    }
   }
   sums[grp][at] = x;
   if (at == 0) tops[grp] = make_float2(m, l);
@@ -680,8 +703,8 @@ __global__ __launch_bounds__(256) void attend_mx_join_kernel(const AttendMxParam
   for (int i = 0; i < kGroups; ++i) {
     const float by = fast_exp2(tops[i].x - top);
     const float4 y = sums[i][at];
-    l += tops[i].y * by;
-    x = make_float4(x.x + y.x * by, x.y + y.y * by, x.z + y.z * by, x.w + y.w * by);
+    l = fmaf(tops[i].y, by, l);
+    x = make_float4(fmaf(y.x, by, x.x), fmaf(y.y, by, x.y), fmaf(y.z, by, x.z), fmaf(y.w, by, x.w));
   }
   const float by = 1.f / l;
   char* to = prm.O.group_row(bh / prm.H, bh % prm.H, prm.q_per_kv, prm.n_resp, q) + at * 4 * (int)sizeof(T);
@@ -767,7 +790,7 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), C::kLds, stream, prm);
   if (int e = check_launch("attend_mx")) return e;
   if (!deal.chunk) return MASKKV_OK;
-  hipLaunchKernelGGL((attend_mx_join_kernel<T, D>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(256), 0, stream, prm);
+  hipLaunchKernelGGL((attend_mx_join_kernel<T, D>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(512), 0, stream, prm);
   return check_launch("attend_mx (join)");
 }
 

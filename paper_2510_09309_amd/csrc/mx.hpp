@@ -96,25 +96,35 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return plus_dpp<0x143, 0xc>(v);
 }
 
-// The head of a unit of work when head bh has count(bh) units, -1 behind the last; what it is the first of, and how many the head
-// has.  Found by a wave, which counts 64 heads at a time.
+// The head of a unit of work when a head of n cached rows has units_of(n) units (bh -1: behind the last), which is its first and how
+// many it has, and where its rows lie.  Found by a wave, which counts 64 heads at a time.
+struct UnitHead {
+  int bh, first_unit, units;
+  int first, rows;
+};
 template <typename F>
-__device__ __forceinline__ int head_of_unit(int BH, int unit, F count, int& first, int& units) {
+__device__ __forceinline__ UnitHead head_of_unit(const int32_t* cu, int BH, int capacity, int unit, F units_of) {
   const int lane = threadIdx.x & 63;
+  UnitHead x = {-1, 0, 0, 0, 0};
   int before = 0;
   for (int base = 0; base < BH; base += 64) {
-    const int own = base + lane < BH ? count(base + lane) : 0;
+    const int bh = min(base + lane, BH - 1);
+    const int first = min(cu[bh], capacity), rows = max(min(cu[bh + 1], capacity) - first, 0);
+    const int own = base + lane < BH ? units_of(rows) : 0;
     const int upto = wave_prefix(own);
     const uint64_t over = __ballot(before + upto > unit);
     if (over) {
       const int at = __builtin_ctzll(over);
-      units = __builtin_amdgcn_readlane(own, at);
-      first = before + __builtin_amdgcn_readlane(upto, at) - units;
-      return __builtin_amdgcn_readfirstlane(base + at);
+      x.units = __builtin_amdgcn_readlane(own, at);
+      x.first_unit = before + __builtin_amdgcn_readlane(upto, at) - x.units;
+      x.first = __builtin_amdgcn_readlane(first, at);
+      x.rows = __builtin_amdgcn_readlane(rows, at);
+      x.bh = __builtin_amdgcn_readfirstlane(base + at);
+      return x;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
-  return -1;
+  return x;
 }
 
 }  // namespace maskkv
