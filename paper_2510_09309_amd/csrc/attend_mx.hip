@@ -103,22 +103,19 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     u32x4 k[D / 64], v[D / 64];
     uint32_t ks, vs;
   } one, two;
-  auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {  // tile t of the cache; rows behind the last one are the last one
-    const int64_t row = head.first + min(t * kTile + r, cached - 1);
-    const int64_t at = row * (D / 2) + g * (D / 4);
+  // (A tile's first row is the same in all lanes: their offsets from it are all that is formed for each.)
+  auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {
+    const int64_t base = (int64_t)head.first + t * kTile;
+    const uint32_t row = min(r, cached - t * kTile - 1);  // (rows behind the last one are the last one)
+    const uint32_t at = row * (D / 2) + g * (D / 4), scale = row * (D / 32) + g * (D / 64);
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      x.k[j] = *reinterpret_cast<const u32x4*>(prm.cache.k_codes + at + 16 * j);
-      x.v[j] = *reinterpret_cast<const u32x4*>(prm.cache.v_codes + at + 16 * j);
+      x.k[j] = *reinterpret_cast<const u32x4*>(prm.cache.k_codes + base * (D / 2) + at + 16 * j);
+      x.v[j] = *reinterpret_cast<const u32x4*>(prm.cache.v_codes + base * (D / 2) + at + 16 * j);
     }
-    const int64_t s = row * (D / 32) + g * (D / 64);
-    if (D == 128) {
-      x.ks = *reinterpret_cast<const uint16_t*>(prm.cache.k_scales + s);
-      x.vs = *reinterpret_cast<const uint16_t*>(prm.cache.v_scales + s);
-    } else {
-      x.ks = *reinterpret_cast<const uint8_t*>(prm.cache.k_scales + s);
-      x.vs = *reinterpret_cast<const uint8_t*>(prm.cache.v_scales + s);
-    }
+    const char *ks = prm.cache.k_scales + base * (D / 32) + scale, *vs = prm.cache.v_scales + base * (D / 32) + scale;
+    x.ks = D == 128 ? *reinterpret_cast<const uint16_t*>(ks) : *reinterpret_cast<const uint8_t*>(ks);
+    x.vs = D == 128 ? *reinterpret_cast<const uint16_t*>(vs) : *reinterpret_cast<const uint8_t*>(vs);
   };
   u32x4 kr[C::kLoads], vr[C::kLoads];
   auto load_resp = [&](int t) __attribute__((always_inline)) {
@@ -341,6 +338,241 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     }
     if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
   }
+}
+
+// ---- up to 16 query rows of bf16 (single tokens, a few of a grouped head): eight waves on the 16-row form of the matrix instructions.
+//
+// The layout is that of the kernel above with quarters of a wave for halves: a lane's share of a key is a quarter of its row, at head_dim
+// 128 one group with one scale, and a lane has 8 instead of 16 probabilities of a tile.  What a call of few queries takes is the reading
+// of the cache and the time of one tile from its first load to its last product; half the registers leave room for twice the
+// waves, so that most waves have one tile or two.
+template <int D>
+struct FewCfg {
+  static constexpr int kWaves = 8;
+  static constexpr int kQueries = 16;
+  static constexpr int kRowB = 2 * D;
+  static constexpr int kPPR = kRowB / 16;
+  static constexpr int kWords = D / 32;                // code words of a lane's quarter row
+  static constexpr int kBlocks = D / 16;               // of 16 output rows
+  static constexpr int kLoads = kTile * kPPR / 64;     // of 16 bytes a lane, of a tile's V
+  static constexpr int kWaveB = kTile * kRowB;         // V
+  static constexpr int kSumP = D + 4;
+  static constexpr int kSumB = kQueries * kSumP * 4;
+  static constexpr int kLds = kWaves * (kWaveB > kSumB ? kWaveB : kSumB) + kWaves * kQueries * 8;
+};
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+__device__ __forceinline__ void mfma16(const u32x4& a, const u32x4& b, f32x4& acc) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+// Over the quarters of a wave.
+__device__ __forceinline__ float max_quarters(float v) {
+  const auto x = __builtin_amdgcn_permlane16_swap(as_u32(v), as_u32(v), false, false);
+  const uint32_t a = x[0], b = x[1];
+  return max_halves(fmaxf(as_f32(a), as_f32(b)));
+}
+__device__ __forceinline__ float sum_quarters(float v) {
+  const auto x = __builtin_amdgcn_permlane16_swap(as_u32(v), as_u32(v), false, false);
+  const uint32_t a = x[0], b = x[1];
+  return sum_halves(as_f32(a) + as_f32(b));
+}
+
+template <int D>
+__global__ __launch_bounds__(512, 4) void attend_mx_few_kernel(const AttendMxParams prm) {
+  using C = FewCfg<D>;
+  constexpr int kWaves = C::kWaves;
+  extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
+  fetch_attend_mx_arguments();
+  const int unit = blockIdx.x;
+  const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
+  auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kTile - 1) / kTile) + resp_tiles; };  // those of the response first
+  const int capacity = (int)prm.capacity;
+  UnitHead head;
+  if (prm.chunk) {
+    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
+    if (head.bh < 0) return;
+  } else {
+    const int first = min(prm.cu[unit], capacity);
+    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
+  }
+  const int bh = head.bh, units = head.units, cached = head.rows, tiles = tiles_of(cached);
+  const int b = bh / prm.H, h = bh % prm.H;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  if (prm.chunk && unit == head.first_unit && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, units);
+  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
+  const int t1 = prm.chunk ? min(tiles, t0 + prm.chunk) : tiles;
+  char* const v_lds = mx_lds + wave * C::kWaveB;
+  const uint32_t v_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)v_lds;
+
+  typedef __attribute__((ext_vector_type(C::kWords))) uint32_t Codes;
+  struct Cached {  // of keys r and 16 + r of a tile
+    Codes k[2], v[2];
+    uint32_t ks[2], vs[2];
+  } ahead;
+  // (A tile's first row is the same in all lanes: their offsets from it are all that is formed for each.)
+  auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {
+    const int64_t base = (int64_t)head.first + t * kTile;
+    const int last = cached - t * kTile - 1;  // (rows behind the last one are the last one)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t row = min(16 * u + r, last);
+      const uint32_t at = row * (D / 2) + g * (D / 8), scale = row * (D / 32) + g * (D / 32) / 4;
+      x.k[u] = *reinterpret_cast<const Codes*>(prm.cache.k_codes + base * (D / 2) + at);
+      x.v[u] = *reinterpret_cast<const Codes*>(prm.cache.v_codes + base * (D / 2) + at);
+      x.ks[u] = *reinterpret_cast<const uint8_t*>(prm.cache.k_scales + base * (D / 32) + scale);
+      x.vs[u] = *reinterpret_cast<const uint8_t*>(prm.cache.v_scales + base * (D / 32) + scale);
+    }
+  };
+  // This wave's tiles: t0 + wave, and every eighth from there; those of the response are the first `resp` of them.
+  const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
+  const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
+  auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
+  u32x4 qf[C::kWords];
+  {
+    const char* q = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, min(r, prm.n_q - 1)) + g * (C::kRowB / 4);
+#pragma unroll
+    for (int i = 0; i < C::kWords; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
+  }
+  f32x4 o[C::kBlocks], s[2];
+#pragma unroll
+  for (int i = 0; i < C::kBlocks; ++i) o[i] = f32x4{};
+  float m = kNegBig, l = 0.f;
+
+  // Rows 4g .. 4g+3 and 16 on of V: lane i of 16 points at 8 bytes of row i / 4 of them and receives column i of a block.
+  const uint32_t read_row = 4 * g + (r >> 2);
+  const uint32_t read_at = v_at + read_row * C::kRowB + (v_swizzle<D>(read_row) << 5) + (r & 3) * 8;
+  const uint32_t write_at = v_at + r * C::kRowB + ((g * C::kWords ^ v_swizzle<D>(r) << 1) << 4);
+
+  // Softmax of a tile with `left` rows, and the output update.  Lanes with the same r have the same query.
+  auto update = [&](int left) __attribute__((always_inline)) {
+    if (left < kTile) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * u + i >= left - 4 * g) s[u][i] = -INFINITY;
+    }
+    float bm = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) bm = fmaxf(bm, s[i / 4][i % 4]);
+    const float cand = max_quarters(bm) * prm.c;
+    const bool bump = cand > m + kLazyBump;  // (see attend.hip)
+    if (__any(bump)) {
+      const float m_new = bump ? cand : m;
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int n = 0; n < C::kBlocks; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][i] *= alpha;
+    }
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = fast_exp2(fmaf(s[i / 4][i % 4], prm.c, -m));
+      l += p[i];
+    }
+    const u32x4 pf = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])};
+    uint32_t from = read_at;
+    asm volatile("" : "+v"(from));  // (an address for each block would be kept in a register of its own)
+#pragma unroll
+    for (int n = 0; n < C::kBlocks; ++n) {
+      const u32x2 lo = read_transposed(from ^ n << 5, 0), hi = read_transposed(from ^ n << 5, 16 * C::kRowB);
+      mfma16(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[n]);
+    }
+  };
+
+  for (int i = 0; i < resp; ++i) {
+    const int t = tile_of(i);
+    u32x4 v[C::kLoads];
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const int row = j * (64 / C::kPPR) + lane / C::kPPR;
+      v[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, min(t * kTile + row, prm.n_resp - 1)) + lane % C::kPPR * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const uint32_t row = j * (64 / C::kPPR) + lane / C::kPPR, p = lane % C::kPPR;
+      *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + ((p ^ v_swizzle<D>(row) << 1) << 4)) = v[j];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const char* k = prm.K2.row(b, h, min(t * kTile + 16 * u + r, prm.n_resp - 1)) + g * (C::kRowB / 4);
+      s[u] = f32x4{};
+#pragma unroll
+      for (int w = 0; w < C::kWords; ++w) mfma16(*reinterpret_cast<const u32x4*>(k + 16 * w), qf[w], s[u]);
+    }
+    asm volatile("" ::: "memory");
+    update(prm.n_resp - t * kTile);
+    asm volatile("" ::: "memory");
+  }
+  auto take = [&](int i, Cached& x) __attribute__((always_inline)) {
+    const int t = tile_of(i) - resp_tiles;
+    uint32_t to = write_at;
+    asm volatile("" : "+v"(to));
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        *in_lds<u32x4>(to ^ w << 4, 16 * u * C::kRowB) = mx_decode_bf16(x.v[u][w], mx_unit(x.vs[u]));
+    s[0] = s[1] = f32x4{};
+#pragma unroll
+    for (int w = 0; w < C::kWords; ++w) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) mfma16(mx_decode_bf16(x.k[u][w], mx_unit(x.ks[u])), qf[w], s[u]);
+      if (w % 2) __builtin_amdgcn_sched_barrier(0);  // (all words converted before the first product: 35 registers more than there are)
+    }
+    if (i + 1 < mine) load_cached(t + kWaves, x);
+    asm volatile("" ::: "memory");
+    update(cached - t * kTile);
+    asm volatile("" ::: "memory");
+  };
+  // (The response is one tile of one wave of a head: what is asked for ahead of it would take the registers of all.)
+  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, ahead);
+  for (int i = resp; i < mine; ++i) take(i, ahead);
+
+  // ---- the waves' results become one
+  l = sum_quarters(l);
+  float2* const ml = reinterpret_cast<float2*>(mx_lds + C::kLds - kWaves * C::kQueries * 8);
+  if (g == 0) ml[wave * C::kQueries + r] = make_float2(m, l);
+  __syncthreads();
+  float top = kNegBig;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * C::kQueries + r].x);
+  const float mine_by = fast_exp2(m - top);
+  float* const sums = reinterpret_cast<float*>(mx_lds);
+  if (r < prm.n_q)
+#pragma unroll
+    for (int n = 0; n < C::kBlocks; ++n)
+      *reinterpret_cast<float4*>(sums + (wave * C::kQueries + r) * C::kSumP + 16 * n + 4 * g) =
+          make_float4(o[n][0] * mine_by, o[n][1] * mine_by, o[n][2] * mine_by, o[n][3] * mine_by);
+  __syncthreads();
+  constexpr int kPerRow = D / 4;
+  const int q = threadIdx.x / kPerRow, at = threadIdx.x % kPerRow * 4;  // (512 threads: 16 rows at head_dim 128)
+  if (q >= prm.n_q) return;
+  float mq = kNegBig, lq = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) mq = fmaxf(mq, ml[w * C::kQueries + q].x);
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    lq += ml[w * C::kQueries + q].y * fast_exp2(ml[w * C::kQueries + q].x - mq);
+    const float4 z = *reinterpret_cast<const float4*>(sums + (w * C::kQueries + q) * C::kSumP + at);
+    x = make_float4(x.x + z.x, x.y + z.y, x.z + z.z, x.w + z.w);
+  }
+  if (units > 1) {
+    const int64_t part = (int64_t)unit * prm.part_rows + q;
+    *reinterpret_cast<float4*>(prm.part_o + part * D + at) = x;
+    if (at == 0) prm.part_ml[part] = make_float2(mq, lq);
+    return;
+  }
+  const float by = 1.f / lq;
+  *reinterpret_cast<u32x2*>(prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + at * 2) =
+      u32x2{pack_bf16x2(x.x * by, x.y * by), pack_bf16x2(x.z * by, x.w * by)};
+  if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
 }
 
 // ---- many query rows of bf16: a workgroup of four waves serves 128 of a head, 32 a wave, over tiles of 64 keys that all of them read
@@ -717,6 +949,7 @@ __global__ __launch_bounds__(512) void attend_mx_join_kernel(const AttendMxParam
 
 // How the tiles are dealt out.
 struct Deal {
+  bool few;       // up to 16 query rows
   bool wide;      // 128 query rows a workgroup, heads whole
   int qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
@@ -730,6 +963,7 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int64_t BH = (int64_t)d->B * d->H;
   Deal x;
   x.wide = d->dtype == MASKKV_BF16 && n_q > kWideQueries / 2 && BH * ((n_q + kWideQueries - 1) / kWideQueries) >= kUnits / 2;
+  x.few = d->dtype == MASKKV_BF16 && n_q <= 16;
   x.qtiles = (n_q + kTile - 1) / kTile;
   x.part_rows = n_q < kTile ? n_q : kTile;
   x.chunk = 0;
@@ -768,26 +1002,33 @@ int launch_wide(const AttendMxParams& prm, hipStream_t stream) {
 
 template <typename T, int D>
 int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) {
-  if constexpr (sizeof(T) == 2) {
-    if (deal.wide) return launch_wide<D>(prm, stream);
-  }
   using C = MxCfg<T, D>;
   static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
-  const int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
+  auto kernel = &attend_mx_kernel<T, D>;
+  int threads = kWaves * 64, lds = C::kLds;
+  int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
+  if constexpr (sizeof(T) == 2) {
+    if (deal.wide) return launch_wide<D>(prm, stream);
+    if (deal.few) {
+      kernel = &attend_mx_few_kernel<D>;
+      threads = FewCfg<D>::kWaves * 64;
+      lds = FewCfg<D>::kLds;
+      groups = deal.units;
+    }
+  }
   if (groups > 0x7FFFFFFF) {
     set_error("attend_mx: %lld workgroups are more than a launch can have", (long long)groups);
     return MASKKV_ESHAPE;
   }
-  const auto kernel = attend_mx_kernel<T, D>;
-  if (C::kLds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+  if (lds > 48 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) {
       set_error("attend_mx: hipFuncSetAttribute: %s", hipGetErrorString(e));
       (void)hipGetLastError();
       return MASKKV_EHIP;
     }
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), C::kLds, stream, prm);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, stream, prm);
   if (int e = check_launch("attend_mx")) return e;
   if (!deal.chunk) return MASKKV_OK;
   hipLaunchKernelGGL((attend_mx_join_kernel<T, D>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(512), 0, stream, prm);
