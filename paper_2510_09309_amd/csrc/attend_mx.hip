@@ -48,17 +48,14 @@ template <typename T, int D>
 struct MxCfg {
   static constexpr int kRowB = D * (int)sizeof(T);
   static constexpr int kPPR = kRowB / 16;        // pieces of 16 bytes in a row
-  static constexpr int kLoads = kPPR / 2;        // of 16 bytes a lane, of a tile's K (and V)
+  static constexpr int kLoads = kPPR / 2;        // of 16 bytes a lane, of a tile's V
   static constexpr int kRPL = 64 / kPPR;         // rows of such a load
   static constexpr int kWords = D / 16;          // code words of a lane's half row
   static constexpr int kDB = D / 32;
-  static constexpr int kTileB = kTile * kRowB;
-  static constexpr int kWaveB = 2 * kTileB;      // K (of the response) and V
-  static constexpr int kSumP = D + 4;            // floats from one query's sums to the next while the waves are merged
+  static constexpr int kTileB = kTile * kRowB;     // V of a wave
+  static constexpr int kSumP = D / 2 + 4;          // floats from one query's sums to the next while the waves are merged, half a row at a time
   static constexpr int kSumB = kTile * kSumP * 4;
-  static constexpr int kLds = kWaves * (kWaveB > kSumB ? kWaveB : kSumB) + kWaves * kTile * 8;
-  // K: piece p of a row in slot p ^ swz_k(row).
-  __device__ static uint32_t swz_k(uint32_t row) { return sizeof(T) == 2 && D == 64 ? (row >> 1) & 7 : row & 15; }
+  static constexpr int kLds = kWaves * (kTileB > kSumB ? kTileB : kSumB) + kWaves * kTile * 8;
   // V: bf16 see v_swizzle; fp32: blocks of 32 columns, exchanged in every other four rows.
   __device__ static uint32_t v_slot(uint32_t row, uint32_t p) {
     return sizeof(T) == 2 ? (p ^ v_swizzle<D>(row) << 1) : p ^ ((row >> 2) & 1) << 3;
@@ -66,7 +63,7 @@ struct MxCfg {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx_kernel(const AttendMxParams prm) {
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx_kernel(const AttendMxParams prm) {
   using C = MxCfg<T, D>;
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
@@ -94,15 +91,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
   const int t1 = prm.chunk ? min(tiles, t0 + prm.chunk) : tiles;
 
-  char* const k_lds = mx_lds + wave * C::kWaveB;
-  char* const v_lds = k_lds + C::kTileB;
+  char* const v_lds = mx_lds + wave * C::kTileB;
   const uint32_t v_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)v_lds;
 
-  // ---- what is under way: two tiles of the cache, and one of the response
+  // ---- what is under way: a tile of the cache
   struct Cached {
     u32x4 k[D / 64], v[D / 64];
     uint32_t ks, vs;
-  } one, two;
+  } ahead;
   // (A tile's first row is the same in all lanes: their offsets from it are all that is formed for each.)
   auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {
     const int64_t base = (int64_t)head.first + t * kTile;
@@ -117,23 +113,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     x.ks = D == 128 ? *reinterpret_cast<const uint16_t*>(ks) : *reinterpret_cast<const uint8_t*>(ks);
     x.vs = D == 128 ? *reinterpret_cast<const uint16_t*>(vs) : *reinterpret_cast<const uint8_t*>(vs);
   };
-  u32x4 kr[C::kLoads], vr[C::kLoads];
-  auto load_resp = [&](int t) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < C::kLoads; ++j) {
-      const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
-      kr[j] = *reinterpret_cast<const u32x4*>(prm.K2.row(b, h, row) + lane % C::kPPR * 16);
-      vr[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, row) + lane % C::kPPR * 16);
-    }
-  };
-
   // This wave's tiles: t0 + wave, and every fourth from there; those of the response are the first `resp` of them.
   const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
   const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
   auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
-  if (resp > 0) load_resp(tile_of(0));
-  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, one);
-  if (mine > resp + 1) load_cached(tile_of(resp + 1) - resp_tiles, two);
+  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, ahead);
 
   // ---- this lane's query: half of its row, as the B operand of the first product
   u32x4 qf[C::kPPR / 2];
@@ -188,6 +172,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
       l += p;
     }
     if constexpr (!F32) {
+      uint32_t from = v_at + v_read_offset<D>(lane, 0);
+      asm volatile("" : "+v"(from));  // (an address for each block would be kept in a register of its own)
 #pragma unroll
       for (int tp = 0; tp < 2; ++tp) {
         u32x4 pf;
@@ -195,8 +181,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
         for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(s[8 * tp + 2 * w], s[8 * tp + 2 * w + 1]);
 #pragma unroll
         for (int db = 0; db < C::kDB; ++db) {
-          const uint32_t from = v_at + v_read_offset<D>(lane, db);
-          const u32x2 lo = read_transposed(from, 16 * tp * C::kRowB), hi = read_transposed(from, (16 * tp + 8) * C::kRowB);
+          const u32x2 lo = read_transposed(from ^ db << 6, 16 * tp * C::kRowB), hi = read_transposed(from ^ db << 6, (16 * tp + 8) * C::kRowB);
           mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[db]);
         }
       }
@@ -215,33 +200,36 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
 
   for (int i = 0; i < resp; ++i) {
     const int t = tile_of(i);
+    {
+      u32x4 v[C::kLoads];
 #pragma unroll
-    for (int j = 0; j < C::kLoads; ++j) {
-      const uint32_t row = j * C::kRPL + lane / C::kPPR, p = lane % C::kPPR;
-      *reinterpret_cast<u32x4*>(k_lds + row * C::kRowB + ((p ^ C::swz_k(row)) << 4)) = kr[j];
-      *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + (C::v_slot(row, p) << 4)) = vr[j];
-    }
-    if (i + 1 < resp) load_resp(tile_of(i + 1));
-    asm volatile("" ::: "memory");
-    s = f32x16{};
+      for (int j = 0; j < C::kLoads; ++j) {
+        const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
+        v[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, row) + lane % C::kPPR * 16);
+      }
 #pragma unroll
-    for (int w = 0; w < C::kWords; ++w) {
-      auto piece = [&](int p) { return *reinterpret_cast<const u32x4*>(k_lds + r * C::kRowB + ((p ^ C::swz_k(r)) << 4)); };
-      if constexpr (F32) {
-        const u32x4 a = piece(g * (C::kPPR / 2) + 2 * w), c = piece(g * (C::kPPR / 2) + 2 * w + 1);
-        const uint32_t a0 = a[0], a1 = a[1], a2 = a[2], a3 = a[3], c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
-        const float x[8] = {as_f32(a0), as_f32(a1), as_f32(a2), as_f32(a3), as_f32(c0), as_f32(c1), as_f32(c2), as_f32(c3)};
-        logits_step_f32(w, x);
-      } else {
-        logits_step(w, piece(g * (C::kPPR / 2) + w));
+      for (int j = 0; j < C::kLoads; ++j) {
+        const uint32_t row = j * C::kRPL + lane / C::kPPR, p = lane % C::kPPR;
+        *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + (C::v_slot(row, p) << 4)) = v[j];
       }
     }
+    __builtin_amdgcn_sched_barrier(0);  // (K's fragments take the registers that V has passed through)
+    const char* k = prm.K2.row(b, h, min(t * kTile + r, prm.n_resp - 1)) + g * (C::kRowB / 2);
+    u32x4 kf[C::kPPR / 2];
+#pragma unroll
+    for (int w = 0; w < C::kPPR / 2; ++w) kf[w] = *reinterpret_cast<const u32x4*>(k + 16 * w);
+    s = f32x16{};
+#pragma unroll
+    for (int w = 0; w < C::kPPR / 2; ++w) mfma_step<T>(kf[w], qf[w], s);
+    asm volatile("" ::: "memory");
     update(prm.n_resp - t * kTile);
     asm volatile("" ::: "memory");
   }
   auto take = [&](int i, Cached& x) __attribute__((always_inline)) {
     const int t = tile_of(i) - resp_tiles;
     // V on its way into LDS, K into the first product
+    uint32_t to = v_at + r * C::kRowB + (C::v_slot(r, g * (C::kPPR / 2)) << 4);
+    asm volatile("" : "+v"(to));
 #pragma unroll
     for (int w = 0; w < C::kWords; ++w) {
       const uint32_t word = x.v[w / 4][w % 4];
@@ -249,11 +237,10 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
       if constexpr (F32) {
         float y[8];
         mx_decode_f32(word, unit, y);
-        const uint32_t p = g * (C::kPPR / 2) + 2 * w;
-        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p) << 4)) = make_float4(y[0], y[1], y[2], y[3]);
-        *reinterpret_cast<float4*>(v_lds + r * C::kRowB + (C::v_slot(r, p + 1) << 4)) = make_float4(y[4], y[5], y[6], y[7]);
+        *in_lds<u32x4>(to ^ 2 * w << 4) = u32x4{as_u32(y[0]), as_u32(y[1]), as_u32(y[2]), as_u32(y[3])};
+        *in_lds<u32x4>(to ^ (2 * w + 1) << 4) = u32x4{as_u32(y[4]), as_u32(y[5]), as_u32(y[6]), as_u32(y[7])};
       } else {
-        *reinterpret_cast<u32x4*>(v_lds + r * C::kRowB + (C::v_slot(r, g * (C::kPPR / 2) + w) << 4)) = mx_decode_bf16(word, unit);
+        *in_lds<u32x4>(to ^ w << 4) = mx_decode_bf16(word, unit);
       }
     }
     asm volatile("" ::: "memory");
@@ -270,14 +257,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
         logits_step(w, mx_decode_bf16(word, unit));
       }
     }
-    if (i + 2 < mine) load_cached(t + 2 * kWaves, x);
+    if (i + 1 < mine) load_cached(t + kWaves, x);
     update(cached - t * kTile);
     asm volatile("" ::: "memory");
   };
-  for (int i = resp; i < mine; i += 2) {
-    take(i, one);
-    if (i + 1 < mine) take(i + 1, two);
-  }
+  for (int i = resp; i < mine; ++i) take(i, ahead);
 
   // ---- the waves' results become one: sums of each wave, in units of the largest reference, through LDS
   l = sum_halves(l);
@@ -289,20 +273,23 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kTile + r].x);
   const float mine_by = fast_exp2(m - top);
   float* const sums = reinterpret_cast<float*>(mx_lds);
-  if (qtile * kTile + r < prm.n_q)
+  constexpr int kEach = 8;                // elements of a row that a thread writes
+  constexpr int kPerRow = D / 2 / kEach;  // threads of half a row
 #pragma unroll
-    for (int db = 0; db < C::kDB; ++db)
+  for (int half = 0; half < 2; ++half) {
+    if (half) __syncthreads();
+    if (qtile * kTile + r < prm.n_q)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 x = make_float4(o[db][4 * i] * mine_by, o[db][4 * i + 1] * mine_by, o[db][4 * i + 2] * mine_by, o[db][4 * i + 3] * mine_by);
-        *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * db + 8 * i + 4 * g) = x;
-      }
-  __syncthreads();
-  constexpr int kEach = 8;               // elements of a row that a thread writes
-  constexpr int kPerRow = D / kEach;     // threads of a row
-  for (int row = threadIdx.x / kPerRow; row < kTile; row += kWaves * 64 / kPerRow) {
-    const int q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;
-    if (q >= prm.n_q) break;
+      for (int n = 0; n < C::kDB / 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& from = o[half * (C::kDB / 2) + n];
+          *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * n + 8 * i + 4 * g) =
+              make_float4(from[4 * i] * mine_by, from[4 * i + 1] * mine_by, from[4 * i + 2] * mine_by, from[4 * i + 3] * mine_by);
+        }
+    __syncthreads();
+    const int row = threadIdx.x / kPerRow, q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;  // (256 threads: 32 rows or more)
+    if (row >= kTile || q >= prm.n_q) continue;
     float mq = kNegBig, lq = 0.f;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) mq = fmaxf(mq, ml[w * kTile + row].x);
@@ -319,16 +306,17 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
       }
       x[e] = y.x, x[e + 1] = y.y, x[e + 2] = y.z, x[e + 3] = y.w;
     }
+    const int to_at = half * (D / 2) + at;
     if (units > 1) {
       const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + row;
-      float4* to = reinterpret_cast<float4*>(prm.part_o + part * D + at);
+      float4* to = reinterpret_cast<float4*>(prm.part_o + part * D + to_at);
       to[0] = make_float4(x[0], x[1], x[2], x[3]);
       to[1] = make_float4(x[4], x[5], x[6], x[7]);
-      if (at == 0) prm.part_ml[part] = make_float2(mq, lq);
+      if (to_at == 0) prm.part_ml[part] = make_float2(mq, lq);
       continue;
     }
     const float by = 1.f / lq;
-    char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + at * (int)sizeof(T);
+    char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + to_at * (int)sizeof(T);
     if constexpr (F32) {
       reinterpret_cast<float4*>(to)[0] = make_float4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
       reinterpret_cast<float4*>(to)[1] = make_float4(x[4] * by, x[5] * by, x[6] * by, x[7] * by);
@@ -336,7 +324,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
       *reinterpret_cast<u32x4*>(to) = u32x4{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by),
                                             pack_bf16x2(x[4] * by, x[5] * by), pack_bf16x2(x[6] * by, x[7] * by)};
     }
-    if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
+    if (to_at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
   }
 }
 
@@ -880,30 +868,33 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   if (prm.lse && g == 0 && q0 + r < prm.n_q) prm.lse[(int64_t)bh * prm.n_q + q0 + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// The partial results of the heads that have several units, a query row at a time: sums in units of the largest reference, dealt
-// to groups of D/4 threads, each of which asks for kAtOnce partial results before it uses the first.
-template <typename T, int D>
-__global__ __launch_bounds__(512) void attend_mx_join_kernel(const AttendMxParams prm) {
-  constexpr int kPer = D / 4, kGroups = 512 / kPer, kAtOnce = 8;
-  __shared__ float4 sums[kGroups][kPer];
-  __shared__ float2 tops[kGroups];
+// The partial results of the heads that have several units: sums in units of the largest reference.  D/4 threads take a query row and
+// ask for kAtOnce of its partial results before they use the first; where a head has many, the eight groups of a workgroup share one
+// row (SHARED) and meet in LDS, else each has a row of its own.
+constexpr int kJoinGroups = 8;
+template <typename T, int D, bool SHARED>
+__global__ __launch_bounds__(kJoinGroups * D / 4) void attend_mx_join_kernel(const AttendMxParams prm) {
+  constexpr int kPer = D / 4, kAtOnce = 8, kStep = SHARED ? kJoinGroups : 1;
+  __shared__ float4 sums[kJoinGroups][kPer];
+  __shared__ float2 tops[kJoinGroups];
+  fetch_attend_mx_arguments();
   const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer;
   const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
-  const int bh = blockIdx.y, q = blockIdx.x;
+  const int bh = blockIdx.y, q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
   const int first = prm.parts[bh].x, units = prm.parts[bh].y;
-  if (units <= 1) return;
+  if (units <= 1 || q >= prm.n_q) return;
   const int64_t part0 = first * step + (int64_t)(q / kTile) * prm.part_rows + q % kTile;
   float m = kNegBig, l = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int u0 = grp; u0 < units; u0 += kAtOnce * kGroups) {
+  for (int u0 = SHARED ? grp : 0; u0 < units; u0 += kAtOnce * kStep) {
     float2 ml[kAtOnce];
     float4 y[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       ml[i] = make_float2(kNegBig, 0.f);
       y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (u0 + i * kGroups < units) {
-        const int64_t part = part0 + (u0 + i * kGroups) * step;
+      if (u0 + i * kStep < units) {
+        const int64_t part = part0 + (u0 + i * kStep) * step;
         ml[i] = prm.part_ml[part];
         y[i] = *reinterpret_cast<const float4*>(prm.part_o + part * D + at * 4);
       }
@@ -922,21 +913,23 @@ __global__ __launch_bounds__(512) void attend_mx_join_kernel(const AttendMxParam
       x = make_float4(fmaf(y[i].x, by, x.x), fmaf(y[i].y, by, x.y), fmaf(y[i].z, by, x.z), fmaf(y[i].w, by, x.w));
     }
   }
-  sums[grp][at] = x;
-  if (at == 0) tops[grp] = make_float2(m, l);
-  __syncthreads();
-  if (grp > 0) return;
-  float top = kNegBig;
+  if constexpr (SHARED) {
+    sums[grp][at] = x;
+    if (at == 0) tops[grp] = make_float2(m, l);
+    __syncthreads();
+    if (grp > 0) return;
+    m = kNegBig;
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, tops[i].x);
-  l = 0.f;
-  x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < kJoinGroups; ++i) m = fmaxf(m, tops[i].x);
+    l = 0.f;
+    x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    const float by = fast_exp2(tops[i].x - top);
-    const float4 y = sums[i][at];
-    l = fmaf(tops[i].y, by, l);
-    x = make_float4(fmaf(y.x, by, x.x), fmaf(y.y, by, x.y), fmaf(y.z, by, x.z), fmaf(y.w, by, x.w));
+    for (int i = 0; i < kJoinGroups; ++i) {
+      const float by = fast_exp2(tops[i].x - m);
+      const float4 y = sums[i][at];
+      l = fmaf(tops[i].y, by, l);
+      x = make_float4(fmaf(y.x, by, x.x), fmaf(y.y, by, x.y), fmaf(y.z, by, x.z), fmaf(y.w, by, x.w));
+    }
   }
   const float by = 1.f / l;
   char* to = prm.O.group_row(bh / prm.H, bh % prm.H, prm.q_per_kv, prm.n_resp, q) + at * 4 * (int)sizeof(T);
@@ -944,7 +937,7 @@ __global__ __launch_bounds__(512) void attend_mx_join_kernel(const AttendMxParam
     *reinterpret_cast<float4*>(to) = make_float4(x.x * by, x.y * by, x.z * by, x.w * by);
   else
     *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(x.x * by, x.y * by), pack_bf16x2(x.z * by, x.w * by)};
-  if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (top + __builtin_amdgcn_logf(l)) * kLn2;
+  if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // How the tiles are dealt out.
@@ -955,7 +948,8 @@ struct Deal {
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
 };
-constexpr int kLeastChunk = 8;      // tiles of a unit: two of each wave
+constexpr int kSharedUnits = 16;    // units of a head on average above which a query row's partial results are read by a whole workgroup
+constexpr int kLeastChunk = 16;     // tiles of a unit
 constexpr int kLongHead = 1 << 14;  // keys up to which the heads of a launch that fills the chip are left whole
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
@@ -976,7 +970,7 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
   if (BH * x.qtiles >= kUnits && most <= kLongHead) return x;
   const int64_t tiles = capacity / kTile + BH * (1 + (d->n_resp + kTile - 1) / kTile);
-  int64_t chunk = (tiles * x.qtiles + 2 * kUnits - 1) / (2 * kUnits);
+  int64_t chunk = (tiles * x.qtiles + kUnits - 1) / kUnits;
   if (chunk < kLeastChunk) chunk = kLeastChunk;
   if (chunk * kTile >= most + 2 * kTile) return x;  // (a head's last tiles of both kinds may be short)
   x.chunk = (int)chunk;
@@ -1031,7 +1025,11 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, stream, prm);
   if (int e = check_launch("attend_mx")) return e;
   if (!deal.chunk) return MASKKV_OK;
-  hipLaunchKernelGGL((attend_mx_join_kernel<T, D>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(512), 0, stream, prm);
+  if (deal.units > (int64_t)kSharedUnits * prm.BH)
+    hipLaunchKernelGGL((attend_mx_join_kernel<T, D, true>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(kJoinGroups * D / 4), 0, stream, prm);
+  else
+    hipLaunchKernelGGL((attend_mx_join_kernel<T, D, false>), dim3((unsigned)(prm.n_q + kJoinGroups - 1) / kJoinGroups, (unsigned)prm.BH),
+                       dim3(kJoinGroups * D / 4), 0, stream, prm);
   return check_launch("attend_mx (join)");
 }
 
