@@ -63,7 +63,7 @@ struct MxCfg {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx_kernel(const AttendMxParams prm) {
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx_kernel(const AttendMxParams prm) {
   using C = MxCfg<T, D>;
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
@@ -94,11 +94,24 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx
   char* const v_lds = mx_lds + wave * C::kTileB;
   const uint32_t v_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)v_lds;
 
-  // ---- what is under way: a tile of the cache
+  // ---- what is under way: two tiles of the cache, and one of the response
   struct Cached {
     u32x4 k[D / 64], v[D / 64];
     uint32_t ks, vs;
+  } one, two;
+  struct Resp {
+    u32x4 k[C::kPPR / 2], v[C::kLoads];  // this lane's half row of K, and V as it is moved
   } ahead;
+  auto load_resp = [&](int t, Resp& x) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::kLoads; ++j) {
+      const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
+      x.v[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, row) + lane % C::kPPR * 16);
+    }
+    const char* k = prm.K2.row(b, h, min(t * kTile + r, prm.n_resp - 1)) + g * (C::kRowB / 2);
+#pragma unroll
+    for (int w = 0; w < C::kPPR / 2; ++w) x.k[w] = *reinterpret_cast<const u32x4*>(k + 16 * w);
+  };
   // (A tile's first row is the same in all lanes: their offsets from it are all that is formed for each.)
   auto load_cached = [&](int t, Cached& x) __attribute__((always_inline)) {
     const int64_t base = (int64_t)head.first + t * kTile;
@@ -117,7 +130,9 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx
   const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
   const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
   auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
-  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, ahead);
+  if (resp > 0) load_resp(tile_of(0), ahead);
+  if (mine > resp) load_cached(tile_of(resp) - resp_tiles, one);
+  if (mine > resp + 1) load_cached(tile_of(resp + 1) - resp_tiles, two);
 
   // ---- this lane's query: half of its row, as the B operand of the first product
   u32x4 qf[C::kPPR / 2];
@@ -200,27 +215,15 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx
 
   for (int i = 0; i < resp; ++i) {
     const int t = tile_of(i);
-    {
-      u32x4 v[C::kLoads];
 #pragma unroll
-      for (int j = 0; j < C::kLoads; ++j) {
-        const int row = min(t * kTile + j * C::kRPL + lane / C::kPPR, prm.n_resp - 1);
-        v[j] = *reinterpret_cast<const u32x4*>(prm.V2.row(b, h, row) + lane % C::kPPR * 16);
-      }
-#pragma unroll
-      for (int j = 0; j < C::kLoads; ++j) {
-        const uint32_t row = j * C::kRPL + lane / C::kPPR, p = lane % C::kPPR;
-        *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + (C::v_slot(row, p) << 4)) = v[j];
-      }
+    for (int j = 0; j < C::kLoads; ++j) {
+      const uint32_t row = j * C::kRPL + lane / C::kPPR, p = lane % C::kPPR;
+      *reinterpret_cast<u32x4*>(v_lds + row * C::kRowB + (C::v_slot(row, p) << 4)) = ahead.v[j];
     }
-    __builtin_amdgcn_sched_barrier(0);  // (K's fragments take the registers that V has passed through)
-    const char* k = prm.K2.row(b, h, min(t * kTile + r, prm.n_resp - 1)) + g * (C::kRowB / 2);
-    u32x4 kf[C::kPPR / 2];
-#pragma unroll
-    for (int w = 0; w < C::kPPR / 2; ++w) kf[w] = *reinterpret_cast<const u32x4*>(k + 16 * w);
     s = f32x16{};
 #pragma unroll
-    for (int w = 0; w < C::kPPR / 2; ++w) mfma_step<T>(kf[w], qf[w], s);
+    for (int w = 0; w < C::kPPR / 2; ++w) mfma_step<T>(ahead.k[w], qf[w], s);
+    if (i + 1 < resp) load_resp(tile_of(i + 1), ahead);
     asm volatile("" ::: "memory");
     update(prm.n_resp - t * kTile);
     asm volatile("" ::: "memory");
@@ -257,11 +260,14 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 3 : 1) void attend_mx
         logits_step(w, mx_decode_bf16(word, unit));
       }
     }
-    if (i + 1 < mine) load_cached(t + kWaves, x);
+    if (i + 2 < mine) load_cached(t + 2 * kWaves, x);
     update(cached - t * kTile);
     asm volatile("" ::: "memory");
   };
-  for (int i = resp; i < mine; ++i) take(i, ahead);
+  for (int i = resp; i < mine; i += 2) {
+    take(i, one);
+    if (i + 1 < mine) take(i + 1, two);
+  }
 
   // ---- the waves' results become one: sums of each wave, in units of the largest reference, through LDS
   l = sum_halves(l);
