@@ -4,9 +4,9 @@
 // budgets, and which of the head's rows they are by itself, from all of the head's weights: several workgroups of a head do
 // the same search, which costs the latency of one, where a list made by one of them would cost a launch between the two.
 //
-// The search is for the smallest weight that stays, two bits of the weights' order a round: every wave counts its rows at or above
-// three candidates by ballots and the waves' counts meet in LDS, one barrier a round; it ends when a candidate has as many rows as
-// stay.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again every round.
+// The search is for the smallest weight that stays, and ends when a candidate has as many rows as stay.  Up to 512 rows every wave
+// holds all of them and goes through the bits of the weights' order by itself, by ballots: no barrier and no LDS.  Beyond that it goes
+// by histograms of eight bits in LDS.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again every round.
 #include "mx.hpp"
 
 namespace maskkv {
@@ -36,8 +36,7 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 struct HeadRows {
   int first, n, stay;
 };
-__device__ __forceinline__ HeadRows rows_of(const EvictParams& prm, int bh) {
-  const int capacity = (int)prm.capacity;
+__device__ __forceinline__ HeadRows rows_of(const EvictParams& prm, int bh, int capacity) {
   const int budget = prm.budgets[bh], a = min(prm.cu[bh], capacity), z = min(prm.cu[bh + 1], capacity);
   HeadRows x;
   x.first = a;
@@ -52,7 +51,7 @@ __device__ __forceinline__ void write_prefix(const EvictParams& prm) {
   int before = 0;
   for (int base = 0; base < prm.BH; base += 64) {
     const int bh = base + lane;
-    const int stay = bh < prm.BH ? rows_of(prm, bh).stay : 0;
+    const int stay = bh < prm.BH ? rows_of(prm, bh, (int)prm.capacity).stay : 0;
     const int upto = wave_prefix(stay);
     if (bh < prm.BH) prm.cu_out[bh] = before + upto - stay;
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -60,9 +59,50 @@ __device__ __forceinline__ void write_prefix(const EvictParams& prm) {
   if (lane == 0) prm.cu_out[prm.BH] = before;
 }
 
-// The numbers of the rows that stay with ranks lo .. hi-1 among the head's, into `list`.  VALUES: rows of a thread, in registers, or 0.
+// The numbers of the rows that stay with ranks lo .. hi-1 among the head's, into `list`; every wave by itself, up to 64 * VALUES rows.
+// (All waves come to the same ranks; each writes those of its share of the rows.)
 template <int THREADS, int VALUES>
-__device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int32_t* list, int (*counts)[THREADS / 64][4]) {
+__device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, int lo, int hi, int32_t* list) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t held[VALUES];
+#pragma unroll
+  for (int v = 0; v < VALUES; ++v) {
+    const float x = w[min(v * 64 + lane, n - 1)];
+    held[v] = v * 64 + lane < n ? order_of(x) : 0u;
+  }
+  uint32_t least = 0;   // a row at or above it stays, or may
+  bool exact = k == n;  // just those stay
+  for (uint32_t bit = 0x80000000u; bit && !exact; bit >>= 1) {
+    int c = 0;
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) c += __popcll(__ballot(held[v] >= (least | bit)));
+    if (c >= k) least |= bit;
+    exact = c == k;
+  }
+  int ties = k;  // so many of the rows at `least` stay, the first ones
+  if (!exact) {
+#pragma unroll
+    for (int v = 0; v < VALUES; ++v) ties -= __popcll(__ballot(held[v] > least));
+  }
+  int overs = 0, sames = 0;
+#pragma unroll
+  for (int v = 0; v < VALUES; ++v) {
+    const bool live = v * 64 + lane < n;
+    const uint64_t a = __ballot(live && (exact ? held[v] >= least : held[v] > least)), b = __ballot(live && !exact && held[v] == least);
+    if (v % (THREADS / 64) == wave) {
+      const uint64_t below = (1ull << lane) - 1;
+      const int before = sames + __popcll(b & below), rank = overs + __popcll(a & below) + min(before, ties);
+      const bool stays = (a >> lane & 1) || ((b >> lane & 1) && before < ties);
+      if (stays && rank >= lo && rank < hi) list[rank - lo] = v * 64 + lane;
+    }
+    overs += __popcll(a);
+    sames += __popcll(b);
+  }
+}
+
+// The same by the whole workgroup.  VALUES: rows of a thread, in registers, or 0.
+template <int THREADS, int VALUES>
+__device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int32_t* list, int* bins, int (*counts)[4]) {
   constexpr int kWaves = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = VALUES ? VALUES : (n + THREADS - 1) / THREADS;
@@ -87,43 +127,32 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
     }
   };
 
-  uint32_t least = 0;     // a row at or above it stays, or may
-  bool exact = k == n;    // just those stay
-  for (int shift = 30, round = 0; shift >= 0 && !exact; shift -= 2, ++round) {
-    int c[3] = {0, 0, 0};
-    over_rows([&](uint32_t o, int) {
-#pragma unroll
-      for (int j = 0; j < 3; ++j) c[j] += __popcll(__ballot(o >= (least | (uint32_t)(j + 1) << shift)));
-    });
-    int* mine = counts[round & 1][wave];
-    if (lane == 0) {
-      mine[0] = c[0];
-      mine[1] = c[1];
-      mine[2] = c[2];
-    }
+  // Eight bits of `least` a round: how many of the rows that agree with it so far have which next eight bits; then the highest
+  // of these with at least as many rows at or above it as are still to be found.
+  uint32_t least = 0;   // a row at or above it stays, or may
+  bool exact = k == n;  // just those stay
+  int wanted = k;       // of the rows that agree with `least` in the bits so far
+  for (int shift = 24; shift >= 0 && !exact; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += THREADS) bins[i] = 0;
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      int s;
-      if (kWaves == 4) {
-        s = counts[round & 1][0][j] + counts[round & 1][1][j] + counts[round & 1][2][j] + counts[round & 1][3][j];
-      } else {
-        s = counts[round & 1][lane % kWaves][j];  // (16 waves: the sum over a row of 16 lanes)
-        s = plus_dpp<0x121, 0xf>(s);
-        s = plus_dpp<0x122, 0xf>(s);
-        s = plus_dpp<0x124, 0xf>(s);
-        s = plus_dpp<0x128, 0xf>(s);
-      }
-      c[j] = __builtin_amdgcn_readfirstlane(s);
-    }
-    uint32_t digit = 0;
-#pragma unroll
-    for (int j = 0; j < 3; ++j)
-      if (c[j] >= k) {
-        digit = j + 1;
-        exact = c[j] == k;
-      }
-    least |= digit << shift;
+    over_rows([&](uint32_t o, int v) {
+      if (row0 + v * 64 < n && (shift == 24 || (o ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[o >> shift & 255], 1);
+    });
+    __syncthreads();
+    // every wave by itself: a lane holds four bins from the top, 255 - 4 lane ..
+    const int4 four = *reinterpret_cast<const int4*>(bins + 252 - 4 * lane);
+    const int own = four.x + four.y + four.z + four.w;
+    const int upto = wave_prefix(own);
+    const int at = __builtin_ctzll(__ballot(upto >= wanted));  // (there is one: all the rows that agree are `wanted` or more)
+    int above = __builtin_amdgcn_readlane(upto - own, at);     // rows above the bin in question
+    const int in[4] = {__builtin_amdgcn_readlane(four.w, at), __builtin_amdgcn_readlane(four.z, at), __builtin_amdgcn_readlane(four.y, at),
+                       __builtin_amdgcn_readlane(four.x, at)};
+    int j = 0;
+    while (j < 3 && above + in[j] < wanted) above += in[j++];
+    least |= (uint32_t)(255 - 4 * at - j) << shift;
+    exact = above + in[j] == wanted;
+    wanted -= above;
+    __syncthreads();
   }
   const auto over = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && (exact ? o >= least : o > least)); };
   const auto same = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && !exact && o == least); };
@@ -136,17 +165,16 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
 #pragma unroll
     for (int v = 0; v < VALUES; ++v) asm volatile("" : "+v"(held[v]));
   }
-  __syncthreads();
   if (lane == 0) {
-    counts[0][wave][0] = overs;
-    counts[0][wave][1] = sames;
+    counts[wave][0] = overs;
+    counts[wave][1] = sames;
   }
   __syncthreads();
   int ties = k;  // so many of the rows at `least` stay, the first ones
   overs = sames = 0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    const int a = counts[0][i][0], b = counts[0][i][1];
+    const int a = counts[i][0], b = counts[i][1];
     ties -= a;
     overs += i < wave ? a : 0;
     sames += i < wave ? b : 0;
@@ -169,46 +197,62 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams prm) {
   extern __shared__ int32_t list[];  // [per]
-  __shared__ int counts[2][THREADS / 64][4];
+  __shared__ __attribute__((aligned(16))) int bins[256];
+  __shared__ int counts[THREADS / 64][4];
+  typedef EvictParams A;
+  fetch_arguments({MASKKV_ARGUMENT(A, weights), MASKKV_ARGUMENT(A, rows), MASKKV_ARGUMENT(A, moved), (uint32_t)(offsetof(A, moved) + 64)});
   const int lane = threadIdx.x & 63;
   if (blockIdx.x == 0 && threadIdx.x < 64) write_prefix(prm);
 
   // ---- the head of this workgroup's rows, how many rows stay of the heads before it, and which of its own these are
-  const int unit = blockIdx.x;
+  constexpr int kSets = 4;
+  const int unit = blockIdx.x, capacity = (int)prm.capacity;
   int before = 0, units_before = 0, bh = -1, part = 0;
-  for (int base = 0; base < prm.BH && bh < 0; base += 64) {
-    const int stay = base + lane < prm.BH ? rows_of(prm, base + lane).stay : 0;
-    const int units = (int)(((uint32_t)stay + prm.per - 1) / prm.per);
-    const int rows_upto = wave_prefix(stay), upto = wave_prefix(units);
-    const uint64_t found = __ballot(units_before + upto > unit);
-    if (found) {
-      const int at = __builtin_ctzll(found);
-      bh = base + at;
-      part = unit - units_before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
-      before += __builtin_amdgcn_readlane(rows_upto, at) - __builtin_amdgcn_readlane(stay, at);
-    } else {
-      units_before += __builtin_amdgcn_readlane(upto, 63);
-      before += __builtin_amdgcn_readlane(rows_upto, 63);
+  HeadRows x = {0, 0, 0};
+  for (int base = 0; base < prm.BH && bh < 0; base += 64 * kSets) {
+    HeadRows some[kSets];
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) some[i] = rows_of(prm, min(base + i * 64 + lane, prm.BH - 1), capacity);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+      if (base + i * 64 >= prm.BH || bh >= 0) break;
+      const int stay = base + i * 64 + lane < prm.BH ? some[i].stay : 0;
+      const int units = (int)(((uint32_t)stay + prm.per - 1) / prm.per);
+      const int rows_upto = wave_prefix(stay), upto = wave_prefix(units);
+      const uint64_t found = __ballot(units_before + upto > unit);
+      if (found) {
+        const int at = __builtin_ctzll(found);
+        bh = base + i * 64 + at;
+        x = {__builtin_amdgcn_readlane(some[i].first, at), __builtin_amdgcn_readlane(some[i].n, at), __builtin_amdgcn_readlane(stay, at)};
+        part = unit - units_before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
+        before += __builtin_amdgcn_readlane(rows_upto, at) - x.stay;
+      } else {
+        units_before += __builtin_amdgcn_readlane(upto, 63);
+        before += __builtin_amdgcn_readlane(rows_upto, 63);
+      }
     }
   }
   if (bh < 0) return;
-  const HeadRows x = rows_of(prm, bh);
   const int lo = part * prm.per;
   const int64_t to = (int64_t)before + lo;
   const int rows = (int)min((int64_t)min(x.stay - lo, prm.per), prm.capacity_out - to);
   if (rows <= 0) return;
 
   const float* w = prm.weights + x.first;
-  if (x.n <= THREADS)
-    list_rows<THREADS, 1>(w, x.n, x.stay, lo, lo + rows, list, counts);
+  if (x.n <= 64)
+    list_rows_alone<THREADS, 1>(w, x.n, x.stay, lo, lo + rows, list);
+  else if (x.n <= 256)
+    list_rows_alone<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list);
+  else if (x.n <= 512)
+    list_rows_alone<THREADS, 8>(w, x.n, x.stay, lo, lo + rows, list);
   else if (x.n <= THREADS * 4)
-    list_rows<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list, counts);
+    list_rows<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
   else if (x.n <= THREADS * 16)
-    list_rows<THREADS, 16>(w, x.n, x.stay, lo, lo + rows, list, counts);
+    list_rows<THREADS, 16>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
   else if (x.n <= THREADS * 32)
-    list_rows<THREADS, 32>(w, x.n, x.stay, lo, lo + rows, list, counts);
+    list_rows<THREADS, 32>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
   else
-    list_rows<THREADS, 0>(w, x.n, x.stay, lo, lo + rows, list, counts);
+    list_rows<THREADS, 0>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
   __syncthreads();
 
   // ---- the rows, 16 bytes a thread and step

@@ -97,32 +97,43 @@ __device__ __forceinline__ int wave_prefix(int v) {
 }
 
 // The head of a unit of work when a head of n cached rows has units_of(n) units (bh -1: behind the last), which is its first and how
-// many it has, and where its rows lie.  Found by a wave, which counts 64 heads at a time.
+// many it has, and where its rows lie.  Found by a wave, which asks for 256 heads at a time and counts 64.
 struct UnitHead {
   int bh, first_unit, units;
   int first, rows;
 };
 template <typename F>
 __device__ __forceinline__ UnitHead head_of_unit(const int32_t* cu, int BH, int capacity, int unit, F units_of) {
+  constexpr int kSets = 4;
   const int lane = threadIdx.x & 63;
   UnitHead x = {-1, 0, 0, 0, 0};
   int before = 0;
-  for (int base = 0; base < BH; base += 64) {
-    const int bh = min(base + lane, BH - 1);
-    const int first = min(cu[bh], capacity), rows = max(min(cu[bh + 1], capacity) - first, 0);
-    const int own = base + lane < BH ? units_of(rows) : 0;
-    const int upto = wave_prefix(own);
-    const uint64_t over = __ballot(before + upto > unit);
-    if (over) {
-      const int at = __builtin_ctzll(over);
-      x.units = __builtin_amdgcn_readlane(own, at);
-      x.first_unit = before + __builtin_amdgcn_readlane(upto, at) - x.units;
-      x.first = __builtin_amdgcn_readlane(first, at);
-      x.rows = __builtin_amdgcn_readlane(rows, at);
-      x.bh = __builtin_amdgcn_readfirstlane(base + at);
-      return x;
+  for (int base = 0; base < BH; base += 64 * kSets) {
+    int from[kSets], to[kSets];
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+      const int bh = min(base + i * 64 + lane, BH - 1);
+      from[i] = cu[bh];
+      to[i] = cu[bh + 1];
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+      if (base + i * 64 >= BH) break;
+      const int first = min(from[i], capacity), rows = max(min(to[i], capacity) - first, 0);
+      const int own = base + i * 64 + lane < BH ? units_of(rows) : 0;
+      const int upto = wave_prefix(own);
+      const uint64_t over = __ballot(before + upto > unit);
+      if (over) {
+        const int at = __builtin_ctzll(over);
+        x.units = __builtin_amdgcn_readlane(own, at);
+        x.first_unit = before + __builtin_amdgcn_readlane(upto, at) - x.units;
+        x.first = __builtin_amdgcn_readlane(first, at);
+        x.rows = __builtin_amdgcn_readlane(rows, at);
+        x.bh = __builtin_amdgcn_readfirstlane(base + i * 64 + at);
+        return x;
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
+    }
   }
   return x;
 }
