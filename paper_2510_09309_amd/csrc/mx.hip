@@ -56,25 +56,74 @@ __device__ __forceinline__ void store_group(const u32x4& x, char* codes, char* s
   if (piece % kLanes == 0) scales[piece / kLanes] = (char)scale;
 }
 
+// A wave stores kRounds times as many rows as it has room for in its lanes, side by side, and asks for all of them before it uses the first.
+// Positions and the heads' ends are asked for at once, so that three waits in turn come before the first row is stored:
+// arguments, these, and the rows.
+constexpr int kRounds = 2;
+constexpr int kEnds = 256;  // heads up to which a wave holds the ends of all of them in its lanes
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxParams prm) {
+  typedef CompactMxParams A;
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, K), MASKKV_VIEW_ARGUMENTS(A, V), MASKKV_ARGUMENT(A, lens), MASKKV_ARGUMENT(A, H),
+                   MASKKV_ARGUMENT(A, out)});
   const int pieces = prm.d * (int)sizeof(T) / 16;  // of a row: 8, 16 or 32
-  const int64_t total = min((int64_t)prm.cu[prm.BH], prm.capacity);
-  const int lane = threadIdx.x & 63;
-  const int64_t first = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * (64 / pieces);  // of this wave
-  if (first >= total) return;
-  const int64_t row = first + lane / pieces;
-  const int64_t at = min(row, total - 1);  // (lanes behind the last row do it again, and store nothing)
-  int bh = head_of_row(prm.cu, prm.BH, (int)first);
-  while (bh + 1 < prm.BH && prm.cu[bh + 1] <= at) ++bh;
-  const int b = bh / prm.H, h = bh % prm.H, piece = lane % pieces;
-  // a position outside the prompt is clamped rather than read out of bounds
-  const int src = min(max(prm.idx[at], 0), max(prm.lens.P[b] - 1, 0));
-  const u32x4 k = *reinterpret_cast<const u32x4*>(prm.K.row(b, h, src) + piece * 16);
-  const u32x4 v = *reinterpret_cast<const u32x4*>(prm.V.row(b, h, src) + piece * 16);
-  if (row >= total) return;  // (all lanes of a row at once: the exchanges below stay inside a row)
-  store_group<T>(k, prm.out.k_codes + row * (prm.d / 2), prm.out.k_scales + row * (prm.d / kMxGroup), piece);
-  store_group<T>(v, prm.out.v_codes + row * (prm.d / 2), prm.out.v_scales + row * (prm.d / kMxGroup), piece);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int mine = 64 / pieces, piece = lane % pieces;
+  const int capacity = (int)prm.capacity;
+  const int64_t first64 = ((int64_t)blockIdx.x * (kThreads / 64) + wave) * (mine * kRounds);  // of this wave
+  if (first64 >= capacity) return;
+  const int first = (int)first64;
+  int position[kRounds];
+#pragma unroll
+  for (int u = 0; u < kRounds; ++u) position[u] = prm.idx[min(first + u * mine + lane / pieces, capacity - 1)];
+  int total, bh, end;  // the head of the first row, and where its rows end
+  if (prm.BH <= kEnds) {
+    int ends[kEnds / 64];
+#pragma unroll
+    for (int i = 0; i < kEnds / 64; ++i) ends[i] = prm.cu[min(i * 64 + lane + 1, prm.BH)];
+    total = min(__builtin_amdgcn_readlane(ends[kEnds / 64 - 1], 63), capacity);
+    if (first >= total) return;
+    bh = 0;
+#pragma unroll
+    for (int i = 0; i < kEnds / 64; ++i) bh += __popcll(__ballot(ends[i] <= first));  // (heads behind the last count as it does)
+    end = 0;
+#pragma unroll
+    for (int i = 0; i < kEnds / 64; ++i)
+      if (i == bh / 64) end = __builtin_amdgcn_readlane(ends[i], bh % 64);
+  } else {
+    total = min(prm.cu[prm.BH], capacity);
+    if (first >= total) return;
+    bh = head_of_row(prm.cu, prm.BH, first);
+    end = prm.cu[bh + 1];
+  }
+  u32x4 k[kRounds], v[kRounds];
+  auto load = [&](int u, int h, int b) {
+    // a position outside the prompt is clamped rather than read out of bounds
+    const int src = min(max(position[u], 0), max(prm.lens.P[b] - 1, 0));
+    k[u] = *reinterpret_cast<const u32x4*>(prm.K.row(b, h, src) + piece * 16);
+    v[u] = *reinterpret_cast<const u32x4*>(prm.V.row(b, h, src) + piece * 16);
+  };
+  if (min(first + kRounds * mine, total) <= end) {  // all rows are of one head
+    const int b = bh / prm.H, h = bh % prm.H;
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) load(u, h, b);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kRounds; ++u) {
+      const int row = min(first + u * mine + lane / pieces, total - 1);  // (lanes behind the last row do it again, and store nothing)
+      int own = bh;
+      while (own + 1 < prm.BH && prm.cu[own + 1] <= row) ++own;
+      load(u, own % prm.H, own / prm.H);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kRounds; ++u) {
+    const int64_t row = first + u * mine + lane / pieces;
+    if (row >= total) return;  // (all lanes of a row at once: the exchanges below stay inside a row)
+    store_group<T>(k[u], prm.out.k_codes + row * (prm.d / 2), prm.out.k_scales + row * (prm.d / kMxGroup), piece);
+    store_group<T>(v[u], prm.out.v_codes + row * (prm.d / 2), prm.out.v_scales + row * (prm.d / kMxGroup), piece);
+  }
 }
 
 struct ExpandParams {
@@ -125,7 +174,7 @@ int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, con
   prm.cu = cu_budget;
   prm.capacity = capacity;
   prm.out = cache;
-  const int rows = kThreads / (d->d * (d->dtype == MASKKV_BF16 ? 2 : 4) / 16);  // of a workgroup
+  const int rows = kRounds * kThreads / (d->d * (d->dtype == MASKKV_BF16 ? 2 : 4) / 16);  // of a workgroup
   const dim3 grid((unsigned)((capacity + rows - 1) / rows));
   if (d->dtype == MASKKV_BF16)
     hipLaunchKernelGGL(compact_mx_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, prm);
