@@ -5,8 +5,10 @@
 // them, 32 at a step: a lane then owns one query, whose normaliser is one number, and adds up what that query gives to 16 of the
 // rows; the lanes' sums meet once, at the end.  The queries come through LDS, moved as whole rows.
 //
-// Where there are many cached rows the four waves of a workgroup hold 32 each and share the queries (SHARE); where there
-// are few, all waves hold the same 32 and take the steps in turn.  Sums have a fixed order either way.
+// Where there are many cached rows the four waves of a workgroup hold 32 each and share the queries (SHARE), which come by direct
+// transfers into a ring of four steps, three ahead, one barrier a step; where there are few, all waves hold the same 32 and take the steps
+// in turn.  Sums have a fixed order either way.
+#include "lds.hpp"
 #include "mx.hpp"
 
 namespace maskkv {
@@ -37,7 +39,11 @@ struct AccCfg {
   static constexpr int kRPL = kMovers * 64 / kPPR;    // rows of a load of theirs
   static constexpr int kLoads = kTile / kRPL;
   static constexpr int kStepB = kTile * kRowB;
-  static constexpr int kLds = (SHARE ? 2 : WAVES) * kStepB;  // two steps, or one of each wave
+  static constexpr int kRing = 4;                                // steps
+  static constexpr int kMoves = kStepB / 1024 / WAVES;           // direct transfers of a wave and step, of 1 KiB
+  static constexpr int kNormB = 256;                             // of a wave and step: the queries' normalisers (twice)
+  static constexpr int kNormAt = kRing * kStepB;
+  static constexpr int kLds = SHARE ? kNormAt + kRing * WAVES * kNormB : WAVES * kStepB;
   __device__ static uint32_t swz(uint32_t row) { return sizeof(T) == 2 && D == 64 ? (row >> 1) & 7 : row & 15; }
 };
 
@@ -81,8 +87,40 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
       *reinterpret_cast<u32x4*>(to + i * C::kRowB + ((p ^ C::swz(i)) << 4)) = moved[j];
     }
   };
-  const int s0 = SHARE ? 0 : wave;
-  if (s0 < steps) load_step(s0);
+  // SHARE: a wave moves a quarter of a step's queries, and its own copy of their normalisers.  Rows behind the last one are the last one.
+  // (A whole step of a head without a group has a base that all lanes share and offsets that they keep; else every row's head is
+  // found by a division.)
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)acc_lds;
+  const uint32_t norm_at = lds0 + C::kNormAt + wave * C::kNormB;
+  const char* const queries = prm.Q.row(b, h * prm.q_per_kv, 0);
+  uint32_t offset[SHARE ? C::kMoves : 1];
+  auto row_of = [&](int j) { return (wave * C::kMoves + j) * (1024 / C::kRowB) + lane / C::kPPR; };
+  auto piece_of = [&](int j) { return ((uint32_t)lane % C::kPPR ^ C::swz(row_of(j))) * 16; };
+  if constexpr (SHARE) {
+#pragma unroll
+    for (int j = 0; j < C::kMoves; ++j) offset[j] = row_of(j) * (uint32_t)prm.Q.stride_t + piece_of(j);
+  }
+  auto move_step = [&](int s) {
+    const uint32_t to = lds0 + s % C::kRing * C::kStepB + wave * C::kMoves * 1024;
+    const int from = s * kTile;
+    if (prm.q_per_kv == 1 && from + kTile <= prm.n_q) {
+      const char* base = queries + (int64_t)from * prm.Q.stride_t;
+#pragma unroll
+      for (int j = 0; j < C::kMoves; ++j) dma16(base, offset[j], to + j * 1024);
+    } else {
+#pragma unroll
+      for (int j = 0; j < C::kMoves; ++j)
+        dma16_from(prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, min(from + row_of(j), prm.n_q - 1)) + piece_of(j), to + j * 1024);
+    }
+    dma4(reinterpret_cast<const char*>(prm.lse + (int64_t)bh * prm.n_q), (uint32_t)min(from + r, prm.n_q - 1) * 4,
+         norm_at + s % C::kRing * (WAVES * C::kNormB));
+  };
+  if constexpr (SHARE) {
+    for (int s = 0; s < C::kRing - 1; ++s)
+      if (s < steps) move_step(s);
+  }
+  const int s0 = wave;
+  if (!SHARE && s0 < steps) load_step(s0);
 
   // ---- this lane's half of a cached row
   u32x4 kf[C::kPPR / 2];
@@ -133,14 +171,19 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
     }
   };
   if constexpr (SHARE) {
-    store_step(acc_lds);
-    __syncthreads();
     for (int s = 0; s < steps; ++s) {
-      const float lse_now = lse;
-      if (s + 1 < steps) load_step(s + 1);
-      take(acc_lds + (s & 1) * C::kStepB, lse_now);
-      if (s + 1 < steps) store_step(acc_lds + ((s + 1) & 1) * C::kStepB);
-      __syncthreads();
+      // This wave's part of step s is there when only those of the two steps behind it are under way; behind the barrier so are the other
+      // waves', and all of them have read step s - 1, whose place step s + 3 takes.
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + 2 < steps)
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(2 * (C::kMoves + 1)) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      if (s + 3 < steps) move_step(s + 3);
+      const float norm = *in_lds<const float>(norm_at + r * 4, s % C::kRing * (WAVES * C::kNormB));
+      take(acc_lds + s % C::kRing * C::kStepB, s * kTile + r < prm.n_q ? norm : INFINITY);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before the barrier)
     }
   } else {
     char* own = acc_lds + wave * C::kStepB;
