@@ -20,7 +20,8 @@ GROUP = 32
 
 def store(x):
     """Rows [n, d] -> codes uint8 [n, d/2] (even element in the low four bits) and scale bytes uint8 [n, d/32]."""
-    x = np.asarray(x, dtype=np.float64)
+    with np.errstate(invalid="ignore"):                # (NaN of any kind)
+        x = np.asarray(x, dtype=np.float64)
     n, d = x.shape
     codes, scales = np.zeros((n, d), dtype=np.uint8), np.zeros((n, d // GROUP), dtype=np.uint8)
     groups = x.reshape(n, d // GROUP, GROUP)

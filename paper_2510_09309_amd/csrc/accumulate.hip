@@ -8,6 +8,8 @@
 // Where there are many cached rows the four waves of a workgroup hold 32 each and share the queries (SHARE), which come by direct
 // transfers into a ring of four steps, three ahead, one barrier a step; where there are few, all waves hold the same 32 and take the steps
 // in turn.  Sums have a fixed order either way.
+#include <type_traits>
+
 #include "lds.hpp"
 #include "mx.hpp"
 
@@ -54,6 +56,8 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   constexpr int kRows = SHARE ? WAVES * kTile : kTile;  // cached rows of a workgroup
   extern __shared__ __attribute__((aligned(16))) char acc_lds[];
   __shared__ float part[WAVES][kTile];
+  typedef AccumulateParams A;
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_ARGUMENT(A, Kc), MASKKV_ARGUMENT(A, BH), (uint32_t)(offsetof(A, out) + 8)});
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
   // Each XCD (workgroups whose numbers are congruent modulo 8) takes a run of units: a head's queries stay in one L2.
@@ -155,23 +159,32 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   float sum[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-  auto take = [&](const char* from, float lse_now) {
+  uint32_t fragment[C::kPPR / 2];  // where this lane's half of its query's row lies in a step
+#pragma unroll
+  for (int i = 0; i < C::kPPR / 2; ++i) fragment[i] = r * C::kRowB + (((g * (C::kPPR / 2) + i) ^ C::swz(r)) << 4);
+  auto take = [&](uint32_t base, int imm, float lse_now) __attribute__((always_inline)) {
     f32x16 x = {};
 #pragma unroll
-    for (int i = 0; i < C::kPPR / 2; ++i)
-      mfma_step<T>(kf[i], *reinterpret_cast<const u32x4*>(from + r * C::kRowB + (((g * (C::kPPR / 2) + i) ^ C::swz(r)) << 4)), x);
+    for (int i = 0; i < C::kPPR / 2; ++i) {
+      const u32x4 q = *in_lds<const u32x4>(base + fragment[i], imm);
+      mfma_step<T>(kf[i], q, x);
+    }
     const float by = -lse_now * kLog2e;
     const bool none = lse_now == INFINITY;  // (adds nothing, whatever the query holds)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = fast_exp2(fmaf(x[i], prm.c, by));
     if (__any(none)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] += none ? 0.f : fast_exp2(fmaf(x[i], prm.c, by));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] += fast_exp2(fmaf(x[i], prm.c, by));
+      for (int i = 0; i < 16; ++i) x[i] = none ? 0.f : x[i];
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] += x[i];
   };
   if constexpr (SHARE) {
-    for (int s = 0; s < steps; ++s) {
+#pragma unroll
+    for (int i = 0; i < C::kPPR / 2; ++i) fragment[i] += lds0;
+    auto step = [&](int s, auto place) __attribute__((always_inline)) {
+      constexpr int kPlace = decltype(place)::value;  // s % kRing
       // This wave's part of step s is there when only those of the two steps behind it are under way; behind the barrier so are the other
       // waves', and all of them have read step s - 1, whose place step s + 3 takes.
       __builtin_amdgcn_sched_barrier(0);
@@ -181,9 +194,15 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
         asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       if (s + 3 < steps) move_step(s + 3);
-      const float norm = *in_lds<const float>(norm_at + r * 4, s % C::kRing * (WAVES * C::kNormB));
-      take(acc_lds + s % C::kRing * C::kStepB, s * kTile + r < prm.n_q ? norm : INFINITY);
+      const float norm = *in_lds<const float>(norm_at + r * 4, kPlace * (WAVES * C::kNormB));
+      take(0, kPlace * C::kStepB, s * kTile + r < prm.n_q ? norm : INFINITY);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (read before the barrier)
+    };
+    for (int s = 0; s < steps; s += C::kRing) {
+      step(s, std::integral_constant<int, 0>());
+      if (s + 1 < steps) step(s + 1, std::integral_constant<int, 1>());
+      if (s + 2 < steps) step(s + 2, std::integral_constant<int, 2>());
+      if (s + 3 < steps) step(s + 3, std::integral_constant<int, 3>());
     }
   } else {
     char* own = acc_lds + wave * C::kStepB;
@@ -192,7 +211,7 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
       const float lse_now = lse;
       if (s + kEvery < steps) load_step(s + kEvery);
       asm volatile("" ::: "memory");
-      take(own, lse_now);
+      take(lds0 + wave * C::kStepB, 0, lse_now);
       asm volatile("" ::: "memory");
     }
   }
