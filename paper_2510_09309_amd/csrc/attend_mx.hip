@@ -30,7 +30,8 @@ struct AttendMxParams {
   int64_t capacity;
   int H, BH, q_per_kv, n_resp, n_q, qtiles;
   int chunk;      // tiles of a workgroup, or 0: all of its head
-  int part_rows;  // query rows of a partial result
+  int tile_rows;  // query rows of a workgroup
+  int part_rows;  // of a partial result
   float c;        // scale * log2(e)
   float* lse;
   float* part_o;    // [units * qtiles][part_rows][D]
@@ -633,19 +634,27 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
   fetch_attend_mx_arguments();
   const int slot = blockIdx.x / 8;
-  int bh = slot / prm.qtiles * 8 + blockIdx.x % 8;
-  const int qtile = slot % prm.qtiles;
-  if (bh >= prm.BH) return;
+  const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
   const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
   const int capacity = (int)prm.capacity;
-  auto cached_of = [&](int i) { return max(min(prm.cu[i + 1], capacity) - min(prm.cu[i], capacity), 0); };
-  if (prm.BH <= kRanked) bh = head_of_rank(prm.BH, bh, [&](int i) { return (cached_of(i) + kWideTile - 1) / kWideTile + resp_tiles; });
-  bh = __builtin_amdgcn_readfirstlane(bh);
+  auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kWideTile - 1) / kWideTile) + resp_tiles; };  // those of the response first
+  UnitHead head;
+  if (prm.chunk) {
+    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
+    if (head.bh < 0) return;
+  } else {
+    if (unit >= prm.BH) return;
+    auto cached_of = [&](int i) { return max(min(prm.cu[i + 1], capacity) - min(prm.cu[i], capacity), 0); };
+    const int i = __builtin_amdgcn_readfirstlane(prm.BH <= kRanked ? head_of_rank(prm.BH, unit, [&](int n) { return tiles_of(cached_of(n)); }) : unit);
+    head = {i, unit, 1, min(prm.cu[i], capacity), cached_of(i)};
+  }
+  const int bh = head.bh, first = head.first, cached = head.rows;
   const int b = bh / prm.H, h = bh % prm.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
-  const int first = min(prm.cu[bh], capacity), cached = cached_of(bh);
-  const int tiles = resp_tiles + (cached + kWideTile - 1) / kWideTile;  // those of the response first
+  if (prm.chunk && unit == head.first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, head.units);
+  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
+  const int tiles = prm.chunk ? min(tiles_of(cached), t0 + prm.chunk) : tiles_of(cached);  // this workgroup's: t0 .. tiles - 1
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mx_lds;
 
   // ---- tiles on their way.  Of the cache a thread takes a quarter of a row; of the response a wave takes a quarter of the rows.
@@ -688,7 +697,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
     for (int w = 0; w < C::kWords; ++w) *in_lds<u32x4>(lds0 + (to ^ w << 4)) = mx_decode_bf16(c[w], unit);
   };
-  // K(t), V(t) into the buffer of an even or odd tile
+  // K(t), V(t) into the buffer of an even or odd tile (counted from the first one of this workgroup)
   auto bring_k = [&](int t, uint32_t odd) {
     if (t >= tiles) return;
     if (t < resp_tiles)
@@ -711,8 +720,8 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  read_k(0);
-  read_v(0);
+  read_k(t0);
+  read_v(t0);
   const int q0 = qtile * kWideQueries + wave * 32;
   u32x4 qf[C::kSteps];
   {
@@ -720,12 +729,12 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 #pragma unroll
     for (int i = 0; i < C::kSteps; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
   }
-  bring_k(0, 0);
-  read_k(1);
-  bring_v(0, 0);
-  read_v(1);
-  bring_k(1, 1);
-  read_k(2);
+  bring_k(t0, 0);
+  read_k(t0 + 1);
+  bring_v(t0, 0);
+  read_v(t0 + 1);
+  bring_k(t0 + 1, 1);
+  read_k(t0 + 2);
   arrive();
 
   f32x16 o[C::kDB], even[2], odd[2];
@@ -767,7 +776,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
     if (n < 2) even[n] = f32x16{};
     mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], even[n % 2]);
   }
-  mask(0, even);
+  mask(t0, even);
   top = even[0][0];
 #pragma unroll
   for (int i = 0; i < 32; ++i) top = fmaxf(top, even[i / 16][i % 16]);
@@ -841,7 +850,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   };
   using Yes = std::true_type;
   using No = std::false_type;
-  int t = 0;
+  int t = t0;
   for (; t + 2 < tiles; t += 2) {
     step(t, No(), Yes(), even, odd);
     step(t + 1, Yes(), Yes(), odd, even);
@@ -855,6 +864,18 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
 
   // ---- out, by way of LDS: whole rows
   l = sum_halves(l);
+  if (head.units > 1) {
+    if (q0 + r >= prm.n_q) return;
+    const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + wave * 32 + r;
+#pragma unroll
+    for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(prm.part_o + part * D + 32 * db + 8 * i + 4 * g) =
+            make_float4(o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]);
+    if (g == 0) prm.part_ml[part] = make_float2(m, l);
+    return;
+  }
   const float by = 1.f / l;
   char* own = mx_lds + wave * 32 * (C::kRowB + 16);
 #pragma unroll
@@ -889,7 +910,7 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_mx_join_kernel(con
   const int bh = blockIdx.y, q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
   const int first = prm.parts[bh].x, units = prm.parts[bh].y;
   if (units <= 1 || q >= prm.n_q) return;
-  const int64_t part0 = first * step + (int64_t)(q / kTile) * prm.part_rows + q % kTile;
+  const int64_t part0 = first * step + (int64_t)(q / prm.tile_rows) * prm.part_rows + q % prm.tile_rows;
   float m = kNegBig, l = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int u0 = SHARED ? grp : 0; u0 < units; u0 += kAtOnce * kStep) {
@@ -949,56 +970,49 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_mx_join_kernel(con
 // How the tiles are dealt out.
 struct Deal {
   bool few;       // up to 16 query rows
-  bool wide;      // 128 query rows a workgroup, heads whole
-  int qtiles, part_rows;
+  bool wide;      // 128 query rows a workgroup
+  int tile_rows, qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
 };
 constexpr int kSharedUnits = 16;    // units of a head on average above which a query row's partial results are read by a whole workgroup
-constexpr int kLeastChunk = 16;     // tiles of a unit
-constexpr int kLongHead = 1 << 14;  // keys up to which the heads of a launch that fills the chip are left whole
+constexpr int kLongHead = 1 << 14, kLongWide = 1 << 16;  // keys up to which the heads of a launch that fills the chip are left whole
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
+  const bool bf16 = d->dtype == MASKKV_BF16;
   Deal x;
-  x.wide = d->dtype == MASKKV_BF16 && n_q > kWideQueries / 2 && BH * ((n_q + kWideQueries - 1) / kWideQueries) >= kUnits / 2;
-  x.few = d->dtype == MASKKV_BF16 && n_q <= 16;
-  x.qtiles = (n_q + kTile - 1) / kTile;
-  x.part_rows = n_q < kTile ? n_q : kTile;
+  // What the host knows of the heads' lengths: no head has more rows than the longest prompt, and all of them as many as there is room for.
+  const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
+  auto tiles_of = [&](int keys) { return capacity / keys + BH * (1 + (d->n_resp + keys - 1) / keys); };
+  x.few = bf16 && n_q <= 16;
+  x.wide = bf16 && n_q > kWideQueries / 2 && tiles_of(kWideTile) * ((n_q + kWideQueries - 1) / kWideQueries) >= 4 * kUnits;
+  const int keys = x.wide ? kWideTile : kTile;
+  x.tile_rows = x.wide ? kWideQueries : kTile;
+  x.qtiles = (n_q + x.tile_rows - 1) / x.tile_rows;
+  x.part_rows = n_q < x.tile_rows ? n_q : x.tile_rows;
   x.chunk = 0;
   x.units = BH;
-  if (x.wide) {
-    x.qtiles = (n_q + kWideQueries - 1) / kWideQueries;
-    return x;
-  }
-  // what the host knows of the heads' lengths: no head has more rows than the longest prompt, and all of them as many as there is room for
-  const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
-  if (BH * x.qtiles >= kUnits && most <= kLongHead) return x;
-  const int64_t tiles = capacity / kTile + BH * (1 + (d->n_resp + kTile - 1) / kTile);
-  int64_t chunk = (tiles * x.qtiles + kUnits - 1) / kUnits;
-  if (chunk < kLeastChunk) chunk = kLeastChunk;
-  if (chunk * kTile >= most + 2 * kTile) return x;  // (a head's last tiles of both kinds may be short)
+  if (BH * x.qtiles >= kUnits && most <= (x.wide ? kLongWide : kLongHead)) return x;
+  // Partial results are written and read again, and their joining is a launch: a unit for every compute unit, and two where that
+  // leaves a unit many tiles.
+  const int64_t tiles = tiles_of(keys), mean = (tiles + BH - 1) / BH;
+  const int least = x.wide ? 3 : bf16 ? 16 : 8, many = x.wide ? 8 : 24;
+  auto chunk_for = [&](int64_t units) {
+    const int64_t each = units / (BH * x.qtiles);  // of a head
+    const int64_t c = each > 1 ? (mean + each - 1) / each : mean;
+    return c < least ? (int64_t)least : c;
+  };
+  int64_t chunk = chunk_for(kUnits);
+  if (chunk > many) chunk = chunk_for(2 * kUnits);
+  if (chunk * keys >= most + 2 * keys) return x;  // (a head's last tiles of both kinds may be short)
   x.chunk = (int)chunk;
   x.units = tiles / chunk + BH;
   return x;
 }
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
-
-template <int D>
-int launch_wide(const AttendMxParams& prm, hipStream_t stream) {
-  using C = WideCfg<D>;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_mx_wide_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
-  if (e != hipSuccess) {
-    set_error("attend_mx: hipFuncSetAttribute: %s", hipGetErrorString(e));
-    (void)hipGetLastError();
-    return MASKKV_EHIP;
-  }
-  const int64_t groups = (int64_t)(prm.BH + 7) / 8 * 8 * prm.qtiles;  // (no more than 2^16 heads of 2^20 / 128 tiles: 2^29)
-  hipLaunchKernelGGL(attend_mx_wide_kernel<D>, dim3((unsigned)groups), dim3(256), C::kLds, stream, prm);
-  return check_launch("attend_mx (wide)");
-}
 
 template <typename T, int D>
 int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) {
@@ -1008,7 +1022,10 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
   int threads = kWaves * 64, lds = C::kLds;
   int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
   if constexpr (sizeof(T) == 2) {
-    if (deal.wide) return launch_wide<D>(prm, stream);
+    if (deal.wide) {
+      kernel = &attend_mx_wide_kernel<D>;
+      lds = WideCfg<D>::kLds;
+    }
     if (deal.few) {
       kernel = &attend_mx_few_kernel<D>;
       threads = FewCfg<D>::kWaves * 64;
@@ -1066,6 +1083,7 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
   prm.n_q = prm.q_per_kv * d->n_resp;
   prm.qtiles = deal.qtiles;
   prm.chunk = deal.chunk;
+  prm.tile_rows = deal.tile_rows;
   prm.part_rows = deal.part_rows;
   prm.c = scale * kLog2e;
   prm.lse = lse;

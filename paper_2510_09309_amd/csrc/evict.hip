@@ -1,17 +1,22 @@
 // Further eviction from a packed cache: of each head the rows of largest weight stay.
 //
-// One launch.  A workgroup moves up to `per` rows of the smaller cache that belong to one head.  It finds that head from the
-// budgets, and which of the head's rows they are by itself, from all of the head's weights: several workgroups of a head do
-// the same search, which costs the latency of one, where a list made by one of them would cost a launch between the two.
+// Short heads take one launch.  A workgroup moves up to `per` rows of the smaller cache that belong to one head; it finds that head from
+// the budgets, and which of the head's rows they are by itself, from all of the head's weights: several workgroups of a head do
+// the same search, which costs the latency of one, where a list made by one of them would cost a launch between the two.  Long
+// heads take that launch: a workgroup of 1024 per head lists the rows that stay, and a second kernel moves them.
 //
 // The search is for the smallest weight that stays, and ends when a candidate has as many rows as stay.  Up to 512 rows every wave
-// holds all of them and goes through the bits of the weights' order by itself, by ballots: no barrier and no LDS.  Beyond that it goes
-// by histograms of eight bits in LDS.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again every round.
+// holds all of them and goes through the bits of the weights' order by itself, by ballots: no barrier and no LDS.  Beyond that the workgroup
+// goes by histograms of eight bits in LDS.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again
+// every round.
 #include "mx.hpp"
 
 namespace maskkv {
 
 namespace {
+
+constexpr int kShortHead = 512;   // rows of a head on average up to which the rows that stay are not listed by a launch of their own
+constexpr int kMostRows = 4096;   // of a workgroup's list
 
 struct EvictParams {
   const float* weights;
@@ -59,10 +64,10 @@ __device__ __forceinline__ void write_prefix(const EvictParams& prm) {
   if (lane == 0) prm.cu_out[prm.BH] = before;
 }
 
-// The numbers of the rows that stay with ranks lo .. hi-1 among the head's, into `list`; every wave by itself, up to 64 * VALUES rows.
+// The numbers (from `base` on) of the rows that stay with ranks lo .. hi-1 among the head's, into `list`; every wave by itself, up to 64 * VALUES rows.
 // (All waves come to the same ranks; each writes those of its share of the rows.)
 template <int THREADS, int VALUES>
-__device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, int lo, int hi, int32_t* list) {
+__device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, int lo, int hi, int base, int32_t* list) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t held[VALUES];
 #pragma unroll
@@ -93,17 +98,24 @@ __device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, in
       const uint64_t below = (1ull << lane) - 1;
       const int before = sames + __popcll(b & below), rank = overs + __popcll(a & below) + min(before, ties);
       const bool stays = (a >> lane & 1) || ((b >> lane & 1) && before < ties);
-      if (stays && rank >= lo && rank < hi) list[rank - lo] = v * 64 + lane;
+      if (stays && rank >= lo && rank < hi) list[rank - lo] = v * 64 + lane + base;
     }
     overs += __popcll(a);
     sames += __popcll(b);
   }
 }
 
+// Of each count of a histogram: as many as keep a workgroup's additions apart.
+template <int THREADS>
+struct Bins {
+  static constexpr int kCopies = THREADS == 256 ? 2 : 8;
+  static constexpr int kRound = 256 * kCopies;
+};
+
 // The same by the whole workgroup.  VALUES: rows of a thread, in registers, or 0.
 template <int THREADS, int VALUES>
-__device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int32_t* list, int* bins, int (*counts)[4]) {
-  constexpr int kWaves = THREADS / 64;
+__device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int base, int32_t* list, int* all_bins, int (*counts)[4]) {
+  constexpr int kWaves = THREADS / 64, kCopies = Bins<THREADS>::kCopies, kBins = Bins<THREADS>::kRound;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = VALUES ? VALUES : (n + THREADS - 1) / THREADS;
   const int row0 = wave * each * 64 + lane;  // a wave's rows lie side by side, 64 a step
@@ -127,44 +139,61 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
     }
   };
 
+  // (Weights have a few exponents between them: several counts of each, side by side in LDS, keep a wave's additions apart.)
   // Eight bits of `least` a round: how many of the rows that agree with it so far have which next eight bits; then the highest
   // of these with at least as many rows at or above it as are still to be found.
   uint32_t least = 0;   // a row at or above it stays, or may
   bool exact = k == n;  // just those stay
   int wanted = k;       // of the rows that agree with `least` in the bits so far
+  for (int i = threadIdx.x; i < 4 * kBins / 4; i += THREADS) reinterpret_cast<int4*>(all_bins)[i] = make_int4(0, 0, 0, 0);
+  __syncthreads();
   for (int shift = 24; shift >= 0 && !exact; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += THREADS) bins[i] = 0;
-    __syncthreads();
+    int* const bins = all_bins + shift / 8 * kBins;  // (a round has its own: one barrier each)
     over_rows([&](uint32_t o, int v) {
-      if (row0 + v * 64 < n && (shift == 24 || (o ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[o >> shift & 255], 1);
+      if (row0 + v * 64 < n && (shift == 24 || (o ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[(o >> shift & 255) * kCopies + lane % kCopies], 1);
     });
     __syncthreads();
     // every wave by itself: a lane holds four bins from the top, 255 - 4 lane ..
-    const int4 four = *reinterpret_cast<const int4*>(bins + 252 - 4 * lane);
-    const int own = four.x + four.y + four.z + four.w;
+    int in[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int2* some = reinterpret_cast<const int2*>(bins + (255 - 4 * lane - j) * kCopies);
+      in[j] = 0;
+#pragma unroll
+      for (int c = 0; c < kCopies / 2; ++c) in[j] += some[c].x + some[c].y;
+    }
+    const int own = (in[0] + in[1]) + (in[2] + in[3]);
     const int upto = wave_prefix(own);
     const int at = __builtin_ctzll(__ballot(upto >= wanted));  // (there is one: all the rows that agree are `wanted` or more)
     int above = __builtin_amdgcn_readlane(upto - own, at);     // rows above the bin in question
-    const int in[4] = {__builtin_amdgcn_readlane(four.w, at), __builtin_amdgcn_readlane(four.z, at), __builtin_amdgcn_readlane(four.y, at),
-                       __builtin_amdgcn_readlane(four.x, at)};
-    int j = 0;
-    while (j < 3 && above + in[j] < wanted) above += in[j++];
-    least |= (uint32_t)(255 - 4 * at - j) << shift;
-    exact = above + in[j] == wanted;
-    wanted -= above;
-    __syncthreads();
-  }
-  const auto over = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && (exact ? o >= least : o > least)); };
-  const auto same = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && !exact && o == least); };
-  int overs = 0, sames = 0;
-  over_rows([&](uint32_t o, int v) {
-    overs += __popcll(over(o, v));
-    sames += __popcll(same(o, v));
-  });
-  if constexpr (VALUES > 0) {  // (the ballots are formed again below: kept from here to there they would take all registers)
+    int digit = 255 - 4 * at, upto_it = above;
 #pragma unroll
-    for (int v = 0; v < VALUES; ++v) asm volatile("" : "+v"(held[v]));
+    for (int j = 0; j < 4; ++j) {
+      const int n_j = __builtin_amdgcn_readlane(in[j], at);
+      if (upto_it < wanted) {
+        digit = 255 - 4 * at - j;
+        above = upto_it;
+        upto_it += n_j;
+      }
+    }
+    least |= (uint32_t)digit << shift;
+    exact = upto_it == wanted;
+    wanted -= above;
   }
+  // Where `exact`, those at or above `least` stay, else those above it and the first ones of those at it.
+  const uint32_t surely = exact ? least : least + 1;  // (`least` is not the largest of all numbers: that would be a NaN's)
+  const auto over = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && o >= surely); };
+  const auto same = [&](uint32_t o, int v) { return __ballot(row0 + v * 64 < n && o == least); };
+  auto fresh = [&] {  // (the ballots are formed again further on: kept from here to there they would take all registers)
+    if constexpr (VALUES > 0) {
+#pragma unroll
+      for (int v = 0; v < VALUES; ++v) asm volatile("" : "+v"(held[v]));
+    }
+  };
+  int overs = 0, sames = 0;
+  over_rows([&](uint32_t o, int v) { overs += __popcll(over(o, v)); });
+  if (!exact) over_rows([&](uint32_t o, int v) { sames += __popcll(same(o, v)); });
+  fresh();
   if (lane == 0) {
     counts[wave][0] = overs;
     counts[wave][1] = sames;
@@ -182,88 +211,37 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
   ties = __builtin_amdgcn_readfirstlane(ties);
   overs = __builtin_amdgcn_readfirstlane(overs);
   sames = __builtin_amdgcn_readfirstlane(sames);
-  const uint64_t below = (1ull << lane) - 1;
-  over_rows([&](uint32_t o, int v) {
-    const uint64_t a = over(o, v), b = same(o, v);
-    const int before = sames + __popcll(b & below);
-    const int rank = overs + __popcll(a & below) + min(before, ties);
-    const bool stays = (a >> lane & 1) || ((b >> lane & 1) && before < ties);
-    if (stays && rank >= lo && rank < hi) list[rank - lo] = row0 + v * 64;
-    overs += __popcll(a);
-    sames += __popcll(b);
-  });
+  auto before_me = [](uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); };
+  if (exact) {
+    over_rows([&](uint32_t o, int v) {
+      const uint64_t a = over(o, v);
+      const int rank = overs + before_me(a);
+      if (row0 + v * 64 < n && o >= surely && rank >= lo && rank < hi) list[rank - lo] = row0 + v * 64 + base;
+      overs += __popcll(a);
+    });
+  } else {
+    over_rows([&](uint32_t o, int v) {
+      const uint64_t a = over(o, v), b = same(o, v);
+      const int before = sames + before_me(b), rank = overs + before_me(a) + min(before, ties);
+      const bool stays = row0 + v * 64 < n && (o >= surely || (o == least && before < ties));
+      if (stays && rank >= lo && rank < hi) list[rank - lo] = row0 + v * 64 + base;
+      overs += __popcll(a);
+      sames += __popcll(b);
+    });
+  }
 }
 
+// `rows` rows from `list` (packed rows) to row `to` of the smaller cache on.
 template <int THREADS>
-__global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams prm) {
-  extern __shared__ int32_t list[];  // [per]
-  __shared__ __attribute__((aligned(16))) int bins[256];
-  __shared__ int counts[THREADS / 64][4];
-  typedef EvictParams A;
-  fetch_arguments({MASKKV_ARGUMENT(A, weights), MASKKV_ARGUMENT(A, rows), MASKKV_ARGUMENT(A, moved), (uint32_t)(offsetof(A, moved) + 64)});
-  const int lane = threadIdx.x & 63;
-  if (blockIdx.x == 0 && threadIdx.x < 64) write_prefix(prm);
-
-  // ---- the head of this workgroup's rows, how many rows stay of the heads before it, and which of its own these are
-  constexpr int kSets = 4;
-  const int unit = blockIdx.x, capacity = (int)prm.capacity;
-  int before = 0, units_before = 0, bh = -1, part = 0;
-  HeadRows x = {0, 0, 0};
-  for (int base = 0; base < prm.BH && bh < 0; base += 64 * kSets) {
-    HeadRows some[kSets];
-#pragma unroll
-    for (int i = 0; i < kSets; ++i) some[i] = rows_of(prm, min(base + i * 64 + lane, prm.BH - 1), capacity);
-#pragma unroll
-    for (int i = 0; i < kSets; ++i) {
-      if (base + i * 64 >= prm.BH || bh >= 0) break;
-      const int stay = base + i * 64 + lane < prm.BH ? some[i].stay : 0;
-      const int units = (int)(((uint32_t)stay + prm.per - 1) / prm.per);
-      const int rows_upto = wave_prefix(stay), upto = wave_prefix(units);
-      const uint64_t found = __ballot(units_before + upto > unit);
-      if (found) {
-        const int at = __builtin_ctzll(found);
-        bh = base + i * 64 + at;
-        x = {__builtin_amdgcn_readlane(some[i].first, at), __builtin_amdgcn_readlane(some[i].n, at), __builtin_amdgcn_readlane(stay, at)};
-        part = unit - units_before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
-        before += __builtin_amdgcn_readlane(rows_upto, at) - x.stay;
-      } else {
-        units_before += __builtin_amdgcn_readlane(upto, 63);
-        before += __builtin_amdgcn_readlane(rows_upto, 63);
-      }
-    }
-  }
-  if (bh < 0) return;
-  const int lo = part * prm.per;
-  const int64_t to = (int64_t)before + lo;
-  const int rows = (int)min((int64_t)min(x.stay - lo, prm.per), prm.capacity_out - to);
-  if (rows <= 0) return;
-
-  const float* w = prm.weights + x.first;
-  if (x.n <= 64)
-    list_rows_alone<THREADS, 1>(w, x.n, x.stay, lo, lo + rows, list);
-  else if (x.n <= 256)
-    list_rows_alone<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list);
-  else if (x.n <= 512)
-    list_rows_alone<THREADS, 8>(w, x.n, x.stay, lo, lo + rows, list);
-  else if (x.n <= THREADS * 4)
-    list_rows<THREADS, 4>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
-  else if (x.n <= THREADS * 16)
-    list_rows<THREADS, 16>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
-  else if (x.n <= THREADS * 32)
-    list_rows<THREADS, 32>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
-  else
-    list_rows<THREADS, 0>(w, x.n, x.stay, lo, lo + rows, list, bins, counts);
-  __syncthreads();
-
-  // ---- the rows, 16 bytes a thread and step
+__device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t* list, int64_t to, int rows) {
   const int pieces = 1 << prm.row_shift, half = pieces / 2;
   constexpr int kAtOnce = 4;
-  for (int i0 = threadIdx.x; i0 < rows << prm.row_shift; i0 += kAtOnce * THREADS) {
+  for (int i0 = threadIdx.x; i0 < rows << prm.row_shift; i0 += kAtOnce * THREADS) {  // 16 bytes a thread and step
     u32x4 x4[kAtOnce];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = min(i0 + u * THREADS, (rows << prm.row_shift) - 1), piece = i & (pieces - 1), m = piece >= half;
-      const int64_t from = x.first + list[i >> prm.row_shift];
+      const int64_t from = list[i >> prm.row_shift];
       x4[u] = *reinterpret_cast<const u32x4*>(prm.moved.from[m] + (from * half + (piece - m * half)) * 16);
     }
 #pragma unroll
@@ -274,8 +252,7 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams prm) {
     }
   }
   for (int i = threadIdx.x; i < rows; i += THREADS) {
-    const int64_t from = x.first + list[i];
-    prm.rows[to + i] = (int32_t)from;
+    const int64_t from = list[i];
     if (prm.idx) prm.idx_out[to + i] = prm.idx[from];
     if (prm.weights_out) prm.weights_out[to + i] = prm.weights[from];
     if (prm.moved.bytes[2] == 4) {
@@ -286,6 +263,114 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictParams prm) {
       reinterpret_cast<uint16_t*>(prm.moved.to[3])[to + i] = reinterpret_cast<const uint16_t*>(prm.moved.from[3])[from];
     }
   }
+}
+
+// The head of a unit of `per` rows that stay (bh -1: behind the last), which of its own units it is, and the rows that stay before it.
+struct UnitRows {
+  int bh, part, before;
+  HeadRows head;
+};
+__device__ __forceinline__ UnitRows rows_of_unit(const EvictParams& prm, int unit, int per) {
+  constexpr int kSets = 4;
+  const int lane = threadIdx.x & 63, capacity = (int)prm.capacity;
+  UnitRows x = {-1, 0, 0, {0, 0, 0}};
+  int units_before = 0;
+  for (int base = 0; base < prm.BH; base += 64 * kSets) {
+    HeadRows some[kSets];
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) some[i] = rows_of(prm, min(base + i * 64 + lane, prm.BH - 1), capacity);
+#pragma unroll
+    for (int i = 0; i < kSets; ++i) {
+      if (base + i * 64 >= prm.BH) break;
+      const int stay = base + i * 64 + lane < prm.BH ? some[i].stay : 0;
+      const int units = (int)(((uint32_t)stay + per - 1) / per);
+      const int rows_upto = wave_prefix(stay), upto = wave_prefix(units);
+      const uint64_t found = __ballot(units_before + upto > unit);
+      if (found) {
+        const int at = __builtin_ctzll(found);
+        x.bh = base + i * 64 + at;
+        x.head = {__builtin_amdgcn_readlane(some[i].first, at), __builtin_amdgcn_readlane(some[i].n, at), __builtin_amdgcn_readlane(stay, at)};
+        x.part = unit - units_before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(units, at));
+        x.before += __builtin_amdgcn_readlane(rows_upto, at) - x.head.stay;
+        return x;
+      }
+      units_before += __builtin_amdgcn_readlane(upto, 63);
+      x.before += __builtin_amdgcn_readlane(rows_upto, 63);
+    }
+  }
+  return x;
+}
+
+__device__ __forceinline__ void fetch_evict_arguments() {
+  typedef EvictParams A;
+  fetch_arguments({MASKKV_ARGUMENT(A, weights), MASKKV_ARGUMENT(A, rows), MASKKV_ARGUMENT(A, moved), (uint32_t)(offsetof(A, moved) + 64)});
+}
+
+// Short heads.
+__global__ __launch_bounds__(256) void evict_kernel(const EvictParams prm) {
+  extern __shared__ int32_t list[];  // [per]
+  __shared__ __attribute__((aligned(16))) int bins[4 * Bins<256>::kRound];
+  __shared__ int counts[4][4];
+  fetch_evict_arguments();
+  if (blockIdx.x == 0 && threadIdx.x < 64) write_prefix(prm);
+  const UnitRows x = rows_of_unit(prm, blockIdx.x, prm.per);
+  if (x.bh < 0) return;
+  const int lo = x.part * prm.per, n = x.head.n, k = x.head.stay, first = x.head.first;
+  const int64_t to = (int64_t)x.before + lo;
+  const int rows = (int)min((int64_t)min(k - lo, prm.per), prm.capacity_out - to);
+  if (rows <= 0) return;
+  const float* w = prm.weights + first;
+  if (n <= 64)
+    list_rows_alone<256, 1>(w, n, k, lo, lo + rows, first, list);
+  else if (n <= 256)
+    list_rows_alone<256, 4>(w, n, k, lo, lo + rows, first, list);
+  else if (n <= 512)
+    list_rows_alone<256, 8>(w, n, k, lo, lo + rows, first, list);
+  else if (n <= 256 * 4)
+    list_rows<256, 4>(w, n, k, lo, lo + rows, first, list, bins, counts);
+  else if (n <= 256 * 16)
+    list_rows<256, 16>(w, n, k, lo, lo + rows, first, list, bins, counts);
+  else
+    list_rows<256, 0>(w, n, k, lo, lo + rows, first, list, bins, counts);
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows; i += 256) prm.rows[to + i] = list[i];
+  move_rows<256>(prm, list, to, rows);
+}
+
+// Long heads: the rows that stay of a head, ...
+__global__ __launch_bounds__(1024) void evict_rows_kernel(const EvictParams prm) {
+  __shared__ __attribute__((aligned(16))) int bins[4 * Bins<1024>::kRound];
+  __shared__ int counts[16][4];
+  fetch_evict_arguments();
+  if (blockIdx.x == 0 && threadIdx.x < 64) write_prefix(prm);
+  const UnitRows x = rows_of_unit(prm, blockIdx.x, 0x7FFFFFFF);  // (a head of which rows stay is one unit)
+  if (x.bh < 0) return;
+  const int n = x.head.n, k = x.head.stay, first = x.head.first, rows = (int)min((int64_t)k, prm.capacity_out - x.before);
+  if (rows <= 0) return;
+  const float* w = prm.weights + first;
+  int32_t* list = prm.rows + x.before;
+  if (n <= 1024 * 2)
+    list_rows<1024, 2>(w, n, k, 0, rows, first, list, bins, counts);
+  else if (n <= 1024 * 4)
+    list_rows<1024, 4>(w, n, k, 0, rows, first, list, bins, counts);
+  else if (n <= 1024 * 8)
+    list_rows<1024, 8>(w, n, k, 0, rows, first, list, bins, counts);
+  else if (n <= 1024 * 32)
+    list_rows<1024, 32>(w, n, k, 0, rows, first, list, bins, counts);
+  else
+    list_rows<1024, 0>(w, n, k, 0, rows, first, list, bins, counts);
+}
+
+// ... and their moving, `per` a workgroup.
+__global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams prm) {
+  extern __shared__ int32_t list[];  // [per]
+  fetch_evict_arguments();
+  const int64_t to = (int64_t)blockIdx.x * prm.per;
+  const int rows = (int)min((int64_t)prm.per, min((int64_t)prm.cu_out[prm.BH], prm.capacity_out) - to);
+  if (rows <= 0) return;
+  for (int i = threadIdx.x; i < rows; i += 256) list[i] = prm.rows[to + i];
+  __syncthreads();
+  move_rows<256>(prm, list, to, rows);
 }
 
 }  // namespace
@@ -311,14 +396,18 @@ int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_b
   // Workgroups for two of every compute unit, of 16 rows at least and of no more than the list has room for.
   const int64_t most = capacity_out < capacity ? capacity_out : capacity;  // (no more rows stay than there are)
   int64_t per = (most + 511) / 512;
-  per = per < 16 ? 16 : per > 8192 ? 8192 : per;
+  per = per < 16 ? 16 : per > kMostRows ? kMostRows : per;
   prm.per = (int)per;
-  const int64_t groups = most / per + prm.BH;  // (each head's last one may have fewer)
-  if (capacity / prm.BH <= 2048)
-    hipLaunchKernelGGL(evict_kernel<256>, dim3((unsigned)groups), dim3(256), per * 4, stream, prm);
-  else
-    hipLaunchKernelGGL(evict_kernel<1024>, dim3((unsigned)groups), dim3(1024), per * 4, stream, prm);
-  return check_launch("evict");
+  if (capacity <= (int64_t)kShortHead * prm.BH) {
+    const int64_t groups = most / per + prm.BH;  // (each head's last one may have fewer)
+    hipLaunchKernelGGL(evict_kernel, dim3((unsigned)groups), dim3(256), per * 4, stream, prm);
+    return check_launch("evict");
+  }
+  hipLaunchKernelGGL(evict_rows_kernel, dim3((unsigned)prm.BH), dim3(1024), 0, stream, prm);
+  if (int e = check_launch("evict (rows)")) return e;
+  if (most == 0) return MASKKV_OK;
+  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)((most + per - 1) / per)), dim3(256), per * 4, stream, prm);
+  return check_launch("evict (move)");
 }
 
 }  // namespace maskkv

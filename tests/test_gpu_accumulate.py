@@ -73,6 +73,14 @@ def test_long_and_many(mx):
 
 
 @pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("d,dtype,n,g", [(64, "bf16", 300, 1), (128, "bf16", 130, 1), (64, "f32", 70, 1), (64, "bf16", 50, 3), (128, "bf16", 33, 2)])
+def test_many_rows_share_the_queries(mx, d, dtype, n, g):
+    """So many cached rows that a workgroup's waves share the queries: one step of 32 to ten, whole ones and a rest."""
+    rng = np.random.default_rng(n)
+    check(n, 8, 32, d, dtype, n, rng.integers(60, 260, 256).tolist(), mx, g=g, decay=0.5, heads=(0, 1, 99, 200, 255))
+
+
+@pytest.mark.parametrize("mx", [False, True])
 @pytest.mark.parametrize("capacity", [0, 1, 50, 59, 60, 61, 100])
 def test_rows_are_clipped_to_the_capacity(mx, capacity):
     check(6, 1, 3, 64, "bf16", 9, [40, 0, 20], mx, decay=0.25, capacity=capacity)

@@ -24,7 +24,7 @@ class Case:
         m = hp.mk()
         capacity = int(self.cu[-1]) if capacity is None else capacity
         self.desc = mh.desc(self.B, self.H, self.d, self.dtype, self.n, self.P_max, self.g)
-        cache = mh.cache(self.K, self.V, spare=3) if cache is None else cache
+        cache = mh.cache(self.K, self.V, spare=max(capacity - int(self.cu[-1]), 0) + 3) if cache is None else cache
         up = lambda x: hp.upload(x, self.dtype)
         O = torch.full((self.B, self.H * self.g, self.n, self.d), 7.0, dtype=hp.torch_dtype(self.dtype), device="cuda") if O is None else O
         lse = torch.full((self.B * self.H * self.g * self.n,), 7.0, device="cuda") if with_lse else None
@@ -88,6 +88,33 @@ def test_many_heads_and_sequences():
 def test_more_queries_than_a_workgroup_has(n):
     Case(n, 2, 4, 128, "bf16", n, [100, 0, 513, 64, 1024, 31, 7, 200]).run().check()
     Case(n, 1, 2, 64, "bf16", n, [777, 3], g=4).run().check()
+
+
+@pytest.mark.parametrize("d,n,g,lens", [(128, 300, 1, [24000, 100]), (64, 40, 7, [0, 30000]), (128, 70, 1, [9001, 40000, 17])])
+def test_many_queries_over_few_long_heads(d, n, g, lens):
+    """128 query rows a workgroup, and the keys of a head dealt to several."""
+    Case(n, 1, len(lens), d, "bf16", n, lens, g=g).run().check()
+
+
+def test_many_queries_of_many_heads():
+    """128 query rows a workgroup, heads whole: in the order of their lengths, and more of them than are ordered."""
+    rng = np.random.default_rng(18)
+    Case(18, 1, 300, 64, "bf16", 70, rng.integers(0, 100, 300).tolist()).run().check(heads=range(0, 300, 7))
+    lens = rng.integers(0, 200, 240)
+    lens[[3, 77]] = 1500
+    lens[100:110] = 0
+    Case(19, 3, 80, 64, "bf16", 66, lens.tolist()).run().check(heads=[0, 3, 50, 77, 100, 105, 200, 239])
+
+
+@pytest.mark.parametrize("n", [1, 20, 70])
+def test_heads_that_may_be_long_where_the_launch_fills_the_chip(n):
+    """Room for far longer heads than there are: the keys are dealt out all the same, and most heads have one part."""
+    rng = np.random.default_rng(19)
+    lens = rng.integers(0, 60, 260)
+    lens[[5, 200]] = 2000
+    c = Case(20, 2, 130, 64, "bf16", n, lens.tolist())
+    c.P_max = 100000
+    c.run(capacity=80000).check(heads=[0, 5, 6, 100, 200, 201, 259])
 
 
 @pytest.mark.parametrize("capacity", [0, 1, 40, 99, 100, 101, 150])

@@ -76,6 +76,13 @@ def test_long_heads(mx, n, k):
     check([30, n, 7], [10, k, 7], heavy(rng, n + 37), 128, "bf16", mx)
 
 
+def test_a_long_head_among_short_ones():
+    rng = np.random.default_rng(6)
+    for n in (700, 3000, 4097, 9000):
+        lens = [10] * 120 + [n] + [5] * 80
+        check(lens, [4] * 120 + [n // 3] + [5] * 80, heavy(rng, sum(lens)), mx=n == 3000)
+
+
 def test_ties():
     rng = np.random.default_rng(1)
     for n in (5, 64, 300, 1500, 5000, 20000):
