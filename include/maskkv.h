@@ -254,6 +254,7 @@ int maskkv_attend_full(const maskkv_desc* desc, const maskkv_tensor* Q_resp,
  * writes the bytes 3 .. 252 and 255 (above 252 the largest sizes would pass the range of fp32).
  * Pointers are multiples of 16 bytes.  A row takes 17/64 of what it takes in bf16.
  */
+#define MASKKV_MX_MAX_ROWS 0x7FFF0000 /* capacity of the calls below, rows */
 typedef struct maskkv_mx_cache {
   void* k_codes;
   void* k_scales;
@@ -299,7 +300,8 @@ int maskkv_attend_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const
  * over all g * n_resp query rows i of the head's group (numbered as in Q_resp: query head first, then query), with the natural-log
  * normalisers that maskkv_attend or maskkv_attend_mx returned for the same queries, cache, response rows and scale
  * (row_lse[(b*H + h)*g*n_resp + i]).  A query row whose row_lse is +infinity adds nothing.  Kc: DEVICE [capacity, d] in
- * desc->dtype; weights: DEVICE float [capacity]; weights_in may be weights_out.  0 <= decay <= 1; with decay 0 weights_in is not
+ * desc->dtype; weights: DEVICE float [capacity]; weights_in may be weights_out (but not
+ * overlap it otherwise).  0 <= decay <= 1; with decay 0 weights_in is not
  * read and may be NULL.  fp32 accumulation in a fixed order: equal calls give equal bits.  Rows >= min(capacity,
  * cu_budget[B*H]) are left untouched.  _mx: the same over a cache in 4 bits, of which only the keys are read (v_codes and
  * v_scales may be NULL).

@@ -69,7 +69,7 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   const int b = bh / prm.H, h = bh % prm.H;
   const int last = head.first + head.rows - 1;
   const int row0 = head.first + (unit - head.first_unit) * kRows + (SHARE ? wave * kTile : 0);  // of this wave
-  const int64_t row = min(row0 + r, last);
+  const int64_t row = min(row0 + r, last);  // (row0 may lie behind the head's end: nothing of such a wave is stored)
 
   const int steps = (prm.n_q + kTile - 1) / kTile;
   constexpr int kEvery = SHARE ? 1 : WAVES;  // a wave's steps: every so many

@@ -136,9 +136,10 @@ int check_packed(const char* what, const char* name, const void* p, int64_t rows
   return MASKKV_OK;
 }
 
+// (Kernels count rows in 32 bits, also a tile's worth past the last one.)
 int check_capacity(const char* what, const char* name, int64_t capacity) {
-  if (capacity >= 0 && capacity <= 0x7FFFFFFF) return MASKKV_OK;
-  set_error("%s: %s %lld outside 0..2^31-1", what, name, (long long)capacity);
+  if (capacity >= 0 && capacity <= MASKKV_MX_MAX_ROWS) return MASKKV_OK;
+  set_error("%s: %s %lld outside 0..%d", what, name, (long long)capacity, MASKKV_MX_MAX_ROWS);
   return MASKKV_EINVAL;
 }
 
@@ -539,6 +540,11 @@ static int accumulate_entry(const char* what, const maskkv_desc* desc, const mas
   }
   if (!cu_budget || !row_lse || (capacity > 0 && (!weights_out || (decay > 0.f && !weights_in)))) {
     set_error("%s: cu_budget, row_lse, weights_out or (with a decay above 0) weights_in is NULL", what);
+    return MASKKV_EINVAL;
+  }
+  const float *in0 = weights_in, *in1 = weights_in + capacity, *out0 = weights_out, *out1 = weights_out + capacity;
+  if (decay > 0.f && in0 != out0 && in0 < out1 && out0 < in1) {
+    set_error("%s: weights_in and weights_out overlap without being the same", what);
     return MASKKV_EINVAL;
   }
   return launch_accumulate(desc, q, mx ? nullptr : Kc, keys, cu_budget, capacity, pick_scale(desc, scale), row_lse, decay,

@@ -43,7 +43,7 @@ struct Fns {
   decltype(&maskkv_value_shift) value_shift;
 } fn;
 
-PyObject *kB, *kH, *kd, *kdtype, *kn_resp, *kn_query, *kP_max, *kq_per_kv, *kprompt_len, *kcuda_stream, *kdata_ptr, *kk_codes, *kk_scales, *kv_codes, *kv_scales;
+PyObject *kB, *kH, *kd, *kdtype, *kn_resp, *kn_query, *kP_max, *kq_per_kv, *kprompt_len, *kcuda_stream, *kdata_ptr, *kdevice_index, *kk_codes, *kk_scales, *kv_codes, *kv_scales;
 
 struct Error {};  // a Python exception has been set
 
@@ -411,6 +411,15 @@ void on_this_device(const at::Tensor& t, const char* what) {
   throw Error{};
 }
 
+// As as_stream, of the current device.
+void* stream_here(PyObject* o) {
+  if (o != Py_None && PyObject_HasAttr(o, kdevice_index)) {
+    if (attr_i32(o, kdevice_index) != c10::hip::getCurrentHIPStream().device_index())
+      fail(PyExc_AssertionError, "stream: need one of the current device");
+  }
+  return as_stream(o);
+}
+
 // A contiguous tensor of `type` with at least `least` elements on the current device, or None where `optional`.
 template <typename T>
 T* buffer(PyObject* o, at::ScalarType type, int64_t least, const char* what, bool optional = false) {
@@ -480,7 +489,7 @@ PyObject* compact_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, K, V, idx, cu,
     CheckedView k(a[1], d.d, d.d.H, longest_prompt(d.d), "K"), v(a[2], d.d, d.d.H, longest_prompt(d.d), "V");
     const int32_t *idx = buffer<int32_t>(a[3], at::kInt, cap, "idx"), *cu = buffer<int32_t>(a[4], at::kInt, heads_of(d.d) + 1, "cu_budget");
     MxArg mx(a[6], d.d, cap);
-    void* st = as_stream(a[7]);
+    void* st = stream_here(a[7]);
     return without_gil([&] { return fn.compact_mx(&d.d, &k.v, &v.v, idx, cu, cap, &mx.c, st); });
   });
 }
@@ -491,7 +500,7 @@ PyObject* expand_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, cache, cu, capa
     MxArg mx(a[1], d.d, cap);
     const int32_t* cu = buffer<int32_t>(a[2], at::kInt, heads_of(d.d) + 1, "cu_budget");
     void *kc = buffer<void>(a[4], element_type(d.d), cap * d.d.d, "Kc"), *vc = buffer<void>(a[5], element_type(d.d), cap * d.d.d, "Vc");
-    void* st = as_stream(a[6]);
+    void* st = stream_here(a[6]);
     return without_gil([&] { return fn.expand_mx(&d.d, &mx.c, cu, cap, kc, vc, st); });
   });
 }
@@ -514,7 +523,7 @@ PyObject* attend_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, Q, cache, cu, c
     const float scale = (float)as_f64(a[7]);
     float* lse = buffer<float>(a[9], at::kFloat, heads_of(d.d) * g * d.d.n_resp, "lse", true);
     const size_t wn = nbytes(a[10]);
-    void *ws = wn ? buffer<void>(a[10], THPVariable_Unpack(a[10]).scalar_type(), 0, "workspace") : nullptr, *st = as_stream(a[11]);
+    void *ws = wn ? buffer<void>(a[10], THPVariable_Unpack(a[10]).scalar_type(), 0, "workspace") : nullptr, *st = stream_here(a[11]);
     return without_gil([&] { return fn.attend_mx(&d.d, &q.v, &mx.c, cu, cap, &k2.v, &v2.v, scale, &o.v, lse, ws, wn, st); });
   });
 }
@@ -529,7 +538,7 @@ PyObject* accumulate_any(Args a, Py_ssize_t n, bool mx) {
     const float* lse = buffer<float>(a[6], at::kFloat, heads_of(d.d) * g * d.d.n_resp, "row_lse");
     const float* in = buffer<float>(a[8], at::kFloat, cap, "weights_in", true);
     float* out = buffer<float>(a[9], at::kFloat, cap, "weights_out");
-    void* st = as_stream(a[10]);
+    void* st = stream_here(a[10]);
     if (mx) {
       MxArg c(a[2], d.d, cap, true);
       return without_gil([&] { return fn.accumulate_mx(&d.d, &q.v, &c.c, cu, cap, scale, lse, decay, in, out, st); });
@@ -559,7 +568,7 @@ struct EvictArgs {  // weights, cu, capacity, budgets ... idx ... idx_out, rows,
     rows = buffer<int32_t>(out[1], at::kInt, cap_out, "rows");
     weights_out = buffer<float>(out[2], at::kFloat, cap_out, "weights_out", true);
     cu_out = buffer<int32_t>(out[3], at::kInt, heads_of(d) + 1, "cu_out");
-    st = as_stream(out[5]);
+    st = stream_here(out[5]);
   }
 };
 // desc, weights, cu, capacity, budgets, Kc, Vc, idx, Kc_out, Vc_out, idx_out, rows, weights_out, cu_out, capacity_out, stream
@@ -630,7 +639,7 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     const char* text;
   } names[] = {{&kB, "B"}, {&kH, "H"}, {&kd, "d"}, {&kdtype, "dtype"}, {&kn_resp, "n_resp"}, {&kn_query, "n_query"},
                {&kP_max, "P_max"}, {&kq_per_kv, "q_per_kv"}, {&kprompt_len, "prompt_len"},
-               {&kcuda_stream, "cuda_stream"}, {&kdata_ptr, "data_ptr"}, {&kk_codes, "k_codes"}, {&kk_scales, "k_scales"},
+               {&kcuda_stream, "cuda_stream"}, {&kdata_ptr, "data_ptr"}, {&kdevice_index, "device_index"}, {&kk_codes, "k_codes"}, {&kk_scales, "k_scales"},
                {&kv_codes, "v_codes"}, {&kv_scales, "v_scales"}};
   for (const auto& n : names) {
     *n.to = PyUnicode_InternFromString(n.text);

@@ -81,7 +81,7 @@ def test_bad_descriptions(mk, what, kw, status):
 def test_bad_capacities_and_prefix_sums(mk, what):
     c = Calls(mk)
     assert getattr(c, what)(cap=-1) == 1 and "capacity" in c.error()
-    assert getattr(c, what)(cap=1 << 31) == 1
+    assert getattr(c, what)(cap=1 << 31) == 1 and getattr(c, what)(cap=0x7FFF0001) == 1
     assert getattr(c, what)(cu=None) == 1 and "cu_budget" in c.error()
 
 
@@ -112,6 +112,8 @@ def test_bad_arguments_of_each_call(mk):
         assert call(lse=None) == 1 and call(w_out=None) == 1 and call(w_in=None) == 1
         for decay in (-0.1, 1.5, float("nan")):
             assert call(decay=decay) == 1 and "decay" in c.error()
+        for w_in in (F + (9 << 20) + 4, F + (9 << 20) - 36):                   # ten weights that overlap the other ten
+            assert call(w_in=w_in) == 1 and "overlap" in c.error()
     assert c.accumulate(K=None) == 1 and "Kc" in c.error()
     for call in (c.evict, c.evict_mx):
         assert call(weights=None) == 1 and call(budgets=None) == 1 and call(cu_out=None) == 1 and call(rows=None) == 1
