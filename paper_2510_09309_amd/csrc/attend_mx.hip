@@ -10,6 +10,7 @@
 //
 // Where heads x query tiles are fewer than the compute units, or a head may be far longer than the others, the tiles are dealt to
 // several workgroups, and a second kernel joins their partial results.
+#include <cmath>
 #include <type_traits>
 
 #include "attend.hpp"
@@ -29,6 +30,7 @@ struct AttendMxParams {
   const int32_t* cu;
   int64_t capacity;
   int H, BH, q_per_kv, n_resp, n_q, qtiles;
+  int units;      // at most
   int chunk;      // tiles of a workgroup, or 0: all of its head
   int tile_rows;  // query rows of a workgroup
   int part_rows;  // of a partial result
@@ -43,6 +45,17 @@ __device__ __forceinline__ void fetch_attend_mx_arguments() {
   typedef AttendMxParams A;
   fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_VIEW_ARGUMENTS(A, K2), MASKKV_VIEW_ARGUMENTS(A, V2), MASKKV_VIEW_ARGUMENTS(A, O),
                    MASKKV_ARGUMENT(A, cache), MASKKV_ARGUMENT(A, H), (uint32_t)(offsetof(A, parts) + 4)});
+}
+
+// Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there, but those of the
+// last units, fewer than eight, are dealt to all XCDs (4 heads x 60 query tiles on half of the chip: 16.8 us, on all of it 10.6).
+struct Place {
+  int unit, qtile;
+};
+__device__ __forceinline__ Place place_of(int block, int units, int qtiles) {
+  const int even = units / 8 * 8 * qtiles;
+  if (block < even) return {block / 8 / qtiles * 8 + block % 8, block / 8 % qtiles};
+  return {units / 8 * 8 + (block - even) / qtiles, (block - even) % qtiles};
 }
 
 template <typename T, int D>
@@ -69,9 +82,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
   fetch_attend_mx_arguments();
-  // Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there.
-  const int slot = blockIdx.x / 8;
-  const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
+  const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
+  const int unit = place.unit, qtile = place.qtile;
   const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
   auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kTile - 1) / kTile) + resp_tiles; };  // those of the response first
   const int capacity = (int)prm.capacity;
@@ -80,7 +92,6 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
     head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
     if (head.bh < 0) return;
   } else {
-    if (unit >= prm.BH) return;
     const int first = min(prm.cu[unit], capacity);
     head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
   }
@@ -633,8 +644,8 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   using C = WideCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char mx_lds[];
   fetch_attend_mx_arguments();
-  const int slot = blockIdx.x / 8;
-  const int unit = slot / prm.qtiles * 8 + blockIdx.x % 8, qtile = slot % prm.qtiles;
+  const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
+  const int unit = place.unit, qtile = place.qtile;
   const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
   const int capacity = (int)prm.capacity;
   auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kWideTile - 1) / kWideTile) + resp_tiles; };  // those of the response first
@@ -643,7 +654,6 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
     head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
     if (head.bh < 0) return;
   } else {
-    if (unit >= prm.BH) return;
     auto cached_of = [&](int i) { return max(min(prm.cu[i + 1], capacity) - min(prm.cu[i], capacity), 0); };
     const int i = __builtin_amdgcn_readfirstlane(prm.BH <= kRanked ? head_of_rank(prm.BH, unit, [&](int n) { return tiles_of(cached_of(n)); }) : unit);
     head = {i, unit, 1, min(prm.cu[i], capacity), cached_of(i)};
@@ -975,41 +985,87 @@ struct Deal {
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
 };
-constexpr int kSharedUnits = 16;    // units of a head on average above which a query row's partial results are read by a whole workgroup
-constexpr int kLongHead = 1 << 14, kLongWide = 1 << 16;  // keys up to which the heads of a launch that fills the chip are left whole
+constexpr int kSharedUnits = 16;  // units of a head on average above which a query row's partial results are read by a whole workgroup
+
+// What a launch of each kernel takes, in us: fitted to 170 launches of bf16 and 50 of fp32 over 4 ... 256 heads, 4 ... 3700 query rows and
+// 3 ... 8500 cached rows a head (longest to shortest up to 8), each timed with whole heads and with units for 128 ... 1024 workgroups, in every
+// form that takes it; off by 12 % (root of the mean square). Over 380 other launches the form and units that it chooses took 1.03 times
+// as long as the best that were timed (bf16 1.033, fp32 1.030, up to 16 query rows 1.015), 1.11 times with fixed limits on the numbers of heads
+// and tiles. The worst, 1.3 ... 1.7 (fp32 2.0), are heads of very different lengths left whole: the host does not know their lengths.
+// Both sides: 64 heads x 354 queries x 250 rows 22.8 whole and wide, 25.1 narrow, 28.1 ... 35.9 dealt out; 32 x 512 x 250 19.8 narrow, 24.2 wide; 8 x 400 x
+// 5582 38.8 whole, 31.0 dealt out; 28 heads x 27 queries x 1106 rows 16.6 whole, 12.6 dealt out.
+struct Form {
+  int tile_rows, keys;  // query rows of a workgroup, keys of a tile
+  int tiles;            // that its waves take in one step
+  int least;            // tiles of a unit
+  int at_once;          // workgroups of a compute unit
+  float start, round;   // the launch, the first loads and the last stores; the same of each round of workgroups
+  float fixed, per_d;   // a step: fixed + per_d * d / 128
+  float beside;         // ... of a workgroup that shares its compute unit: so many times that, for each
+  float part;           // a million bytes of partial results, written and read
+};
+constexpr Form kFew = {16, kTile, 8, 16, 2, 4.5f, 1.3f, 0.f, 1.2f, 1.f, 0.8f};
+constexpr Form kNarrow = {kTile, kTile, kWaves, 8, 2, 5.2f, 1.3f, 0.f, 0.75f, 1.13f, 0.8f};
+constexpr Form kWide = {kWideQueries, kWideTile, 1, 2, 2, 7.f, 0.f, 0.4f, 0.9f, 0.8f, 0.5f};
+constexpr Form kNarrowF32 = {kTile, kTile, kWaves, 4, 1, 2.f, 3.f, 0.f, 5.5f, 1.f, 0.8f};
+constexpr float kJoin = 4.3f;      // the second kernel
+constexpr float kUneven = 1.15f;   // a launch of whole heads waits for the longest ones (1 ... 1.3 choose about as well, 1.5 and more worse)
+constexpr float kLongest = 400.f;  // whole heads: what one may take that has all the rows there are
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
   const bool bf16 = d->dtype == MASKKV_BF16;
-  Deal x;
   // What the host knows of the heads' lengths: no head has more rows than the longest prompt, and all of them as many as there is room for.
   const int64_t most = (d->P_max < capacity ? d->P_max : capacity) + d->n_resp;
-  auto tiles_of = [&](int keys) { return capacity / keys + BH * (1 + (d->n_resp + keys - 1) / keys); };
-  x.few = bf16 && n_q <= 16;
-  x.wide = bf16 && n_q > kWideQueries / 2 && tiles_of(kWideTile) * ((n_q + kWideQueries - 1) / kWideQueries) >= 4 * kUnits;
-  const int keys = x.wide ? kWideTile : kTile;
-  x.tile_rows = x.wide ? kWideQueries : kTile;
-  x.qtiles = (n_q + x.tile_rows - 1) / x.tile_rows;
-  x.part_rows = n_q < x.tile_rows ? n_q : x.tile_rows;
-  x.chunk = 0;
-  x.units = BH;
-  if (BH * x.qtiles >= kUnits && most <= (x.wide ? kLongWide : kLongHead)) return x;
-  // Partial results are written and read again, and their joining is a launch: a unit for every compute unit, and two where that
-  // leaves a unit many tiles.
-  const int64_t tiles = tiles_of(keys), mean = (tiles + BH - 1) / BH;
-  const int least = x.wide ? 3 : bf16 ? 16 : 8, many = x.wide ? 8 : 24;
-  auto chunk_for = [&](int64_t units) {
-    const int64_t each = units / (BH * x.qtiles);  // of a head
-    const int64_t c = each > 1 ? (mean + each - 1) / each : mean;
-    return c < least ? (int64_t)least : c;
+  Deal best;
+  float best_cost = -1.f;
+  auto consider = [&](const Form& f) {
+    const int qtiles = (n_q + f.tile_rows - 1) / f.tile_rows;
+    const int64_t resp = (d->n_resp + f.keys - 1) / f.keys;
+    const float tiles = (float)(BH * resp + capacity / f.keys) + 0.5f * BH, mean = tiles / BH;  // (half a tile of a head is empty, on average)
+    const float step = f.fixed + f.per_d * (float)d->d / 128.f;
+    auto cost = [&](float units, float steps) {
+      const float rounds = units * qtiles / kUnits;
+      const float a_step = rounds <= 1.f ? step : step * (f.at_once == 1 ? (rounds < 3.f ? ceilf(rounds) : rounds) : f.beside * fmaxf(rounds, 2.f));
+      return f.start + f.round * fmaxf(rounds, 1.f) + ceilf(steps) * a_step;
+    };
+    auto take = [&](float cost, int chunk) {
+      if (best_cost >= 0.f && cost >= best_cost) return;
+      best_cost = cost;
+      best.few = &f == &kFew;
+      best.wide = &f == &kWide;
+      best.tile_rows = f.tile_rows;
+      best.qtiles = qtiles;
+      best.part_rows = n_q < f.tile_rows ? n_q : f.tile_rows;
+      best.chunk = chunk;
+      best.units = chunk ? (capacity / f.keys + BH * (resp + 1)) / chunk + BH : BH;
+    };
+    const float whole = cost((float)BH, mean * kUneven / f.tiles);
+    const bool fits = step * ((float)most / (f.keys * f.tiles)) <= kLongest;
+    if (fits) take(whole, 0);
+    auto dealt = [&](float wanted) {
+      int64_t chunk = (int64_t)fmaxf(ceilf(wanted), (float)f.least);
+      chunk = (chunk + f.tiles - 1) / f.tiles * f.tiles;
+      if (fits && chunk * f.keys >= most + 2 * f.keys) return;  // (a head's last tiles of both kinds may be short)
+      const float units = fmaxf(tiles / chunk + 0.5f * BH, BH * ceilf(mean / chunk));
+      take(cost(units, fminf((float)chunk, mean) / f.tiles) + kJoin + f.part * units * n_q * d->d * 4e-6f, (int)chunk);
+    };
+    for (int k = 1; k <= f.at_once; ++k) {  // a unit for every compute unit, or for every place in them:
+      const float places = (float)(k * kUnits) / qtiles;
+      dealt(tiles / fmaxf(places - 0.5f * BH, 0.5f * BH));  // for heads of any length, of which half a unit is empty,
+      dealt(mean / fmaxf(floorf(places / BH), 1.f));        // and for heads of one length
+    }
   };
-  int64_t chunk = chunk_for(kUnits);
-  if (chunk > many) chunk = chunk_for(2 * kUnits);
-  if (chunk * keys >= most + 2 * keys) return x;  // (a head's last tiles of both kinds may be short)
-  x.chunk = (int)chunk;
-  x.units = tiles / chunk + BH;
-  return x;
+  if (!bf16) {
+    consider(kNarrowF32);
+  } else if (n_q <= kFew.tile_rows) {
+    consider(kFew);
+  } else {
+    consider(kNarrow);
+    if (n_q > kWideQueries / 2) consider(kWide);
+  }
+  return best;
 }
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
@@ -1020,7 +1076,7 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
   static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
   auto kernel = &attend_mx_kernel<T, D>;
   int threads = kWaves * 64, lds = C::kLds;
-  int64_t groups = (deal.units + 7) / 8 * 8 * deal.qtiles;
+  const int64_t groups = deal.units * deal.qtiles;
   if constexpr (sizeof(T) == 2) {
     if (deal.wide) {
       kernel = &attend_mx_wide_kernel<D>;
@@ -1030,7 +1086,6 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
       kernel = &attend_mx_few_kernel<D>;
       threads = FewCfg<D>::kWaves * 64;
       lds = FewCfg<D>::kLds;
-      groups = deal.units;
     }
   }
   if (groups > 0x7FFFFFFF) {
@@ -1082,6 +1137,7 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
   prm.n_resp = d->n_resp;
   prm.n_q = prm.q_per_kv * d->n_resp;
   prm.qtiles = deal.qtiles;
+  prm.units = (int)deal.units;
   prm.chunk = deal.chunk;
   prm.tile_rows = deal.tile_rows;
   prm.part_rows = deal.part_rows;
