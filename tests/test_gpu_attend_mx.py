@@ -96,6 +96,21 @@ def test_many_queries_over_few_long_heads(d, n, g, lens):
     Case(n, 1, len(lens), d, "bf16", n, lens, g=g).run().check()
 
 
+@pytest.mark.parametrize("d,H,n", [(128, 16, 256), (64, 32, 384)])
+def test_many_queries_over_long_heads(d, H, n):
+    """128 query rows a workgroup, the keys of heads of several lengths dealt to several."""
+    rng = np.random.default_rng(21)
+    lens = rng.integers(3000, 5600, H)
+    lens[[2, 5]] = [0, 9001]
+    Case(21, 1, H, d, "bf16", n, lens.tolist()).run().check(heads=[0, 2, 5, H - 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("BH,n", [(4, 478), (9, 100), (13, 33)])
+def test_heads_that_the_xcds_do_not_share_evenly(dtype, BH, n):
+    Case(22, 1, BH, 64, dtype, n, [11, 0, 40, 3, 90, 1, 64, 33, 17, 5, 32, 2, 100][:BH]).run().check()
+
+
 def test_many_queries_of_many_heads():
     """128 query rows a workgroup, heads whole: in the order of their lengths, and more of them than are ordered."""
     rng = np.random.default_rng(18)
