@@ -989,11 +989,12 @@ constexpr int kSharedUnits = 16;  // units of a head on average above which a qu
 
 // What a launch of each kernel takes, in us: fitted to 170 launches of bf16 and 50 of fp32 over 4 ... 256 heads, 4 ... 3700 query rows and
 // 3 ... 8500 cached rows a head (longest to shortest up to 8), each timed with whole heads and with units for 128 ... 1024 workgroups, in every
-// form that takes it; off by 12 % (root of the mean square). Over 380 other launches the form and units that it chooses took 1.03 times
-// as long as the best that were timed (bf16 1.033, fp32 1.030, up to 16 query rows 1.015), 1.11 times with fixed limits on the numbers of heads
+// form that takes it; off by 12 % (root of the mean square). Over 400 other launches the form and units that it chooses took 1.03 times
+// as long as the best that were timed (bf16 1.024, fp32 1.030, up to 16 query rows 1.015), 1.11 times with fixed limits on the numbers of heads
 // and tiles. The worst, 1.3 ... 1.7 (fp32 2.0), are heads of very different lengths left whole: the host does not know their lengths.
 // Both sides: 64 heads x 354 queries x 250 rows 22.8 whole and wide, 25.1 narrow, 28.1 ... 35.9 dealt out; 32 x 512 x 250 19.8 narrow, 24.2 wide; 8 x 400 x
-// 5582 38.8 whole, 31.0 dealt out; 28 heads x 27 queries x 1106 rows 16.6 whole, 12.6 dealt out.
+// 5582 38.8 whole, 31.0 dealt out; 28 heads x 27 queries x 1106 rows 16.6 whole, 12.6 dealt out; 28 heads (head_dim 64) of 455 ... 6037 rows, 115
+// queries: 27 whole, 14 dealt out.
 struct Form {
   int tile_rows, keys;  // query rows of a workgroup, keys of a tile
   int tiles;            // that its waves take in one step
@@ -1003,13 +1004,14 @@ struct Form {
   float fixed, per_d;   // a step: fixed + per_d * d / 128
   float beside;         // ... of a workgroup that shares its compute unit: so many times that, for each
   float part;           // a million bytes of partial results, written and read
+  float uneven;         // kUneven where no compute unit has a second workgroup that would fill the wait for the longest head
 };
-constexpr Form kFew = {16, kTile, 8, 16, 2, 4.5f, 1.3f, 0.f, 1.2f, 1.f, 0.8f};
-constexpr Form kNarrow = {kTile, kTile, kWaves, 8, 2, 5.2f, 1.3f, 0.f, 0.75f, 1.13f, 0.8f};
-constexpr Form kWide = {kWideQueries, kWideTile, 1, 2, 2, 7.f, 0.f, 0.4f, 0.9f, 0.8f, 0.5f};
-constexpr Form kNarrowF32 = {kTile, kTile, kWaves, 4, 1, 2.f, 3.f, 0.f, 5.5f, 1.f, 0.8f};
+constexpr Form kFew = {16, kTile, 8, 16, 2, 4.5f, 1.3f, 0.f, 1.2f, 1.f, 0.8f, 1.15f};
+constexpr Form kNarrow = {kTile, kTile, kWaves, 8, 2, 5.2f, 1.3f, 0.f, 0.75f, 1.13f, 0.8f, 1.5f};
+constexpr Form kWide = {kWideQueries, kWideTile, 1, 2, 2, 7.f, 0.f, 0.4f, 0.9f, 0.8f, 0.5f, 1.15f};
+constexpr Form kNarrowF32 = {kTile, kTile, kWaves, 4, 1, 2.f, 3.f, 0.f, 5.5f, 1.f, 0.8f, 1.15f};
 constexpr float kJoin = 4.3f;      // the second kernel
-constexpr float kUneven = 1.15f;   // a launch of whole heads waits for the longest ones (1 ... 1.3 choose about as well, 1.5 and more worse)
+constexpr float kUneven = 1.15f;   // a launch of whole heads waits for the longest ones: by so much on average (1 ... 1.3 choose about as well)
 constexpr float kLongest = 400.f;  // whole heads: what one may take that has all the rows there are
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
@@ -1041,7 +1043,7 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
       best.chunk = chunk;
       best.units = chunk ? (capacity / f.keys + BH * (resp + 1)) / chunk + BH : BH;
     };
-    const float whole = cost((float)BH, mean * kUneven / f.tiles);
+    const float whole = cost((float)BH, mean * (BH * qtiles <= kUnits ? f.uneven : kUneven) / f.tiles);
     const bool fits = step * ((float)most / (f.keys * f.tiles)) <= kLongest;
     if (fits) take(whole, 0);
     auto dealt = [&](float wanted) {
