@@ -8,6 +8,16 @@
 // Where there are many cached rows the four waves of a workgroup hold 32 each and share the queries (SHARE), which come by direct
 // transfers into a ring of four steps, three ahead, one barrier a step; where there are few, all waves hold the same 32 and take the steps
 // in turn.  Sums have a fixed order either way.
+//
+// Probabilities stay in fp32: nothing is rounded but the inputs.  A lane's sums of 16 rows run over its queries, so a row's sum has a chain of
+// n / 32 additions and five more, in fp32.
+//
+// Bound by vector instructions where there is much to do: an exponential, a multiply-add and an addition for every (query, row), 24 cycles of the
+// vector pipe for 64 of them beside 16 of the matrix pipe at head_dim 128.  512 queries of 256 heads x 64 ... 1024 rows (89 k): 21.9 us, the vector
+// pipe busy half and the matrix pipe a third of the time; the busiest compute units have four workgroups, the average 3.25.  256 queries x 32
+// heads x 250 rows: 5.8, the latency of arguments, heads' ends, rows and queries in turn.
+// Two blocks of rows a wave, which halves the reads of LDS, leaves two waves a SIMD instead of four: 25.6 us.  Units dealt to the XCDs in runs of eight
+// instead of an eighth each: 23.2 against 23.8, and 16.2 against 15.3 with grouped queries; one at a time 27.3.
 #include <type_traits>
 
 #include "lds.hpp"
@@ -259,12 +269,14 @@ int launch_form(const AccumulateParams& prm, hipStream_t stream) {
   return check_launch("accumulate");
 }
 
-// Few: there are fewer tiles of cached rows than waves that fill the chip, and more than one step of queries to deal to waves instead.
+// Few: tiles of cached rows for less than two workgroups a compute unit, and more than one step of queries to deal to waves instead.  In turn and
+// shared, 512 queries: 132 tiles 7.7 and 10.4 us, 282 9.3 and 10.7, 465 9.7 and 10.6, 532 11.9 and 10.6, 832 16.3 and 10.7; 128 queries: 212 tiles
+// 5.4 and 5.9, 382 6.1 and 5.8; 40 queries the same to within 0.4; fp32, 128 queries, 312 tiles 10.5 and 12.9.
 template <typename T, int D, bool MX>
 int launch_rows(const AccumulateParams& prm, hipStream_t stream) {
   const int64_t tiles = prm.capacity / kTile + prm.BH;
   const int steps = (prm.n_q + kTile - 1) / kTile;
-  if (steps > 1 && tiles < 4 * kUnits) return launch_form<T, D, MX, 4, false>(prm, stream);
+  if (steps > 1 && tiles < 2 * kUnits) return launch_form<T, D, MX, 4, false>(prm, stream);
   return launch_form<T, D, MX, 4, true>(prm, stream);
 }
 

@@ -9,13 +9,20 @@
 // holds all of them and goes through the bits of the weights' order by itself, by ballots: no barrier and no LDS.  Beyond that the workgroup
 // goes by histograms of eight bits in LDS.  The rows of a thread stay in registers, up to 32 of them; a longer head's are read again
 // every round.
+//
+// Nothing is computed but comparisons and counts: latency, and where there are many rows the copying.  32 heads x 250 bf16 rows, half of them moved: 6.5 us
+// a call; 256 heads x 64 ... 1024 rows in 4 bits (89 k, half of them moved: 6 MB in, 7 out) 11.5 us, 60 % of its waves' time spent waiting.
 #include "mx.hpp"
 
 namespace maskkv {
 
 namespace {
 
-constexpr int kShortHead = 512;   // rows of a head on average up to which the rows that stay are not listed by a launch of their own
+// Rows of a head up to which the rows that stay are not listed by a launch of their own: on average, or all of the longest one's.  One and two
+// launches: 32 heads x 250 rows 9.5 and 15.4 us, x 900 11.0 and 17.3, x 2500 22.4 and 23.7, x 4000 25.8 and 26.5; 256 heads x 600 20.1 and 27.4, x 1200 43.0 and
+// 43.3; heads of 1000 ... 8000 rows, 32 of them, 48.9 and 27.7, 4 x 8000 40.7 and 20.4: beyond 4096 a workgroup of 256 reads its head again and again.
+// (With the expansion of what is left, 0.5 ... 5 us.)
+constexpr int kShortHead = 1024, kLongestHead = 4096;
 constexpr int kMostRows = 4096;   // of a workgroup's list
 
 struct EvictParams {
@@ -398,7 +405,7 @@ int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_b
   int64_t per = (most + 511) / 512;
   per = per < 16 ? 16 : per > kMostRows ? kMostRows : per;
   prm.per = (int)per;
-  if (capacity <= (int64_t)kShortHead * prm.BH) {
+  if (capacity <= (int64_t)kShortHead * prm.BH || d->P_max <= kLongestHead || capacity <= kLongestHead) {
     const int64_t groups = most / per + prm.BH;  // (each head's last one may have fewer)
     hipLaunchKernelGGL(evict_kernel, dim3((unsigned)groups), dim3(256), per * 4, stream, prm);
     return check_launch("evict");

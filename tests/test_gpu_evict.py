@@ -76,6 +76,13 @@ def test_long_heads(mx, n, k):
     check([30, n, 7], [10, k, 7], heavy(rng, n + 37), 128, "bf16", mx)
 
 
+@pytest.mark.parametrize("mx", [False, True])
+def test_heads_of_all_lengths_listed_by_a_launch_of_their_own(mx):
+    rng = np.random.default_rng(8)
+    lens = [2049, 5000, 2048, 1, 4096, 3001, 0, 33000, 100, 12000]
+    check(lens, [1000, 4999, 2047, 1, 1, 3001, 5, 20000, 99, 64], heavy(rng, sum(lens)), 64, "bf16", mx, B=2)
+
+
 def test_a_long_head_among_short_ones():
     rng = np.random.default_rng(6)
     for n in (700, 3000, 4097, 9000):
