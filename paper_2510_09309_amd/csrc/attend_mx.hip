@@ -1,6 +1,8 @@
-// Attention of the response span over a cache in 4 bits and the response's own rows.
+// Attention of the response span over a cache in 4 bits and the response's own rows: one pass over the keys with the running maximum and
+// sum of a softmax.  Three kernels: up to 16 query rows a head (bf16), 32 a workgroup, and 128 a workgroup (bf16); which of them a launch
+// takes, and whether a head's keys go to several workgroups, is chosen by what it is expected to take (`deal_of`).
 //
-// A workgroup of four waves serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row
+// 32 query rows: four waves serve 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row
 // axis), so that a lane owns one query and its probabilities are the B operand of O^T = V^T P^T as they stand.  The waves take
 // tiles of 32 keys in turn, each through registers and LDS of its own, without a barrier, and are merged at the end.  A
 // row's two halves along the head dimension belong to the two halves of a wave: a lane's codes of a key are 16 (8) whole words
@@ -8,8 +10,17 @@
 // their way into LDS, from where a transposing read brings them as V^T.  The response's tiles come first: what is read of the
 // cache for the first of its tiles is under way meanwhile.
 //
-// Where heads x query tiles are fewer than the compute units, or a head may be far longer than the others, the tiles are dealt to
-// several workgroups, and a second kernel joins their partial results.
+// The values of 4 bits are exact in bf16, so the logits are those of the stored values; sums, maxima and outputs are fp32 throughout.
+// Probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product: fp32 operands have a sixteenth of its rate.
+// The sum that divides them is of the unrounded ones.  Partial results are fp32.
+//
+// Where the keys are dealt out, a second kernel joins the partial results: in the same launch it would take a counter that is zero
+// when the call begins, and a workspace need not be.
+//
+// Bound by latency where there is little to do: 32 heads x 256 queries x 250 + 256 rows, head_dim 128, 10.1 us, of which 6.5 are the launch, the
+// first loads and the merging of the waves; one query row of 7 heads over 4 x 30k rows 7.6 + 3.0 us (16 MB, 3.2 at a large copy's rate).
+// By the two phases of a tile where there is much: 256 heads x 512 queries x 64 ... 1024 rows 78.5 us, 733 TFLOP/s, the matrix pipe busy 37 % and the
+// vector pipe 43 % of the time, at a clock that the board's power lowers to 1.85 GHz; the same from a cache in bf16 takes 75.5.
 #include <cmath>
 #include <type_traits>
 
@@ -48,7 +59,7 @@ __device__ __forceinline__ void fetch_attend_mx_arguments() {
 }
 
 // Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there, but those of the
-// last units, fewer than eight, are dealt to all XCDs (4 heads x 60 query tiles on half of the chip: 16.8 us, on all of it 10.6).
+// last units, fewer than eight, are dealt to all XCDs (4 heads x 60 query tiles on half of the chip: 16.8 us, on all of it 10.7).
 struct Place {
   int unit, qtile;
 };
@@ -351,7 +362,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_mx
 // The layout is that of the kernel above with quarters of a wave for halves: a lane's share of a key is a quarter of its row, at head_dim
 // 128 one group with one scale, and a lane has 8 instead of 16 probabilities of a tile.  What a call of few queries takes is the reading
 // of the cache and the time of one tile from its first load to its last product; half the registers leave room for twice the
-// waves, so that most waves have one tile or two.
+// waves, so that most waves have one tile or two.  Against 32 query rows a workgroup: one token of 7 heads over 4 x 30k rows 11.4 and 12.5 us, of 32 heads
+// x 1000 rows 8.2 and 10.5, 16 tokens 8.8 and 11.0; 16 heads x 5 queries x 60 rows 6.6 and 6.4.
 template <int D>
 struct FewCfg {
   static constexpr int kWaves = 8;
@@ -985,7 +997,9 @@ struct Deal {
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
 };
-constexpr int kSharedUnits = 16;  // units of a head on average above which a query row's partial results are read by a whole workgroup
+// Units of a head on average above which a query row's partial results are read by a whole workgroup instead of an eighth of one: 59 units 11.4 and
+// 16.1 us a call, 32 11.4 and 12.6; 8 units 15.0 and 14.1.
+constexpr int kSharedUnits = 16;
 
 // What a launch of each kernel takes, in us: fitted to 170 launches of bf16 and 50 of fp32 over 4 ... 256 heads, 4 ... 3700 query rows and
 // 3 ... 8500 cached rows a head (longest to shortest up to 8), each timed with whole heads and with units for 128 ... 1024 workgroups, in every
