@@ -31,6 +31,7 @@ struct EvictParams {
   int64_t capacity, capacity_out;
   int BH;
   int per;        // rows of a workgroup at most
+  int once;       // the old cache goes past the memory-side cache
   int row_shift;  // 16-byte pieces of a row, both large arrays together: 1 << row_shift
   int32_t *rows, *idx_out, *cu_out;
   float* weights_out;
@@ -239,8 +240,8 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
 }
 
 // `rows` rows from `list` (packed rows) to row `to` of the smaller cache on.
-template <int THREADS>
-__device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t* list, int64_t to, int rows) {
+template <int THREADS, bool ONCE>
+__device__ __forceinline__ void copy_rows(const EvictParams& prm, const int32_t* list, int64_t to, int rows) {
   const int pieces = 1 << prm.row_shift, half = pieces / 2;
   constexpr int kAtOnce = 4;
   for (int i0 = threadIdx.x; i0 < rows << prm.row_shift; i0 += kAtOnce * THREADS) {  // 16 bytes a thread and step
@@ -249,7 +250,7 @@ __device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t*
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = min(i0 + u * THREADS, (rows << prm.row_shift) - 1), piece = i & (pieces - 1), m = piece >= half;
       const int64_t from = list[i >> prm.row_shift];
-      x4[u] = *reinterpret_cast<const u32x4*>(prm.moved.from[m] + (from * half + (piece - m * half)) * 16);
+      x4[u] = read_piece<ONCE>(prm.moved.from[m] + (from * half + (piece - m * half)) * 16);
     }
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
@@ -258,6 +259,13 @@ __device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t*
         *reinterpret_cast<u32x4*>(prm.moved.to[m] + ((to + (i >> prm.row_shift)) * half + (piece - m * half)) * 16) = x4[u];
     }
   }
+}
+template <int THREADS>
+__device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t* list, int64_t to, int rows) {
+  if (prm.once)
+    copy_rows<THREADS, true>(prm, list, to, rows);
+  else
+    copy_rows<THREADS, false>(prm, list, to, rows);
   for (int i = threadIdx.x; i < rows; i += THREADS) {
     const int64_t from = list[i];
     if (prm.idx) prm.idx_out[to + i] = prm.idx[from];
@@ -398,6 +406,9 @@ int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_b
   prm.cu_out = cu_out;
   prm.weights_out = weights_out;
   prm.moved = moved;
+  // (A third of the memory-side cache: the new cache and others are beside it.  Past it and through it, 256 heads of bf16 rows, half of them moved: 66 MB
+  // 21.3 and 18.5 us, 79 MB 22.3 and 22.4, 92 MB 24.9 and 25.8, 131 MB 32.0 and 37.9; 139 MB in 4 bits, with their expansion, 117 and 128.)
+  prm.once = 2 * capacity * moved.bytes[0] > kSideCache / 3;
   prm.row_shift = 0;
   while (16 << prm.row_shift < 2 * moved.bytes[0]) ++prm.row_shift;
   // Workgroups for two of every compute unit, of 16 rows at least and of no more than the list has room for.

@@ -7,7 +7,7 @@
 // The scale is a power of two, so the only rounding is the one to 4 bits: dividing by it and multiplying with it again are exact.
 //
 // Bound by HBM where there are many rows, by the latency of arguments, positions and rows where there are few.  256 heads x 64 ... 1024 bf16
-// rows of 128 (89 k in all): stored in 12.9 us (45 MB by rows of 256 bytes in, 12 MB out, 4.5 TB/s; without the conversion 12.4),
+// rows of 128 (89 k in all): stored in 15.0 us (45 MB by rows of 256 bytes in, 12 MB out; from the memory-side cache 12.9, 12.4 without the conversion),
 // expanded in 10.2 (5 TB/s).  32 heads x 250 rows: 4.4 and 3.0 on the device, as long as the host takes to launch them.
 #include "mx.hpp"
 
@@ -63,13 +63,13 @@ __device__ __forceinline__ void store_group(const u32x4& x, char* codes, char* s
 }
 
 // A wave stores kRounds times as many rows as it has room for in its lanes, side by side, and asks for all of them before it uses the first
-// (one round 14.5 us for the 89 k rows above, two 12.9, three 13.0, four 13.4).
+// (the 89 k rows above from the memory-side cache: one round 14.5 us, two 12.9, three 13.0, four 13.4).
 // Positions and the heads' ends are asked for at once, so that three waits in turn come before the first row is stored:
 // arguments, these, and the rows.
 constexpr int kRounds = 2;
 constexpr int kEnds = 256;  // heads up to which a wave holds the ends of all of them in its lanes; more are searched, a latency for each halving
 
-template <typename T>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxParams prm) {
   typedef CompactMxParams A;
   fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, K), MASKKV_VIEW_ARGUMENTS(A, V), MASKKV_ARGUMENT(A, lens), MASKKV_ARGUMENT(A, H),
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxPar
   auto load = [&](int u, int h, int b) {
     // a position outside the prompt is clamped rather than read out of bounds
     const int src = min(max(position[u], 0), max(prm.lens.P[b] - 1, 0));
-    k[u] = *reinterpret_cast<const u32x4*>(prm.K.row(b, h, src) + piece * 16);
-    v[u] = *reinterpret_cast<const u32x4*>(prm.V.row(b, h, src) + piece * 16);
+    k[u] = read_piece<ONCE>(prm.K.row(b, h, src) + piece * 16);
+    v[u] = read_piece<ONCE>(prm.V.row(b, h, src) + piece * 16);
   };
   if (min(first + kRounds * mine, total) <= end) {  // all rows are of one head
     const int b = bh / prm.H, h = bh % prm.H;
@@ -183,10 +183,11 @@ int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, con
   prm.out = cache;
   const int rows = kRounds * kThreads / (d->d * (d->dtype == MASKKV_BF16 ? 2 : 4) / 16);  // of a workgroup
   const dim3 grid((unsigned)((capacity + rows - 1) / rows));
-  if (d->dtype == MASKKV_BF16)
-    hipLaunchKernelGGL(compact_mx_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, prm);
-  else
-    hipLaunchKernelGGL(compact_mx_kernel<float>, grid, dim3(kThreads), 0, stream, prm);
+  // (89 k rows of 2.1 GB of prompt: 15.0 us past the cache, 16.8 through it, and 12.9 through it where just these rows were there)
+  const bool bf16 = d->dtype == MASKKV_BF16, once = 2ll * prm.BH * d->P_max * d->d * (bf16 ? 2 : 4) > kSideCache;
+  const auto kernel = bf16 ? once ? compact_mx_kernel<bf16_t, true> : compact_mx_kernel<bf16_t, false>
+                           : once ? compact_mx_kernel<float, true> : compact_mx_kernel<float, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, prm);
   return check_launch("compact_mx");
 }
 
