@@ -405,8 +405,18 @@ PyObject* value_shift(PyObject*, Args a, Py_ssize_t n) {  // V_now, V_prev, delt
 // ---- the cache in 4 bits and further eviction: these calls look at what they are given as far as Python knows it, before the
 // library does (it sees pointers): type, size, device.
 
+// The current device, found once a call, and only for what may be on it.
+thread_local int here;
+struct DescHere : DescArg {
+  explicit DescHere(PyObject* o) : DescArg(o) { here = -1; }
+};
+int current_device() {
+  if (here < 0) here = c10::hip::getCurrentHIPStream().device_index();
+  return here;
+}
+
 void on_this_device(const at::Tensor& t, const char* what) {
-  if (t.is_cuda() && t.get_device() == c10::hip::getCurrentHIPStream().device_index()) return;
+  if (t.is_cuda() && t.get_device() == current_device()) return;
   PyErr_Format(PyExc_AssertionError, "%s: need a tensor on the current device", what);
   throw Error{};
 }
@@ -414,7 +424,7 @@ void on_this_device(const at::Tensor& t, const char* what) {
 // As as_stream, of the current device.
 void* stream_here(PyObject* o) {
   if (o != Py_None && PyObject_HasAttr(o, kdevice_index)) {
-    if (attr_i32(o, kdevice_index) != c10::hip::getCurrentHIPStream().device_index())
+    if (attr_i32(o, kdevice_index) != current_device())
       fail(PyExc_AssertionError, "stream: need one of the current device");
   }
   return as_stream(o);
@@ -484,7 +494,7 @@ struct MxArg {
 
 PyObject* compact_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, K, V, idx, cu, capacity, cache, stream
   return call<8>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     const int64_t cap = as_i64(a[5]);
     CheckedView k(a[1], d.d, d.d.H, longest_prompt(d.d), "K"), v(a[2], d.d, d.d.H, longest_prompt(d.d), "V");
     const int32_t *idx = buffer<int32_t>(a[3], at::kInt, cap, "idx"), *cu = buffer<int32_t>(a[4], at::kInt, heads_of(d.d) + 1, "cu_budget");
@@ -495,7 +505,7 @@ PyObject* compact_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, K, V, idx, cu,
 }
 PyObject* expand_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, cache, cu, capacity, Kc, Vc, stream
   return call<7>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     const int64_t cap = as_i64(a[3]);
     MxArg mx(a[1], d.d, cap);
     const int32_t* cu = buffer<int32_t>(a[2], at::kInt, heads_of(d.d) + 1, "cu_budget");
@@ -514,7 +524,7 @@ PyObject* attend_mx_ws(PyObject*, Args a, Py_ssize_t n) {
 }
 PyObject* attend_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, Q, cache, cu, capacity, Kr, Vr, scale, O, lse, workspace, stream
   return call<12>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     const int64_t cap = as_i64(a[4]), g = group_of(d.d);
     CheckedView q(a[1], d.d, d.d.H * g, d.d.n_resp, "Q_resp"), k2(a[5], d.d, d.d.H, d.d.n_resp, "K_resp"),
         v2(a[6], d.d, d.d.H, d.d.n_resp, "V_resp"), o(a[8], d.d, d.d.H * g, d.d.n_resp, "O");
@@ -530,7 +540,7 @@ PyObject* attend_mx(PyObject*, Args a, Py_ssize_t n) {  // desc, Q, cache, cu, c
 // desc, Q, Kc or cache, cu, capacity, scale, lse, decay, weights_in, weights_out, stream
 PyObject* accumulate_any(Args a, Py_ssize_t n, bool mx) {
   return call<11>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     const int64_t cap = as_i64(a[4]), g = group_of(d.d);
     CheckedView q(a[1], d.d, d.d.H * g, d.d.n_resp, "Q_resp");
     const int32_t* cu = buffer<int32_t>(a[3], at::kInt, heads_of(d.d) + 1, "cu_budget");
@@ -574,7 +584,7 @@ struct EvictArgs {  // weights, cu, capacity, budgets ... idx ... idx_out, rows,
 // desc, weights, cu, capacity, budgets, Kc, Vc, idx, Kc_out, Vc_out, idx_out, rows, weights_out, cu_out, capacity_out, stream
 PyObject* evict(PyObject*, Args a, Py_ssize_t n) {
   return call<16>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     EvictArgs e(d.d, a, a[7], a + 10);
     const at::ScalarType t = element_type(d.d);
     const int64_t in = e.cap * d.d.d, out = e.cap_out * d.d.d;
@@ -589,7 +599,7 @@ PyObject* evict(PyObject*, Args a, Py_ssize_t n) {
 // desc, weights, cu, capacity, budgets, cache, idx, cache_out, idx_out, rows, weights_out, cu_out, capacity_out, stream
 PyObject* evict_mx(PyObject*, Args a, Py_ssize_t n) {
   return call<14>(n, [&] {
-    DescArg d(a[0]);
+    DescHere d(a[0]);
     EvictArgs e(d.d, a, a[6], a + 8);
     MxArg from(a[5], d.d, e.cap), to(a[7], d.d, e.cap_out);
     return without_gil([&] {
