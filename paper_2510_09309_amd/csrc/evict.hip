@@ -117,13 +117,15 @@ __device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, in
 template <int THREADS>
 struct Bins {
   static constexpr int kCopies = THREADS == 256 ? 2 : 8;
-  static constexpr int kRound = 256 * kCopies;
+  static constexpr int kCopy = 256 + 8;  // from one copy to the next: those of a count lie in banks of their own
+  static constexpr int kRound = kCopy * kCopies;
 };
 
 // The same by the whole workgroup.  VALUES: rows of a thread, in registers, or 0.
 template <int THREADS, int VALUES>
 __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, int hi, int base, int32_t* list, int* all_bins, int (*counts)[4]) {
   constexpr int kWaves = THREADS / 64, kCopies = Bins<THREADS>::kCopies, kBins = Bins<THREADS>::kRound;
+  constexpr bool kOneScans = kWaves == 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = VALUES ? VALUES : (n + THREADS - 1) / THREADS;
   const int row0 = wave * each * 64 + lane;  // a wave's rows lie side by side, 64 a step
@@ -158,35 +160,42 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
   for (int shift = 24; shift >= 0 && !exact; shift -= 8) {
     int* const bins = all_bins + shift / 8 * kBins;  // (a round has its own: one barrier each)
     over_rows([&](uint32_t o, int v) {
-      if (row0 + v * 64 < n && (shift == 24 || (o ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[(o >> shift & 255) * kCopies + lane % kCopies], 1);
+      if (row0 + v * 64 < n && (shift == 24 || (o ^ least) >> (shift + 8) == 0)) atomicAdd(&bins[lane % kCopies * Bins<THREADS>::kCopy + (o >> shift & 255)], 1);
     });
     __syncthreads();
-    // every wave by itself: a lane holds four bins from the top, 255 - 4 lane ..
-    int in[4];
+    // A lane holds four bins from the top, 255 - 4 lane ..: every wave by itself, or, of sixteen, one for all.
+    if (!kOneScans || wave == 0) {
+      int in[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int2* some = reinterpret_cast<const int2*>(bins + (255 - 4 * lane - j) * kCopies);
-      in[j] = 0;
-#pragma unroll
-      for (int c = 0; c < kCopies / 2; ++c) in[j] += some[c].x + some[c].y;
-    }
-    const int own = (in[0] + in[1]) + (in[2] + in[3]);
-    const int upto = wave_prefix(own);
-    const int at = __builtin_ctzll(__ballot(upto >= wanted));  // (there is one: all the rows that agree are `wanted` or more)
-    int above = __builtin_amdgcn_readlane(upto - own, at);     // rows above the bin in question
-    int digit = 255 - 4 * at, upto_it = above;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n_j = __builtin_amdgcn_readlane(in[j], at);
-      if (upto_it < wanted) {
-        digit = 255 - 4 * at - j;
-        above = upto_it;
-        upto_it += n_j;
+      for (int c = 0; c < kCopies; ++c) {
+        const int4 some = *reinterpret_cast<const int4*>(bins + c * Bins<THREADS>::kCopy + 252 - 4 * lane);
+        in[0] += some.w, in[1] += some.z, in[2] += some.y, in[3] += some.x;
       }
+      const int own = (in[0] + in[1]) + (in[2] + in[3]);
+      const int upto = wave_prefix(own);
+      const int at = __builtin_ctzll(__ballot(upto >= wanted));  // (there is one: all the rows that agree are `wanted` or more)
+      int above = __builtin_amdgcn_readlane(upto - own, at);     // rows above the bin in question
+      int digit = 255 - 4 * at, upto_it = above;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int n_j = __builtin_amdgcn_readlane(in[j], at);
+        if (upto_it < wanted) {
+          digit = 255 - 4 * at - j;
+          above = upto_it;
+          upto_it += n_j;
+        }
+      }
+      least |= (uint32_t)digit << shift;
+      exact = upto_it == wanted;
+      wanted -= above;
     }
-    least |= (uint32_t)digit << shift;
-    exact = upto_it == wanted;
-    wanted -= above;
+    if constexpr (kOneScans) {
+      if (threadIdx.x == 0) counts[0][2] = (int)least, counts[0][3] = exact ? 0 : wanted;
+      __syncthreads();
+      least = (uint32_t)__builtin_amdgcn_readfirstlane(counts[0][2]);
+      wanted = __builtin_amdgcn_readfirstlane(counts[0][3]);
+      exact = wanted == 0;
+    }
   }
   // Where `exact`, those at or above `least` stay, else those above it and the first ones of those at it.
   const uint32_t surely = exact ? least : least + 1;  // (`least` is not the largest of all numbers: that would be a NaN's)
