@@ -46,6 +46,18 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Of rows row, row + 64 ... of a head's n.  (All are asked for before the first is used: as the compiler has it, under a condition each, one after the other.)
+template <int VALUES>
+__device__ __forceinline__ void read_orders(const float* w, int row, int n, uint32_t (&held)[VALUES]) {
+  float x[VALUES];
+#pragma unroll
+  for (int v = 0; v < VALUES; ++v) x[v] = w[min(row + v * 64, n - 1)];
+#pragma unroll
+  for (int v = 0; v < VALUES; ++v) asm volatile("" : "+v"(x[v]));
+#pragma unroll
+  for (int v = 0; v < VALUES; ++v) held[v] = row + v * 64 < n ? order_of(x[v]) : 0u;
+}
+
 struct HeadRows {
   int first, n, stay;
 };
@@ -78,11 +90,7 @@ template <int THREADS, int VALUES>
 __device__ __forceinline__ void list_rows_alone(const float* w, int n, int k, int lo, int hi, int base, int32_t* list) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t held[VALUES];
-#pragma unroll
-  for (int v = 0; v < VALUES; ++v) {
-    const float x = w[min(v * 64 + lane, n - 1)];
-    held[v] = v * 64 + lane < n ? order_of(x) : 0u;
-  }
+  read_orders<VALUES>(w, lane, n, held);
   uint32_t least = 0;   // a row at or above it stays, or may
   bool exact = k == n;  // just those stay
   for (uint32_t bit = 0x80000000u; bit && !exact; bit >>= 1) {
@@ -130,22 +138,19 @@ __device__ __forceinline__ void list_rows(const float* w, int n, int k, int lo, 
   const int each = VALUES ? VALUES : (n + THREADS - 1) / THREADS;
   const int row0 = wave * each * 64 + lane;  // a wave's rows lie side by side, 64 a step
   uint32_t held[VALUES ? VALUES : 1];
-  auto read = [&](int v) {
-    const int row = row0 + v * 64;
-    const float x = w[min(row, n - 1)];
-    return row < n ? order_of(x) : 0u;
-  };
-  if constexpr (VALUES > 0) {
-#pragma unroll
-    for (int v = 0; v < VALUES; ++v) held[v] = read(v);
-  }
+  if constexpr (VALUES > 0) read_orders<VALUES>(w, row0, n, held);
   auto over_rows = [&](auto f) {
     if constexpr (VALUES > 0) {
 #pragma unroll
       for (int v = 0; v < VALUES; ++v) f(held[v], v);
     } else {
-#pragma unroll 8
-      for (int v = 0; v < each; ++v) f(read(v), v);
+      for (int v0 = 0; v0 < each; v0 += 8) {
+        uint32_t some[8];
+        read_orders<8>(w, row0 + v0 * 64, n, some);
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+          if (v0 + v < each) f(some[v], v0 + v);  // (behind these come the next wave's rows)
+      }
     }
   };
 
