@@ -618,15 +618,27 @@ struct WideCfg {
 };
 
 // The head of a given rank by descending number of tiles, equal ones by ascending number: the lanes of a wave hold all heads'
-// counts, a bit of the wanted count takes a ballot per 64 heads.
+// ends, which are asked for at once; a bit of the wanted count of tiles takes a ballot per 64 heads.
 constexpr int kRanked = 256;  // heads up to which their order is found so
 template <typename F>
-__device__ __forceinline__ int head_of_rank(int BH, int rank, F tiles_of) {
+__device__ __forceinline__ UnitHead head_of_rank(const int32_t* cu, int BH, int capacity, int rank, F tiles_of) {
   constexpr int N = kRanked / 64;
   const int lane = threadIdx.x & 63;
-  int tiles[N];
+  int from[N], to[N], tiles[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) tiles[i] = i * 64 + lane < BH ? min(tiles_of(i * 64 + lane), 0xFFFF) : 0;
+  for (int i = 0; i < N; ++i) {
+    const int bh = min(i * 64 + lane, BH - 1);
+    from[i] = cu[bh];
+    to[i] = cu[bh + 1];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(from[i]), "+v"(to[i]));
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    from[i] = min(from[i], capacity);
+    to[i] = max(min(to[i], capacity) - from[i], 0);  // (rows)
+    tiles[i] = i * 64 + lane < BH ? min(tiles_of(to[i]), 0xFFFF) : 0;
+  }
   int found = 0, above = 0;  // the count, and how many heads have more tiles
   for (int bit = 1 << 15; bit > 0; bit >>= 1) {
     int n = 0;
@@ -637,18 +649,25 @@ __device__ __forceinline__ int head_of_rank(int BH, int rank, F tiles_of) {
     else
       above = n;
   }
-  int left = rank - above, head = 0;
+  int left = rank - above;
+  UnitHead x = {0, rank, 1, 0, 0};
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     uint64_t same = __ballot(tiles[i] == found);
     const int n = __popcll(same);
     if (left >= 0 && left < n) {
       const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
-      head = i * 64 + __builtin_ctzll(__ballot(tiles[i] == found && before == left));
+      const int at = __builtin_ctzll(__ballot(tiles[i] == found && before == left));
+      x.bh = i * 64 + at;
+      x.first = __builtin_amdgcn_readlane(from[i], at);
+      x.rows = __builtin_amdgcn_readlane(to[i], at);
     }
     left -= n;
   }
-  return head;
+  x.bh = __builtin_amdgcn_readfirstlane(x.bh);
+  x.first = __builtin_amdgcn_readfirstlane(x.first);
+  x.rows = __builtin_amdgcn_readfirstlane(x.rows);
+  return x;
 }
 
 template <int D>
@@ -665,10 +684,11 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   if (prm.chunk) {
     head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
     if (head.bh < 0) return;
+  } else if (prm.BH <= kRanked) {
+    head = head_of_rank(prm.cu, prm.BH, capacity, unit, tiles_of);
   } else {
-    auto cached_of = [&](int i) { return max(min(prm.cu[i + 1], capacity) - min(prm.cu[i], capacity), 0); };
-    const int i = __builtin_amdgcn_readfirstlane(prm.BH <= kRanked ? head_of_rank(prm.BH, unit, [&](int n) { return tiles_of(cached_of(n)); }) : unit);
-    head = {i, unit, 1, min(prm.cu[i], capacity), cached_of(i)};
+    const int first = min(prm.cu[unit], capacity);
+    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
   }
   const int bh = head.bh, first = head.first, cached = head.rows;
   const int b = bh / prm.H, h = bh % prm.H;

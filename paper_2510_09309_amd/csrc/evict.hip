@@ -280,16 +280,28 @@ __device__ __forceinline__ void move_rows(const EvictParams& prm, const int32_t*
     copy_rows<THREADS, true>(prm, list, to, rows);
   else
     copy_rows<THREADS, false>(prm, list, to, rows);
-  for (int i = threadIdx.x; i < rows; i += THREADS) {
+  for (int i = threadIdx.x; i < rows; i += THREADS) {  // (what is small, all of it asked for before the first is stored)
     const int64_t from = list[i];
-    if (prm.idx) prm.idx_out[to + i] = prm.idx[from];
-    if (prm.weights_out) prm.weights_out[to + i] = prm.weights[from];
+    int32_t position = 0;
+    float weight = 0.f;
+    uint32_t scale[2] = {0, 0};
+    if (prm.idx) position = prm.idx[from];
+    if (prm.weights_out) weight = prm.weights[from];
     if (prm.moved.bytes[2] == 4) {
-      reinterpret_cast<uint32_t*>(prm.moved.to[2])[to + i] = reinterpret_cast<const uint32_t*>(prm.moved.from[2])[from];
-      reinterpret_cast<uint32_t*>(prm.moved.to[3])[to + i] = reinterpret_cast<const uint32_t*>(prm.moved.from[3])[from];
+      scale[0] = reinterpret_cast<const uint32_t*>(prm.moved.from[2])[from];
+      scale[1] = reinterpret_cast<const uint32_t*>(prm.moved.from[3])[from];
     } else if (prm.moved.bytes[2] == 2) {
-      reinterpret_cast<uint16_t*>(prm.moved.to[2])[to + i] = reinterpret_cast<const uint16_t*>(prm.moved.from[2])[from];
-      reinterpret_cast<uint16_t*>(prm.moved.to[3])[to + i] = reinterpret_cast<const uint16_t*>(prm.moved.from[3])[from];
+      scale[0] = reinterpret_cast<const uint16_t*>(prm.moved.from[2])[from];
+      scale[1] = reinterpret_cast<const uint16_t*>(prm.moved.from[3])[from];
+    }
+    if (prm.idx) prm.idx_out[to + i] = position;
+    if (prm.weights_out) prm.weights_out[to + i] = weight;
+    if (prm.moved.bytes[2] == 4) {
+      reinterpret_cast<uint32_t*>(prm.moved.to[2])[to + i] = scale[0];
+      reinterpret_cast<uint32_t*>(prm.moved.to[3])[to + i] = scale[1];
+    } else if (prm.moved.bytes[2] == 2) {
+      reinterpret_cast<uint16_t*>(prm.moved.to[2])[to + i] = (uint16_t)scale[0];
+      reinterpret_cast<uint16_t*>(prm.moved.to[3])[to + i] = (uint16_t)scale[1];
     }
   }
 }

@@ -89,6 +89,8 @@ __global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxPar
     int ends[kEnds / 64];
 #pragma unroll
     for (int i = 0; i < kEnds / 64; ++i) ends[i] = prm.cu[min(i * 64 + lane + 1, prm.BH)];
+    static_assert(kEnds == 256 && kRounds == 2, "what is waited for at once");
+    asm volatile("" : "+v"(ends[0]), "+v"(ends[1]), "+v"(ends[2]), "+v"(ends[3]), "+v"(position[0]), "+v"(position[1]));
     total = min(__builtin_amdgcn_readlane(ends[kEnds / 64 - 1], 63), capacity);
     if (first >= total) return;
     bh = 0;
@@ -147,13 +149,13 @@ __global__ __launch_bounds__(kThreads) void expand_mx_kernel(const ExpandParams 
   const int pieces = prm.d / 8;
   const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   if (i >= min((int64_t)prm.total[0], prm.capacity) * pieces) return;
-  const char* codes[2] = {prm.in.k_codes, prm.in.v_codes};
-  const char* scales[2] = {prm.in.k_scales, prm.in.v_scales};
-  char* to[2] = {prm.Kc, prm.Vc};
+  const uint32_t codes[2] = {reinterpret_cast<const uint32_t*>(prm.in.k_codes)[i], reinterpret_cast<const uint32_t*>(prm.in.v_codes)[i]};
+  const uint32_t scales[2] = {reinterpret_cast<const uint8_t*>(prm.in.k_scales)[i / 4], reinterpret_cast<const uint8_t*>(prm.in.v_scales)[i / 4]};
+  char* const to[2] = {prm.Kc, prm.Vc};
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
-    const uint32_t c = reinterpret_cast<const uint32_t*>(codes[n])[i];
-    const float unit = mx_unit(reinterpret_cast<const uint8_t*>(scales[n])[i / 4]);
+    const uint32_t c = codes[n];
+    const float unit = mx_unit(scales[n]);
     if (sizeof(T) == 2) {
       reinterpret_cast<u32x4*>(to[n])[i] = mx_decode_bf16(c, unit);
     } else {
