@@ -11,7 +11,7 @@
 // every round.
 //
 // Nothing is computed but comparisons and counts: latency, and where there are many rows the copying.  32 heads x 250 bf16 rows, half of them moved: 6.5 us
-// a call; 256 heads x 64 ... 1024 rows in 4 bits (89 k, half of them moved: 6 MB in, 7 out) 11.5 us, 60 % of its waves' time spent waiting.
+// a call; 256 heads x 64 ... 1024 rows in 4 bits (89 k, half of them moved: 6 MB in, 7 out) 11.0 us, 60 % of its waves' time spent waiting.
 #include "mx.hpp"
 
 namespace maskkv {
@@ -19,9 +19,9 @@ namespace maskkv {
 namespace {
 
 // Rows of a head up to which the rows that stay are not listed by a launch of their own: on average, or all of the longest one's.  One and two
-// launches: 32 heads x 250 rows 9.5 and 15.4 us, x 900 11.0 and 17.3, x 2500 22.4 and 23.7, x 4000 25.8 and 26.5; 256 heads x 600 20.1 and 27.4, x 1200 43.0 and
-// 43.3; heads of 1000 ... 8000 rows, 32 of them, 48.9 and 27.7, 4 x 8000 40.7 and 20.4: beyond 4096 a workgroup of 256 reads its head again and again.
-// (With the expansion of what is left, 0.5 ... 5 us.)
+// launches: 32 heads x 250 rows 8.3 and 11.7 us, x 900 10.8 and 13.9, x 1800 14.6 and 16.4, x 4000 21.5 and 21.1; 4 x 1800 9.4 and 11.8, x 4000 12.8 and 12.9; 256 heads x
+// 600 19.2 and 22.7, x 1200 36.1 and 36.9; heads of 1000 ... 8000 rows, 32 of them, 34.0 and 21.3, 4 x 8000 30.0 and 15.4: beyond 4096 a workgroup of 256 reads its
+// head again and again.  (With the expansion of what is left, 0.5 ... 5 us.)
 constexpr int kShortHead = 1024, kLongestHead = 4096;
 constexpr int kMostRows = 4096;   // of a workgroup's list
 
@@ -369,6 +369,8 @@ __global__ __launch_bounds__(256) void evict_kernel(const EvictParams prm) {
     list_rows_alone<256, 8>(w, n, k, lo, lo + rows, first, list);
   else if (n <= 256 * 4)
     list_rows<256, 4>(w, n, k, lo, lo + rows, first, list, bins, counts);
+  else if (n <= 256 * 8)
+    list_rows<256, 8>(w, n, k, lo, lo + rows, first, list, bins, counts);
   else if (n <= 256 * 16)
     list_rows<256, 16>(w, n, k, lo, lo + rows, first, list, bins, counts);
   else
@@ -396,6 +398,8 @@ __global__ __launch_bounds__(1024) void evict_rows_kernel(const EvictParams prm)
     list_rows<1024, 4>(w, n, k, 0, rows, first, list, bins, counts);
   else if (n <= 1024 * 8)
     list_rows<1024, 8>(w, n, k, 0, rows, first, list, bins, counts);
+  else if (n <= 1024 * 16)
+    list_rows<1024, 16>(w, n, k, 0, rows, first, list, bins, counts);
   else if (n <= 1024 * 32)
     list_rows<1024, 32>(w, n, k, 0, rows, first, list, bins, counts);
   else
