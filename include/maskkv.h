@@ -322,7 +322,8 @@ int maskkv_accumulate_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, c
  *   Kc_out[r'] = Kc[rows[r']], and V, weights_out[r'] = weights[rows[r']] and idx_out[r'] = idx[rows[r']] likewise
  *   cu_out     = exclusive prefix sum of the rows that stay, B*H+1 entries.
  * rows, idx, idx_out: DEVICE int32 [capacity_out], [capacity], [capacity_out]; idx and idx_out (the rows' prompt positions)
- * may both be NULL, and so may weights_out.  Where more than capacity_out rows stay, those beyond it are not written while
+ * may both be NULL, and so may weights_out; arrays of no rows (capacity or capacity_out 0) may be NULL too.  Where more than
+ * capacity_out rows stay, those beyond it are not written while
  * cu_out holds the unclipped sums; sum_h budgets[bh] and capacity are always enough.  The smaller cache has buffers
  * of its own: an output that overlaps an input is MASKKV_EINVAL.  P_max may not exceed 4 Mi tokens, as in maskkv_select.  _mx: the same
  * for a cache in 4 bits, whose bytes are moved as they are.

@@ -569,7 +569,9 @@ int maskkv_accumulate_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, c
 static int evict_entry(const char* what, const maskkv_desc* desc, const float* weights, const int32_t* cu_budget,
                        int64_t capacity, const int32_t* budgets, const MovedRows& moved, const int32_t* idx, int32_t* idx_out,
                        int32_t* rows, float* weights_out, int32_t* cu_out, int64_t capacity_out, void* stream) {
-  if (!cu_budget || !budgets || !cu_out || (capacity > 0 && !weights) || (capacity_out > 0 && !rows) || !idx != !idx_out) {
+  // (An empty array may have no address: positions are asked for on both sides or on neither only where both caches have room for rows.)
+  if (!cu_budget || !budgets || !cu_out || (capacity > 0 && !weights) || (capacity_out > 0 && !rows) ||
+      (capacity > 0 && capacity_out > 0 && !idx != !idx_out)) {
     set_error("%s: cu_budget, budgets, cu_out, weights or rows is NULL, or only one of idx and idx_out is", what);
     return MASKKV_EINVAL;
   }
