@@ -37,6 +37,7 @@ struct AccumulateParams {
   const int32_t* cu;
   int64_t capacity;
   int H, BH, q_per_kv, n_resp, n_q;
+  int groups;  // workgroups, a multiple of 8
   float c;  // scale * log2(e)
   float decay;
   const float *lse, *in;
@@ -67,11 +68,13 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   extern __shared__ __attribute__((aligned(16))) char acc_lds[];
   __shared__ float part[WAVES][kTile];
   typedef AccumulateParams A;
-  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_ARGUMENT(A, Kc), MASKKV_ARGUMENT(A, BH), (uint32_t)(offsetof(A, out) + 8)});
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_ARGUMENT(A, Kc), MASKKV_ARGUMENT(A, BH), MASKKV_ARGUMENT(A, out)});
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
   // Each XCD (workgroups whose numbers are congruent modulo 8) takes a run of units: a head's queries stay in one L2.
-  const int unit = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  const int group = group_number();
+  if (group >= prm.groups) return;
+  const int unit = group % 8 * (prm.groups / 8) + group / 8;
   const int capacity = (int)prm.capacity;
   const UnitHead head = head_of_unit(prm.cu, prm.BH, capacity, unit, [](int n) { return (int)(((uint32_t)n + kRows - 1) / kRows); });
   const int bh = head.bh;
@@ -251,11 +254,11 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
 }
 
 template <typename T, int D, bool MX, int WAVES, bool SHARE>
-int launch_form(const AccumulateParams& prm, hipStream_t stream) {
+int launch_form(AccumulateParams prm, hipStream_t stream) {
   using C = AccCfg<T, D, WAVES, SHARE>;
   static_assert(C::kLds + WAVES * kTile * 4 <= 160 * 1024, "a workgroup's LDS");
   const int rows = SHARE ? WAVES * kTile : kTile;
-  const int64_t groups = (prm.capacity / rows + prm.BH + 7) / 8 * 8;  // (each head's last ones may be short)
+  prm.groups = (int)((prm.capacity / rows + prm.BH + 7) / 8 * 8);  // (each head's last ones may be short)
   const auto kernel = accumulate_kernel<T, D, MX, WAVES, SHARE>;
   if (C::kLds > 48 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
@@ -265,7 +268,7 @@ int launch_form(const AccumulateParams& prm, hipStream_t stream) {
       return MASKKV_EHIP;
     }
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(WAVES * 64), C::kLds, stream, prm);
+  hipLaunchKernelGGL(kernel, grid_of(prm.groups), dim3(WAVES * 64), C::kLds, stream, prm);
   return check_launch("accumulate");
 }
 

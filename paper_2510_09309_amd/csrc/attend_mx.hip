@@ -1133,7 +1133,7 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
       lds = FewCfg<D>::kLds;
     }
   }
-  if (groups > 0x7FFFFFFF) {
+  if (groups * threads > 0xFFFFFFFF) {  // (threads of a launch along a dimension)
     set_error("attend_mx: %lld workgroups are more than a launch can have", (long long)groups);
     return MASKKV_ESHAPE;
   }

@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void compact_mx_kernel(const CompactMxPar
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int mine = 64 / pieces, piece = lane % pieces;
   const int capacity = (int)prm.capacity;
-  const int64_t first64 = ((int64_t)blockIdx.x * (kThreads / 64) + wave) * (mine * kRounds);  // of this wave
+  const int64_t first64 = ((int64_t)group_number() * (kThreads / 64) + wave) * (mine * kRounds);  // of this wave
   if (first64 >= capacity) return;
   const int first = (int)first64;
   int position[kRounds];
@@ -147,7 +147,7 @@ struct ExpandParams {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void expand_mx_kernel(const ExpandParams prm) {
   const int pieces = prm.d / 8;
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t i = (int64_t)group_number() * kThreads + threadIdx.x;
   if (i >= min((int64_t)prm.total[0], prm.capacity) * pieces) return;
   const uint32_t codes[2] = {reinterpret_cast<const uint32_t*>(prm.in.k_codes)[i], reinterpret_cast<const uint32_t*>(prm.in.v_codes)[i]};
   const uint32_t scales[2] = {reinterpret_cast<const uint8_t*>(prm.in.k_scales)[i / 4], reinterpret_cast<const uint8_t*>(prm.in.v_scales)[i / 4]};
@@ -184,7 +184,7 @@ int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, con
   prm.capacity = capacity;
   prm.out = cache;
   const int rows = kRounds * kThreads / (d->d * (d->dtype == MASKKV_BF16 ? 2 : 4) / 16);  // of a workgroup
-  const dim3 grid((unsigned)((capacity + rows - 1) / rows));
+  const dim3 grid = grid_of((capacity + rows - 1) / rows);
   // (89 k rows of 2.1 GB of prompt: 15.0 us past the cache, 16.8 through it, and 12.9 through it where just these rows were there)
   const bool bf16 = d->dtype == MASKKV_BF16, once = 2ll * prm.BH * d->P_max * d->d * (bf16 ? 2 : 4) > kSideCache;
   const auto kernel = bf16 ? once ? compact_mx_kernel<bf16_t, true> : compact_mx_kernel<bf16_t, false>
@@ -203,7 +203,7 @@ int launch_expand_mx(const maskkv_desc* d, const MxCache& cache, const int32_t* 
   prm.d = d->d;
   prm.Kc = reinterpret_cast<char*>(Kc);
   prm.Vc = reinterpret_cast<char*>(Vc);
-  const dim3 grid((unsigned)((capacity * (d->d / 8) + kThreads - 1) / kThreads));
+  const dim3 grid = grid_of((capacity * (d->d / 8) + kThreads - 1) / kThreads);
   if (d->dtype == MASKKV_BF16)
     hipLaunchKernelGGL(expand_mx_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, prm);
   else

@@ -14,6 +14,14 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kMxGroup = 32;
+
+// A launch has fewer than 2^32 threads along a dimension; a workgroup for every few rows of a cache may be more: those beyond
+// 2^20 go on along the second dimension, and the last ones may lie behind the last row.
+constexpr int kGridBits = 20;
+inline dim3 grid_of(int64_t groups) {
+  return groups <= 1 << kGridBits ? dim3((unsigned)groups) : dim3(1u << kGridBits, (unsigned)((groups + (1 << kGridBits) - 1) >> kGridBits));
+}
+__device__ __forceinline__ uint32_t group_number() { return blockIdx.x + (blockIdx.y << kGridBits); }
 constexpr uint32_t kMxLeast = 3, kMxMost = 252, kMxNan = 255;
 
 // The scale byte of a group from the largest of its elements' magnitudes (their bits as fp32): the smallest 2^e with most <= 6 * 2^e.
