@@ -227,6 +227,14 @@ int score_plan(const maskkv_desc* desc, SweepPlan* plan, RowsSplit* split) {
   return MASKKV_OK;
 }
 
+int attend_mx_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendMxPlan* plan) {
+  Lens lens;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("attend_mx", "capacity", capacity)) return e;
+  *plan = attend_mx_plan(desc, capacity);
+  return MASKKV_OK;
+}
+
 }  // namespace maskkv
 
 using namespace maskkv;

@@ -1158,6 +1158,12 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
 
 }  // namespace
 
+AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity) {
+  const Deal x = deal_of(d, capacity);
+  const int64_t BH = (int64_t)d->B * d->H;
+  return {x.tile_rows, x.qtiles, x.chunk, x.units, x.wide && !x.chunk && BH <= kRanked, x.chunk && x.units > kSharedUnits * BH};
+}
+
 size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
   if (!x.chunk) return 0;

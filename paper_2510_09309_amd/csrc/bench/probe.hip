@@ -5,7 +5,8 @@
 //                              of maskkv_score inside libmaskkv.so);
 //   maskkv_bench_hold_sweep    makes maskkv_score take its fallback.
 //   maskkv_bench_score_plan    how maskkv_score would score a description;
-//   maskkv_bench_score_split   whether it would deal out rows and keys of a short fp32 prompt.
+//   maskkv_bench_score_split   whether it would deal out rows and keys of a short fp32 prompt;
+//   maskkv_bench_attend_mx_plan   how maskkv_attend_mx would deal a cache out.
 #include <stdio.h>
 
 #include "../kernels.hpp"
@@ -363,6 +364,14 @@ int maskkv_bench_score_split(const maskkv_desc* desc, int32_t* split) {
   split[0] = s.groups;
   split[1] = s.part_keys;
   split[2] = s.parts;
+  return MASKKV_OK;
+}
+
+int maskkv_bench_attend_mx_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan) {
+  AttendMxPlan p;
+  if (int e = attend_mx_plan_entry(desc, capacity, &p)) return e;
+  const int64_t v[6] = {p.tile_rows, p.qtiles, p.chunk, p.units, p.ranked, p.shared};
+  for (int i = 0; i < 6; ++i) plan[i] = v[i];
   return MASKKV_OK;
 }
 

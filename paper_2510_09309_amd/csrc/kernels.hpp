@@ -102,7 +102,16 @@ int launch_compact_mx(const maskkv_desc* d, const Lens& lens, const View& K, con
 int launch_expand_mx(const maskkv_desc* d, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, void* Kc, void* Vc,
                      hipStream_t stream);
 
-// attend_mx.hip
+// attend_mx.hip.  How a description and capacity are dealt out (see deal_of).
+struct AttendMxPlan {
+  int tile_rows;  // query rows of a workgroup: 16, 32 or 128, which of the kernels
+  int qtiles;     // workgroups of a unit
+  int chunk;      // tiles of a unit, or 0: a unit is a head
+  int64_t units;  // at most
+  bool ranked;    // heads are taken in the order of their lengths
+  bool shared;    // partial results of a row are joined by a whole workgroup
+};
+AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity);
 size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity);
 int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,
                      const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream);
@@ -137,5 +146,6 @@ int score_entry(const maskkv_desc* desc, const maskkv_tensor* Q_mask, const mask
                 void* stream, void* const* events);
 // The plan that it makes for a description, and whether it deals out rows and keys instead.
 int score_plan(const maskkv_desc* desc, SweepPlan* plan, RowsSplit* split);
+int attend_mx_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendMxPlan* plan);
 
 }  // namespace maskkv
