@@ -281,7 +281,8 @@ int maskkv_expand_mx(const maskkv_desc* desc, const maskkv_mx_cache* cache, cons
                      void* Kc, void* Vc, void* stream);
 
 /* Workspace (DEVICE bytes) for maskkv_attend_mx with this description and capacity: partial results where few query rows
- * attend to many rows and the key axis is dealt to several workgroups; 0 where it is not.  256-byte alignment.  Nothing in it has to
+ * attend to many rows and the key axis is dealt to several workgroups; 0 where it is not.  256-byte alignment.  It is enough for every
+ * smaller capacity too: a program that goes on evicting keeps the workspace of its first cache.  Nothing in it has to
  * be set before a call or outlives one; calls that may run at the same time (two streams, two captured graphs) need one each. */
 int maskkv_attend_mx_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes);
 

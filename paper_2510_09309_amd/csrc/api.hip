@@ -526,7 +526,7 @@ int maskkv_attend_mx(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const
     return MASKKV_EINVAL;
   }
   if (int e = check_mx("attend_mx", "cache", cache, capacity, false, &mx)) return e;
-  if (int e = check_workspace("attend_mx", workspace, workspace_bytes, attend_mx_workspace_bytes(desc, capacity))) return e;
+  if (int e = check_workspace("attend_mx", workspace, workspace_bytes, attend_mx_needs(desc, capacity))) return e;
   return launch_attend_mx(desc, q, mx, cu_budget, capacity, k2, v2, pick_scale(desc, scale), o, lse, workspace,
                           reinterpret_cast<hipStream_t>(stream));
 }

@@ -1057,7 +1057,16 @@ constexpr float kJoin = 4.3f;      // the second kernel
 constexpr float kUneven = 1.15f;   // a launch of whole heads waits for the longest ones: by so much on average (1 ... 1.3 choose about as well)
 constexpr float kLongest = 400.f;  // whole heads: what one may take that has all the rows there are
 
-Deal deal_of(const maskkv_desc* d, int64_t capacity) {
+// Capacities are planned for in steps of a sixteenth of the power of two below (up to 6 % more rows than there are; the units past the last
+// head end at once): so few different plans can be looked over for the workspace of all smaller capacities.
+int64_t planned(int64_t capacity) {
+  int64_t step = 1;
+  while (step * 32 <= capacity) step *= 2;
+  return (capacity + step - 1) / step * step;
+}
+
+Deal deal_of(const maskkv_desc* d, int64_t room) {
+  const int64_t capacity = planned(room);
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
   const bool bf16 = d->dtype == MASKKV_BF16;
@@ -1164,11 +1173,24 @@ AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity) {
   return {x.tile_rows, x.qtiles, x.chunk, x.units, x.wide && !x.chunk && BH <= kRanked, x.chunk && x.units > kSharedUnits * BH};
 }
 
-size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
+size_t attend_mx_needs(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
   if (!x.chunk) return 0;
   const size_t rows = (size_t)x.units * x.qtiles * x.part_rows;
   return pad256(rows * d->d * 4) + pad256(rows * 8) + pad256((size_t)d->B * d->H * 8);
+}
+
+// The most that any capacity up to this one needs: fewer rows may be dealt out finer.  (A cache that shrinks keeps its workspace.)
+size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
+  size_t most = 0;
+  for (int64_t rows = planned(capacity);;) {
+    const size_t bytes = attend_mx_needs(d, rows);
+    most = bytes > most ? bytes : most;
+    if (rows == 0) return most;
+    int64_t step = 1;
+    while (step * 32 < rows) step *= 2;
+    rows -= step;
+  }
 }
 
 int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,

@@ -112,7 +112,8 @@ struct AttendMxPlan {
   bool shared;    // partial results of a row are joined by a whole workgroup
 };
 AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity);
-size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity);
+size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity);  // of this capacity and of all smaller ones
+size_t attend_mx_needs(const maskkv_desc* d, int64_t capacity);            // of this one
 int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,
                      const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream);
 

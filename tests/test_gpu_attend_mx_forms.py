@@ -59,9 +59,9 @@ def test_128_query_rows_a_workgroup_and_more_heads_than_are_ordered(d):
     run(Case(41, 1, 257, d, "bf16", 130, lengths(41, 257, 0, 100, h0=300, h256=299)), 128, False, heads=[0, 1, 64, 255, 256])
 
 
-@pytest.mark.parametrize("d,heads,n,lo,hi,shared", [(64, 32, 384, 3000, 5600, False), (128, 12, 512, 6000, 9000, False), (128, 4, 512, 23000, 24001, True)])
+@pytest.mark.parametrize("d,heads,n,lo,hi,shared", [(64, 32, 384, 3000, 5600, False), (128, 12, 512, 6000, 9000, False), (128, 3, 512, 33000, 34001, True)])
 def test_128_query_rows_a_workgroup_with_the_keys_dealt_out(d, heads, n, lo, hi, shared):
-    run(Case(heads + d, 1, heads, d, "bf16", n, lengths(42, heads, lo, hi, h1=0 if heads > 4 else 22001)), 128, True, shared=shared,
+    run(Case(heads + d, 1, heads, d, "bf16", n, lengths(42, heads, lo, hi, h1=0 if heads > 4 else 32001)), 128, True, shared=shared,
         heads=[0, 1, heads - 1])
 
 
