@@ -104,8 +104,6 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return plus_dpp<0x143, 0xc>(v);
 }
 
-// The head of a unit of work when a head of n cached rows has units_of(n) units (bh -1: behind the last), which is its first and how
-// many it has, and where its rows lie.  Found by a wave, which asks for 256 heads at a time and counts 64.
 // Rows that are read once: those of an array larger than the memory-side cache come from HBM, and go past the cache.
 constexpr int64_t kSideCache = 256 << 20;
 template <bool ONCE>
@@ -117,6 +115,8 @@ __device__ __forceinline__ u32x4 read_piece(const char* from) {
     return *p;
 }
 
+// The head of a unit of work when a head of n cached rows has units_of(n) units (bh -1: behind the last), which is its first and how
+// many it has, and where its rows lie.  Found by a wave, which asks for 256 heads at a time and counts 64.
 struct UnitHead {
   int bh, first_unit, units;
   int first, rows;
