@@ -280,8 +280,9 @@ int maskkv_compact_mx(const maskkv_desc* desc, const maskkv_tensor* K, const mas
 int maskkv_expand_mx(const maskkv_desc* desc, const maskkv_mx_cache* cache, const int32_t* cu_budget, int64_t capacity,
                      void* Kc, void* Vc, void* stream);
 
-/* Workspace (DEVICE bytes) for maskkv_attend_mx with this description and capacity: partial results where few query rows
- * attend to many rows and the key axis is dealt to several workgroups; 0 where it is not.  256-byte alignment.  It is enough for every
+/* Workspace (DEVICE bytes) for maskkv_attend_mx with this description and capacity: partial results where the rows of a
+ * head go to several workgroups: where few query rows attend to many rows, or where P_max and capacity leave room for a head that would
+ * keep one workgroup busy for long; 0 where they do not.  256-byte alignment.  It is enough for every
  * smaller capacity too: a program that goes on evicting keeps the workspace of its first cache.  Nothing in it has to
  * be set before a call or outlives one; calls that may run at the same time (two streams, two captured graphs) need one each. */
 int maskkv_attend_mx_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes);

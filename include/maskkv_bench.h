@@ -88,10 +88,11 @@ int maskkv_bench_score_plan(const maskkv_desc* desc, int32_t* plan);
 int maskkv_bench_score_split(const maskkv_desc* desc, int32_t* split);
 
 /*
- * How maskkv_attend_mx would deal out a description and capacity.  plan: HOST array of 6:
+ * How maskkv_attend_mx would deal out a description and capacity.  plan: HOST array of 8:
  *   [0] query rows of a workgroup: 16, 32 or 128, a kernel each; [1] workgroups of a unit; [2] tiles of keys (64 at 128 rows, else 32) of a unit,
  *   or 0: a unit is a head; [3] units, at most; [4] 1: heads are taken in the order of their lengths; [5] 1: the partial results of a
- *   query row are joined by a workgroup of its own.
+ *   query row are joined by a workgroup of its own; [6] not 0: only heads of more tiles than [2] are cut, and what is left of them are so many
+ *   units, at most; [7] how many heads that may be.
  * Enqueues nothing.  Errors are reported through maskkv_last_error() of libmaskkv.so.
  */
 int maskkv_bench_attend_mx_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan);

@@ -98,10 +98,12 @@ class AttendMxPlan(NamedTuple):
     units: int
     ranked: int
     shared: int
+    extras: int
+    cut: int
 
 
 def maskkv_bench_attend_mx_plan(desc: "_b.Desc", capacity: int) -> AttendMxPlan:
-    plan = (ct.c_int64 * 6)()
+    plan = (ct.c_int64 * 8)()
     _b._check(_lib.maskkv_bench_attend_mx_plan(ct.byref(desc.c()), ct.c_int64(capacity), plan), "maskkv_bench_attend_mx_plan")
     return AttendMxPlan(*plan)
 

@@ -15,7 +15,7 @@
 // Probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product: fp32 operands have a sixteenth of its rate.
 // The sum that divides them is of the unrounded ones.  Partial results are fp32.
 //
-// Where the keys are dealt out, a second kernel joins the partial results: in the same launch it would take a counter that is zero
+// Where the keys are dealt out, or only those of long heads, a second kernel joins the partial results: in the same launch it would take a counter that is zero
 // when the call begins, and a workspace need not be.
 //
 // Bound by latency where there is little to do: 32 heads x 256 queries x 250 + 256 rows, head_dim 128, 10.1 us, of which 6.5 are the launch, the
@@ -44,13 +44,14 @@ struct AttendMxParams {
   int H, BH, q_per_kv, n_resp, n_q, qtiles;
   int units;      // at most
   int chunk;      // tiles of a workgroup, or 0: all of its head
+  int extras;     // (see Work) or 0
   int tile_rows;  // query rows of a workgroup
   int part_rows;  // of a partial result
   float c;        // scale * log2(e)
   float* lse;
-  float* part_o;    // [units * qtiles][part_rows][D]
-  float2* part_ml;  // [units * qtiles][part_rows]
-  int2* parts;      // [BH] a head's first unit, and how many it has
+  float* part_o;    // [places * qtiles][part_rows][D], a place a unit (with extras: see Work)
+  float2* part_ml;  // [places * qtiles][part_rows]
+  int2* parts;      // [BH] a head's first unit, and how many it has (with extras: not used)
 };
 
 __device__ __forceinline__ void fetch_attend_mx_arguments() {
@@ -679,6 +680,59 @@ __device__ __forceinline__ UnitHead head_of_rank(const int32_t* cu, int BH, int 
   return x;
 }
 
+// What a unit is: tiles t0 .. t1 - 1 of a head, and the place of its partial result where the head has several units.  Three ways:
+//   no chunk         a unit is a head, by rank up to kRanked of them;
+//   chunk            units of so many tiles, head after head, a place each;
+//   chunk, extras    (up to kRanked heads) units of what is left of the heads behind their first `chunk` tiles, which take longest, head after
+//                    head, as many as there are; then each head's first tiles, which is all of most, by rank.  Places: `extras` for the
+//                    former, then one for the first tiles of each head that is cut.  (The units that there may be, but are not, come last: in front
+//                    of 1024 workgroups 124 of them cost 5 us, as the heads' order then is not that of the compute units.)
+// False: a unit behind the last one.
+struct Work {
+  UnitHead head;
+  int t0, t1, place;
+};
+__device__ __forceinline__ int units_of_tiles(int tiles, int chunk) { return (tiles + chunk - 1) / chunk; }
+template <typename F>
+__device__ __forceinline__ bool work_of(const AttendMxParams& prm, int unit, int qtile, F tiles_of, Work& w) {
+  const int capacity = (int)prm.capacity;
+  int part = 0;
+  w.place = unit;
+  if (prm.chunk && !prm.extras) {
+    w.head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return units_of_tiles(tiles_of(rows), prm.chunk); });
+    if (w.head.bh < 0) return false;
+    part = unit - w.head.first_unit;
+    if (part == 0 && qtile == 0 && threadIdx.x == 0) prm.parts[w.head.bh] = make_int2(unit, w.head.units);
+  } else {
+    int others = 0;  // units of what is left
+    if (prm.extras) {
+      w.head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return units_of_tiles(tiles_of(rows), prm.chunk) - 1; });
+      others = w.head.first_unit;
+      part = unit - others + 1;
+      w.head.units += 1;
+    }
+    if (!prm.extras || w.head.bh < 0) {
+      part = 0;
+      const int i = unit - others;
+      if (i >= prm.BH) return false;
+      if (prm.BH <= kRanked) {
+        w.head = head_of_rank(prm.cu, prm.BH, capacity, i, tiles_of);
+      } else {
+        const int first = min(prm.cu[i], capacity);
+        w.head = {i, i, 1, first, max(min(prm.cu[i + 1], capacity) - first, 0)};
+      }
+      if (prm.extras && tiles_of(w.head.rows) > prm.chunk) {
+        w.head.units = units_of_tiles(tiles_of(w.head.rows), prm.chunk);
+        w.place = prm.extras + sum_before(prm.cu, w.head.bh, capacity, [&](int rows) { return tiles_of(rows) > prm.chunk ? 1 : 0; });
+      }
+    }
+  }
+  const int tiles = tiles_of(w.head.rows);
+  w.t0 = part * prm.chunk;
+  w.t1 = prm.chunk ? min(tiles, w.t0 + prm.chunk) : tiles;
+  return true;
+}
+
 template <int D>
 __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxParams prm) {
   using C = WideCfg<D>;
@@ -687,25 +741,14 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
   const int unit = place.unit, qtile = place.qtile;
   const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
-  const int capacity = (int)prm.capacity;
   auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kWideTile - 1) / kWideTile) + resp_tiles; };  // those of the response first
-  UnitHead head;
-  if (prm.chunk) {
-    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
-    if (head.bh < 0) return;
-  } else if (prm.BH <= kRanked) {
-    head = head_of_rank(prm.cu, prm.BH, capacity, unit, tiles_of);
-  } else {
-    const int first = min(prm.cu[unit], capacity);
-    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
-  }
-  const int bh = head.bh, first = head.first, cached = head.rows;
+  Work work;
+  if (!work_of(prm, unit, qtile, tiles_of, work)) return;
+  const UnitHead& head = work.head;
+  const int bh = head.bh, first = head.first, cached = head.rows, t0 = work.t0, tiles = work.t1;  // this workgroup's: t0 .. tiles - 1
   const int b = bh / prm.H, h = bh % prm.H;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
-  if (prm.chunk && unit == head.first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, head.units);
-  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
-  const int tiles = prm.chunk ? min(tiles_of(cached), t0 + prm.chunk) : tiles_of(cached);  // this workgroup's: t0 .. tiles - 1
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)mx_lds;
 
   // ---- tiles on their way.  Of the cache a thread takes a quarter of a row; of the response a wave takes a quarter of the rows.
@@ -917,7 +960,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_wide_kernel(const AttendMxPa
   l = sum_halves(l);
   if (head.units > 1) {
     if (q0 + r >= prm.n_q) return;
-    const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + wave * 32 + r;
+    const int64_t part = ((int64_t)work.place * prm.qtiles + qtile) * prm.part_rows + wave * 32 + r;
 #pragma unroll
     for (int db = 0; db < C::kDB; ++db)
 #pragma unroll
@@ -958,10 +1001,23 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_mx_join_kernel(con
   fetch_attend_mx_arguments();
   const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer;
   const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
-  const int bh = blockIdx.y, q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
-  const int first = prm.parts[bh].x, units = prm.parts[bh].y;
+  const int q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
+  int bh = blockIdx.y, units, first, first_place;  // places of a head's units: first_place, first + 1, first + 2, ...
+  if (SHARED || !prm.extras) {
+    first_place = first = prm.parts[bh].x;
+    units = prm.parts[bh].y;
+  } else {  // the head of that number among the ones that are cut
+    const int capacity = (int)prm.capacity, resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
+    auto units_of = [&](int rows) { return units_of_tiles((int)(((uint32_t)rows + kWideTile - 1) / kWideTile) + resp_tiles, prm.chunk); };
+    const UnitHead head = head_of_unit(prm.cu, prm.BH, capacity, bh, [&](int rows) { return units_of(rows) > 1 ? 1 : 0; });
+    if (head.bh < 0) return;
+    first_place = prm.extras + bh;
+    bh = head.bh;
+    units = units_of(head.rows);
+    first = sum_before(prm.cu, bh, capacity, [&](int rows) { return units_of(rows) - 1; }) - 1;
+  }
   if (units <= 1 || q >= prm.n_q) return;
-  const int64_t part0 = first * step + (int64_t)(q / prm.tile_rows) * prm.part_rows + q % prm.tile_rows;
+  const int64_t in_unit = (int64_t)(q / prm.tile_rows) * prm.part_rows + q % prm.tile_rows;
   float m = kNegBig, l = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int u0 = SHARED ? grp : 0; u0 < units; u0 += kAtOnce * kStep) {
@@ -972,7 +1028,8 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_mx_join_kernel(con
       ml[i] = make_float2(kNegBig, 0.f);
       y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (u0 + i * kStep < units) {
-        const int64_t part = part0 + (u0 + i * kStep) * step;
+        const int u = u0 + i * kStep;
+        const int64_t part = (u ? first + u : first_place) * step + in_unit;
         ml[i] = prm.part_ml[part];
         y[i] = *reinterpret_cast<const float4*>(prm.part_o + part * D + at * 4);
       }
@@ -1024,7 +1081,10 @@ struct Deal {
   bool wide;      // 128 query rows a workgroup
   int tile_rows, qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
+  int extras;     // (see Work) or 0
+  int cut;        // heads of more than `chunk` tiles, at most, where there are extras
   int64_t units;  // at most
+  int64_t places() const { return extras ? extras + cut : units; }  // of partial results
 };
 // Units of a head on average above which a query row's partial results are read by a whole workgroup instead of an eighth of one: 59 units 11.4 and
 // 16.1 us a call, 32 11.4 and 12.6; 8 units 15.0 and 14.1.
@@ -1055,7 +1115,10 @@ constexpr Form kWide = {kWideQueries, kWideTile, 1, 2, 2, 7.f, 0.f, 0.4f, 0.9f, 
 constexpr Form kNarrowF32 = {kTile, kTile, kWaves, 4, 1, 2.f, 3.f, 0.f, 5.5f, 1.f, 0.8f, 1.15f};
 constexpr float kJoin = 4.3f;      // the second kernel
 constexpr float kUneven = 1.15f;   // a launch of whole heads waits for the longest ones: by so much on average (1 ... 1.3 choose about as well)
-constexpr float kLongest = 400.f;  // whole heads: what one may take that has all the rows there are
+// Whole heads: what one may take that has all the rows of the longest prompt.  Beyond, the keys are dealt out, though most heads may be short; in the kernel of 128
+// rows only heads are cut that take longer than the launch is expected to.  Both sides, 8 x 32 heads x 512 queries: 64 ... 1024 rows of each, whole
+// 77.5 us, to be cut 82.2 (a second launch, which finds nothing to join), dealt out 96.9; with 18000 rows in one of them 367, 110 and 109 ... 114.
+constexpr float kLongest = 400.f;
 
 // Capacities are planned for in steps of a sixteenth of the power of two below (up to 6 % more rows than there are; the units past the last
 // head end at once): so few different plans can be looked over for the workspace of all smaller capacities.
@@ -1084,7 +1147,7 @@ Deal deal_of(const maskkv_desc* d, int64_t room) {
       const float a_step = rounds <= 1.f ? step : step * (f.at_once == 1 ? (rounds < 3.f ? ceilf(rounds) : rounds) : f.beside * fmaxf(rounds, 2.f));
       return f.start + f.round * fmaxf(rounds, 1.f) + ceilf(steps) * a_step;
     };
-    auto take = [&](float cost, int chunk) {
+    auto take = [&](float cost, int chunk, int extras = 0, int cut = 0) {
       if (best_cost >= 0.f && cost >= best_cost) return;
       best_cost = cost;
       best.few = &f == &kFew;
@@ -1093,11 +1156,23 @@ Deal deal_of(const maskkv_desc* d, int64_t room) {
       best.qtiles = qtiles;
       best.part_rows = n_q < f.tile_rows ? n_q : f.tile_rows;
       best.chunk = chunk;
-      best.units = chunk ? (capacity / f.keys + BH * (resp + 1)) / chunk + BH : BH;
+      best.extras = extras;
+      best.cut = cut;
+      best.units = extras ? extras + BH : chunk ? (capacity / f.keys + BH * (resp + 1)) / chunk + BH : BH;
     };
     const float whole = cost((float)BH, mean * (BH * qtiles <= kUnits ? f.uneven : kUneven) / f.tiles);
     const bool fits = step * ((float)most / (f.keys * f.tiles)) <= kLongest;
     if (fits) take(whole, 0);
+    // (The other kernels, and more heads than are ordered, are better off with all heads dealt out: 512 heads x 16 queries x 100 ... 1000 rows and one of 40000
+    // 23.5 and 21.6 us, 130 x 64 x 100 ... 2000 33.9 and 23.4, 400 x 300 x 50 ... 400 85.3 and 79.5; where none is long -4 ... 15 us.)
+    if (const int64_t chunk = (int64_t)ceilf(whole / step) * f.tiles; !fits && &f == &kWide && BH <= kRanked && chunk >= 2 * mean) {  // (else most are cut)
+      // A head that is cut has more than chunk - resp tiles of the cache, and a unit for every `chunk` tiles, or part of them, behind its first.
+      const int64_t cached = capacity / f.keys + BH, most_cut = cached / (chunk + 1 - resp), cut = most_cut < BH ? most_cut : BH;
+      if (cut == 0)
+        take(whole, 0);  // (there is no room for a head that long)
+      else
+        take(whole + kJoin, (int)chunk, (int)((cached + cut * (resp - 1)) / chunk), (int)cut);
+    }
     auto dealt = [&](float wanted) {
       int64_t chunk = (int64_t)fmaxf(ceilf(wanted), (float)f.least);
       chunk = (chunk + f.tiles - 1) / f.tiles * f.tiles;
@@ -1157,7 +1232,10 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, stream, prm);
   if (int e = check_launch("attend_mx")) return e;
   if (!deal.chunk) return MASKKV_OK;
-  if (deal.units > (int64_t)kSharedUnits * prm.BH)
+  if (deal.extras)
+    hipLaunchKernelGGL((attend_mx_join_kernel<T, D, false>), dim3((unsigned)(prm.n_q + kJoinGroups - 1) / kJoinGroups, (unsigned)deal.cut),
+                       dim3(kJoinGroups * D / 4), 0, stream, prm);
+  else if (deal.units > (int64_t)kSharedUnits * prm.BH)
     hipLaunchKernelGGL((attend_mx_join_kernel<T, D, true>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(kJoinGroups * D / 4), 0, stream, prm);
   else
     hipLaunchKernelGGL((attend_mx_join_kernel<T, D, false>), dim3((unsigned)(prm.n_q + kJoinGroups - 1) / kJoinGroups, (unsigned)prm.BH),
@@ -1170,14 +1248,15 @@ int launch_one(const AttendMxParams& prm, const Deal& deal, hipStream_t stream) 
 AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
   const int64_t BH = (int64_t)d->B * d->H;
-  return {x.tile_rows, x.qtiles, x.chunk, x.units, x.wide && !x.chunk && BH <= kRanked, x.chunk && x.units > kSharedUnits * BH};
+  return {x.tile_rows, x.qtiles, x.chunk, x.units, x.wide && (!x.chunk || x.extras) && BH <= kRanked, x.chunk && !x.extras && x.units > kSharedUnits * BH,
+          x.extras, x.cut};
 }
 
 size_t attend_mx_needs(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
   if (!x.chunk) return 0;
-  const size_t rows = (size_t)x.units * x.qtiles * x.part_rows;
-  return pad256(rows * d->d * 4) + pad256(rows * 8) + pad256((size_t)d->B * d->H * 8);
+  const size_t rows = (size_t)x.places() * x.qtiles * x.part_rows;
+  return pad256(rows * d->d * 4) + pad256(rows * 8) + (x.extras ? 0 : pad256((size_t)d->B * d->H * 8));
 }
 
 // The most that any capacity up to this one needs: fewer rows may be dealt out finer.  (A cache that shrinks keeps its workspace.)
@@ -1212,11 +1291,12 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
   prm.qtiles = deal.qtiles;
   prm.units = (int)deal.units;
   prm.chunk = deal.chunk;
+  prm.extras = deal.extras;
   prm.tile_rows = deal.tile_rows;
   prm.part_rows = deal.part_rows;
   prm.c = scale * kLog2e;
   prm.lse = lse;
-  const size_t rows = (size_t)deal.units * deal.qtiles * deal.part_rows;
+  const size_t rows = (size_t)deal.places() * deal.qtiles * deal.part_rows;
   char* ws = reinterpret_cast<char*>(workspace);
   prm.part_o = reinterpret_cast<float*>(ws);
   prm.part_ml = reinterpret_cast<float2*>(ws + pad256(rows * d->d * 4));

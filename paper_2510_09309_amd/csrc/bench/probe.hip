@@ -370,8 +370,8 @@ int maskkv_bench_score_split(const maskkv_desc* desc, int32_t* split) {
 int maskkv_bench_attend_mx_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan) {
   AttendMxPlan p;
   if (int e = attend_mx_plan_entry(desc, capacity, &p)) return e;
-  const int64_t v[6] = {p.tile_rows, p.qtiles, p.chunk, p.units, p.ranked, p.shared};
-  for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  const int64_t v[8] = {p.tile_rows, p.qtiles, p.chunk, p.units, p.ranked, p.shared, p.extras, p.cut};
+  for (int i = 0; i < 8; ++i) plan[i] = v[i];
   return MASKKV_OK;
 }
 

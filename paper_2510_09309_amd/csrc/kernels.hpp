@@ -110,6 +110,8 @@ struct AttendMxPlan {
   int64_t units;  // at most
   bool ranked;    // heads are taken in the order of their lengths
   bool shared;    // partial results of a row are joined by a whole workgroup
+  int extras;     // not 0: only heads of more than `chunk` tiles are cut, and what is left of them are so many units at most
+  int cut;        // how many heads that may be
 };
 AttendMxPlan attend_mx_plan(const maskkv_desc* d, int64_t capacity);
 size_t attend_mx_workspace_bytes(const maskkv_desc* d, int64_t capacity);  // of this capacity and of all smaller ones

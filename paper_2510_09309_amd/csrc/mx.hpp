@@ -115,8 +115,8 @@ __device__ __forceinline__ u32x4 read_piece(const char* from) {
     return *p;
 }
 
-// The head of a unit of work when a head of n cached rows has units_of(n) units (bh -1: behind the last), which is its first and how
-// many it has, and where its rows lie.  Found by a wave, which asks for 256 heads at a time and counts 64.
+// The head of a unit of work when a head of n cached rows has units_of(n) units, which is its first and how many it has, and where its rows
+// lie (behind the last one: bh -1, and all heads' units before `first_unit`).  Found by a wave, which asks for 256 heads at a time and counts 64.
 struct UnitHead {
   int bh, first_unit, units;
   int first, rows;
@@ -154,7 +154,20 @@ __device__ __forceinline__ UnitHead head_of_unit(const int32_t* cu, int BH, int 
       before += __builtin_amdgcn_readlane(upto, 63);
     }
   }
+  x.first_unit = before;
   return x;
+}
+
+// The sum of units_of(rows) over the heads before one; found by a wave.
+template <typename F>
+__device__ __forceinline__ int sum_before(const int32_t* cu, int bh, int capacity, F units_of) {
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int base = 0; base < bh; base += 64) {
+    const int i = min(base + lane, bh - 1), first = min(cu[i], capacity), rows = max(min(cu[i + 1], capacity) - first, 0);
+    before += __builtin_amdgcn_readlane(wave_prefix(base + lane < bh ? units_of(rows) : 0), 63);
+  }
+  return before;
 }
 
 }  // namespace maskkv
