@@ -81,3 +81,80 @@ def test_accumulating_over_rows_whose_threads_pass_32_bits():
         mh.check_weights(got, Q[0, i], mh.stored(K), lse[i].astype(np.float64), 0.0, None, tag=f"head {i}")
     for a, z in ((cu[1], cu[1] + 1000), (cu[2] - 1000, cu[2])):                           # keys of zeros: exp(-2) each
         assert np.abs(out[a:z].double().cpu().numpy() - np.exp(-2.0)).max() < 1e-6
+
+
+class FarCache:
+    """Rows of 128 in 4 bits, 4.5 GB of codes: one head of 70 million rows of zeros but for a few, the last ones among them, and one of
+    300 rows behind them, which all lie beyond the range of 32-bit byte offsets."""
+
+    def __init__(self, seed, d=128, rows=70_000_000):
+        m, rng = hp.mk(), np.random.default_rng(seed)
+        self.d, self.first, self.last = d, rows, 300
+        self.total = rows + self.last
+        self.cache = m.MxCache.empty(self.total, d)
+        for t in (self.cache.k_codes, self.cache.v_codes):
+            t.zero_()
+        for t in (self.cache.k_scales, self.cache.v_scales):
+            t.fill_(127)
+        self.at = np.concatenate((np.sort(rng.choice(rows, 20, replace=False)), np.arange(rows - 5, rows)))   # of the first head
+        self.K, self.V = (mh.gauss(rng, len(self.at) + self.last, d) for _ in range(2))
+        self.K[:len(self.at), 0] = 96.0                        # far above the zeros for queries with an 8 there: e^68 to one
+        where = mh.device(np.concatenate((self.at, np.arange(rows, self.total))))
+        for x, codes, scales in ((self.K, self.cache.k_codes, self.cache.k_scales), (self.V, self.cache.v_codes, self.cache.v_scales)):
+            c, s = mxo.store(x)
+            codes[where], scales[where] = mh.device(c), mh.device(s)
+        self.K, self.V = mh.stored(self.K), mh.stored(self.V)
+        self.cu = mh.prefix([rows, self.last])
+
+    def heads(self):
+        n = len(self.at)
+        return (self.K[:n], self.V[:n]), (self.K[n:], self.V[n:])
+
+
+@pytest.mark.parametrize("d,dtype,n,rows", [(128, "bf16", 1, 16), (128, "bf16", 40, 32), (128, "bf16", 200, 128), (128, "f32", 3, 32), (64, "bf16", 2, 16)])
+def test_attention_over_rows_beyond_four_gibibytes(d, dtype, n, rows):
+    from paper_2510_09309_amd import bench_binding as bb
+    needs(40)
+    m, rng = hp.mk(), np.random.default_rng(n)
+    far = FarCache(n, d, 70_000_000 * 128 // d)
+    desc = mh.desc(1, 2, d, dtype, n, 1 << 29)
+    assert bb.maskkv_bench_attend_mx_plan(desc, far.total).tile_rows == rows
+    Q, Kr, Vr = (mh.gauss(rng, 1, 2, n, d, dtype=dtype) for _ in range(3))
+    Q[..., 0] = 8.0
+    up = lambda x: hp.upload(x, dtype)
+    O, lse = torch.zeros(1, 2, n, d, dtype=hp.torch_dtype(dtype), device="cuda"), torch.zeros(2 * n, device="cuda")
+    m.maskkv_attend_mx(desc, up(Q), far.cache, mh.device(far.cu), far.total, up(Kr), up(Vr), 0.0, O, lse,
+                       hp.workspace(m.maskkv_attend_mx_workspace_bytes(desc, far.total)))
+    torch.cuda.synchronize()
+    for h, (K, V) in enumerate(far.heads()):
+        mh.check_attention(O[0, h].double().cpu().numpy(), lse.view(2, n)[h].double().cpu().numpy(), Q[0, h], np.concatenate((K, Kr[0, h])),
+                           np.concatenate((V, Vr[0, h])), dtype, tag=f"head {h}")
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 1), ("bf16", 40), ("f32", 3)])
+def test_accumulating_over_rows_beyond_four_gibibytes(dtype, n):
+    needs(40)
+    m, rng = hp.mk(), np.random.default_rng(n)
+    far = FarCache(n + 7)
+    Q = mh.gauss(rng, 1, 2, n, 128, dtype=dtype)
+    Q[..., 0] = 8.0
+    lse = np.stack([np.full(n, 70.0), rng.uniform(3.0, 9.0, n)]).astype(np.float32)
+    out = torch.full((far.total,), 7.0, device="cuda")
+    m.maskkv_accumulate_mx(mh.desc(1, 2, 128, dtype, n, 1 << 29), hp.upload(Q, dtype), m.MxCache(far.cache.k_codes, far.cache.k_scales),
+                           mh.device(far.cu), far.total, 0.0, mh.device(lse.ravel()), 0.0, None, out)
+    torch.cuda.synchronize()
+    got = out[mh.device(far.at)], out[far.first:]
+    for h, (K, _) in enumerate(far.heads()):
+        mh.check_weights(got[h].double().cpu().numpy(), Q[0, h], K, lse[h].astype(np.float64), 0.0, None, tag=f"head {h}")
+
+
+def test_the_values_of_rows_beyond_four_gibibytes():
+    needs(50)
+    m, far = hp.mk(), FarCache(3)
+    Kc, Vc = (torch.empty(far.total, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m.maskkv_expand_mx(mh.desc(1, 2, 128, "bf16", 1, 1 << 29), far.cache, mh.device(far.cu), far.total, Kc, Vc)
+    torch.cuda.synchronize()
+    for want, out in ((far.K, Kc), (far.V, Vc)):
+        look = torch.cat((out[mh.device(far.at)], out[far.first:]))
+        assert np.array_equal(look.float().cpu().numpy(), want.astype(np.float32))
+        assert out[far.first - 1000:far.first - 5].count_nonzero() <= 128 * np.count_nonzero(far.at >= far.first - 1000)
