@@ -550,8 +550,8 @@ static int accumulate_entry(const char* what, const maskkv_desc* desc, const mas
     set_error("%s: cu_budget, row_lse, weights_out or (with a decay above 0) weights_in is NULL", what);
     return MASKKV_EINVAL;
   }
-  const float *in0 = weights_in, *in1 = weights_in + capacity, *out0 = weights_out, *out1 = weights_out + capacity;
-  if (decay > 0.f && in0 != out0 && in0 < out1 && out0 < in1) {
+  const uintptr_t in = (uintptr_t)weights_in, out = (uintptr_t)weights_out, bytes = (uintptr_t)capacity * 4;
+  if (decay > 0.f && in != out && in < out + bytes && out < in + bytes) {
     set_error("%s: weights_in and weights_out overlap without being the same", what);
     return MASKKV_EINVAL;
   }
