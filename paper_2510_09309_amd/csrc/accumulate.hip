@@ -13,11 +13,11 @@
 // n / 32 additions and five more, in fp32.
 //
 // Bound by vector instructions where there is much to do: an exponential, a multiply-add and an addition for every (query, row), 24 cycles of the
-// vector pipe for 64 of them beside 16 of the matrix pipe at head_dim 128.  512 queries of 256 heads x 64 ... 1024 rows (89 k): 21.9 us, the vector
+// vector pipe for 64 of them beside 16 of the matrix pipe at head_dim 128.  512 queries of 256 heads x 64 ... 1024 rows (89 k): 21.9 ... 22.8 us, the vector
 // pipe busy half and the matrix pipe a third of the time; the busiest compute units have four workgroups, the average 3.25.  256 queries x 32
 // heads x 250 rows: 5.8, the latency of arguments, heads' ends, rows and queries in turn.
-// Two blocks of rows a wave, which halves the reads of LDS, leaves two waves a SIMD instead of four: 25.6 us.  Units dealt to the XCDs in runs of eight
-// instead of an eighth each: 23.2 against 23.8, and 16.2 against 15.3 with grouped queries; one at a time 27.3.
+// Units dealt to the XCDs in runs of eight, an eighth each, and one at a time: 21.9, 22.5 and 27.1 us for those, 9.2, 11.6 and 10.8 for 64 queries of 256 heads
+// x 128 ... 1024 rows, 25.8, 32.2 and 25.8 for 64 of 2048 heads x 16 ... 128 rows, 17.2, 17.2 and 18.0 for 128 of 64 heads of a group of four.
 #include <type_traits>
 
 #include "lds.hpp"
@@ -71,10 +71,11 @@ __global__ __launch_bounds__(WAVES * 64) void accumulate_kernel(const Accumulate
   fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_ARGUMENT(A, Kc), MASKKV_ARGUMENT(A, BH), MASKKV_ARGUMENT(A, out)});
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 31, g = lane >> 5;
-  // Each XCD (workgroups whose numbers are congruent modulo 8) takes a run of units: a head's queries stay in one L2.
+  // Each XCD (workgroups whose numbers are congruent modulo 8) takes runs of eight units: most of a head's queries stay in one L2, and the units
+  // that there may be, but are not, are on all XCDs alike.
   const int group = group_number();
   if (group >= prm.groups) return;
-  const int unit = group % 8 * (prm.groups / 8) + group / 8;
+  const int unit = group / 64 * 64 + 64 <= prm.groups ? group / 64 * 64 + group % 8 * 8 + group / 8 % 8 : group;
   const int capacity = (int)prm.capacity;
   const UnitHead head = head_of_unit(prm.cu, prm.BH, capacity, unit, [](int n) { return (int)(((uint32_t)n + kRows - 1) / kRows); });
   const int bh = head.bh;
@@ -273,8 +274,8 @@ int launch_form(AccumulateParams prm, hipStream_t stream) {
 }
 
 // Few: tiles of cached rows for less than two workgroups a compute unit, and more than one step of queries to deal to waves instead.  In turn and
-// shared, 512 queries: 132 tiles 7.7 and 10.4 us, 282 9.3 and 10.7, 465 9.7 and 10.6, 532 11.9 and 10.6, 832 16.3 and 10.7; 128 queries: 212 tiles
-// 5.4 and 5.9, 382 6.1 and 5.8; 40 queries the same to within 0.4; fp32, 128 queries, 312 tiles 10.5 and 12.9.
+// shared, 32 heads of one length, 512 queries: 288 tiles 7.2 and 10.6 us, 448 9.7 and 10.6, 512 9.8 and 10.6, 576 11.9 and 11.3, 832 16.2 and 11.6; 128
+// queries: 288 tiles 4.4 and 5.2, 448 5.4 and 5.3, 576 6.5 and 5.3; 40 queries 4.1 and 4.7, 4.5 and 4.8, 4.9 and 4.8; fp32, 128 queries, 312 tiles 10.5 and 12.9.
 template <typename T, int D, bool MX>
 int launch_rows(const AccumulateParams& prm, hipStream_t stream) {
   const int64_t tiles = prm.capacity / kTile + prm.BH;
