@@ -13,7 +13,7 @@
 // n / 32 additions and five more, in fp32.
 //
 // Bound by vector instructions where there is much to do: an exponential, a multiply-add and an addition for every (query, row), 24 cycles of the
-// vector pipe for 64 of them beside 16 of the matrix pipe at head_dim 128.  512 queries of 256 heads x 64 ... 1024 rows (89 k): 21.9 ... 22.8 us, the vector
+// vector pipe for 64 of them beside 16 of the matrix pipe at head_dim 128.  512 queries of 256 heads x 64 ... 1024 rows (89 k): 21.9 ... 23.3 us, the vector
 // pipe busy half and the matrix pipe a third of the time; the busiest compute units have four workgroups, the average 3.25.  256 queries x 32
 // heads x 250 rows: 5.8, the latency of arguments, heads' ends, rows and queries in turn.
 // Units dealt to the XCDs in runs of eight, an eighth each, and one at a time: 21.9, 22.5 and 27.1 us for those, 9.2, 11.6 and 10.8 for 64 queries of 256 heads

@@ -20,8 +20,10 @@
 //
 // Bound by latency where there is little to do: 32 heads x 256 queries x 250 + 256 rows, head_dim 128, 10.1 us, of which 6.5 are the launch, the
 // first loads and the merging of the waves; one query row of 7 heads over 4 x 30k rows 7.6 + 3.0 us (16 MB, 3.2 at a large copy's rate).
-// By the two phases of a tile where there is much: 256 heads x 512 queries x 64 ... 1024 rows 78.5 us, 733 TFLOP/s, the matrix pipe busy 37 % and the
-// vector pipe 43 % of the time, at a clock that the board's power lowers to 1.85 GHz; the same from a cache in bf16 takes 75.5.
+// By the two phases of a tile where there is much: 256 heads x 512 queries x 64 ... 1024 rows 77 ... 82 us by the board, 700 ... 745 TFLOP/s, the matrix pipe busy
+// 38 % and the vector pipe 44 % of the time, at a clock that the board's power lowers to 1.85 GHz; the same from a cache in bf16 takes 75.5.
+// By the memory where few queries meet a cache that is larger than the memory-side one: a token of 64 heads of four x 16384 rows (143 MB) 33 us, 4.4 TB/s, 128 heads of
+// eight x 32768 (570 MB) 108, 5.3; the former over rows of bf16, 537 MB, takes 171 in maskkv_attend.
 #include <cmath>
 #include <type_traits>
 
