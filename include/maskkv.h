@@ -24,6 +24,11 @@
  *                   rows so, the values that they stand for, and the attention that reads them.
  *   maskkv_accumulate, maskkv_evict (and _mx)   further eviction from the cache: the attention that each cached row has
  *                   got over the denoising steps, and the rows of each head that got most.
+ *   maskkv_rotate   the positions of queries and keys, as rotations of pairs of their elements, before they are scored, cached or
+ *                   attended to.
+ *   maskkv_attend_tree   maskkv_attend where the response rows do not all see each other: trees of drafted tokens, blocks in
+ *                   order; few rows over a long cache.  maskkv_tree_mask: who sees whom in a tree.
+ *   maskkv_sample   a token for every row of logits, and the confidence in it by which a denoising step chooses what it keeps.
  *   maskkv_value_shift   Section 3.1 (feature-cache background): response tokens whose value
  *                   vector turned by more than a threshold between two denoising steps.
  *
@@ -247,6 +252,66 @@ int maskkv_attend_full(const maskkv_desc* desc, const maskkv_tensor* Q_resp,
                        void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Rotary positions.  Pair i < width/2 of a row's first `width` elements is turned by the angle a = position * freq[i] and lengthened:
+ *   (x, y) -> amplitude * (x cos a - y sin a,  y cos a + x sin a)
+ * The pair is elements (i, i + width/2) with MASKKV_ROTARY_HALVES, (2i, 2i + 1) with MASKKV_ROTARY_PAIRS; elements from `width` on stay as they are.
+ */
+typedef enum maskkv_rotary_layout { MASKKV_ROTARY_HALVES = 0, MASKKV_ROTARY_PAIRS = 1 } maskkv_rotary_layout;
+
+typedef struct maskkv_rotary {
+  int32_t width;    /* even, 2 .. head_dim */
+  int32_t layout;   /* a maskkv_rotary_layout */
+  double amplitude; /* 1, or what a scaling for long contexts asks for */
+  double freq[64];  /* radians a position, entries 0 .. width/2 - 1 */
+} maskkv_rotary;
+
+/* How frequencies are scaled for contexts `factor` times as long as the `trained` one (with f_i = base^(-2i/width)):
+ *   PLAIN   f_i (factor, trained, slow and fast are not looked at)
+ *   LINEAR  f_i / factor: positions are interpolated
+ *   BASE    the same with base * factor^(width / (width - 2)) for base (width 2: as PLAIN): the fastest pair keeps its frequency, the slowest is divided by factor
+ *   BANDS   by how often a pair turns within the trained length, r = trained * f_i / (2 pi): f_i where r >= fast, f_i / factor where
+ *           r <= slow, and between them f_i * (w + (1 - w) / factor) with w = (r - slow) / (fast - slow);
+ *           amplitude 1 + 0.1 ln(factor), for queries and for keys. */
+typedef enum maskkv_rotary_scaling {
+  MASKKV_ROTARY_PLAIN = 0,
+  MASKKV_ROTARY_LINEAR = 1,
+  MASKKV_ROTARY_BASE = 2,
+  MASKKV_ROTARY_BANDS = 3
+} maskkv_rotary_scaling;
+
+/*
+ * Host arithmetic, no device work: fills *rotary (once, for all layers and steps of a model; a caller with frequencies of its own
+ * fills it without this call).  width even, 2 .. 128; base > 0; and, where they are looked at, factor >= 1, trained > 0,
+ * 0 <= slow < fast.
+ */
+int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_t scaling, double factor, double trained,
+                              double slow, double fast, maskkv_rotary* rotary);
+
+/*
+ * Rotates the rows of queries, of keys, or of both in one launch.  For b < B and t < token_len[b]:
+ *   Q_out[b,h,t,:] = Q[b,h,t,:] turned by the position positions[b*n_tokens + t],  h < H*g;  K_out from K likewise, h < H.
+ * Q, Q_out: views [B, H*g, n_tokens, d]; K, K_out: views [B, H, n_tokens, d]; a pair of them may be NULL, an output may be its own
+ * input (the same view: in place), and outputs share no element with another view of the call.  positions: DEVICE int32 [B, n_tokens],
+ * any sign: rows turned by p and then by -p are (to rounding, with amplitude 1) what they were, so the rows of a cache can be moved to other
+ * positions.  (A packed cache is a view of one sequence and one head.)  token_len: HOST int32 [B], 0 .. n_tokens, or NULL: n_tokens each; rows from token_len[b] on are left untouched.
+ * 0 <= n_tokens <= 2^25.  Of the description B, H, d, dtype and q_per_kv count.  Angles are formed and reduced in 64 bits, sines and cosines and the
+ * rotation in 32, rounded once to desc->dtype.
+ */
+int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const int32_t* positions, int32_t n_tokens,
+                  const int32_t* token_len, const maskkv_tensor* Q, const maskkv_tensor* Q_out, const maskkv_tensor* K,
+                  const maskkv_tensor* K_out, void* stream);
+
+/*
+ * Who sees whom among n rows of a sequence: bit j % 32 of word j / 32 of a row's W = (n + 31) / 32 words says whether row i sees row j.
+ * mask: DEVICE uint32 [B, n, W].  For a drafted tree (or several next to each other) a row sees itself and the rows above it:
+ *   parents[b*n + i] = the row that row i follows, less than i, or -1: row i follows the cache (a number of i or more counts as -1).
+ *   -2 or less: there is no row i (a batch of trees of different sizes); it sees nothing and nothing follows it: a row that names it
+ *   as its parent follows the cache.
+ * parents: DEVICE int32 [B, n].  All words of every row are written.  B >= 0, 0 <= n <= 2^20, B <= 65535.
+ */
+int maskkv_tree_mask(const int32_t* parents, int32_t B, int32_t n, uint32_t* mask, void* stream);
+
+/*
  * A cache in 4 bits (microscaling: one power of two for 32 neighbours along the head dimension).  All DEVICE, rows contiguous:
  * codes [capacity, d/2] bytes, scales [capacity, d/32] bytes.  Byte i of a row's codes holds element 2i in its low and element
  * 2i+1 in its high four bits: bit 3 is the sign, bits 0-2 number the sizes 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Scale byte s of a row
@@ -337,6 +402,59 @@ int maskkv_evict_mx(const maskkv_desc* desc, const float* weights, const int32_t
                     const int32_t* budgets, const maskkv_mx_cache* cache, const int32_t* idx,
                     const maskkv_mx_cache* cache_out, int32_t* idx_out, int32_t* rows, float* weights_out,
                     int32_t* cu_out, int64_t capacity_out, void* stream);
+
+/* Workspace (DEVICE bytes) for maskkv_attend_tree with this description and capacity: partial results where the rows of a head go to
+ * several workgroups; 0 where they do not.  256-byte alignment.  It is enough for every smaller capacity too.  Nothing in it has to be
+ * set before a call or outlives one; calls that may run at the same time (two streams, two captured graphs) need one each. */
+int maskkv_attend_tree_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes);
+
+/*
+ * maskkv_attend where a response row i sees only the response rows j whose bit it has in `mask` (see maskkv_tree_mask; any bits are
+ * allowed, in any order: blocks in order, windows, padded spans), and all cached rows of its head:
+ *   O[b,hq,i,:] = sum_j softmax_j(Q_resp[b,hq,i,:] . k_j * scale) v_j,  j over the cache and the seen response rows.
+ * mask: DEVICE uint32 [B, n_resp, (n_resp + 31) / 32], the same for all heads; bits from n_resp on are not looked at.  What a row does not see has no
+ * part in its result, be it infinite or NaN.  A row that sees nothing (no bit, and no cached row) gets O = 0 and lse = -infinity.
+ * The keys of a head are dealt to several workgroups where its query rows are few: single tokens and small trees over long caches.
+ * capacity <= MASKKV_MX_MAX_ROWS.  Everything else as in maskkv_attend.
+ */
+int maskkv_attend_tree(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc, const void* Vc,
+                       const int32_t* cu_budget, int64_t capacity, const maskkv_tensor* K_resp, const maskkv_tensor* V_resp,
+                       const uint32_t* mask, float scale, const maskkv_tensor* O, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* What maskkv_sample draws from: DEVICE arrays with an entry a row, or NULL. */
+typedef struct maskkv_sampling {
+  const float* temperature; /* NULL: 1 each */
+  const int32_t* top_k;     /* NULL, or an entry of 0 or less: no limit */
+  const float* top_p;       /* NULL, or an entry of 1 or more: no limit */
+  const float* min_p;       /* NULL, or an entry of 0 or less: no limit */
+  const float* uniform;     /* random numbers, [0, 1) */
+} maskkv_sampling;
+
+/* Workspace (DEVICE bytes) for maskkv_sample of so many rows, and of fewer.  256-byte alignment.  Nothing in it has to be set before a
+ * call or outlives one; calls that may run at the same time need one each. */
+int maskkv_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t dtype, size_t* bytes);
+
+/*
+ * A token for every row of logits l, with given random numbers.  With m the row's largest logit, w_j = exp((l_j - m) / temperature):
+ *   1. tokens are ranked by their logits, the largest first and equal ones by their number;
+ *   2. top_k: the first top_k of them stay;
+ *   3. top_p: of these, in that order, those before which less than top_p of their common mass (sum of w) lies; the first one always;
+ *   4. min_p: of these, those with w_j >= min_p (at 1 and more: with the largest logit);
+ *   token[r]   = in the order of their numbers, the first of the tokens that stay with  sum_{i <= j} w_i > uniform * (the sum of all that stay)
+ *   prob[r]    = w_token / (the sum of all that stay): with which probability it was drawn
+ *   logprob[r] = l_token - log sum_j exp(l_j): without temperature and limits, over all tokens.  Its exp is the confidence by which a
+ *                denoising step chooses which positions it keeps.
+ * A temperature of 0 or less (or NaN) takes the first of the largest logits, prob 1.  A NaN logit counts as -infinity; where +infinity occurs, its tokens share
+ * all mass evenly.  A row without a finite or infinite logit above -infinity has token -1, prob 0 and logprob -infinity.  A random number below 0 counts
+ * as 0, one of 1 and more (or NaN) as the largest below 1; limits that are NaN are none.
+ * logits: DEVICE [rows, vocab] in `dtype` (a maskkv_dtype), rows row_stride >= vocab elements apart, aligned to an element; vocab 1 .. 2^24; 0 <= rows <= 2^20.
+ * token: DEVICE int32 [rows]; prob, logprob: DEVICE float [rows], or NULL.  Masses are held in 64 bits and summed up in a fixed order (or as whole
+ * numbers): equal calls give equal bits, and the tokens are those of the definition in 64 bits.
+ */
+int maskkv_sample(const void* logits, int64_t rows, int32_t vocab, int32_t dtype, int64_t row_stride,
+                  const maskkv_sampling* sampling, int32_t* token, float* prob, float* logprob, void* workspace,
+                  size_t workspace_bytes, void* stream);
 
 /*
  * Stage 2, head level, on the device.  For every b:

@@ -21,6 +21,8 @@ LIB_PATH = os.environ.get("MASKKV_LIB_PATH", os.path.join(_HERE, "libmaskkv.so")
 
 MASKKV_F32, MASKKV_BF16 = 0, 1
 POOL_MEAN, POOL_MAX = 0, 1
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS = 0, 1, 2, 3
 MAX_BATCH = 64
 
 SYMBOLS = [
@@ -31,6 +33,9 @@ SYMBOLS = [
     "maskkv_attend_workspace_bytes", "maskkv_attend", "maskkv_attend_full",
     "maskkv_compact_mx", "maskkv_expand_mx", "maskkv_attend_mx_workspace_bytes", "maskkv_attend_mx",
     "maskkv_accumulate", "maskkv_accumulate_mx", "maskkv_evict", "maskkv_evict_mx",
+    "maskkv_attend_tree_workspace_bytes", "maskkv_attend_tree", "maskkv_tree_mask",
+    "maskkv_rotary_frequencies", "maskkv_rotate",
+    "maskkv_sample_workspace_bytes", "maskkv_sample",
     "maskkv_head_budgets",
     "maskkv_layer_importance_workspace_bytes", "maskkv_layer_importance", "maskkv_layer_budgets",
     "maskkv_value_shift",
@@ -119,6 +124,11 @@ class MxCache:
         """Uninitialised room for `capacity` rows of head_dim d."""
         room = lambda width: torch.empty((capacity, width), dtype=torch.uint8, device=device)
         return cls(room(d // 2), room(d // 32), room(d // 2), room(d // 32))
+
+
+class Rotary(ct.Structure):
+    """Python mirror of maskkv_rotary; filled by maskkv_rotary_frequencies, or by a caller with frequencies of its own."""
+    _fields_ = [("width", ct.c_int32), ("layout", ct.c_int32), ("amplitude", ct.c_double), ("freq", ct.c_double * 64)]
 
 
 def tensor_view(t: torch.Tensor, seq_start: Optional[Sequence[int]] = None) -> _CTensor:
@@ -301,6 +311,59 @@ def maskkv_evict_mx(desc: Desc, weights: torch.Tensor, cu_budget: torch.Tensor, 
                               cu_out, capacity_out, stream)
     if status:
         _check(status, "maskkv_evict_mx")
+
+
+def maskkv_attend_tree_workspace_bytes(desc: Desc, capacity: int) -> int:
+    return _size(_native.attend_tree_ws(desc, capacity), "maskkv_attend_tree_workspace_bytes")
+
+
+def maskkv_attend_tree(desc: Desc, Q_resp, Kc: torch.Tensor, Vc: torch.Tensor, cu_budget: torch.Tensor, capacity: int, K_resp, V_resp,
+                       mask: torch.Tensor, scale: float, O, lse: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                       stream=None) -> None:
+    """maskkv_attend with a mask among the response rows: int32 [B, n_resp, (n_resp + 31) // 32], bit j % 32 of word j // 32 of row i
+    says whether row i sees row j (as maskkv_tree_mask writes it)."""
+    status = _native.attend_tree(desc, Q_resp, Kc, Vc, cu_budget, capacity, K_resp, V_resp, mask, scale, O, lse, workspace, stream)
+    if status:
+        _check(status, "maskkv_attend_tree")
+
+
+def maskkv_tree_mask(parents: torch.Tensor, mask: torch.Tensor, stream=None) -> None:
+    """parents: int32 [B, n], of each row the one that it follows, -1: the cache, -2: no row; mask: int32 [B, n, (n + 31) // 32]."""
+    status = _native.tree_mask(parents, mask, stream)
+    if status:
+        _check(status, "maskkv_tree_mask")
+
+
+def maskkv_rotary_frequencies(width: int, layout: int = ROTARY_HALVES, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
+                              trained: float = 0.0, slow: float = 1.0, fast: float = 32.0) -> Rotary:
+    """Host arithmetic: what maskkv_rotate turns rows by."""
+    rotary = Rotary()
+    _check(_lib.maskkv_rotary_frequencies(ct.c_int32(width), ct.c_int32(layout), ct.c_double(base), ct.c_int32(scaling),
+                                          ct.c_double(factor), ct.c_double(trained), ct.c_double(slow), ct.c_double(fast),
+                                          ct.byref(rotary)), "maskkv_rotary_frequencies")
+    return rotary
+
+
+def maskkv_rotate(desc: Desc, rotary: Rotary, positions: torch.Tensor, n_tokens: int, Q, Q_out, K, K_out, stream=None,
+                  token_len: Optional[Sequence[int]] = None) -> None:
+    """Q and Q_out [B, H*g, n_tokens, d], K and K_out [B, H, n_tokens, d], or None for a pair; an output may be its input (in place).
+    positions: int32 [B, n_tokens]; token_len: how many of its rows each sequence has (all by default)."""
+    status = _native.rotate(desc, rotary, positions, n_tokens, token_len, Q, Q_out, K, K_out, stream)
+    if status:
+        _check(status, "maskkv_rotate")
+
+
+def maskkv_sample_workspace_bytes(rows: int, vocab: int, dtype: int) -> int:
+    return _size(_native.sample_ws(rows, vocab, dtype), "maskkv_sample_workspace_bytes")
+
+
+def maskkv_sample(logits: torch.Tensor, temperature: Optional[torch.Tensor], top_k: Optional[torch.Tensor], top_p: Optional[torch.Tensor],
+                  min_p: Optional[torch.Tensor], uniform: torch.Tensor, token: torch.Tensor, prob: Optional[torch.Tensor],
+                  logprob: Optional[torch.Tensor], workspace: Optional[torch.Tensor], stream=None) -> None:
+    """logits: [rows, vocab]; float32 [rows] but top_k and token, int32; what is None is no limit (temperature: 1) or not asked for."""
+    status = _native.sample(logits, temperature, top_k, top_p, min_p, uniform, token, prob, logprob, workspace, stream)
+    if status:
+        _check(status, "maskkv_sample")
 
 
 def maskkv_head_budgets(desc: Desc, prompt_mass: torch.Tensor, k_l: int, alpha: float, budgets: torch.Tensor,

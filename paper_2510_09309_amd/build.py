@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmaskkv.so")
 BENCH_LIB = os.path.join(HERE, "libmaskkv_bench.so")
 SOURCES = ["api.hip", "score.hip", "sweep.hip", "rows.hip", "select.hip", "compact.hip", "attend.hip", "attend_tiles.hip", "layer.hip",
-           "mx.hip", "attend_mx.hip", "accumulate.hip", "evict.hip"]
+           "mx.hip", "attend_mx.hip", "accumulate.hip", "evict.hip", "rotate.hip", "attend_tree.hip", "sample.hip"]
 MARSHAL = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 BENCH_SOURCES = [os.path.join("bench", "probe.hip")]
 FLAGS = [

@@ -161,6 +161,20 @@ int check_mx(const char* what, const char* name, const maskkv_mx_cache* c, int64
   return MASKKV_OK;
 }
 
+constexpr int kMostTokens = 1 << 25;  // of a sequence, in maskkv_rotate (a launch has fewer than 2^32 threads along a dimension)
+
+int check_rotary_shape(const char* what, int32_t width, int32_t most, int32_t layout) {
+  if (width < 2 || width > most || (width & 1)) {
+    set_error("%s: width %d must be even and in 2..%d", what, width, most);
+    return MASKKV_EINVAL;
+  }
+  if (layout != MASKKV_ROTARY_HALVES && layout != MASKKV_ROTARY_PAIRS) {
+    set_error("%s: layout %d unknown", what, layout);
+    return MASKKV_EINVAL;
+  }
+  return MASKKV_OK;
+}
+
 float pick_scale(const maskkv_desc* d, float scale) { return scale > 0.f ? scale : 1.0f / sqrtf((float)d->d); }
 
 // ---- static scratch of maskkv_score_static: one copy per GPU for the life of the process
@@ -647,6 +661,202 @@ int maskkv_evict_mx(const maskkv_desc* desc, const float* weights, const int32_t
                            {desc->d / 2, desc->d / 2, desc->d / 32, desc->d / 32}};
   return evict_entry("evict_mx", desc, weights, cu_budget, capacity, budgets, moved, idx, idx_out, rows, weights_out, cu_out,
                      capacity_out, stream);
+}
+
+int maskkv_attend_tree_workspace_bytes(const maskkv_desc* desc, int64_t capacity, size_t* bytes) {
+  Lens lens;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("attend_tree", "capacity", capacity)) return e;
+  if (!bytes) {
+    set_error("bytes is NULL");
+    return MASKKV_EINVAL;
+  }
+  *bytes = attend_tree_workspace_bytes(desc, capacity);
+  return MASKKV_OK;
+}
+
+int maskkv_attend_tree(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc, const void* Vc,
+                       const int32_t* cu_budget, int64_t capacity, const maskkv_tensor* K_resp, const maskkv_tensor* V_resp,
+                       const uint32_t* mask, float scale, const maskkv_tensor* O, float* lse, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  Lens lens;
+  View q, k2, v2, o;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = make_view(desc, Q_resp, "Q_resp", &q)) return e;
+  if (int e = make_view(desc, K_resp, "K_resp", &k2)) return e;
+  if (int e = make_view(desc, V_resp, "V_resp", &v2)) return e;
+  if (int e = make_view(desc, O, "O", &o)) return e;
+  if (int e = check_capacity("attend_tree", "capacity", capacity)) return e;
+  if (!cu_budget || !mask) {
+    set_error("attend_tree: cu_budget or mask is NULL");
+    return MASKKV_EINVAL;
+  }
+  if (((uintptr_t)mask & 3) || ((uintptr_t)cu_budget & 3)) {
+    set_error("attend_tree: cu_budget and mask must be 4-byte aligned");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_packed("attend_tree", "Kc", Kc, capacity)) return e;
+  if (int e = check_packed("attend_tree", "Vc", Vc, capacity)) return e;
+  if (int e = check_workspace("attend_tree", workspace, workspace_bytes, attend_tree_needs(desc, capacity))) return e;
+  return launch_attend_tree(desc, q, Kc, Vc, cu_budget, capacity, k2, v2, mask, pick_scale(desc, scale), o, lse, workspace,
+                            reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_tree_mask(const int32_t* parents, int32_t B, int32_t n, uint32_t* mask, void* stream) {
+  if (B < 0 || B > 65535 || n < 0 || n > 1 << 20) {
+    set_error("tree_mask: B %d outside 0..65535 or n %d outside 0..2^20", B, n);
+    return MASKKV_ESHAPE;
+  }
+  if (B == 0 || n == 0) return MASKKV_OK;
+  if (!parents || !mask || ((uintptr_t)parents & 3) || ((uintptr_t)mask & 3)) {
+    set_error("tree_mask: parents or mask is NULL or not 4-byte aligned");
+    return MASKKV_EINVAL;
+  }
+  return launch_tree_mask(parents, B, n, mask, reinterpret_cast<hipStream_t>(stream));
+}
+
+// Rows and tokens of maskkv_sample.
+static int check_sample(int64_t rows, int32_t vocab, int32_t dtype) {
+  if (dtype != MASKKV_F32 && dtype != MASKKV_BF16) {
+    set_error("dtype %d is neither MASKKV_F32 nor MASKKV_BF16", dtype);
+    return MASKKV_EDTYPE;
+  }
+  if (rows < 0 || rows > 1 << 20 || vocab < 1 || vocab > 1 << 24) {
+    set_error("sample: rows %lld outside 0..2^20 or vocab %d outside 1..2^24", (long long)rows, vocab);
+    return MASKKV_ESHAPE;
+  }
+  return MASKKV_OK;
+}
+
+int maskkv_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t dtype, size_t* bytes) {
+  if (int e = check_sample(rows, vocab, dtype)) return e;
+  if (!bytes) {
+    set_error("bytes is NULL");
+    return MASKKV_EINVAL;
+  }
+  *bytes = sample_workspace_bytes(rows, vocab, dtype);
+  return MASKKV_OK;
+}
+
+int maskkv_sample(const void* logits, int64_t rows, int32_t vocab, int32_t dtype, int64_t row_stride,
+                  const maskkv_sampling* sampling, int32_t* token, float* prob, float* logprob, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+  if (int e = check_sample(rows, vocab, dtype)) return e;
+  const int64_t eb = dtype == MASKKV_BF16 ? 2 : 4;
+  if (!sampling || row_stride < vocab || row_stride > INT64_MAX / (1 << 23)) {
+    set_error("sample: sampling is NULL, or row_stride %lld is below vocab %d or too large", (long long)row_stride, vocab);
+    return MASKKV_EINVAL;
+  }
+  if (rows == 0) return MASKKV_OK;
+  if (!logits || !token || !sampling->uniform) {
+    set_error("sample: logits, token or uniform is NULL");
+    return MASKKV_EINVAL;
+  }
+  if ((uintptr_t)logits & (eb - 1)) {
+    set_error("sample: logits must be aligned to an element");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_workspace("sample", workspace, workspace_bytes, sample_workspace_bytes(rows, vocab, dtype))) return e;
+  return launch_sample(logits, rows, vocab, dtype, row_stride * eb, sampling, token, prob, logprob, workspace,
+                       reinterpret_cast<hipStream_t>(stream));
+}
+
+int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_t scaling, double factor, double trained,
+                              double slow, double fast, maskkv_rotary* rotary) {
+  if (int e = check_rotary_shape("rotary_frequencies", width, 128, layout)) return e;
+  if (!rotary || !(base > 0.0) || !isfinite(base)) {
+    set_error("rotary_frequencies: rotary is NULL or base %g is not a positive number", base);
+    return MASKKV_EINVAL;
+  }
+  const bool bands = scaling == MASKKV_ROTARY_BANDS;
+  if (scaling != MASKKV_ROTARY_PLAIN && scaling != MASKKV_ROTARY_LINEAR && scaling != MASKKV_ROTARY_BASE && !bands) {
+    set_error("rotary_frequencies: scaling %d unknown", scaling);
+    return MASKKV_EINVAL;
+  }
+  if (scaling != MASKKV_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) {
+    set_error("rotary_frequencies: factor %g is not a number of 1 or more", factor);
+    return MASKKV_EINVAL;
+  }
+  if (bands && (!(trained > 0.0) || !isfinite(trained) || !(slow >= 0.0) || !(fast > slow) || !isfinite(fast))) {
+    set_error("rotary_frequencies: trained %g must be above 0 and slow %g, fast %g be 0 <= slow < fast", trained, slow, fast);
+    return MASKKV_EINVAL;
+  }
+  if (scaling == MASKKV_ROTARY_BASE && width > 2) base *= pow(factor, width / (width - 2.0));
+  maskkv_rotary r = {width, layout, bands ? 1.0 + 0.1 * log(factor) : 1.0, {}};
+  for (int i = 0; i < width / 2; ++i) {
+    double f = pow(base, -2.0 * i / width);
+    if (scaling == MASKKV_ROTARY_LINEAR) f /= factor;
+    if (bands) {
+      const double turns = trained * f / 6.283185307179586476925;
+      const double keep = fmin(fmax((turns - slow) / (fast - slow), 0.0), 1.0);
+      f *= keep + (1.0 - keep) / factor;
+    }
+    if (!isfinite(f)) {
+      set_error("rotary_frequencies: base %g is beyond the range of frequencies", base);
+      return MASKKV_EINVAL;
+    }
+    r.freq[i] = f;
+  }
+  *rotary = r;
+  return MASKKV_OK;
+}
+
+// One of maskkv_rotate's inputs with its output: both views, or neither.
+static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const maskkv_tensor* out, const char* name, View* from, View* to) {
+  if (!in != !out) {
+    set_error("rotate: only one of %s and %s_out is NULL", name, name);
+    return MASKKV_EINVAL;
+  }
+  if (!in) return MASKKV_OK;
+  if (int e = make_view(desc, in, name, from)) return e;
+  if (int e = make_view(desc, out, name, to)) return e;
+  if (from->ptr != to->ptr) return MASKKV_OK;
+  bool same = from->stride_t == to->stride_t && from->stride_h == to->stride_h;
+  for (int b = 0; b < desc->B; ++b) same = same && from->boff[b] == to->boff[b];
+  if (same) return MASKKV_OK;
+  set_error("rotate: %s_out begins where %s does and is not the same view", name, name);
+  return MASKKV_EINVAL;
+}
+
+int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const int32_t* positions, int32_t n_tokens,
+                  const int32_t* token_len, const maskkv_tensor* Q, const maskkv_tensor* Q_out, const maskkv_tensor* K,
+                  const maskkv_tensor* K_out, void* stream) {
+  Lens lens;
+  View q, qo, k, ko;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (!rotary) {
+    set_error("rotate: rotary is NULL");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_rotary_shape("rotate", rotary->width, desc->d, rotary->layout)) return e;
+  bool finite = isfinite(rotary->amplitude);
+  for (int i = 0; i < rotary->width / 2; ++i) finite = finite && isfinite(rotary->freq[i]);
+  if (!finite) {
+    set_error("rotate: a frequency or the amplitude is not a finite number");
+    return MASKKV_EINVAL;
+  }
+  if (n_tokens < 0 || n_tokens > kMostTokens) {
+    set_error("rotate: n_tokens %d outside 0..%d", n_tokens, kMostTokens);
+    return MASKKV_EINVAL;
+  }
+  if (!Q && !K) {
+    set_error("rotate: neither Q nor K is given");
+    return MASKKV_EINVAL;
+  }
+  if (int e = check_turned(desc, Q, Q_out, "Q", &q, &qo)) return e;
+  if (int e = check_turned(desc, K, K_out, "K", &k, &ko)) return e;
+  for (int b = 0; token_len && b < desc->B; ++b)
+    if (token_len[b] < 0 || token_len[b] > n_tokens) {
+      set_error("rotate: token_len[%d] = %d outside 0..n_tokens = %d", b, token_len[b], n_tokens);
+      return MASKKV_EINVAL;
+    }
+  if (n_tokens == 0) return MASKKV_OK;
+  if (!positions) {
+    set_error("rotate: positions is NULL");
+    return MASKKV_EINVAL;
+  }
+  return launch_rotate(desc, rotary, positions, n_tokens, token_len, Q ? &q : nullptr, &qo, K ? &k : nullptr, &ko,
+                       reinterpret_cast<hipStream_t>(stream));
 }
 
 int maskkv_head_budgets(const maskkv_desc* desc, const float* prompt_mass, int32_t k_l, float alpha, int32_t* budgets,

@@ -59,6 +59,17 @@ __device__ __forceinline__ u32x2 read_transposed(uint32_t addr, int imm) {
   return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(in_lds<s16x4>(addr, imm)));
 }
 
+// Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there, but those of the
+// last units, fewer than eight, are dealt to all XCDs (4 heads x 60 query tiles on half of the chip: 16.8 us, on all of it 10.7).
+struct Place {
+  int unit, qtile;
+};
+__device__ __forceinline__ Place place_of(int block, int units, int qtiles) {
+  const int even = units / 8 * 8 * qtiles;
+  if (block < even) return {block / 8 / qtiles * 8 + block % 8, block / 8 % qtiles};
+  return {units / 8 * 8 + (block - even) / qtiles, (block - even) % qtiles};
+}
+
 // attend_tiles.hip: the tiled kernel for bf16.
 // Queries per workgroup for `units` heads of n_q query rows.
 int attend_tiles_queries(int64_t units, int n_q, bool full);

@@ -62,17 +62,6 @@ __device__ __forceinline__ void fetch_attend_mx_arguments() {
                    MASKKV_ARGUMENT(A, cache), MASKKV_ARGUMENT(A, H), (uint32_t)(offsetof(A, parts) + 4)});
 }
 
-// Workgroups whose numbers are congruent modulo 8 share an XCD's L2: the query tiles of a unit follow each other there, but those of the
-// last units, fewer than eight, are dealt to all XCDs (4 heads x 60 query tiles on half of the chip: 16.8 us, on all of it 10.7).
-struct Place {
-  int unit, qtile;
-};
-__device__ __forceinline__ Place place_of(int block, int units, int qtiles) {
-  const int even = units / 8 * 8 * qtiles;
-  if (block < even) return {block / 8 / qtiles * 8 + block % 8, block / 8 % qtiles};
-  return {units / 8 * 8 + (block - even) / qtiles, (block - even) % qtiles};
-}
-
 template <typename T, int D>
 struct MxCfg {
   static constexpr int kRowB = D * (int)sizeof(T);

@@ -1,0 +1,584 @@
+// Attention of response rows that do not all see each other - trees of drafted tokens, blocks in order - over a packed cache and the
+// response's own rows: one pass over the keys with the running maximum and sum of a softmax, a bit per query and response row.
+//
+// A workgroup has four waves and serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row axis), so that a
+// lane owns one query, its word of the mask covers a tile of 32 response rows, and its probabilities are the B operand of
+// O^T = V^T P^T as they stand.  The waves take tiles of 32 keys in turn, each through LDS of its own and without a barrier: K and V come by direct
+// transfers, K of the next tile while this one's softmax runs, V of the next behind this one's product.  The waves are merged at the end.
+//
+// The keys of a head go to several workgroups where the launch would not fill the chip (`deal_of`), and a second kernel joins the partial results.
+//
+// What a row does not see must not reach it, be it infinite or NaN: a product of the matrix pipe would turn a probability of 0 times such
+// a value into NaN.  Tiles of the response are looked through for them, and one that has any takes the product key by key (`add_seen`).  Cached rows
+// are seen by all queries of their head, and a tile's places behind the last row hold that row again.
+//
+// Sums, maxima and outputs are fp32; probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product.
+#include <type_traits>
+
+#include "attend.hpp"
+#include "mx.hpp"
+
+namespace maskkv {
+
+namespace {
+
+constexpr int kUnits = 256;  // compute units
+constexpr int kTile = 32;    // keys of a tile, and query rows of a workgroup
+constexpr int kWaves = 4;
+
+struct TreeParams {
+  View Q, K2, V2, O;
+  const char* Kc;
+  const char* Vc;
+  const int32_t* cu;
+  const uint32_t* mask;
+  int64_t capacity;
+  int H, BH, q_per_kv, n_resp, n_q, qtiles, words;
+  int units;      // at most
+  int chunk;      // tiles of a workgroup, or 0: all of its head
+  int part_rows;  // of a partial result
+  float c;        // scale * log2(e)
+  float* lse;
+  float* part_o;    // [units * qtiles][part_rows][D]
+  float2* part_ml;  // [units * qtiles][part_rows]
+  int2* parts;      // [BH] a head's first unit, and how many it has
+};
+
+template <typename T, int D>
+struct TreeCfg {
+  static constexpr int kRowB = D * (int)sizeof(T);
+  static constexpr int kPPR = kRowB / 16;           // pieces of 16 bytes in a row
+  static constexpr int kDB = D / 32;
+  static constexpr int kTileB = kTile * kRowB;      // K, then V of a wave
+  static constexpr int kMoves = kTileB / 1024;      // direct transfers of a tile
+  static constexpr int kMoveRows = 64 / kPPR;       // rows of one
+  static constexpr int kSumP = D / 2 + 4;           // floats from one query's sums to the next while the waves are merged, half a row at a time
+  static constexpr int kMlAt = kWaves * 2 * kTileB;
+  static constexpr int kLds = kMlAt + kWaves * kTile * 8;
+  static_assert(kTile * kSumP * 4 <= 2 * kTileB && kTile * kTile * 4 <= kTileB, "LDS of a wave");
+  // Rows that are read by halves, 16 bytes a lane: neighbouring rows on different banks.
+  __device__ static uint32_t k_slot(uint32_t row, uint32_t p) { return p ^ (kPPR == 8 ? (row >> 1) & 7 : row & 15); }
+  // V: bf16 see v_swizzle; fp32: blocks of 32 columns, exchanged in every other four rows.
+  __device__ static uint32_t v_slot(uint32_t row, uint32_t p) {
+    return sizeof(T) == 2 ? p ^ v_swizzle<D>(row) << 1 : p ^ ((row >> 2) & 1) << 3;
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void wait_moves() {  // all but the last N transfers have arrived
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_is_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tree_kernel(const TreeParams prm) {
+  using C = TreeCfg<T, D>;
+  constexpr bool F32 = sizeof(T) == 4;
+  extern __shared__ __attribute__((aligned(1024))) char tree_lds[];
+  const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
+  const int unit = place.unit, qtile = place.qtile;
+  const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
+  auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kTile - 1) / kTile) + resp_tiles; };  // those of the response first
+  const int capacity = (int)prm.capacity;
+  UnitHead head;
+  if (prm.chunk) {
+    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
+    if (head.bh < 0) return;
+  } else {
+    const int first = min(prm.cu[unit], capacity);
+    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
+  }
+  const int bh = head.bh, units = head.units, cached = head.rows, tiles = tiles_of(cached);
+  const int b = bh / prm.H, h = bh % prm.H;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  if (prm.chunk && unit == head.first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, units);
+  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
+  const int t1 = prm.chunk ? min(tiles, t0 + prm.chunk) : tiles;
+
+  char* const k_lds = tree_lds + wave * 2 * C::kTileB;
+  char* const v_lds = k_lds + C::kTileB;
+  const uint32_t k_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)k_lds, v_at = k_at + C::kTileB;
+
+  // This wave's tiles: t0 + wave, and every fourth from there.
+  const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
+  auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
+  // A transfer brings the pieces that belong to consecutive places of LDS.  (Rows behind the last one are the last one.)
+  auto move = [&](const char* from, int64_t stride, int left, uint32_t to, auto slot) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::kMoves; ++j) {
+      const uint32_t row = j * C::kMoveRows + lane / C::kPPR;
+      dma16(from, (uint32_t)min((int)row, left - 1) * (uint32_t)stride + (slot(row, lane % C::kPPR) << 4), to + j * 1024);
+    }
+  };
+  auto move_k = [&](int t) __attribute__((always_inline)) {
+    auto slot = [](uint32_t row, uint32_t p) { return C::k_slot(row, p); };
+    if (t < resp_tiles)
+      move(prm.K2.row(b, h, t * kTile), prm.K2.stride_t, prm.n_resp - t * kTile, k_at, slot);
+    else
+      move(prm.Kc + ((int64_t)head.first + (t - resp_tiles) * kTile) * C::kRowB, C::kRowB, cached - (t - resp_tiles) * kTile, k_at, slot);
+  };
+  auto move_v = [&](int t) __attribute__((always_inline)) {
+    auto slot = [](uint32_t row, uint32_t p) { return C::v_slot(row, p); };
+    if (t < resp_tiles)
+      move(prm.V2.row(b, h, t * kTile), prm.V2.stride_t, prm.n_resp - t * kTile, v_at, slot);
+    else
+      move(prm.Vc + ((int64_t)head.first + (t - resp_tiles) * kTile) * C::kRowB, C::kRowB, cached - (t - resp_tiles) * kTile, v_at, slot);
+  };
+
+  // ---- this lane's query: half of its row, as the B operand of the first product
+  const int query = min(qtile * kTile + r, prm.n_q - 1);
+  u32x4 qf[C::kPPR / 2];
+  {
+    const char* q = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, query) + g * (C::kRowB / 2);
+#pragma unroll
+    for (int i = 0; i < C::kPPR / 2; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
+  }
+  const uint32_t* const my_mask = prm.mask + ((int64_t)b * prm.n_resp + query % prm.n_resp) * prm.words;
+  if (mine > 0) {
+    move_k(tile_of(0));
+    move_v(tile_of(0));
+  }
+
+  f32x16 o[C::kDB], s;
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
+  float m = kNegBig, l = 0.f;
+
+  // The product for a tile of the response that holds an infinity or NaN: key by key, of those that the lane's query sees.
+  auto add_seen = [&](uint32_t word) __attribute__((always_inline)) {
+    float* const p_lds = reinterpret_cast<float*>(k_lds);  // [key][query] (K has been read)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) p_lds[(8 * (i / 4) + 4 * g + i % 4) * kTile + r] = s[i];
+    lds_is_read();
+#pragma unroll 1
+    for (int j = 0; j < kTile; ++j) {
+      const float p = p_lds[j * kTile + r];
+      const bool sees = word >> j & 1;
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // four elements of the row
+          const uint32_t e = 32 * db + 8 * q + 4 * g;
+          float v[4];
+          if constexpr (F32) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(v_lds + j * C::kRowB + (C::v_slot(j, e / 4) << 4));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t bits = w[x];
+              v[x] = as_f32(bits);
+            }
+          } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(v_lds + j * C::kRowB + (C::v_slot(j, e / 8) << 4) + e % 8 * 2);
+            const uint32_t w0 = w[0], w1 = w[1];
+            v[0] = as_f32(w0 << 16), v[1] = as_f32(w0 & 0xFFFF0000u), v[2] = as_f32(w1 << 16), v[3] = as_f32(w1 & 0xFFFF0000u);
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x) o[db][4 * q + x] = sees ? fmaf(p, v[x], o[db][4 * q + x]) : o[db][4 * q + x];
+        }
+    }
+    lds_is_read();
+  };
+  auto holds_infinite = [&]() __attribute__((always_inline)) {
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < C::kMoves; ++j) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(v_lds + j * 1024 + lane * 16);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t bits = w[x];
+        any |= (bits & 0x7F800000u) == 0x7F800000u || (!F32 && (bits & 0x7F80u) == 0x7F80u);
+      }
+    }
+    return __any(any);
+  };
+
+  // ---- a tile: logits, softmax, output.  Lanes l and l ^ 32 have the same query.
+  auto take = [&](int i, auto of_response) __attribute__((always_inline)) {
+    constexpr bool kResp = decltype(of_response)::value;
+    const int t = tile_of(i), left = kResp ? prm.n_resp - t * kTile : cached - (t - resp_tiles) * kTile;
+    const bool more = i + 1 < mine;
+    uint32_t word = 0;
+    if constexpr (kResp) {
+      word = my_mask[t];
+      if (left < kTile) word &= (1u << left) - 1;
+      wait_moves<0>();
+    } else {
+      wait_moves<C::kMoves>();
+    }
+    s = f32x16{};
+#pragma unroll
+    for (int w = 0; w < C::kPPR / 2; ++w)
+      mfma_step<T>(*reinterpret_cast<const u32x4*>(k_lds + r * C::kRowB + (C::k_slot(r, g * (C::kPPR / 2) + w) << 4)), qf[w], s);
+    lds_is_read();
+    if (!kResp && more) move_k(tile_of(i + 1));
+    if constexpr (kResp) {
+      const uint32_t own = word >> (4 * g);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = own >> (8 * (x / 4) + x % 4) & 1 ? s[x] : -INFINITY;
+    } else if (left < kTile) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x)
+        if (8 * (x / 4) + x % 4 >= left - 4 * g) s[x] = -INFINITY;
+    }
+    float bm = s[0];
+#pragma unroll
+    for (int x = 1; x < 16; ++x) bm = fmaxf(bm, s[x]);
+    const float cand = max_halves(bm) * prm.c;
+    const bool bump = cand > m + kLazyBump;  // (see attend.hip)
+    if (__any(bump)) {
+      const float m_new = bump ? cand : m;
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[db][x] *= alpha;
+    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const float p = fast_exp2(fmaf(s[x], prm.c, -m));
+      s[x] = p;
+      l += p;
+    }
+    bool plain = true;
+    if constexpr (kResp) {
+      if (holds_infinite()) {
+        add_seen(word);
+        plain = false;
+      }
+      if (more) move_k(tile_of(i + 1));
+    } else if (more) {
+      wait_moves<C::kMoves>();
+    } else {
+      wait_moves<0>();
+    }
+    if (plain) {
+      if constexpr (!F32) {
+        uint32_t from = v_at + v_read_offset<D>(lane, 0);
+        asm volatile("" : "+v"(from));  // (an address for each block would be kept in a register of its own)
+#pragma unroll
+        for (int tp = 0; tp < 2; ++tp) {
+          u32x4 pf;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(s[8 * tp + 2 * w], s[8 * tp + 2 * w + 1]);
+#pragma unroll
+          for (int db = 0; db < C::kDB; ++db) {
+            const u32x2 lo = read_transposed(from ^ db << 6, 16 * tp * C::kRowB), hi = read_transposed(from ^ db << 6, (16 * tp + 8) * C::kRowB);
+            mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[db]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int row = 8 * (x / 4) + 4 * g + x % 4;
+#pragma unroll
+          for (int db = 0; db < C::kDB; ++db) {
+            const float v = *reinterpret_cast<const float*>(v_lds + row * C::kRowB + ((db ^ ((row >> 2) & 1)) * 32 + r) * 4);
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[x], o[db], 0, 0, 0);
+          }
+        }
+      }
+    }
+    lds_is_read();
+    if (more) move_v(tile_of(i + 1));
+  };
+  {
+    const int resp = min(max(min(resp_tiles, t1) - t0 - wave + kWaves - 1, 0) / kWaves, mine);
+    int i = 0;
+    for (; i < resp; ++i) take(i, std::true_type());
+    for (; i < mine; ++i) take(i, std::false_type());
+  }
+
+  // ---- the waves' results become one: sums of each wave, in units of the largest reference, through LDS
+  l = sum_halves(l);
+  float2* const ml = reinterpret_cast<float2*>(tree_lds + C::kMlAt);
+  if (g == 0) ml[wave * kTile + r] = make_float2(m, l);
+  __syncthreads();
+  float top = kNegBig;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kTile + r].x);
+  const float mine_by = fast_exp2(m - top);
+  float* const sums = reinterpret_cast<float*>(tree_lds);
+  constexpr int kEach = 8;                // elements of a row that a thread writes
+  constexpr int kPerRow = D / 2 / kEach;  // threads of half a row
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (half) __syncthreads();
+    if (qtile * kTile + r < prm.n_q)
+#pragma unroll
+      for (int n = 0; n < C::kDB / 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& from = o[half * (C::kDB / 2) + n];
+          *reinterpret_cast<float4*>(sums + (wave * kTile + r) * C::kSumP + 32 * n + 8 * i + 4 * g) =
+              make_float4(from[4 * i] * mine_by, from[4 * i + 1] * mine_by, from[4 * i + 2] * mine_by, from[4 * i + 3] * mine_by);
+        }
+    __syncthreads();
+    const int row = threadIdx.x / kPerRow, q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;  // (256 threads: 32 rows or more)
+    if (row >= kTile || q >= prm.n_q) continue;
+    float mq = kNegBig, lq = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) mq = fmaxf(mq, ml[w * kTile + row].x);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) lq += ml[w * kTile + row].y * fast_exp2(ml[w * kTile + row].x - mq);
+    float x[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; e += 4) {
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float4 z = *reinterpret_cast<const float4*>(sums + (w * kTile + row) * C::kSumP + at + e);
+        y.x += z.x, y.y += z.y, y.z += z.z, y.w += z.w;
+      }
+      x[e] = y.x, x[e + 1] = y.y, x[e + 2] = y.z, x[e + 3] = y.w;
+    }
+    const int to_at = half * (D / 2) + at;
+    if (units > 1) {
+      const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + row;
+      float4* to = reinterpret_cast<float4*>(prm.part_o + part * D + to_at);
+      to[0] = make_float4(x[0], x[1], x[2], x[3]);
+      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+      if (to_at == 0) prm.part_ml[part] = make_float2(mq, lq);
+      continue;
+    }
+    const float by = lq == 0.f ? 0.f : 1.f / lq;  // (a row that sees nothing)
+    char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + to_at * (int)sizeof(T);
+    if constexpr (F32) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
+      reinterpret_cast<float4*>(to)[1] = make_float4(x[4] * by, x[5] * by, x[6] * by, x[7] * by);
+    } else {
+      *reinterpret_cast<u32x4*>(to) = u32x4{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by),
+                                            pack_bf16x2(x[4] * by, x[5] * by), pack_bf16x2(x[6] * by, x[7] * by)};
+    }
+    if (to_at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
+  }
+}
+
+// The partial results of the heads that have several units: sums in units of the largest reference.  D/4 threads take a query row and ask for
+// kAtOnce of its partial results before they use the first; where a head has many, the eight groups of a workgroup share one row
+// (SHARED) and meet in LDS, else each has a row of its own.
+constexpr int kJoinGroups = 8;
+template <typename T, int D, bool SHARED>
+__global__ __launch_bounds__(kJoinGroups * D / 4) void attend_tree_join_kernel(const TreeParams prm) {
+  constexpr int kPer = D / 4, kAtOnce = 8, kStep = SHARED ? kJoinGroups : 1;
+  __shared__ float4 sums[kJoinGroups][kPer];
+  __shared__ float2 tops[kJoinGroups];
+  const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer, bh = blockIdx.y;
+  const int q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
+  const int first = prm.parts[bh].x, units = prm.parts[bh].y;
+  if (units <= 1 || q >= prm.n_q) return;
+  const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
+  const int64_t in_unit = (int64_t)(q / kTile) * prm.part_rows + q % kTile;
+  float m = kNegBig, l = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int u0 = SHARED ? grp : 0; u0 < units; u0 += kAtOnce * kStep) {
+    float2 ml[kAtOnce];
+    float4 y[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      ml[i] = make_float2(kNegBig, 0.f);
+      y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (u0 + i * kStep < units) {
+        const int64_t part = (first + u0 + i * kStep) * step + in_unit;
+        ml[i] = prm.part_ml[part];
+        y[i] = *reinterpret_cast<const float4*>(prm.part_o + part * D + at * 4);
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) top = fmaxf(top, ml[i].x);
+    const float old = fast_exp2(m - top);
+    m = top;
+    l *= old;
+    x = make_float4(x.x * old, x.y * old, x.z * old, x.w * old);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float by = fast_exp2(ml[i].x - m);
+      l = fmaf(ml[i].y, by, l);
+      x = make_float4(fmaf(y[i].x, by, x.x), fmaf(y[i].y, by, x.y), fmaf(y[i].z, by, x.z), fmaf(y[i].w, by, x.w));
+    }
+  }
+  if constexpr (SHARED) {
+    sums[grp][at] = x;
+    if (at == 0) tops[grp] = make_float2(m, l);
+    __syncthreads();
+    if (grp > 0) return;
+    m = kNegBig;
+#pragma unroll
+    for (int i = 0; i < kJoinGroups; ++i) m = fmaxf(m, tops[i].x);
+    l = 0.f;
+    x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kJoinGroups; ++i) {
+      const float by = fast_exp2(tops[i].x - m);
+      const float4 y = sums[i][at];
+      l = fmaf(tops[i].y, by, l);
+      x = make_float4(fmaf(y.x, by, x.x), fmaf(y.y, by, x.y), fmaf(y.z, by, x.z), fmaf(y.w, by, x.w));
+    }
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;
+  char* to = prm.O.group_row(bh / prm.H, bh % prm.H, prm.q_per_kv, prm.n_resp, q) + at * 4 * (int)sizeof(T);
+  if constexpr (sizeof(T) == 4)
+    *reinterpret_cast<float4*>(to) = make_float4(x.x * by, x.y * by, x.z * by, x.w * by);
+  else
+    *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16x2(x.x * by, x.y * by), pack_bf16x2(x.z * by, x.w * by)};
+  if (at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---- who sees whom in drafted trees: a thread a row, which walks up from it.  The rows above have ever smaller numbers, so the words are
+// finished one after the other, the last one first.
+__global__ __launch_bounds__(256) void tree_mask_kernel(const int32_t* parents, int n, int words, uint32_t* mask) {
+  const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int32_t* const up = parents + (int64_t)b * n;
+  uint32_t* const to = mask + ((int64_t)b * n + i) * words;
+  int p = up[i], at = words - 1, node = i;
+  uint32_t bits = 0;
+  auto put = [&](int j) {
+    for (; at > j / 32; --at) {
+      to[at] = bits;
+      bits = 0;
+    }
+    bits |= 1u << (j % 32);
+  };
+  if (p >= -1) {
+    put(i);
+    while (p >= 0 && p < node) {
+      const int above = up[p];
+      if (above < -1) break;  // (there is no such row)
+      put(p);
+      node = p;
+      p = above;
+    }
+  }
+  for (; at >= 0; --at) {
+    to[at] = bits;
+    bits = 0;
+  }
+}
+
+// How the tiles are dealt out.
+struct Deal {
+  int qtiles, part_rows;
+  int chunk;      // tiles of a unit, or 0: a unit per head
+  int64_t units;  // at most
+  int64_t most_units;  // more than there are heads: what any capacity up to this one may have
+};
+constexpr int kSharedUnits = 16;  // units of a head on average above which a query row's partial results are read by a whole workgroup
+constexpr int kLeast = 2 * kWaves;  // tiles of a unit
+
+Deal deal_of(const maskkv_desc* d, int64_t capacity) {
+  const int n_q = query_heads_per_kv(d) * d->n_resp;
+  const int64_t BH = (int64_t)d->B * d->H;
+  Deal x;
+  x.qtiles = (n_q + kTile - 1) / kTile;
+  x.part_rows = n_q < kTile ? n_q : kTile;
+  const int64_t resp = (d->n_resp + kTile - 1) / kTile;
+  const int64_t places = (d->dtype == MASKKV_BF16 ? 2 : 1) * kUnits;
+  const int64_t wanted = (places + x.qtiles - 1) / x.qtiles;
+  // whole heads where they fill the chip as they are, or none has more tiles than a unit
+  const int64_t longest = (d->P_max < capacity ? d->P_max : capacity) / kTile + 1 + resp;
+  x.chunk = 0;
+  x.units = x.most_units = BH;
+  if (BH * x.qtiles >= places || longest <= kLeast) return x;
+  x.most_units = wanted + BH;  // (of this capacity and of smaller ones)
+  const int64_t tiles = capacity / kTile + BH * (resp + 1);
+  int64_t chunk = (tiles + wanted - 1) / wanted;
+  if (chunk < kLeast) chunk = kLeast;
+  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+  if (longest <= chunk) return x;
+  x.chunk = (int)chunk;
+  x.units = tiles / chunk + BH;
+  return x;
+}
+
+size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
+
+size_t bytes_of(const maskkv_desc* d, const Deal& x, int64_t units) {
+  const size_t rows = (size_t)units * x.qtiles * x.part_rows;
+  return pad256(rows * d->d * 4) + pad256(rows * 8) + pad256((size_t)d->B * d->H * 8);
+}
+
+template <typename T, int D>
+int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
+  using C = TreeCfg<T, D>;
+  static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
+  const auto kernel = &attend_tree_kernel<T, D>;
+  const int64_t groups = deal.units * deal.qtiles;
+  if (groups * kWaves * 64 > 0xFFFFFFFF) {  // (threads of a launch along a dimension)
+    set_error("attend_tree: %lld workgroups are more than a launch can have", (long long)groups);
+    return MASKKV_ESHAPE;
+  }
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+  if (e != hipSuccess) {
+    set_error("attend_tree: hipFuncSetAttribute: %s", hipGetErrorString(e));
+    (void)hipGetLastError();
+    return MASKKV_EHIP;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), C::kLds, stream, prm);
+  if (int e = check_launch("attend_tree")) return e;
+  if (!deal.chunk) return MASKKV_OK;
+  if (deal.units > (int64_t)kSharedUnits * prm.BH)
+    hipLaunchKernelGGL((attend_tree_join_kernel<T, D, true>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(kJoinGroups * D / 4), 0, stream, prm);
+  else
+    hipLaunchKernelGGL((attend_tree_join_kernel<T, D, false>), dim3((unsigned)(prm.n_q + kJoinGroups - 1) / kJoinGroups, (unsigned)prm.BH),
+                       dim3(kJoinGroups * D / 4), 0, stream, prm);
+  return check_launch("attend_tree (join)");
+}
+
+}  // namespace
+
+size_t attend_tree_needs(const maskkv_desc* d, int64_t capacity) {
+  const Deal x = deal_of(d, capacity);
+  return x.chunk ? bytes_of(d, x, x.units) : 0;
+}
+
+size_t attend_tree_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
+  const Deal x = deal_of(d, capacity);
+  return x.most_units > (int64_t)d->B * d->H ? bytes_of(d, x, x.most_units) : 0;
+}
+
+int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, const void* Vc, const int32_t* cu_budget, int64_t capacity,
+                       const View& K2, const View& V2, const uint32_t* mask, float scale, const View& O, float* lse, void* workspace,
+                       hipStream_t stream) {
+  const Deal deal = deal_of(d, capacity);
+  TreeParams prm;
+  prm.Q = Q;
+  prm.K2 = K2;
+  prm.V2 = V2;
+  prm.O = O;
+  prm.Kc = reinterpret_cast<const char*>(Kc);
+  prm.Vc = reinterpret_cast<const char*>(Vc);
+  prm.cu = cu_budget;
+  prm.mask = mask;
+  prm.capacity = capacity;
+  prm.H = d->H;
+  prm.BH = d->B * d->H;
+  prm.q_per_kv = query_heads_per_kv(d);
+  prm.n_resp = d->n_resp;
+  prm.n_q = prm.q_per_kv * d->n_resp;
+  prm.words = (d->n_resp + 31) / 32;
+  prm.qtiles = deal.qtiles;
+  prm.units = (int)deal.units;
+  prm.chunk = deal.chunk;
+  prm.part_rows = deal.part_rows;
+  prm.c = scale * kLog2e;
+  prm.lse = lse;
+  const size_t rows = (size_t)deal.units * deal.qtiles * deal.part_rows;
+  char* ws = reinterpret_cast<char*>(workspace);
+  prm.part_o = reinterpret_cast<float*>(ws);
+  prm.part_ml = reinterpret_cast<float2*>(ws + pad256(rows * d->d * 4));
+  prm.parts = reinterpret_cast<int2*>(ws + pad256(rows * d->d * 4) + pad256(rows * 8));
+  if (d->dtype == MASKKV_BF16)
+    return d->d == 128 ? launch_one<bf16_t, 128>(prm, deal, stream) : launch_one<bf16_t, 64>(prm, deal, stream);
+  return d->d == 128 ? launch_one<float, 128>(prm, deal, stream) : launch_one<float, 64>(prm, deal, stream);
+}
+
+int launch_tree_mask(const int32_t* parents, int B, int n, uint32_t* mask, hipStream_t stream) {
+  hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)((n + 255) / 256), (unsigned)B), dim3(256), 0, stream, parents, n, (n + 31) / 32, mask);
+  return check_launch("tree_mask");
+}
+
+}  // namespace maskkv

@@ -119,6 +119,14 @@ size_t attend_mx_needs(const maskkv_desc* d, int64_t capacity);            // of
 int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, const int32_t* cu_budget, int64_t capacity, const View& K2,
                      const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream);
 
+// attend_tree.hip
+size_t attend_tree_workspace_bytes(const maskkv_desc* d, int64_t capacity);  // of this capacity and of all smaller ones
+size_t attend_tree_needs(const maskkv_desc* d, int64_t capacity);            // of this one
+int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, const void* Vc, const int32_t* cu_budget, int64_t capacity,
+                       const View& K2, const View& V2, const uint32_t* mask, float scale, const View& O, float* lse, void* workspace,
+                       hipStream_t stream);
+int launch_tree_mask(const int32_t* parents, int B, int n, uint32_t* mask, hipStream_t stream);
+
 // accumulate.hip.  Kc or, where that is null, the keys of `cache`.
 int launch_accumulate(const maskkv_desc* d, const View& Q, const void* Kc, const MxCache& cache, const int32_t* cu_budget, int64_t capacity,
                       float scale, const float* row_lse, float decay, const float* weights_in, float* weights_out, hipStream_t stream);
@@ -133,6 +141,15 @@ struct MovedRows {
 int launch_evict(const maskkv_desc* d, const float* weights, const int32_t* cu_budget, int64_t capacity, const int32_t* budgets,
                  const MovedRows& moved, const int32_t* idx, int32_t* idx_out, int32_t* rows, float* weights_out, int32_t* cu_out,
                  int64_t capacity_out, hipStream_t stream);
+
+// rotate.hip.  Q and Q_out, or K and K_out, may be null.
+int launch_rotate(const maskkv_desc* d, const maskkv_rotary* rotary, const int32_t* positions, int n_tokens, const int32_t* lens,
+                  const View* Q, const View* Q_out, const View* K, const View* K_out, hipStream_t stream);
+
+// sample.hip
+size_t sample_workspace_bytes(int64_t rows, int vocab, int dtype);
+int launch_sample(const void* logits, int64_t rows, int vocab, int dtype, int64_t row_bytes, const maskkv_sampling* sampling,
+                  int32_t* token, float* prob, float* logprob, void* workspace, hipStream_t stream);
 
 // layer.hip
 size_t layer_importance_workspace_bytes();

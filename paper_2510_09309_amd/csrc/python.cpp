@@ -38,6 +38,12 @@ struct Fns {
   decltype(&maskkv_accumulate_mx) accumulate_mx;
   decltype(&maskkv_evict) evict;
   decltype(&maskkv_evict_mx) evict_mx;
+  decltype(&maskkv_attend_tree_workspace_bytes) attend_tree_ws;
+  decltype(&maskkv_attend_tree) attend_tree;
+  decltype(&maskkv_tree_mask) tree_mask;
+  decltype(&maskkv_rotate) rotate;
+  decltype(&maskkv_sample_workspace_bytes) sample_ws;
+  decltype(&maskkv_sample) sample;
   decltype(&maskkv_head_budgets) head_budgets;
   decltype(&maskkv_layer_importance) layer_importance;
   decltype(&maskkv_value_shift) value_shift;
@@ -609,6 +615,120 @@ PyObject* evict_mx(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// ---- around the attention: positions, masks among the response rows, tokens
+
+// A workspace as the calls above take it: any contiguous tensor on the current device, or none.
+void* workspace_here(PyObject* o, size_t* bytes) {
+  *bytes = nbytes(o);
+  return *bytes ? buffer<void>(o, THPVariable_Unpack(o).scalar_type(), 0, "workspace") : nullptr;
+}
+
+PyObject* attend_tree_ws(PyObject*, Args a, Py_ssize_t n) {
+  return call<2>(n, [&]() -> long long {
+    DescArg d(a[0]);
+    size_t bytes = 0;
+    const int s = fn.attend_tree_ws(&d.d, as_i64(a[1]), &bytes);
+    return s ? -s : (long long)bytes;
+  });
+}
+PyObject* attend_tree(PyObject*, Args a, Py_ssize_t n) {  // desc, Q, Kc, Vc, cu, capacity, Kr, Vr, mask, scale, O, lse, workspace, stream
+  return call<14>(n, [&] {
+    DescHere d(a[0]);
+    const int64_t cap = as_i64(a[5]), g = group_of(d.d), rows = d.d.n_resp;
+    CheckedView q(a[1], d.d, d.d.H * g, rows, "Q_resp"), k2(a[6], d.d, d.d.H, rows, "K_resp"), v2(a[7], d.d, d.d.H, rows, "V_resp"),
+        o(a[10], d.d, d.d.H * g, rows, "O");
+    const at::ScalarType t = element_type(d.d);
+    const void *kc = buffer<void>(a[2], t, cap * d.d.d, "Kc"), *vc = buffer<void>(a[3], t, cap * d.d.d, "Vc");
+    const int32_t* cu = buffer<int32_t>(a[4], at::kInt, heads_of(d.d) + 1, "cu_budget");
+    const uint32_t* mask = buffer<uint32_t>(a[8], at::kInt, d.d.B * rows * ((rows + 31) / 32), "mask");
+    const float scale = (float)as_f64(a[9]);
+    float* lse = buffer<float>(a[11], at::kFloat, heads_of(d.d) * g * rows, "lse", true);
+    size_t wn;
+    void *ws = workspace_here(a[12], &wn), *st = stream_here(a[13]);
+    return without_gil([&] { return fn.attend_tree(&d.d, &q.v, kc, vc, cu, cap, &k2.v, &v2.v, mask, scale, &o.v, lse, ws, wn, st); });
+  });
+}
+PyObject* tree_mask(PyObject*, Args a, Py_ssize_t n) {  // parents, mask, stream
+  return call<3>(n, [&] {
+    here = -1;
+    if (!THPVariable_Check(a[0])) fail(PyExc_TypeError, "parents: expected a tensor");
+    const at::Tensor& t = THPVariable_Unpack(a[0]);
+    if (t.dim() != 2) fail(PyExc_AssertionError, "parents: need [B, n]");
+    const int64_t B = t.size(0), rows = t.size(1);
+    const int32_t* parents = buffer<int32_t>(a[0], at::kInt, 0, "parents");
+    uint32_t* mask = buffer<uint32_t>(a[1], at::kInt, B * rows * ((rows + 31) / 32), "mask");
+    void* st = stream_here(a[2]);
+    if (B > INT32_MAX || rows > INT32_MAX) fail(PyExc_AssertionError, "parents: too large");
+    return without_gil([&] { return fn.tree_mask(parents, (int32_t)B, (int32_t)rows, mask, st); });
+  });
+}
+// desc, rotary, positions, n_tokens, token_len, Q, Q_out, K, K_out, stream
+PyObject* rotate(PyObject*, Args a, Py_ssize_t n) {
+  return call<10>(n, [&] {
+    DescHere d(a[0]);
+    maskkv_rotary rotary;
+    Py_buffer b;
+    if (PyObject_GetBuffer(a[1], &b, PyBUF_SIMPLE) != 0) throw Error{};
+    const bool fits = b.len == (Py_ssize_t)sizeof(rotary);
+    if (fits) memcpy(&rotary, b.buf, sizeof(rotary));
+    PyBuffer_Release(&b);
+    if (!fits) fail(PyExc_TypeError, "rotary: expected what maskkv_rotary_frequencies returns");
+    const int64_t tokens = as_i64(a[3]), g = group_of(d.d);
+    if (tokens < INT32_MIN || tokens > INT32_MAX) fail(PyExc_ValueError, "n_tokens: too large");
+    Ints lens;
+    if (a[4] != Py_None) {
+      lens.read(a[4]);
+      if (lens.n < d.d.B) fail(PyExc_ValueError, "token_len has fewer than B entries");
+    }
+    const int32_t* positions = buffer<int32_t>(a[2], at::kInt, d.d.B * tokens, "positions");
+    struct Side {
+      maskkv_tensor v;
+      const maskkv_tensor* p = nullptr;
+      Side(PyObject* o, const maskkv_desc& desc, int64_t heads, int64_t rows, const char* what) {
+        if (o == Py_None) return;
+        v = CheckedView(o, desc, heads, rows, what).v;
+        p = &v;
+      }
+    } q(a[5], d.d, d.d.H * g, tokens, "Q"), qo(a[6], d.d, d.d.H * g, tokens, "Q_out"), k(a[7], d.d, d.d.H, tokens, "K"),
+        ko(a[8], d.d, d.d.H, tokens, "K_out");
+    void* st = stream_here(a[9]);
+    return without_gil([&] { return fn.rotate(&d.d, &rotary, positions, (int32_t)tokens, lens.data, q.p, qo.p, k.p, ko.p, st); });
+  });
+}
+PyObject* sample_ws(PyObject*, Args a, Py_ssize_t n) {  // rows, vocab, dtype
+  return call<3>(n, [&]() -> long long {
+    const int64_t vocab = as_i64(a[1]);
+    if (vocab < INT32_MIN || vocab > INT32_MAX) fail(PyExc_ValueError, "vocab: too large");
+    size_t bytes = 0;
+    const int s = fn.sample_ws(as_i64(a[0]), (int32_t)vocab, as_i32(a[2]), &bytes);
+    return s ? -s : (long long)bytes;
+  });
+}
+// logits, temperature, top_k, top_p, min_p, uniform, token, prob, logprob, workspace, stream
+PyObject* sample(PyObject*, Args a, Py_ssize_t n) {
+  return call<11>(n, [&] {
+    here = -1;
+    if (!THPVariable_Check(a[0])) fail(PyExc_TypeError, "logits: expected a tensor");
+    const at::Tensor& t = THPVariable_Unpack(a[0]);
+    on_this_device(t, "logits");
+    if (t.dim() != 2 || (t.stride(1) != 1 && t.size(1) > 1)) fail(PyExc_AssertionError, "logits: need [rows, vocab] with contiguous rows");
+    const int64_t rows = t.size(0), vocab = t.size(1), stride = rows > 1 ? t.stride(0) : vocab;
+    if (vocab > INT32_MAX) fail(PyExc_AssertionError, "logits: too large");
+    if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != at::kFloat) fail(PyExc_TypeError, "logits: unsupported tensor dtype");
+    const int32_t dtype = t.scalar_type() == at::kBFloat16 ? MASKKV_BF16 : MASKKV_F32;
+    const maskkv_sampling given = {buffer<float>(a[1], at::kFloat, rows, "temperature", true), buffer<int32_t>(a[2], at::kInt, rows, "top_k", true),
+                                   buffer<float>(a[3], at::kFloat, rows, "top_p", true), buffer<float>(a[4], at::kFloat, rows, "min_p", true),
+                                   buffer<float>(a[5], at::kFloat, rows, "uniform")};
+    int32_t* token = buffer<int32_t>(a[6], at::kInt, rows, "token");
+    float *prob = buffer<float>(a[7], at::kFloat, rows, "prob", true), *logprob = buffer<float>(a[8], at::kFloat, rows, "logprob", true);
+    size_t wn;
+    void *ws = workspace_here(a[9], &wn), *st = stream_here(a[10]);
+    const void* logits = t.data_ptr();
+    return without_gil(
+        [&] { return fn.sample(logits, rows, (int32_t)vocab, dtype, stride, &given, token, prob, logprob, ws, wn, st); });
+  });
+}
+
 // bind({name: address}): the loaded library's entry points.
 PyObject* bind(PyObject*, PyObject* table) {
   const struct {
@@ -622,7 +742,9 @@ PyObject* bind(PyObject*, PyObject* table) {
       {"maskkv_attend_full", &fn.attend_full}, {"maskkv_compact_mx", &fn.compact_mx}, {"maskkv_expand_mx", &fn.expand_mx},
       {"maskkv_attend_mx_workspace_bytes", &fn.attend_mx_ws}, {"maskkv_attend_mx", &fn.attend_mx},
       {"maskkv_accumulate", &fn.accumulate}, {"maskkv_accumulate_mx", &fn.accumulate_mx}, {"maskkv_evict", &fn.evict},
-      {"maskkv_evict_mx", &fn.evict_mx}, {"maskkv_head_budgets", &fn.head_budgets},
+      {"maskkv_evict_mx", &fn.evict_mx}, {"maskkv_attend_tree_workspace_bytes", &fn.attend_tree_ws},
+      {"maskkv_attend_tree", &fn.attend_tree}, {"maskkv_tree_mask", &fn.tree_mask}, {"maskkv_rotate", &fn.rotate},
+      {"maskkv_sample_workspace_bytes", &fn.sample_ws}, {"maskkv_sample", &fn.sample}, {"maskkv_head_budgets", &fn.head_budgets},
       {"maskkv_layer_importance", &fn.layer_importance}, {"maskkv_value_shift", &fn.value_shift}};
   for (const auto& e : all) {
     PyObject* v = PyDict_GetItemString(table, e.name);
@@ -637,7 +759,8 @@ PyObject* bind(PyObject*, PyObject* table) {
 PyMethodDef methods[] = {FAST(score_ws), FAST(select_ws), FAST(attend_ws), FAST(score), FAST(score_given_lse),
                          FAST(score_static), FAST(select), FAST(compact), FAST(attend), FAST(attend_full),
                          FAST(compact_mx), FAST(expand_mx), FAST(attend_mx_ws), FAST(attend_mx), FAST(accumulate),
-                         FAST(accumulate_mx), FAST(evict), FAST(evict_mx), FAST(head_budgets), FAST(layer_importance), FAST(value_shift),
+                         FAST(accumulate_mx), FAST(evict), FAST(evict_mx), FAST(attend_tree_ws), FAST(attend_tree), FAST(tree_mask),
+                         FAST(rotate), FAST(sample_ws), FAST(sample), FAST(head_budgets), FAST(layer_importance), FAST(value_shift),
                          {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
