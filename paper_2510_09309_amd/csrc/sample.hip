@@ -25,9 +25,16 @@ constexpr int kGroupBlocks = 8;   // ... of a group
 constexpr int kGroups = kPartBlocks / kGroupBlocks;
 
 struct Part {
-  double mass;  // sum of exp((l - top) / temperature)
-  float top;    // largest logit
-  float plain;  // sum of exp(l - top)
+  double mass;   // sum of exp((l - top) / temperature)
+  double plain;  // sum of exp(l - top)
+  union {
+    float top;   // largest logit
+    int first;   // once that is known: where its tokens lie in a list,
+  };
+  int many;      // and how many
+  __device__ Part() {}
+  __device__ Part(double a, double b, float c) : mass(a), plain(b), top(c), many(0) {}
+  __device__ Part(double a, double b, int c, int n) : mass(a), plain(b), first(c), many(n) {}
 };
 
 struct SampleParams {
@@ -68,11 +75,15 @@ struct Limits {
   __device__ __forceinline__ double c() const { return 1.4426950408889634074 / (double)T; }
 };
 
-// 2^t, t <= 0 (what is below 2^-1100, or NaN, is 0; 2^0 is 1 exactly)
+// 2^t, t <= 0 (what is below 2^-1000, or NaN, is 2^-1000; 2^0 is 1 exactly).  A sum with 1.5 * 2^52 rounds t to a whole number, which is the low word of the
+// sum; it is added to the exponent as it is.  (rint, a conversion to an integer and ldexp took as long, but were exact below.)
 __device__ __forceinline__ double exp2_64(double t) {
-  t = fmax(t, -1100.0);
-  const double n = rint(t), f = t - n;
-  double q = 1.0203121070622722e-07;
+  constexpr double kRound = 0x1.8p52;
+  double kFirst = 1.0203121070622722e-07;
+  asm("" : "+v"(kFirst));  // (two constants are more than an instruction takes: this one in registers, once)
+  t = fmax(t, -1000.0);
+  const double n = t + kRound, f = t - (n - kRound);
+  double q = kFirst;
   q = fma(q, f, 1.325522487501112e-06);
   q = fma(q, f, 1.5252686846270554e-05);
   q = fma(q, f, 0.00015403455852469646);
@@ -81,9 +92,10 @@ __device__ __forceinline__ double exp2_64(double t) {
   q = fma(q, f, 0.055504108664760424);
   q = fma(q, f, 0.2402265069581299);
   q = fma(q, f, 0.6931471805599453);
-  return ldexp(fma(q, f, 1.0), (int)n);
+  const double m = fma(q, f, 1.0);
+  return __hiloint2double(__double2hiint(m) + (__double2loint(n) << 20), __double2loint(m));
 }
-// Mass of a logit relative to the largest one.
+// Mass of a logit relative to the largest one.  (That of -infinity is 2^-1000, which is nothing beside the largest one's 1.)
 __device__ __forceinline__ double mass_of(float l, float top, double c) { return exp2_64(((double)l - (double)top) * c); }
 
 // A row in blocks of 16 bytes that begin at multiples of 16 bytes: its first and last one may be another row's in part.
@@ -106,8 +118,8 @@ struct Row {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const uint32_t u = sizeof(T) == 4 ? w[i] : w[i / 2];
-      // (NaN counts as -infinity, -0 as 0)
-      x[i] = fmaxf(as_f32(sizeof(T) == 4 ? u : i % 2 ? u & 0xFFFF0000u : u << 16), -INFINITY) + 0.f;
+      // (-0 counts as 0, NaN as -infinity)
+      x[i] = fmaxf(as_f32(sizeof(T) == 4 ? u : i % 2 ? u & 0xFFFF0000u : u << 16) + 0.f, -INFINITY);
     }
   }
   // Elements of a block that is not wholly this row's: -infinity for the others.
@@ -120,7 +132,7 @@ struct Row {
         const char* p = first + ((int64_t)block * 16 + i * (int)sizeof(T));
         v = sizeof(T) == 4 ? *reinterpret_cast<const float*>(p) : as_f32((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
       }
-      x[i] = fmaxf(v, -INFINITY) + 0.f;
+      x[i] = fmaxf(v + 0.f, -INFINITY);
     }
   }
   __device__ __forceinline__ void read(int block, float (&x)[E]) const {
@@ -209,14 +221,15 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleParams pr
 #pragma unroll
       for (int e = 0; e < E; ++e) x[j][e] = finite_top(x[j][e]);
   }
-  double mass = 0.0;
-  float plain = 0.f;
+  double mass = 0.0, plain = 0.0;
   if (ref > -INFINITY) {
     if (prm.logprob) {
+      // (of bf16 the differences are exact but for logits below 2^-12 or so; of fp32 they are not)
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-        for (int e = 0; e < E; ++e) plain += fast_exp2((x[j][e] - ref) * kLog2e);
+        for (int e = 0; e < E; ++e)
+          plain += sizeof(T) == 2 ? (double)fast_exp2((x[j][e] - ref) * kLog2e) : mass_of(x[j][e], ref, 1.4426950408889634074);
     }
     if (lim.masses) {
       const double c = lim.c();
@@ -226,111 +239,151 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleParams pr
         for (int e = 0; e < E; ++e) mass += mass_of(x[j][e], ref, c);
     }
   }
-  if (prm.logprob) plain = (float)sum_wave((double)plain);
+  if (prm.logprob) plain = sum_wave(plain);
   if (lim.masses) mass = sum_wave(mass);
-  if (lane == 0) prm.part[(int64_t)r * prm.parts + i] = Part{mass, top, plain};
+  if (lane == 0) prm.part[(int64_t)r * prm.parts + i] = Part(mass, plain, top);
 }
 
 // ---- a token for every row
-constexpr int kDraw = 1024;      // threads
-constexpr int kWaves = kDraw / 64;
 constexpr int kBins = 1024;      // of the groups' largest logits
+constexpr int kWide = 4096;      // bins of a row's logits
 constexpr int kFewGroups = 4096; // that are looked into, at most
+constexpr int kRounds = 4;       // groups of a thread that are asked for at once
 constexpr int kFew = 2048;       // tokens that are ranked, at most
+constexpr int kList = 4096;      // tokens among which the last one that stays is looked for, at most
 constexpr int kDigits = 2048;    // values of eleven bits
 
-struct DrawShared {
-  double sums[2][kWaves];
-  int ints[2][kWaves];
+template <int N>
+struct AskShared {
+  double sums[2][N / 64];
+  int ints[2][N / 64];
+  float floats[2][2][N / 64];
+  int found;
+  int count;
+  double value;
+};
+// (rows without limits need no more)
+template <int N>
+struct DrawShared : AskShared<N> {
   union {
     struct {
       uint32_t count[kBins];
       unsigned long long mass[kBins];
     } bins;
+    uint32_t wide[kWide];
     struct {
       uint32_t count[kDigits];
       unsigned long long mass[kDigits];
     } digits;
-    struct {
-      float logit[kFew];
-      int number[kFew];
-      double mass[kFew];    // in the order of their numbers
-      double ranked[kFew];  // in the order of their ranks: the mass before each
-    } few;
+    double ranked[kFew];  // in the order of their ranks: the mass before each
   };
+  float logit[kList];
+  int number[kList];
   uint32_t groups[kFewGroups];
-  int found;
-  int count;
-  double value;
+  int rounds[2][kRounds][N / 64];
+  int taken;
   unsigned long long whole;
   uint32_t key;
 };
 
-// What all threads of a workgroup of kDraw ask each other.  `turn` alternates between two places, so that one barrier a question is enough.
+// What is added up over the lanes up to this one: inside rows of sixteen by shifts, then the ends of rows into the rows behind.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned long long shifted(unsigned long long v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (unsigned long long)hi << 32 | lo;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double v) {
+  return __builtin_bit_cast(double, shifted<CTRL, ROWS>(__builtin_bit_cast(unsigned long long, v)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int shifted(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+template <typename V>
+__device__ __forceinline__ V upto_lane(V v) {
+  v += shifted<0x111, 0xf>(v);
+  v += shifted<0x112, 0xf>(v);
+  v += shifted<0x114, 0xf>(v);
+  v += shifted<0x118, 0xf>(v);
+  v += shifted<0x142, 0xa>(v);
+  v += shifted<0x143, 0xc>(v);
+  return v;
+}
+
+// What all N threads of a workgroup ask each other.  `turn` alternates between two places, so that one barrier a question is enough.
+template <int N>
 struct Ask {
-  DrawShared& s;
+  static constexpr int kWaves = N / 64;
+  AskShared<N>& s;
   int turn = 0;
-  __device__ __forceinline__ explicit Ask(DrawShared& shared) : s(shared) {}
+  __device__ __forceinline__ explicit Ask(AskShared<N>& shared) : s(shared) {}
   __device__ __forceinline__ int wave() const { return threadIdx.x >> 6; }
   __device__ __forceinline__ int lane() const { return threadIdx.x & 63; }
   // The sum before this thread; of all in `total`.
-  __device__ double before(double v, double& total) {
-    double upto = v;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const double o = __shfl_up(upto, i);
-      if (lane() >= i) upto += o;
-    }
-    turn ^= 1;
-    if (lane() == 63) s.sums[turn][wave()] = upto;
+  template <typename V>
+  __device__ __forceinline__ V before_in(V* places, V v, V& total) {
+    const V upto = upto_lane(v);
+    if (lane() == 63) places[wave()] = upto;
     __syncthreads();
-    double base = 0.0;
-    total = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w == wave()) base = total;
-      total += s.sums[turn][w];
-    }
-    const double o = __shfl_up(upto, 1);
-    return base + (lane() ? o : 0.0);
-  }
-  __device__ int before(int v, int& total) {
-    int upto = v;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const int o = __shfl_up(upto, i);
-      if (lane() >= i) upto += o;
-    }
-    turn ^= 1;
-    if (lane() == 63) s.ints[turn][wave()] = upto;
-    __syncthreads();
-    int base = 0;
+    V base = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       if (w == wave()) base = total;
-      total += s.ints[turn][w];
+      total += places[w];
     }
-    return base + upto - v;
+    // (of masses not `upto - v`, which would round once more: the lane before has it)
+    return base + shifted<0x138, 0xf>(upto);
   }
-  __device__ int least(int v) {
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) v = min(v, __shfl_xor(v, i));
+  __device__ __forceinline__ double before(double v, double& total) {
     turn ^= 1;
-    if (lane() == 0) s.ints[turn][wave()] = v;
+    return before_in(s.sums[turn], v, total);
+  }
+  __device__ __forceinline__ unsigned long long before(unsigned long long v, unsigned long long& total) {
+    turn ^= 1;
+    return before_in(reinterpret_cast<unsigned long long*>(s.sums[turn]), v, total);
+  }
+  __device__ __forceinline__ int before(int v, int& total) {
+    turn ^= 1;
+    return before_in(s.ints[turn], v, total);
+  }
+  // The first (last) thread for which it is so, or -1.
+  __device__ __forceinline__ int first(bool so) {
+    const uint64_t b = __ballot(so);
+    turn ^= 1;
+    if (lane() == 0) s.ints[turn][wave()] = b ? (wave() << 6) + __builtin_ctzll(b) : -1;
     __syncthreads();
+    int v = -1;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v = min(v, s.ints[turn][w]);
+    for (int w = kWaves - 1; w >= 0; --w) v = s.ints[turn][w] >= 0 ? s.ints[turn][w] : v;
     return v;
   }
-  __device__ float most(float v) {
-    v = max_wave(v);
+  __device__ __forceinline__ int last(bool so) {
+    const uint64_t b = __ballot(so);
     turn ^= 1;
-    if (lane() == 0) s.ints[turn][wave()] = (int)as_u32(v);
+    if (lane() == 0) s.ints[turn][wave()] = b ? (wave() << 6) + 63 - __builtin_clzll(b) : -1;
+    __syncthreads();
+    int v = -1;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v = s.ints[turn][w] >= 0 ? s.ints[turn][w] : v;
+    return v;
+  }
+  __device__ __forceinline__ void most(float& a, float& b) {
+    a = max_wave(a);
+    b = max_wave(b);
+    turn ^= 1;
+    if (lane() == 0) {
+      s.floats[turn][0][wave()] = a;
+      s.floats[turn][1][wave()] = b;
+    }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v = fmaxf(v, as_f32((uint32_t)s.ints[turn][w]));
-    return v;
+    for (int w = 0; w < kWaves; ++w) {
+      a = fmaxf(a, s.floats[turn][0][w]);
+      b = fmaxf(b, s.floats[turn][1][w]);
+    }
   }
 };
 
@@ -341,26 +394,35 @@ __device__ __forceinline__ uint32_t key_of(float l) {
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return as_f32(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-constexpr int kNone = 0x7FFFFFFF;
-
-template <typename T>
+// kDraw threads draw the token of a row.
+template <typename T, int kDraw, typename Shared>
 struct Drawer {
-  static constexpr int E = Row<T>::E;
+  static constexpr int E = Row<T>::E, kWaves = kDraw / 64;
+  static constexpr int kCounted = kDraw / 2;  // tokens that are ranked by comparing each with each
+  static_assert(kDraw >= kPartBlocks, "a part is drawn from by a thread a block");
   const SampleParams& prm;
-  DrawShared& s;
-  Ask ask;
+  Shared& s;
+  Ask<kDraw> ask;
   const Row<T> row;
   const Limits lim;
   const int r;
   Part* const part;
-  float top = 0.f, ref = 0.f;  // the largest logit, and what masses are relative to
+  const float* const group;
+  const int groups, groups_each, parts_each;  // of the row; of a thread
+  float4 first_groups;                        // the first of a thread
+  float top = 0.f, ref = 0.f;                 // the largest logit, and what masses are relative to
+  float least = 0.f;                          // the smallest of the groups' largest
   double c = 0.0, u = 0.0;
   double masses = 0.0, plain = 0.0;  // of all tokens
-  double mine = 0.0;   // of this thread's parts, and before them
+  double mine = 0.0;                 // of this thread's parts, and before them
   double before = 0.0;
+  int number = -1;  // the token,
+  double prob = 0.0;
 
-  __device__ Drawer(const SampleParams& p, DrawShared& shared, int number)
-      : prm(p), s(shared), ask(shared), row(p, number), lim(p, number), r(number), part(p.part + (int64_t)number * p.parts) {}
+  __device__ __forceinline__ Drawer(const SampleParams& p, Shared& shared, int number)
+      : prm(p), s(shared), ask(shared), row(p, number), lim(p, number), r(number), part(p.part + (int64_t)number * p.parts),
+        group(p.group + (int64_t)number * p.parts * kGroups), groups((row.blocks + kGroupBlocks - 1) / kGroupBlocks),
+        groups_each((groups + 4 * kDraw - 1) / (4 * kDraw) * 4), parts_each((p.parts + kDraw - 1) / kDraw) {}
 
   __device__ __forceinline__ float seen(float l) const { return top == INFINITY ? finite_top(l) : l; }
   __device__ __forceinline__ void read(int block, float (&x)[E]) const {
@@ -370,13 +432,28 @@ struct Drawer {
       for (int e = 0; e < E; ++e) x[e] = finite_top(x[e]);
     }
   }
-  __device__ __forceinline__ double mass(float l) const { return mass_of(l, ref, c); }
+  // (What is about 2^-1000 is nothing: a part of which no token has a mass is none that is drawn from.)
+  static __device__ __forceinline__ double or_nothing(double m, double least) { return m > least ? m : 0.0; }
+  __device__ __forceinline__ double mass(float l) const { return or_nothing(mass_of(l, ref, c), 0x1p-999); }
   __device__ __forceinline__ double part_unit(float part_top, double by) const {
-    return part_top == top ? 1.0 : part_top == -INFINITY || top == INFINITY ? 0.0 : exp2_64(((double)part_top - (double)ref) * by);
+    return part_top == top ? 1.0 : top == INFINITY ? 0.0 : or_nothing(exp2_64(((double)part_top - (double)ref) * by), 0x1p-990);
   }
-  __device__ __forceinline__ int per() const { return (prm.parts + kDraw - 1) / kDraw; }
+  // This thread's parts, and its groups' largest logits in their order (f(logit, group)).
+  __device__ __forceinline__ int from_part() const { return min((int)threadIdx.x * parts_each, prm.parts); }
+  __device__ __forceinline__ int to_part() const { return min((int)(threadIdx.x + 1) * parts_each, prm.parts); }
+  template <typename F>
+  __device__ __forceinline__ void each_group(F f) {
+    const int from = threadIdx.x * groups_each;
+    for (int i = 0; i < groups_each && from + i < groups; i += 4) {
+      const float4 v = i ? *reinterpret_cast<const float4*>(group + from + i) : first_groups;
+      if (from + i < groups) f(v.x, from + i);
+      if (from + i + 1 < groups) f(v.y, from + i + 1);
+      if (from + i + 2 < groups) f(v.z, from + i + 2);
+      if (from + i + 3 < groups) f(v.w, from + i + 3);
+    }
+  }
 
-  __device__ void answer(int number, double prob) {
+  __device__ __forceinline__ void answer() {
     if (threadIdx.x) return;
     prm.token[r] = number;
     if (prm.prob) prm.prob[r] = (float)prob;
@@ -392,15 +469,22 @@ struct Drawer {
   }
 
   // The parts together.
-  __device__ void sum_up() {
-    const int from = threadIdx.x * per(), to = min(from + per(), prm.parts);
-    float most = -INFINITY;
-    for (int i = from; i < to; ++i) most = fmaxf(most, part[i].top);
-    top = ask.most(most);
+  __device__ __forceinline__ void sum_up() {
+    const int from = from_part(), to = to_part();
+    Part one;
+    one.top = -INFINITY;
+    if (from < to) one = part[from];
+    if (lim.some && (int)threadIdx.x * groups_each < groups) first_groups = *reinterpret_cast<const float4*>(group + threadIdx.x * groups_each);
+    float most = -INFINITY, low = -INFINITY;
+    for (int i = from; i < to; ++i) most = fmaxf(most, i == from ? one.top : part[i].top);
+    if (lim.some) each_group([&](float l, int) { low = l > -INFINITY ? fmaxf(low, -l) : low; });
+    ask.most(most, low);
+    top = most;
     ref = top == INFINITY ? 0.f : top;
+    least = top == INFINITY ? 0.f : -low;
     double own = 0.0;
     for (int i = from; i < to; ++i) {
-      const Part x = part[i];
+      const Part x = i == from ? one : part[i];
       if (lim.masses) mine += x.mass * part_unit(x.top, c);
       if (prm.logprob) own += x.plain * part_unit(x.top, 1.4426950408889634074);
     }
@@ -408,35 +492,44 @@ struct Drawer {
     if (lim.masses) before = ask.before(mine, masses);
   }
 
-  __device__ void greedy() {
-    const int from = threadIdx.x * per(), to = min(from + per(), prm.parts);
-    int own = kNone;
+  __device__ __forceinline__ void greedy() {
+    const int from = from_part(), to = to_part();
+    int own = -1;
     for (int i = to - 1; i >= from; --i)
       if (part[i].top == top) own = i;
-    const int i = ask.least(own);
-    int at = kNone;
-    if (threadIdx.x < kPartBlocks && i * kPartBlocks + (int)threadIdx.x < row.blocks) {
-      const int block = i * kPartBlocks + threadIdx.x;
+    const int who = ask.first(own >= 0);
+    if ((int)threadIdx.x == who) s.found = own;
+    __syncthreads();
+    const int block = s.found * kPartBlocks + threadIdx.x;
+    int at = -1;
+    if (threadIdx.x < kPartBlocks && block < row.blocks) {
       float x[E];
       row.read(block, x);
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
         if (x[e] == top) at = row.number(block) + e;
     }
-    answer(ask.least(at), 1.0);
+    const int has = ask.first(at >= 0);
+    if ((int)threadIdx.x == has) s.count = at;
+    __syncthreads();
+    number = s.count;
+    prob = 1.0;
   }
 
-  // Of the parts' masses (own: of a thread's from `from` on, before: of the ones before) the part in which `target` is exceeded, or the last one with any.
+  // The thread in whose masses (`own`, behind `base`) `target` is exceeded, or the last one with any.
+  __device__ __forceinline__ int thread_with(double target, double own, double base) {
+    const int who = ask.first(own > 0.0 && base + own > target);
+    return who >= 0 ? who : ask.last(own > 0.0);  // (roundings)
+  }
+
+  // Of the parts' masses (own: of a thread's, behind `base`) the part in which `target` is exceeded, or the last one with any.
   template <typename F>
-  __device__ int part_with(double target, double own, double base, F mass_in, double& base_of_part) {
-    const int from = threadIdx.x * per(), to = min(from + per(), prm.parts);
-    const bool over = own > 0.0 && base + own > target;
-    int who = ask.least(over ? (int)threadIdx.x : kNone);
-    if (who == kNone) who = -ask.least(own > 0.0 ? -(int)threadIdx.x : kNone);  // (roundings: the last one)
+  __device__ __forceinline__ int part_with(double target, double own, double base, F mass_in, double& base_of_part) {
+    const int who = thread_with(target, own, base);
     if ((int)threadIdx.x == who) {
-      int at = from;
+      int at = from_part();
       double sum = base, before_it = base;
-      for (int i = from; i < to; ++i) {
+      for (int i = from_part(); i < to_part(); ++i) {
         const double m = mass_in(i);
         if (m > 0.0) {
           at = i;
@@ -453,31 +546,38 @@ struct Drawer {
     return s.found;
   }
 
-  // The token: in part i, before which the tokens that stay have the mass `base` and `equal` of them are as large as `last`: those
-  // above `last` stay, and of its equals the first `left`.
-  __device__ void draw_in(int i, double base, double target, double total, float last, int equal, int left) {
-    const int block = i * kPartBlocks + threadIdx.x;
-    const bool has = threadIdx.x < kPartBlocks && block < row.blocks;
+  // Where the token is: in part i, before which the tokens that stay have the mass `base` and `equal` tokens are as large as `last`: those above
+  // `last` stay, and of its equals the first `left`.
+  struct Where {
+    int i;
+    double base, target, total;
+    float last;
+    int equal, left;
+  };
+  __device__ __forceinline__ void draw_in(const Where& w) {
+    const int block = w.i * kPartBlocks + threadIdx.x;
     float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = -INFINITY;
-    if (has) read(block, x);
-    int same = 0, all;
+    if (threadIdx.x < kPartBlocks && block < row.blocks) read(block, x);
+    int nth = 0;
+    if (w.last > -INFINITY) {
+      int same = 0, all;
 #pragma unroll
-    for (int e = 0; e < E; ++e) same += x[e] == last;
-    int nth = equal + ask.before(same, all);
+      for (int e = 0; e < E; ++e) same += x[e] == w.last;
+      nth = w.equal + ask.before(same, all);
+    }
     double m[E], own = 0.0, unused;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const bool stays = x[e] > last || (x[e] == last && nth < left);
-      nth += x[e] == last;
-      const double w = mass(x[e]);
-      m[e] = stays && x[e] > -INFINITY && w >= (double)lim.m ? w : 0.0;
+      const bool stays = x[e] > w.last || (x[e] == w.last && nth < w.left);
+      nth += x[e] == w.last;
+      const double y = mass(x[e]);
+      m[e] = stays && x[e] > -INFINITY && y >= (double)lim.m ? y : 0.0;
       own += m[e];
     }
-    const double from = base + ask.before(own, unused);
-    int who = ask.least(own > 0.0 && from + own > target ? (int)threadIdx.x : kNone);
-    if (who == kNone) who = -ask.least(own > 0.0 ? -(int)threadIdx.x : kNone);
+    const double from = w.base + ask.before(own, unused);
+    const int who = thread_with(w.target, own, from);
     if ((int)threadIdx.x == who) {
       double sum = from;
       int at = 0;
@@ -487,21 +587,22 @@ struct Drawer {
         if (m[e] > 0.0 && !done) {
           at = e;
           sum += m[e];
-          done = sum > target;
+          done = sum > w.target;
           s.value = m[e];
         }
       }
       s.found = row.number(block) + at;
     }
     __syncthreads();
-    answer(s.found, s.value / total);
+    number = s.found;
+    prob = s.value / w.total;
   }
 
-  __device__ void draw_all() {
+  __device__ __forceinline__ Where draw_all() {
     double base;
     const double target = u * masses;
     const int i = part_with(target, mine, before, [&](int j) { return part[j].mass * part_unit(part[j].top, c); }, base);
-    draw_in(i, base, target, masses, -INFINITY, 0, 0);
+    return {i, base, target, masses, -INFINITY, 0, 0};
   }
 
   // ---- few tokens stay
@@ -511,39 +612,43 @@ struct Drawer {
 
   // The lowest of the bins of logits in which a token that stays can be (from the largest logit down to the smallest of the groups' largest in
   // equal steps).  With a top-k as many groups' largest logits lie above; with a top-p, so much of their mass.
-  __device__ int floor_of() {
-    const int groups = (row.blocks + kGroupBlocks - 1) / kGroupBlocks;
-    const float* group = prm.group + (int64_t)r * prm.parts * kGroups;
-    float least = INFINITY;
-    for (int i = threadIdx.x; i < groups; i += kDraw) {
-      const float l = seen(group[i]);
-      least = l > -INFINITY ? fminf(least, l) : least;
-    }
+  __device__ __forceinline__ int floor_of() {
+    const bool by_mass = lim.masses && lim.p < 1.f;
     for (int i = threadIdx.x; i < kBins; i += kDraw) {
       s.bins.count[i] = 0;
       s.bins.mass[i] = 0;
     }
-    least = -ask.most(-least);
     slope = least < ref ? (kBins - 1) / (ref - least) : 0.f;
-    for (int i = threadIdx.x; i < groups; i += kDraw) {
-      const float l = seen(group[i]);
-      if (l == -INFINITY) continue;
-      atomicAdd(&s.bins.count[bin_of(l)], 1u);
-      if (lim.masses && lim.p < 1.f) atomicAdd(&s.bins.mass[bin_of(l)], (unsigned long long)(mass(l) * 0x1p40));
-    }
+    __syncthreads();
+    each_group([&](float l, int) {
+      l = seen(l);
+      if (l == -INFINITY) return;
+      if (lim.k) atomicAdd(&s.bins.count[bin_of(l)], 1u);
+      if (by_mass) atomicAdd(&s.bins.mass[bin_of(l)], (unsigned long long)(mass(l) * 0x1p40));
+    });
     __syncthreads();
     int floor = kBins - 1;
-    {
-      const int own = s.bins.count[threadIdx.x];
-      int all;
-      const int upto = ask.before(own, all) + own;
-      if (lim.k) floor = min(floor, ask.least(upto >= lim.k ? (int)threadIdx.x : kNone));
-    }
-    if (lim.masses && lim.p < 1.f) {
-      const double own = (double)s.bins.mass[threadIdx.x] * 0x1p-40;
-      double all;
-      const double upto = ask.before(own, all) + own;
-      floor = min(floor, ask.least(upto >= masses * (double)lim.p * (1.0 + 1e-9) ? (int)threadIdx.x : kNone));
+    constexpr int kOwn = kBins / kDraw;
+    auto lower = [&](auto sum_in, auto reached) __attribute__((always_inline)) {  // the first bin up to which the sum has been reached
+      decltype(sum_in(0)) own[kOwn], sum = 0, all;
+#pragma unroll
+      for (int q = 0; q < kOwn; ++q) sum += own[q] = sum_in(threadIdx.x * kOwn + q);
+      auto upto = ask.before(sum, all);
+      int at = -1;
+#pragma unroll
+      for (int q = 0; q < kOwn; ++q) {
+        upto += own[q];
+        if (at < 0 && reached(upto)) at = threadIdx.x * kOwn + q;
+      }
+      const int who = ask.first(at >= 0);
+      if (who == (int)threadIdx.x) s.found = at;
+      __syncthreads();
+      if (who >= 0) floor = min(floor, s.found);
+    };
+    if (lim.k) lower([&](int i) { return (int)s.bins.count[i]; }, [&](int n) { return n >= lim.k; });
+    if (by_mass) {
+      const double goal = masses * (double)lim.p * (1.0 + 1e-9);
+      lower([&](int i) { return s.bins.mass[i]; }, [&](unsigned long long m) { return (double)m * 0x1p-40 >= goal; });
     }
     mass_floor = floor;
     // a little below the smallest logit that min_p lets stay (a top-p of what top-k leaves asks for the mass of all of that)
@@ -555,104 +660,80 @@ struct Drawer {
     return floor;
   }
 
-  // False: too many.
-  __device__ bool draw_few(int floor) {
-    const int groups = (row.blocks + kGroupBlocks - 1) / kGroupBlocks;
-    const float* group = prm.group + (int64_t)r * prm.parts * kGroups;
-    int chosen = 0;  // groups, in their order
-    for (int base = 0; base < groups; base += kDraw) {
-      const int i = base + threadIdx.x;
-      const float l = i < groups ? seen(group[i]) : -INFINITY;
-      const bool in = l > -INFINITY && bin_of(l) <= floor;
-      int all;
-      const int at = chosen + ask.before((int)in, all);
-      chosen += all;
-      if (chosen > kFewGroups) return false;
-      if (in) s.groups[at] = i;
-    }
+  // The tokens down to a bin into s.logit and s.number, in their order; how many, or -1: too many.
+  __device__ __forceinline__ int list_down_to(int floor) {
+    int own = 0, chosen;
+    each_group([&](float l, int) {
+      l = seen(l);
+      own += l > -INFINITY && bin_of(l) <= floor;
+    });
+    int at = ask.before(own, chosen);
+    if (chosen > kFewGroups) return -1;
+    each_group([&](float l, int i) {
+      l = seen(l);
+      if (l > -INFINITY && bin_of(l) <= floor) s.groups[at++] = i;
+    });
     __syncthreads();
     int n = 0;
-    for (int base = 0; base < chosen; base += kDraw / kGroupBlocks) {
-      const int g = base + threadIdx.x / kGroupBlocks;
-      float x[E];
-      int own = 0, block = 0;
+    for (int base = 0; base < chosen; base += kRounds * (kDraw / kGroupBlocks)) {
+      float x[kRounds][E];
+      int block[kRounds], many[kRounds], upto[kRounds];
+      ask.turn ^= 1;
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = -INFINITY;
-      if (g < chosen) {
-        block = s.groups[g] * kGroupBlocks + threadIdx.x % kGroupBlocks;
-        if (block < row.blocks) read(block, x);
+      for (int q = 0; q < kRounds; ++q) {
+        const int g = base + q * (kDraw / kGroupBlocks) + threadIdx.x / kGroupBlocks;
+        block[q] = row.blocks;
+        if (g < chosen) block[q] = s.groups[g] * kGroupBlocks + threadIdx.x % kGroupBlocks;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[q][e] = -INFINITY;
+        if (block[q] < row.blocks) read(block[q], x[q]);
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) own += x[e] > -INFINITY && bin_of(x[e]) <= floor;
-      int all;
-      int at = n + ask.before(own, all);
-      n += all;
-      if (n > kFew) return false;
+      for (int q = 0; q < kRounds; ++q) {
+        many[q] = upto[q] = 0;
+        if (base + q * (kDraw / kGroupBlocks) < chosen) {
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (x[e] > -INFINITY && bin_of(x[e]) <= floor) {
-          s.few.logit[at] = x[e];
-          s.few.number[at] = row.number(block) + e;
-          ++at;
+          for (int e = 0; e < E; ++e) {
+            if (bin_of(x[q][e]) > floor) x[q][e] = -INFINITY;
+            many[q] += x[q][e] > -INFINITY;
+          }
+          upto[q] = upto_lane(many[q]);
         }
-    }
-    __syncthreads();
-    constexpr int kOwn = kFew / kDraw;
-    float l[kOwn];
-    int rank[kOwn];
-    double m[kOwn];
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {  // (thread t has the tokens kOwn * t on)
-      const int i = threadIdx.x * kOwn + q;
-      l[q] = i < n ? s.few.logit[i] : -INFINITY;
-      m[q] = i < n ? mass(l[q]) : 0.0;
-      rank[q] = 0;
-    }
-    if ((int)threadIdx.x * kOwn < n) {
-      for (int j = 0; j < n; ++j) {
-        const float o = s.few.logit[j];
-#pragma unroll
-        for (int q = 0; q < kOwn; ++q) rank[q] += o > l[q] || (o == l[q] && j < (int)threadIdx.x * kOwn + q);
+        if (ask.lane() == 63) s.rounds[ask.turn][q][ask.wave()] = upto[q];
       }
-    }
+      __syncthreads();
+      int sum = n;
 #pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const int i = threadIdx.x * kOwn + q;
-      if (i >= n) continue;
-      s.few.mass[i] = m[q];
-      s.few.ranked[rank[q]] = lim.k && rank[q] >= lim.k ? 0.0 : m[q];
+      for (int q = 0; q < kRounds; ++q)
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          if (w == ask.wave()) upto[q] += sum - many[q];
+          sum += s.rounds[ask.turn][q][w];
+        }
+      n = sum;
+      if (n > kFew) return -1;
+#pragma unroll
+      for (int q = 0; q < kRounds; ++q)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (x[q][e] > -INFINITY) {
+            s.logit[upto[q]] = x[q][e];
+            s.number[upto[q]] = row.number(block[q]) + e;
+            ++upto[q];
+          }
     }
     __syncthreads();
-    double own[kOwn], sum = 0.0, ranked;
+    return n;
+  }
+
+  // The n tokens of the list and which of them stay (a thread has the tokens kOwn * t on).
+  template <int kOwn>
+  __device__ __forceinline__ void draw_of(int n, const double (&stay)[kOwn]) {
+    double own = 0.0, total;
 #pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const int i = threadIdx.x * kOwn + q;
-      own[q] = i < n ? s.few.ranked[i] : 0.0;
-      sum += own[q];
-    }
-    double at = ask.before(sum, ranked);
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const int i = threadIdx.x * kOwn + q;
-      if (i < n) s.few.ranked[i] = at;
-      at += own[q];
-    }
-    __syncthreads();
-    const double limit = (double)lim.p * (lim.k ? ranked : masses);
-    // (roundings: the last one that stays may not be among these)
-    if (lim.p < 1.f && !lim.k && floor == mass_floor && !(ranked >= limit)) return false;
-    double stay[kOwn], mine_all = 0.0, total;
-#pragma unroll
-    for (int q = 0; q < kOwn; ++q) {
-      const int i = threadIdx.x * kOwn + q;
-      bool in = i < n && (!lim.k || rank[q] < lim.k) && m[q] >= (double)lim.m;
-      if (lim.p < 1.f) in = in && (rank[q] == 0 || s.few.ranked[rank[q]] < limit);
-      stay[q] = in ? m[q] : 0.0;
-      mine_all += stay[q];
-    }
-    const double from = ask.before(mine_all, total), target = u * total;
-    int who = ask.least(mine_all > 0.0 && from + mine_all > target ? (int)threadIdx.x : kNone);
-    if (who == kNone) who = -ask.least(mine_all > 0.0 ? -(int)threadIdx.x : kNone);
+    for (int q = 0; q < kOwn; ++q) own += stay[q];
+    const double from = ask.before(own, total), target = u * total;
+    const int who = thread_with(target, own, from);
     if ((int)threadIdx.x == who) {
       double upto = from;
       bool done = false;
@@ -661,206 +742,502 @@ struct Drawer {
         if (stay[q] > 0.0 && !done) {
           upto += stay[q];
           done = upto > target;
-          s.found = s.few.number[threadIdx.x * kOwn + q];
+          s.found = s.number[threadIdx.x * kOwn + q];
           s.value = stay[q];
         }
     }
     __syncthreads();
-    answer(s.found, s.value / total);
+    number = s.found;
+    prob = s.value / total;
+  }
+
+  // Up to kCounted tokens: each is compared with each, by two threads.
+  __device__ __forceinline__ bool draw_counted(int n, bool all_there) {
+    const int i = threadIdx.x / 2, half = threadIdx.x & 1;
+    const bool in = i < n;
+    const float l = in ? s.logit[i] : -INFINITY;
+    int rank = 0;
+    if (in) {
+#pragma unroll 4
+      for (int j = half; j < n; j += 2) {
+        const float o = s.logit[j];
+        rank += o > l || (o == l && j < i);
+      }
+    }
+    rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, false);  // (the neighbour's half)
+    const double m = in ? mass(l) : 0.0;
+    const bool first_k = !lim.k || rank < lim.k;
+    bool stays = in && first_k && m >= (double)lim.m;
+    if (lim.p < 1.f) {
+      if (in && half == 0) s.ranked[rank] = first_k ? m : 0.0;
+      __syncthreads();
+      double ranked;
+      const double own = threadIdx.x < n ? s.ranked[threadIdx.x] : 0.0;
+      const double upto = ask.before(own, ranked);
+      if ((int)threadIdx.x < n) s.ranked[threadIdx.x] = upto;
+      __syncthreads();
+      const double limit = (double)lim.p * (lim.k ? ranked : masses);
+      // (roundings: the last one that stays may not be among these)
+      if (!lim.k && !all_there && !(ranked >= limit)) return false;
+      stays = stays && (rank == 0 || s.ranked[rank] < limit);
+    }
+    const double stay[1] = {stays && half == 0 ? m : 0.0};
+    // (two threads a token: the list is looked up by the pair)
+    double total;
+    const double from = ask.before(stay[0], total), target = u * total;
+    const int who = thread_with(target, stay[0], from);
+    if ((int)threadIdx.x == who) {
+      s.found = s.number[i];
+      s.value = m;
+    }
+    __syncthreads();
+    number = s.found;
+    prob = s.value / total;
     return true;
   }
 
-  // ---- any number of them stays
-  // The last token in rank that stays when `goal` tokens (by_mass: tokens before which less than `goal` of the mass lies) do: its logit's key, and how many tokens
-  // and how much mass lie above, and how many are equal.
+  // The last token in rank that stays when the first `goal` tokens do (by_mass: those before which less than `goal_mass` lies), found eleven bits of
+  // its logit's place at a time: that logit, and how many tokens and how much mass lie above it, and how many are its equals.
+  // Of the n tokens of the list, or of all of the row where n is negative; `above` and `mass_above` lie above all of these.
   struct Last {
-    uint32_t key;
+    float logit;
     int above, equal;
     double mass_above;
   };
-  __device__ Last last_of(bool by_mass, int goal, double goal_mass, double unit) {
-    Last x = {0, 0, 0, 0.0};
-    unsigned long long above = 0;
-    constexpr int kShifts[] = {21, 10, 0};
+  __device__ __forceinline__ Last last_of(int n, bool by_mass, int goal, double goal_mass, int above, double mass_above) {
+    // masses as whole numbers: of so many units, so that those of all tokens fit
+    const double unit = ldexp(1.0, 62 - (32 - __builtin_clz((unsigned)prm.V)));
+    unsigned long long whole_above = (unsigned long long)rint(mass_above * unit);
     const unsigned long long whole_goal = by_mass ? (unsigned long long)fmin(ceil(goal_mass * unit), 0x1p62) : 0;
-#pragma unroll
+    const bool need_mass = lim.p < 1.f;
+    uint32_t key = 0;
+    int equal = 0;
+#pragma unroll 1
     for (int level = 0; level < (sizeof(T) == 2 ? 2 : 3); ++level) {
-      const int shift = kShifts[level], bits = level == 2 ? 10 : 11;
+      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
       __syncthreads();
       for (int i = threadIdx.x; i < kDigits; i += kDraw) {
         s.digits.count[i] = 0;
         s.digits.mass[i] = 0;
       }
       __syncthreads();
-      for (int block = threadIdx.x; block < row.blocks; block += kDraw) {
-        float v[E];
-        read(block, v);
+      auto take = [&](float l) {
+        const uint32_t k = key_of(l);
+        if (l == -INFINITY || (level && k >> (shift + bits) != key >> (shift + bits))) return;
+        const int digit = k >> shift & ((1 << bits) - 1);
+        atomicAdd(&s.digits.count[digit], 1u);
+        if (need_mass) atomicAdd(&s.digits.mass[digit], (unsigned long long)rint(mass(l) * unit));
+      };
+      if (n >= 0) {
+        for (int i = threadIdx.x; i < n; i += kDraw) take(s.logit[i]);
+      } else {
+        each_logit(take);
+      }
+      __syncthreads();
+      // some digits a thread, the largest first
+      constexpr int kOwn = kDigits / kDraw;
+      int many[kOwn], sum = 0, all;
+      unsigned long long whole[kOwn], whole_sum = 0, whole_upto = 0, whole_all;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const uint32_t key = key_of(v[e]);
-          if (v[e] == -INFINITY || (level && key >> (shift + bits) != x.key >> (shift + bits))) continue;
-          const int digit = key >> shift & ((1 << bits) - 1);
-          atomicAdd(&s.digits.count[digit], 1u);
-          if (lim.p < 1.f) atomicAdd(&s.digits.mass[digit], (unsigned long long)rint(mass(v[e]) * unit));
+      for (int q = 0; q < kOwn; ++q) {
+        const int digit = kDigits - 1 - (threadIdx.x * kOwn + q);
+        sum += many[q] = s.digits.count[digit];
+        whole_sum += whole[q] = s.digits.mass[digit];
+      }
+      int upto = above + ask.before(sum, all);
+      if (need_mass) whole_upto = whole_above + ask.before(whole_sum, whole_all);
+      // the first one with which the goal is reached; or the last one there is
+      int at = -1, last = -1, at_above = 0, last_above = 0, at_many = 0, last_many = 0;
+      unsigned long long at_whole = 0, last_whole = 0;
+#pragma unroll
+      for (int q = 0; q < kOwn; ++q) {
+        if (!many[q]) continue;
+        last = threadIdx.x * kOwn + q;
+        last_above = upto, last_many = many[q], last_whole = whole_upto;
+        upto += many[q];
+        whole_upto += whole[q];
+        if (at < 0 && (by_mass ? whole_upto >= whole_goal : upto >= goal)) {
+          at = last;
+          at_above = last_above, at_many = last_many, at_whole = last_whole;
         }
       }
-      __syncthreads();
-      // two digits a thread, the largest first
-      const int high = kDigits - 1 - 2 * (int)threadIdx.x, low = high - 1;
-      const int n_high = s.digits.count[high], n_low = s.digits.count[low];
-      const unsigned long long m_high = s.digits.mass[high], m_low = s.digits.mass[low];
-      int all;
-      const int n_before = x.above + ask.before(n_high + n_low, all);
-      const unsigned long long m_before = above + before_whole(m_high + m_low);
-      int found = kNone;
-      if (by_mass) {
-        if (n_low && m_before + m_high + m_low >= whole_goal) found = 2 * threadIdx.x + 1;
-        if (n_high && m_before + m_high >= whole_goal) found = 2 * threadIdx.x;
-      } else {
-        if (n_low && n_before + n_high + n_low >= goal) found = 2 * threadIdx.x + 1;
-        if (n_high && n_before + n_high >= goal) found = 2 * threadIdx.x;
+      int who = ask.first(at >= 0);
+      if (who < 0) {
+        who = ask.last(last >= 0);
+        at = last, at_above = last_above, at_many = last_many, at_whole = last_whole;
       }
-      int first = ask.least(found);
-      if (first == kNone) first = -ask.least(n_low ? -(2 * (int)threadIdx.x + 1) : n_high ? -2 * (int)threadIdx.x : kNone);  // (the last one there is)
-      if (first / 2 == (int)threadIdx.x) {
-        const bool is_low = first % 2;
-        s.key = x.key | (uint32_t)(is_low ? low : high) << shift;
-        s.found = n_before + (is_low ? n_high : 0);
-        s.count = is_low ? n_low : n_high;
-        s.whole = m_before + (is_low ? m_high : 0);
+      if (who == (int)threadIdx.x) {
+        s.key = key | (uint32_t)(kDigits - 1 - at) << shift;
+        s.found = at_above;
+        s.count = at_many;
+        s.whole = at_whole;
       }
       __syncthreads();
-      x.key = s.key;
-      x.above = s.found;
-      x.equal = s.count;
-      above = s.whole;
+      key = s.key;
+      above = s.found;
+      equal = s.count;
+      whole_above = s.whole;
     }
-    if (sizeof(T) == 2 && !(x.key & 0x80000000u)) x.key |= (1u << kShifts[1]) - 1;  // (of bf16 the low bits are all alike)
-    x.mass_above = (double)above / unit;
-    return x;
-  }
-  // (whole numbers: in any order)
-  __device__ unsigned long long before_whole(unsigned long long v) {
-    unsigned long long upto = v;
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) {
-      const unsigned long long o = __shfl_up(upto, i);
-      if (ask.lane() >= i) upto += o;
-    }
-    ask.turn ^= 1;
-    unsigned long long* sums = reinterpret_cast<unsigned long long*>(s.sums[ask.turn]);
-    if (ask.lane() == 63) sums[ask.wave()] = upto;
-    __syncthreads();
-    unsigned long long base = 0;
-    for (int w = 0; w < ask.wave(); ++w) base += sums[w];
-    return base + upto - v;
+    if (sizeof(T) == 2 && !(key & 0x80000000u)) key |= (1u << 10) - 1;  // (of bf16 the low bits are all alike)
+    return {logit_of(key), above, equal, (double)whole_above / unit};
   }
 
-  __device__ void draw_any() {
-    float last = -INFINITY;  // those above stay, and the first `left` of its equals
-    int left = 0;
-    // masses as whole numbers: of so many units, so that those of all tokens fit
-    const double unit = ldexp(1.0, 62 - (32 - __builtin_clz((unsigned)prm.V)));
+  // Which tokens stay: those above `last`, and the first `left` of its equals.
+  struct Border {
+    float last;
+    int left;
+  };
+  __device__ __forceinline__ Border border_of(int n, int above, double mass_above) {
+    Border x = {-INFINITY, 0};
     double all = masses;
-    if (lim.k) {
-      const Last x = last_of(false, lim.k, 0.0, unit);
-      last = logit_of(x.key);
-      left = min(lim.k - x.above, x.equal);
-      all = x.mass_above + left * mass(last);
-    }
-    if (lim.p < 1.f) {
+#pragma unroll 1
+    for (int by_mass = lim.k ? 0 : 1; by_mass < (lim.p < 1.f ? 2 : 1); ++by_mass) {
       const double goal = (double)lim.p * all;
-      const Last x = last_of(true, 0, goal, unit);
-      const float l = logit_of(x.key);
-      const double room = ceil((goal - x.mass_above) / mass(l));
-      int n = room < x.equal ? (int)fmax(room, 0.0) : x.equal;
-      if (x.above == 0 && n < 1) n = 1;
-      if (lim.k && l == last) n = min(n, left);
-      if (!lim.k || l >= last) {
-        last = l;
-        left = n;
+      const Last y = last_of(n, by_mass, lim.k, goal, above, mass_above);
+      if (!by_mass) {
+        x = {y.logit, min(lim.k - y.above, y.equal)};
+        all = y.mass_above + x.left * mass(x.last);
+        continue;
       }
+      const double room = ceil((goal - y.mass_above) / mass(y.logit));
+      int many = room < y.equal ? (int)fmax(room, 0.0) : y.equal;
+      if (y.above == 0 && many < 1) many = 1;
+      if (lim.k && y.logit == x.last) many = min(many, x.left);
+      if (!lim.k || y.logit >= x.last) x = {y.logit, many};
     }
-    __syncthreads();
-    // the mass of each part that stays for sure, and how many of its tokens are equal to the last one
-    for (int i = threadIdx.x >> 6; i < prm.parts; i += kWaves) {
-      double sum = 0.0;
-      int same = 0;
+    return x;
+  }
+
+  // More than kCounted tokens of the list.
+  __device__ __forceinline__ bool draw_listed(int n, bool all_there) {
+    constexpr int kOwn = kFew / kDraw;
+    float l[kOwn];
+    double m[kOwn], sum = 0.0;
+    int same = 0;
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int block = i * kPartBlocks + j * 64 + (threadIdx.x & 63);
-        if (block >= row.blocks) continue;
-        float x[E];
-        read(block, x);
+    for (int q = 0; q < kOwn; ++q) {
+      const int i = threadIdx.x * kOwn + q;
+      l[q] = i < n ? s.logit[i] : -INFINITY;
+      m[q] = i < n ? mass(l[q]) : 0.0;
+      sum += m[q];
+    }
+    if (lim.p < 1.f && !lim.k && !all_there) {
+      double listed;
+      ask.before(sum, listed);
+      if (!(listed >= (double)lim.p * masses)) return false;
+    }
+    Border x = {-INFINITY, 0};
+    if (lim.k || lim.p < 1.f) x = border_of(n, 0, 0.0);
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) same += l[q] == x.last;
+    int all;
+    int nth = ask.before(same, all);
+    double stay[kOwn];
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+      const bool in = l[q] > x.last || (l[q] == x.last && nth < x.left);
+      nth += l[q] == x.last;
+      stay[q] = in && m[q] >= (double)lim.m ? m[q] : 0.0;
+    }
+    draw_of(n, stay);
+    return true;
+  }
+
+  // ---- any number of them stays
+  // kLoads blocks of a thread, at, at + step, ..., all asked for at once and then taken one by one: f(block, its logits).
+  struct Blocks {
+    u32x4 w0, w1, w2, w3;
+  };
+  __device__ __forceinline__ void ask_for(int at, int step, Blocks& b) const {
+    static_assert(kLoads == 4, "blocks in flight");
+    if (row.whole(at)) b.w0 = row.load(at);
+    if (row.whole(at + step)) b.w1 = row.load(at + step);
+    if (row.whole(at + 2 * step)) b.w2 = row.load(at + 2 * step);
+    if (row.whole(at + 3 * step)) b.w3 = row.load(at + 3 * step);
+  }
+  template <typename F>
+  __device__ __forceinline__ void take(int at, int step, Blocks b, F f) const {
+#pragma unroll 1
+    for (int j = 0; j < kLoads; ++j) {
+      float x[E];
+      row.spread(b.w0, x);
+      if (!row.whole(at)) row.edge(at, x);
+      if (top == INFINITY) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = finite_top(x[e]);
+      }
+      f(at, x);
+      at += step;
+      b.w0 = b.w1, b.w1 = b.w2, b.w2 = b.w3;
+    }
+  }
+  // All logits of the row.
+  template <typename F>
+  __device__ __forceinline__ void each_logit(F f) const {
+    Blocks now = {}, next = {};
+    ask_for(threadIdx.x, kDraw, now);
+    for (int base = threadIdx.x; base < row.blocks; base += kLoads * kDraw) {
+      ask_for(base + kLoads * kDraw, kDraw, next);
+      take(base, kDraw, now, [&](int, const float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) f(x[e]);
+      });
+      now = next;
+    }
+  }
+  // The parts, a wave each: f(part, take_part), and take_part(g) calls g(block, its logits) for its blocks.
+  template <typename F>
+  __device__ __forceinline__ void each_part(F f) const {
+    Blocks now = {}, next = {};
+    auto at = [&](int i) { return i * kPartBlocks + ask.lane(); };
+    ask_for(at(ask.wave()), 64, now);
+    for (int i = ask.wave(); i < prm.parts; i += kWaves) {
+      ask_for(at(i + kWaves), 64, next);
+      f(i, [&](auto g) { take(at(i), 64, now, g); });
+      now = next;
+    }
+  }
+
+  // With a top-p alone: the last token that stays is looked for among those of a few bins.  A token of less than the share (1 - p) / V of all mass never stays (all of them together have
+  // less than 1 - p); from there to the largest logit the row's logits are counted in kWide bins, and from how many are in a bin follows of
+  // how much mass they are at least and at most.  Those above the bins in which the limit can lie stay for sure: their mass is added up part by
+  // part.  False: too many are in those bins.
+  __device__ __forceinline__ bool draw_between(Where& where) {
+    const float depth = -(float)log((1.0 - (double)lim.p) * masses / prm.V) * lim.T;  // (of the smallest that can stay)
+    const float range = depth * 1.0001f + 1e-4f * (fabsf(ref) + lim.T);
+    if (!(range > 0.f) || !(range < 1e30f)) return false;
+    const float to_bin = kWide / range;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kWide; i += kDraw) s.wide[i] = 0;
+    if (threadIdx.x == 0) s.taken = 0;
+    __syncthreads();
+    each_logit([&](float l) {
+      const float at = (ref - l) * to_bin;
+      if (at < (float)kWide) atomicAdd(&s.wide[(int)at], 1u);
+    });
+    __syncthreads();
+    constexpr int kOwn = kWide / kDraw;
+    const double step = -(double)range / kWide * c, goal = (double)lim.p * masses;
+    double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0, all;
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+      const int bin = threadIdx.x * kOwn + q;
+      const double n = s.wide[bin];  // (bins are told apart in 32 bits: their ends are off by 2^-11 of a bin at most)
+      most_sum += most[q] = n * exp2_64((bin - 0.01) * step < 0.0 ? (bin - 0.01) * step : 0.0);
+      least_sum += least[q] = n * exp2_64((bin + 1.01) * step);
+    }
+    double most_upto = ask.before(most_sum, all), least_upto = ask.before(least_sum, all);
+    int begin = kWide, end = kWide;  // the limit lies in no bin before `begin`, and no token behind `end` stays
+#pragma unroll
+    for (int q = 0; q < kOwn; ++q) {
+      most_upto += most[q];
+      least_upto += least[q];
+      if (begin == kWide && most_upto >= goal * (1.0 - 1e-9)) begin = threadIdx.x * kOwn + q;
+      if (end == kWide && least_upto >= goal * (1.0 + 1e-9)) end = threadIdx.x * kOwn + q;
+    }
+    {
+      const int who = ask.first(begin < kWide);
+      if (who < 0) return false;
+      if (who == (int)threadIdx.x) s.found = begin;
+      const int then = ask.first(end < kWide);
+      if (then == (int)threadIdx.x) s.count = end;
+      __syncthreads();
+      begin = s.found;
+      end = then < 0 ? kWide - 1 : s.count;
+    }
+    // the parts' sure masses, and the tokens between: a stretch of the list for each part
+    double sure = 0.0;
+    each_part([&](int i, auto take_part) {
+      double sum = 0.0;
+      int many = 0;
+      // (of 64 blocks, those that stay for sure are put together first: few do, but some in every 64)
+      float* const sure_ones = reinterpret_cast<float*>(s.wide) + ask.wave() * (kWide / kWaves);
+      static_assert(kWide / kWaves >= 64 * E, "room for all of 64 blocks");
+      take_part([&](int, const float (&x)[E]) {
+        int n = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          same += x[e] == last;
-          if (x[e] > last) {
-            const double w = mass(x[e]);
+          const float at = (ref - x[e]) * to_bin;
+          const uint64_t in = __ballot(at < (float)begin);
+          if (at < (float)begin) sure_ones[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = x[e];
+          n += __popcll(in);
+          many += at >= (float)begin && at < (float)(end + 1);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        double two = 0.0;
+        for (int j = ask.lane(); j < n; j += 128) {
+          const float l = sure_ones[j], o = j + 64 < n ? sure_ones[j + 64] : -INFINITY;
+          sum += mass(l);
+          two += mass(o);
+        }
+        sum += two;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      });
+      sum = sum_wave(sum);
+      const int upto = upto_lane(many), all_of = __builtin_amdgcn_readlane(upto, 63);
+      int to = 0;
+      if (ask.lane() == 0) to = atomicAdd(&s.taken, all_of);
+      to = __builtin_amdgcn_readfirstlane(to);
+      if (all_of && to + all_of <= kList) {
+        int at_list = to + upto - many;
+        take_part([&](int block, const float (&x)[E]) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float at = (ref - x[e]) * to_bin;
+            if (at >= (float)begin && at < (float)(end + 1)) {
+              s.logit[at_list] = x[e];
+              s.number[at_list] = row.number(block) + e;
+              ++at_list;
+            }
+          }
+        });
+      }
+      if (ask.lane() == 0) part[i] = Part(sum, 0.0, to, all_of);
+    });
+    __syncthreads();
+    const int n = s.taken;
+    if (n > kList) return false;
+    const int from = from_part(), to = to_part();
+    for (int i = from; i < to; ++i) sure += part[i].mass;
+    double sure_all;
+    ask.before(sure, sure_all);
+    // (in the first place that is not before all of them there is one token at least above: `above` counts as one where any mass lies above)
+    const Border x = border_of(n, begin > 0 && sure_all > 0.0 ? 1 : 0, sure_all);
+    const double each = mass(x.last);
+    int same = 0, unused;
+    for (int i = from; i < to; ++i) {
+      const Part y = part[i];
+      for (int j = 0; j < y.many; ++j) same += s.logit[y.first + j] == x.last;
+    }
+    int nth = ask.before(same, unused);
+    const int same_before = nth;
+    auto mass_in = [&](int i) {
+      const Part y = part[i];
+      double sum = y.mass;
+      int equal = 0;
+      for (int j = 0; j < y.many; ++j) {
+        const float l = s.logit[y.first + j];
+        equal += l == x.last;
+        if (l > x.last) sum += mass(l);
+      }
+      sum += min(max(x.left - nth, 0), equal) * each;
+      nth += equal;
+      return sum;
+    };
+    double own = 0.0, total;
+    for (int i = from; i < to; ++i) own += mass_in(i);
+    const double base = ask.before(own, total), target = u * total;
+    nth = same_before;
+    double base_of_part;
+    const int i = part_with(target, own, base, mass_in, base_of_part);
+    int equal = 0, equal_all;  // in the parts before
+    for (int j = threadIdx.x; j < n; j += kDraw) equal += s.logit[j] == x.last && s.number[j] < row.number(i * kPartBlocks);
+    ask.before(equal, equal_all);
+    where = {i, base_of_part, target, total, x.last, equal_all, x.left};
+    return true;
+  }
+
+  __device__ __forceinline__ Where draw_any() {
+    Border x = {-INFINITY, 0};
+    if (lim.k || lim.p < 1.f) x = border_of(-1, 0, 0.0);
+    __syncthreads();
+    // the mass of each part that stays for sure, and how many of its tokens are equal to the last one
+    each_part([&](int i, auto take_part) {
+      double sum = 0.0;
+      int same = 0;
+      take_part([&](int, const float (&y)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          same += y[e] == x.last;
+          if (y[e] > x.last) {
+            const double w = mass(y[e]);
             sum += w >= (double)lim.m ? w : 0.0;
           }
         }
-      }
+      });
       sum = sum_wave(sum);
-#pragma unroll
-      for (int j = 1; j < 64; j *= 2) same += __shfl_xor(same, j);
-      if ((threadIdx.x & 63) == 0) part[i] = Part{sum, as_f32((uint32_t)same), 0.f};
-    }
+      same = upto_lane(same);
+      if (ask.lane() == 63) part[i] = Part(sum, 0.0, 0, same);
+    });
     __syncthreads();
-    const int from = threadIdx.x * per(), to = min(from + per(), prm.parts);
+    const int from = from_part(), to = to_part();
     int same = 0, unused;
-    for (int i = from; i < to; ++i) same += (int)as_u32(part[i].top);
+    for (int i = from; i < to; ++i) same += part[i].many;
     const int same_before = ask.before(same, unused);
-    double each = last > -INFINITY ? mass(last) : 0.0;
+    double each = x.last > -INFINITY ? mass(x.last) : 0.0;
     if (!(each >= (double)lim.m)) each = 0.0;
     int nth = same_before;
+    auto mass_in = [&](int j) {
+      const Part y = part[j];
+      const int stay = min(max(x.left - nth, 0), y.many);
+      nth += y.many;
+      return y.mass + stay * each;
+    };
     double own = 0.0, total;
-    for (int i = from; i < to; ++i) {
-      const Part x = part[i];
-      const int n = (int)as_u32(x.top), stay = min(max(left - nth, 0), n);
-      own += x.mass + stay * each;
-      nth += n;
-    }
+    for (int i = from; i < to; ++i) own += mass_in(i);
     const double base = ask.before(own, total), target = u * total;
+    nth = same_before;
     double base_of_part;
-    int walked = same_before;
-    const int i = part_with(target, own, base, [&](int j) {
-      const Part x = part[j];
-      const int n = (int)as_u32(x.top), stay = min(max(left - walked, 0), n);
-      walked += n;
-      return x.mass + stay * each;
-    }, base_of_part);
-    int equal = 0;  // in the parts before
-    for (int j = threadIdx.x; j < i; j += kDraw) equal += (int)as_u32(part[j].top);
-    int equal_all;
+    const int i = part_with(target, own, base, mass_in, base_of_part);
+    int equal = 0, equal_all;  // in the parts before
+    for (int j = threadIdx.x; j < i; j += kDraw) equal += part[j].many;
     ask.before(equal, equal_all);
-    draw_in(i, base_of_part, target, total, last, equal_all, left);
+    return {i, base_of_part, target, total, x.last, equal_all, x.left};
   }
 
-  __device__ void draw() {
-    sum_up();
-    if (top == -INFINITY) return answer(-1, 0.0);
-    if (lim.greedy) return greedy();
-    if (!lim.some) return draw_all();
+  __device__ __forceinline__ bool draw_few() {
     const int floor = floor_of();
+    if (floor == kBins - 1 && prm.V > kFew) return false;
     __syncthreads();
-    if (!draw_few(floor)) {
-      __syncthreads();
-      draw_any();
+    const int n = list_down_to(floor);
+    if (n < 0) return false;
+    // (a floor that min_p sets is below all that stay; so is the last bin)
+    const bool all_there = floor != mass_floor || floor == kBins - 1;
+    return n <= kCounted ? draw_counted(n, all_there) : draw_listed(n, all_there);
+  }
+
+  template <bool LIMITS>
+  __device__ __forceinline__ void draw() {
+    sum_up();
+    if (lim.greedy) {
+      if (top > -INFINITY) greedy();
+    } else if (top > -INFINITY) {
+      Where where;
+      bool drawn = false;
+      if (!LIMITS || !lim.some) {
+        where = draw_all();
+      } else if constexpr (LIMITS) {
+        drawn = draw_few();
+        if (!drawn) {
+          __syncthreads();
+          bool found = false;
+          if (lim.p < 1.f && !lim.k && !(lim.m > 0.f)) found = draw_between(where);
+          if (!found) {
+            __syncthreads();
+            where = draw_any();
+          }
+        }
+      }
+      if (!drawn) draw_in(where);
     }
+    answer();
   }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kDraw) void sample_draw_kernel(const SampleParams prm) {
-  __shared__ DrawShared shared;
+// Threads of a row with limits, and of one without.
+constexpr int kLimited = 512, kFree = 256;
+template <typename T, bool LIMITS>
+__global__ __launch_bounds__(LIMITS ? kLimited : kFree) void sample_draw_kernel(const SampleParams prm) {
+  constexpr int N = LIMITS ? kLimited : kFree;
+  typedef std::conditional_t<LIMITS, DrawShared<N>, AskShared<N>> Shared;
+  __shared__ Shared shared;
   const int r = blockIdx.x;
-  Drawer<T> d(prm, shared, r);
+  Drawer<T, N, Shared> d(prm, shared, r);
   float u = prm.uniform[r];
   u = u >= 0.f ? fminf(u, 1.f - 0x1p-24f) : u < 0.f ? 0.f : 1.f - 0x1p-24f;
   d.u = (double)u;
   d.c = d.lim.greedy ? 0.0 : d.lim.c();
-  d.draw();
+  d.template draw<LIMITS>();
 }
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
@@ -902,10 +1279,12 @@ int launch_sample(const void* logits, int64_t rows, int vocab, int dtype, int64_
     return MASKKV_ESHAPE;
   }
   auto parts_kernel = dtype == MASKKV_BF16 ? &sample_parts_kernel<bf16_t> : &sample_parts_kernel<float>;
-  auto draw_kernel = dtype == MASKKV_BF16 ? &sample_draw_kernel<bf16_t> : &sample_draw_kernel<float>;
+  const bool limits = sampling->top_k || sampling->top_p || sampling->min_p;
+  auto draw_kernel = dtype == MASKKV_BF16 ? (limits ? &sample_draw_kernel<bf16_t, true> : &sample_draw_kernel<bf16_t, false>)
+                                          : (limits ? &sample_draw_kernel<float, true> : &sample_draw_kernel<float, false>);
   hipLaunchKernelGGL(parts_kernel, dim3((unsigned)groups), dim3(256), 0, stream, prm);
   if (int e = check_launch("sample (parts)")) return e;
-  hipLaunchKernelGGL(draw_kernel, dim3((unsigned)rows), dim3(kDraw), 0, stream, prm);
+  hipLaunchKernelGGL(draw_kernel, dim3((unsigned)rows), dim3(limits ? kLimited : kFree), 0, stream, prm);
   return check_launch("sample");
 }
 
