@@ -36,6 +36,7 @@ struct TreeParams {
   int H, BH, q_per_kv, n_resp, n_q, qtiles, words;
   int units;      // at most
   int chunk;      // tiles of a workgroup, or 0: all of its head
+  int tile_rows;  // query rows of a workgroup
   int part_rows;  // of a partial result
   float c;        // scale * log2(e)
   float* lse;
@@ -356,6 +357,348 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
   }
 }
 
+// ---- many query rows of bf16: a workgroup of four waves serves 128 of a head, 32 a wave, over tiles of 64 keys that all of them read from LDS.  Two
+// workgroups share a compute unit, so that one's softmax runs beside the other's products, and within a wave the logits of the next
+// tile are formed beside the softmax of this one.
+//
+// Iteration t reads K(t+1) and V(t), and brings K(t+2) and V(t+1) into the other two of four buffers, which iteration t-1 has read: one barrier an
+// iteration.  Tiles of the response are taken first, each by itself: they are few, have a mask, and may hold what must not be multiplied.
+constexpr int kWideTile = 64;
+constexpr int kWideQueries = 128;
+
+template <int D>
+struct WideCfg {
+  static constexpr int kRowB = 2 * D;
+  static constexpr int kPPR = kRowB / 16;
+  static constexpr int kSteps = D / 16;
+  static constexpr int kDB = D / 32;
+  static constexpr int kTileB = kWideTile * kRowB;
+  static constexpr int kMoves = kWideTile * kRowB / 4096;  // direct transfers of 1 KiB a wave and tile
+  static constexpr int kMoveRows = 1024 / kRowB;
+  static constexpr int kProbs = 4 * kTileB;                // then: probabilities of a wave for 32 keys, fp32 (see add_seen)
+  static constexpr int kLds = kProbs + 4 * kTile * kTile * 4;
+  __device__ static uint32_t swz_k(uint32_t row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreeParams prm) {
+  using C = WideCfg<D>;
+  extern __shared__ __attribute__((aligned(1024))) char tree_lds[];
+  const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
+  const int unit = place.unit, qtile = place.qtile;
+  const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
+  auto tiles_of = [&](int rows) { return (int)(((uint32_t)rows + kWideTile - 1) / kWideTile) + resp_tiles; };  // those of the response first
+  const int capacity = (int)prm.capacity;
+  UnitHead head;
+  if (prm.chunk) {
+    head = head_of_unit(prm.cu, prm.BH, capacity, unit, [&](int rows) { return (tiles_of(rows) + prm.chunk - 1) / prm.chunk; });
+    if (head.bh < 0) return;
+  } else {
+    const int first = min(prm.cu[unit], capacity);
+    head = {unit, unit, 1, first, max(min(prm.cu[unit + 1], capacity) - first, 0)};
+  }
+  const int bh = head.bh, cached = head.rows, all_tiles = tiles_of(cached);
+  const int b = bh / prm.H, h = bh % prm.H;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 31, g = lane >> 5;
+  if (prm.chunk && unit == head.first_unit && qtile == 0 && threadIdx.x == 0) prm.parts[bh] = make_int2(head.first_unit, head.units);
+  const int t0 = prm.chunk ? (unit - head.first_unit) * prm.chunk : 0;
+  const int t1 = prm.chunk ? min(all_tiles, t0 + prm.chunk) : all_tiles;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)tree_lds;
+
+  // ---- tiles on their way: a wave takes a quarter of the rows
+  const uint32_t moved = wave * (kWideTile / 4) + (uint32_t)lane / C::kPPR;  // this lane's row of the wave's first transfer
+  const uint32_t piece_k = ((uint32_t)lane % C::kPPR ^ C::swz_k(moved)) << 4, piece_v = ((uint32_t)lane % C::kPPR ^ v_swizzle<D>(moved) << 1) << 4;
+  auto transfer = [&](const char* from, int64_t stride, int left, uint32_t piece, uint32_t step, uint32_t to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < C::kMoves; ++j) {  // (a row's permutation changes from a transfer to the next by an exclusive-or of its own)
+      const uint32_t row = min((int)moved + j * C::kMoveRows, left - 1);
+      dma16(from, row * (uint32_t)stride + (piece ^ (j * step & (C::kRowB - 1))), to + (wave * C::kMoves + j) * 1024);
+    }
+  };
+  const char* const kc = prm.Kc + (int64_t)head.first * C::kRowB;
+  const char* const vc = prm.Vc + (int64_t)head.first * C::kRowB;
+  // K and V of a tile of the cache (t: counted from its first one) into the buffer of even or odd tiles
+  auto bring_k = [&](int t, uint32_t odd) __attribute__((always_inline)) {
+    transfer(kc + (int64_t)t * C::kTileB, C::kRowB, cached - t * kWideTile, piece_k, C::swz_k(C::kMoveRows) << 4, lds0 + odd * C::kTileB);
+  };
+  auto bring_v = [&](int t, uint32_t odd) __attribute__((always_inline)) {
+    transfer(vc + (int64_t)t * C::kTileB, C::kRowB, cached - t * kWideTile, piece_v, 0, lds0 + (2 + odd) * C::kTileB);
+  };
+  auto arrive = [] {  // what this wave has moved is there, and so is everyone's behind the barrier
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  const int q0 = qtile * kWideQueries + wave * 32, query = min(q0 + r, prm.n_q - 1);
+  u32x4 qf[C::kSteps];
+  {
+    const char* q = prm.Q.group_row(b, h, prm.q_per_kv, prm.n_resp, query) + g * D;
+#pragma unroll
+    for (int i = 0; i < C::kSteps; ++i) qf[i] = *reinterpret_cast<const u32x4*>(q + 16 * i);
+  }
+
+  f32x16 o[C::kDB], even[2], odd[2];
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) o[db] = f32x16{};
+  float m = kNegBig, l = 0.f, top = 0.f;  // top: the largest logit of the tile whose turn comes next
+  const float c = prm.c;
+  uint32_t k_at[C::kSteps], v_at[C::kDB];
+#pragma unroll
+  for (int i = 0; i < C::kSteps; ++i) k_at[i] = lds0 + r * C::kRowB + (((C::kPPR / 2 * g + i) ^ C::swz_k(r)) << 4);
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db) v_at[db] = lds0 + 2 * C::kTileB + v_read_offset<D>(lane, db);
+
+  auto raise = [&]() __attribute__((always_inline)) {  // the reference, where the tile's largest logit asks for it
+    const float cand = max_halves(top) * c;
+    const bool bump = cand > m + kLazyBump;  // (see attend.hip)
+    if (__any(bump)) {
+      const float m_new = bump ? cand : m;
+      const float alpha = fast_exp2(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+  };
+
+  // ---- tiles of the response, in buffers 0 and 2
+  for (int t = t0; t < min(t1, resp_tiles); ++t) {
+    const int left = prm.n_resp - t * kWideTile;
+    const uint32_t* words = prm.mask + ((int64_t)b * prm.n_resp + query % prm.n_resp) * prm.words + 2 * t;
+    uint32_t word[2] = {words[0], 2 * t + 1 < prm.words ? words[1] : 0};
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      const int of = left - 32 * kb;
+      if (of < 32) word[kb] = of > 0 ? word[kb] & ((1u << of) - 1) : 0;
+    }
+    if (t > t0) arrive();  // (the tile before has been read)
+    transfer(prm.K2.row(b, h, t * kWideTile), prm.K2.stride_t, left, piece_k, C::swz_k(C::kMoveRows) << 4, lds0);
+    transfer(prm.V2.row(b, h, t * kWideTile), prm.V2.stride_t, left, piece_v, 0, lds0 + 2 * C::kTileB);
+    arrive();
+    if (!__any((word[0] | word[1]) != 0)) continue;  // (none of the wave's queries sees any of it)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      even[kb] = f32x16{};
+#pragma unroll
+      for (int i = 0; i < C::kSteps; ++i) {
+        const u32x4 f = *in_lds<const u32x4>(k_at[i], kb * 32 * C::kRowB);
+        mfma_step<bf16_t>(f, qf[i], even[kb]);
+      }
+      const uint32_t own = word[kb] >> (4 * g);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) even[kb][i] = own >> (8 * (i / 4) + i % 4) & 1 ? even[kb][i] : -INFINITY;
+    }
+    top = even[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, even[i / 16][i % 16]);
+    raise();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float p = fast_exp2(fmaf(even[i / 16][i % 16], c, -m));
+      even[i / 16][i % 16] = p;
+      l += p;
+    }
+    bool any = false;
+#pragma unroll 4
+    for (int j = 0; j < C::kTileB / 1024; ++j) {
+      const u32x4 w = *in_lds<const u32x4>(lds0 + 2 * C::kTileB + j * 1024 + lane * 16);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t bits = w[x];
+        any |= (bits & 0x7F800000u) == 0x7F800000u || (bits & 0x7F80u) == 0x7F80u;
+      }
+    }
+    if (__any(any)) {  // (see attend_tree_kernel: key by key, of those that the lane's query sees)
+      const uint32_t own = lds0 + C::kProbs + wave * kTile * kTile * 4;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        lds_is_read();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) *in_lds<float>(own + ((8 * (i / 4) + 4 * g + i % 4) * kTile + r) * 4) = even[kb][i];
+        lds_is_read();
+#pragma unroll 1
+        for (int j = 0; j < kTile; ++j) {
+          const float p = *in_lds<const float>(own + (j * kTile + r) * 4);
+          const bool sees = word[kb] >> j & 1;
+          const uint32_t row = kb * kTile + j;
+#pragma unroll
+          for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t e = 32 * db + 8 * q + 4 * g;
+              const u32x2 w = *in_lds<const u32x2>(lds0 + 2 * C::kTileB + row * C::kRowB + ((e / 8 ^ v_swizzle<D>(row) << 1) << 4) + e % 8 * 2);
+              const uint32_t w0 = w[0], w1 = w[1];
+              const float v[4] = {as_f32(w0 << 16), as_f32(w0 & 0xFFFF0000u), as_f32(w1 << 16), as_f32(w1 & 0xFFFF0000u)};
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[db][4 * q + x] = sees ? fmaf(p, v[x], o[db][4 * q + x]) : o[db][4 * q + x];
+            }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int tp = 0; tp < 4; ++tp) {
+        u32x4 pf;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(even[tp / 2][tp % 2 * 8 + 2 * w], even[tp / 2][tp % 2 * 8 + 2 * w + 1]);
+#pragma unroll
+        for (int db = 0; db < C::kDB; ++db) {
+          const u32x2 lo = read_transposed(v_at[db], tp * 16 * C::kRowB), hi = read_transposed(v_at[db], (tp * 16 + 8) * C::kRowB);
+          mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[db]);
+        }
+      }
+    }
+  }
+
+  // ---- tiles of the cache: from `begin` on, counted from its first one
+  const int begin = max(t0 - resp_tiles, 0), tiles = t1 - resp_tiles;
+  if (begin < tiles) {
+    if (t0 < resp_tiles) arrive();  // (the response's last tile has been read)
+    bring_k(begin, 0);
+    bring_v(begin, 0);
+    if (begin + 1 < tiles) bring_k(begin + 1, 1);
+    arrive();
+    // Fragment n of a tile: 0 .. kQK-1 of its keys (two chains of products, one for 32 keys each), from kQK on of the values of the tile before.
+    constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 2;
+    u32x4 fr[kAhead + 1];
+    auto fetch = [&](int n, uint32_t odd_k) __attribute__((always_inline)) {
+      u32x4& f = fr[n % (kAhead + 1)];
+      if (n < kQK) {
+        f = *in_lds<const u32x4>(k_at[n / 2], odd_k * C::kTileB + n % 2 * 32 * C::kRowB);
+      } else {
+        const int i = n - kQK, imm = (1 - odd_k) * C::kTileB + i / C::kDB * 16 * C::kRowB;
+        const u32x2 lo = read_transposed(v_at[i % C::kDB], imm), hi = read_transposed(v_at[i % C::kDB], imm + 8 * C::kRowB);
+        f = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    };
+    auto mask = [&](int t, f32x16 (&s)[2]) __attribute__((always_inline)) {  // keys behind the last one
+      const int left = cached - t * kWideTile;
+      if (left >= kWideTile) return;
+      const int mine = left - 4 * g;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (kb * 32 + 8 * (i / 4) + i % 4 >= mine) s[kb][i] = -INFINITY;
+    };
+#pragma unroll
+    for (int n = 0; n < kQK; ++n) {
+      fetch(n, 0);
+      if (n < 2) even[n] = f32x16{};
+      mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], even[n % 2]);
+    }
+    mask(begin, even);
+    top = even[0][0];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, even[i / 16][i % 16]);
+    arrive();  // (K(2) takes the place of K(0))
+
+    // Tile t (odd or not) with its logits in `s`; with MORE those of the next into `next`.  The next tile's logits are formed beside this one's
+    // exponentials, this one's part of the output beside the search for the next one's largest logit.
+    auto step = [&](int t, auto odd_tile, auto more, f32x16 (&s)[2], f32x16 (&next)[2]) __attribute__((always_inline)) {
+      constexpr uint32_t kOdd = decltype(odd_tile)::value;
+      constexpr bool kMore = decltype(more)::value;
+      constexpr int kFrom = kMore ? 0 : kQK;
+      if constexpr (kMore) {
+        if (t + 2 < tiles) bring_k(t + 2, kOdd);
+        bring_v(t + 1, 1 - kOdd);
+      }
+      raise();
+      u32x4 pf[4];
+      auto probabilities = [&](int i) __attribute__((always_inline)) {  // values i and i + 1 of the 32
+        const float p0 = fast_exp2(fmaf(s[i / 16][i % 16], c, -m)), p1 = fast_exp2(fmaf(s[i / 16][i % 16 + 1], c, -m));
+        l += p0 + p1;
+        uint32_t both = pack_bf16x2(p0, p1);
+        asm volatile("" : "+v"(both), "+v"(l));  // (formed here, beside the products, and not where it is first needed)
+        pf[i / 8][i % 8 / 2] = both;
+      };
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = 0; n < kAhead; ++n) fetch(kFrom + n, 1 - kOdd);
+      if constexpr (kMore) {
+#pragma unroll
+        for (int n = 0; n < kQK; ++n) {
+          fetch(n + kAhead, 1 - kOdd);
+          if (n < 2) next[n] = f32x16{};
+          mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], next[n % 2]);
+#pragma unroll
+          for (int i = n * 32 / kQK; i < (n + 1) * 32 / kQK; i += 2) probabilities(i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mask(t + 1, next);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) probabilities(i);
+      }
+      float high = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int n = kQK; n < kQK + kPV; ++n) {
+        if (n + kAhead < kQK + kPV) fetch(n + kAhead, 1 - kOdd);
+        mfma_step<bf16_t>(fr[n % (kAhead + 1)], pf[(n - kQK) / C::kDB], o[(n - kQK) % C::kDB]);
+        if constexpr (kMore) {
+#pragma unroll
+          for (int i = (n - kQK) * 32 / kPV; i < (n + 1 - kQK) * 32 / kPV; ++i) high = fmaxf(high, next[i / 16][i % 16]);
+          asm volatile("" : "+v"(high));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      top = high;
+      arrive();
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    int t = begin;
+    for (; t + 2 < tiles; t += 2) {
+      step(t, No(), Yes(), even, odd);
+      step(t + 1, Yes(), Yes(), odd, even);
+    }
+    if (t + 1 < tiles) {
+      step(t, No(), Yes(), even, odd);
+      step(t + 1, Yes(), No(), odd, even);
+    } else {
+      step(t, No(), No(), even, odd);
+    }
+  } else {
+    arrive();  // (what follows writes where the response's last tile was read)
+  }
+
+  // ---- out, by way of LDS: whole rows
+  l = sum_halves(l);
+  if (head.units > 1) {
+    if (q0 + r >= prm.n_q) return;
+    const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + wave * 32 + r;
+#pragma unroll
+    for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(prm.part_o + part * D + 32 * db + 8 * i + 4 * g) =
+            make_float4(o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]);
+    if (g == 0) prm.part_ml[part] = make_float2(m, l);
+    return;
+  }
+  const float by = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing)
+  char* own = tree_lds + wave * 32 * (C::kRowB + 16);
+#pragma unroll
+  for (int db = 0; db < C::kDB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<u32x2*>(own + r * (C::kRowB + 16) + (32 * db + 8 * i + 4 * g) * 2) =
+          u32x2{pack_bf16x2(o[db][4 * i] * by, o[db][4 * i + 1] * by), pack_bf16x2(o[db][4 * i + 2] * by, o[db][4 * i + 3] * by)};
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 32 * C::kPPR / 64; ++j) {
+    const int row = (j * 64 + lane) / C::kPPR, p = lane % C::kPPR;
+    if (q0 + row < prm.n_q)
+      *reinterpret_cast<u32x4*>(prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q0 + row) + p * 16) =
+          *reinterpret_cast<const u32x4*>(own + row * (C::kRowB + 16) + p * 16);
+  }
+  if (prm.lse && g == 0 && q0 + r < prm.n_q) prm.lse[(int64_t)bh * prm.n_q + q0 + r] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 // The partial results of the heads that have several units: sums in units of the largest reference.  D/4 threads take a query row and ask for
 // kAtOnce of its partial results before they use the first; where a head has many, the eight groups of a workgroup share one row
 // (SHARED) and meet in LDS, else each has a row of its own.
@@ -370,7 +713,7 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_tree_join_kernel(c
   const int first = prm.parts[bh].x, units = prm.parts[bh].y;
   if (units <= 1 || q >= prm.n_q) return;
   const int64_t step = (int64_t)prm.qtiles * prm.part_rows;
-  const int64_t in_unit = (int64_t)(q / kTile) * prm.part_rows + q % kTile;
+  const int64_t in_unit = (int64_t)(q / prm.tile_rows) * prm.part_rows + q % prm.tile_rows;
   float m = kNegBig, l = 0.f;
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int u0 = SHARED ? grp : 0; u0 < units; u0 += kAtOnce * kStep) {
@@ -461,33 +804,39 @@ __global__ __launch_bounds__(256) void tree_mask_kernel(const int32_t* parents, 
 
 // How the tiles are dealt out.
 struct Deal {
-  int qtiles, part_rows;
+  bool wide;      // 128 query rows a workgroup
+  int tile_rows, qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
   int64_t most_units;  // more than there are heads: what any capacity up to this one may have
 };
 constexpr int kSharedUnits = 16;  // units of a head on average above which a query row's partial results are read by a whole workgroup
-constexpr int kLeast = 2 * kWaves;  // tiles of a unit
+constexpr int kWideFrom = 64;     // query rows above which a workgroup has 128
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
+  const bool bf16 = d->dtype == MASKKV_BF16;
   Deal x;
-  x.qtiles = (n_q + kTile - 1) / kTile;
-  x.part_rows = n_q < kTile ? n_q : kTile;
-  const int64_t resp = (d->n_resp + kTile - 1) / kTile;
-  const int64_t places = (d->dtype == MASKKV_BF16 ? 2 : 1) * kUnits;
+  x.wide = bf16 && n_q > kWideFrom;
+  x.tile_rows = x.wide ? kWideQueries : kTile;
+  x.qtiles = (n_q + x.tile_rows - 1) / x.tile_rows;
+  x.part_rows = n_q < x.tile_rows ? n_q : x.tile_rows;
+  const int keys = x.wide ? kWideTile : kTile, once = x.wide ? 1 : kWaves;  // keys of a tile, tiles of a workgroup at once
+  const int64_t least = x.wide ? 4 : 2 * kWaves;                             // tiles of a unit
+  const int64_t resp = (d->n_resp + keys - 1) / keys;
+  const int64_t places = (bf16 ? 2 : 1) * kUnits;
   const int64_t wanted = (places + x.qtiles - 1) / x.qtiles;
   // whole heads where they fill the chip as they are, or none has more tiles than a unit
-  const int64_t longest = (d->P_max < capacity ? d->P_max : capacity) / kTile + 1 + resp;
+  const int64_t longest = (d->P_max < capacity ? d->P_max : capacity) / keys + 1 + resp;
   x.chunk = 0;
   x.units = x.most_units = BH;
-  if (BH * x.qtiles >= places || longest <= kLeast) return x;
+  if (BH * x.qtiles >= places || longest <= least) return x;
   x.most_units = wanted + BH;  // (of this capacity and of smaller ones)
-  const int64_t tiles = capacity / kTile + BH * (resp + 1);
+  const int64_t tiles = capacity / keys + BH * (resp + 1);
   int64_t chunk = (tiles + wanted - 1) / wanted;
-  if (chunk < kLeast) chunk = kLeast;
-  chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+  if (chunk < least) chunk = least;
+  chunk = (chunk + once - 1) / once * once;
   if (longest <= chunk) return x;
   x.chunk = (int)chunk;
   x.units = tiles / chunk + BH;
@@ -503,21 +852,27 @@ size_t bytes_of(const maskkv_desc* d, const Deal& x, int64_t units) {
 
 template <typename T, int D>
 int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
-  using C = TreeCfg<T, D>;
-  static_assert(C::kLds <= 160 * 1024, "a workgroup's LDS");
-  const auto kernel = &attend_tree_kernel<T, D>;
+  static_assert(TreeCfg<T, D>::kLds <= 160 * 1024, "a workgroup's LDS");
+  auto kernel = &attend_tree_kernel<T, D>;
+  int lds = TreeCfg<T, D>::kLds;
+  if constexpr (sizeof(T) == 2) {
+    if (deal.wide) {
+      kernel = &attend_tree_wide_kernel<D>;
+      lds = WideCfg<D>::kLds;
+    }
+  }
   const int64_t groups = deal.units * deal.qtiles;
   if (groups * kWaves * 64 > 0xFFFFFFFF) {  // (threads of a launch along a dimension)
     set_error("attend_tree: %lld workgroups are more than a launch can have", (long long)groups);
     return MASKKV_ESHAPE;
   }
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   if (e != hipSuccess) {
     set_error("attend_tree: hipFuncSetAttribute: %s", hipGetErrorString(e));
     (void)hipGetLastError();
     return MASKKV_EHIP;
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), C::kLds, stream, prm);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), lds, stream, prm);
   if (int e = check_launch("attend_tree")) return e;
   if (!deal.chunk) return MASKKV_OK;
   if (deal.units > (int64_t)kSharedUnits * prm.BH)
@@ -563,6 +918,7 @@ int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, cons
   prm.qtiles = deal.qtiles;
   prm.units = (int)deal.units;
   prm.chunk = deal.chunk;
+  prm.tile_rows = deal.tile_rows;
   prm.part_rows = deal.part_rows;
   prm.c = scale * kLog2e;
   prm.lse = lse;
