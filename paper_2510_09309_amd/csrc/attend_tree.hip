@@ -1,7 +1,7 @@
 // Attention of response rows that do not all see each other - trees of drafted tokens, blocks in order - over a packed cache and the
 // response's own rows: one pass over the keys with the running maximum and sum of a softmax, a bit per query and response row.
 //
-// A workgroup has four waves and serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row axis), so that a
+// A workgroup has eight waves (fp32 at head_dim 128: four) and serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row axis), so that a
 // lane owns one query, its word of the mask covers a tile of 32 response rows, and its probabilities are the B operand of
 // O^T = V^T P^T as they stand.  The waves take tiles of 32 keys in turn, each through LDS of its own and without a barrier: K and V come by direct
 // transfers, K of the next tile while this one's softmax runs, V of the next behind this one's product.  The waves are merged at the end.
@@ -13,6 +13,7 @@
 // are seen by all queries of their head, and a tile's places behind the last row hold that row again.
 //
 // Sums, maxima and outputs are fp32; probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product.
+#include <cmath>
 #include <type_traits>
 
 #include "attend.hpp"
@@ -24,7 +25,6 @@ namespace {
 
 constexpr int kUnits = 256;  // compute units
 constexpr int kTile = 32;    // keys of a tile, and query rows of a workgroup
-constexpr int kWaves = 4;
 
 struct TreeParams {
   View Q, K2, V2, O;
@@ -47,6 +47,8 @@ struct TreeParams {
 
 template <typename T, int D>
 struct TreeCfg {
+  static constexpr int kWaves = D * (int)sizeof(T) == 512 ? 4 : 8;  // as many as LDS has room for, up to two a SIMD
+  static constexpr int kThreads = kWaves * 64;
   static constexpr int kRowB = D * (int)sizeof(T);
   static constexpr int kPPR = kRowB / 16;           // pieces of 16 bytes in a row
   static constexpr int kDB = D / 32;
@@ -65,6 +67,12 @@ struct TreeCfg {
   }
 };
 
+// The larger of each of two numbers of 16 bits.
+__device__ __forceinline__ uint32_t max_pairs(uint32_t a, uint32_t b) {
+  typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 template <int N>
 __device__ __forceinline__ void wait_moves() {  // all but the last N transfers have arrived
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
@@ -72,8 +80,9 @@ __device__ __forceinline__ void wait_moves() {  // all but the last N transfers 
 __device__ __forceinline__ void lds_is_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tree_kernel(const TreeParams prm) {
+__global__ __launch_bounds__((TreeCfg<T, D>::kThreads), (TreeCfg<T, D>::kWaves / 4)) void attend_tree_kernel(const TreeParams prm) {
   using C = TreeCfg<T, D>;
+  constexpr int kWaves = C::kWaves;
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char tree_lds[];
   const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
@@ -101,7 +110,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
   char* const v_lds = k_lds + C::kTileB;
   const uint32_t k_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)k_lds, v_at = k_at + C::kTileB;
 
-  // This wave's tiles: t0 + wave, and every fourth from there.
+  // This wave's tiles: t0 + wave, and every one as many on as there are waves.
   const int mine = max(t1 - t0 - wave + kWaves - 1, 0) / kWaves;
   auto tile_of = [&](int i) { return t0 + wave + i * kWaves; };
   // A transfer brings the pieces that belong to consecutive places of LDS.  (Rows behind the last one are the last one.)
@@ -181,16 +190,16 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
     lds_is_read();
   };
   auto holds_infinite = [&]() __attribute__((always_inline)) {
-    bool any = false;
+    u32x4 most = {};  // of the values, without signs (bf16: as pairs)
 #pragma unroll
     for (int j = 0; j < C::kMoves; ++j) {
       const u32x4 w = *reinterpret_cast<const u32x4*>(v_lds + j * 1024 + lane * 16);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint32_t bits = w[x];
-        any |= (bits & 0x7F800000u) == 0x7F800000u || (!F32 && (bits & 0x7F80u) == 0x7F80u);
-      }
+      for (int x = 0; x < 4; ++x) most[x] = F32 ? max(most[x], w[x] & 0x7FFFFFFFu) : max_pairs(most[x], w[x] & 0x7FFF7FFFu);
     }
+    bool any = false;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) any |= most[x] >= 0x7F800000u || (!F32 && (most[x] & 0xFFFFu) >= 0x7F80u);
     return __any(any);
   };
 
@@ -302,8 +311,8 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w * kTile + r].x);
   const float mine_by = fast_exp2(m - top);
   float* const sums = reinterpret_cast<float*>(tree_lds);
-  constexpr int kEach = 8;                // elements of a row that a thread writes
-  constexpr int kPerRow = D / 2 / kEach;  // threads of half a row
+  constexpr int kEach = kTile * D / 2 / C::kThreads < 4 ? 4 : kTile * D / 2 / C::kThreads;  // elements of a row that a thread writes
+  constexpr int kPerRow = D / 2 / kEach;                                                    // threads of half a row
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     if (half) __syncthreads();
@@ -317,7 +326,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
               make_float4(from[4 * i] * mine_by, from[4 * i + 1] * mine_by, from[4 * i + 2] * mine_by, from[4 * i + 3] * mine_by);
         }
     __syncthreads();
-    const int row = threadIdx.x / kPerRow, q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;  // (256 threads: 32 rows or more)
+    const int row = threadIdx.x / kPerRow, q = qtile * kTile + row, at = threadIdx.x % kPerRow * kEach;  // (32 rows or more)
     if (row >= kTile || q >= prm.n_q) continue;
     float mq = kNegBig, lq = 0.f;
 #pragma unroll
@@ -339,19 +348,19 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void attend_tr
     if (units > 1) {
       const int64_t part = ((int64_t)unit * prm.qtiles + qtile) * prm.part_rows + row;
       float4* to = reinterpret_cast<float4*>(prm.part_o + part * D + to_at);
-      to[0] = make_float4(x[0], x[1], x[2], x[3]);
-      to[1] = make_float4(x[4], x[5], x[6], x[7]);
+#pragma unroll
+      for (int e = 0; e < kEach; e += 4) to[e / 4] = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
       if (to_at == 0) prm.part_ml[part] = make_float2(mq, lq);
       continue;
     }
     const float by = lq == 0.f ? 0.f : 1.f / lq;  // (a row that sees nothing)
     char* to = prm.O.group_row(b, h, prm.q_per_kv, prm.n_resp, q) + to_at * (int)sizeof(T);
-    if constexpr (F32) {
-      reinterpret_cast<float4*>(to)[0] = make_float4(x[0] * by, x[1] * by, x[2] * by, x[3] * by);
-      reinterpret_cast<float4*>(to)[1] = make_float4(x[4] * by, x[5] * by, x[6] * by, x[7] * by);
-    } else {
-      *reinterpret_cast<u32x4*>(to) = u32x4{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by),
-                                            pack_bf16x2(x[4] * by, x[5] * by), pack_bf16x2(x[6] * by, x[7] * by)};
+#pragma unroll
+    for (int e = 0; e < kEach; e += 4) {
+      if constexpr (F32)
+        reinterpret_cast<float4*>(to)[e / 4] = make_float4(x[e] * by, x[e + 1] * by, x[e + 2] * by, x[e + 3] * by);
+      else
+        reinterpret_cast<u32x2*>(to)[e / 4] = u32x2{pack_bf16x2(x[e] * by, x[e + 1] * by), pack_bf16x2(x[e + 2] * by, x[e + 3] * by)};
     }
     if (to_at == 0 && prm.lse) prm.lse[(int64_t)bh * prm.n_q + q] = (mq + __builtin_amdgcn_logf(lq)) * kLn2;
   }
@@ -465,29 +474,67 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
     }
   };
 
-  // ---- tiles of the response, in buffers 0 and 2
-  for (int t = t0; t < min(t1, resp_tiles); ++t) {
-    const int left = prm.n_resp - t * kWideTile;
-    const uint32_t* words = prm.mask + ((int64_t)b * prm.n_resp + query % prm.n_resp) * prm.words + 2 * t;
-    uint32_t word[2] = {words[0], 2 * t + 1 < prm.words ? words[1] : 0};
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      const int of = left - 32 * kb;
-      if (of < 32) word[kb] = of > 0 ? word[kb] & ((1u << of) - 1) : 0;
+  // Fragment n of a tile: 0 .. kQK-1 of its keys (two chains of products, one for 32 keys each), from kQK on of values; in which buffers.
+  constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 2;
+  u32x4 fr[kAhead + 1];
+  auto fetch = [&](int n, uint32_t odd_k, uint32_t odd_v) __attribute__((always_inline)) {
+    u32x4& f = fr[n % (kAhead + 1)];
+    if (n < kQK) {
+      f = *in_lds<const u32x4>(k_at[n / 2] + odd_k * C::kTileB, n % 2 * 32 * C::kRowB);
+    } else {
+      const int i = n - kQK, imm = i / C::kDB * 16 * C::kRowB;
+      const uint32_t at = v_at[i % C::kDB] + odd_v * C::kTileB;
+      const u32x2 lo = read_transposed(at, imm), hi = read_transposed(at, imm + 8 * C::kRowB);
+      f = u32x4{lo[0], lo[1], hi[0], hi[1]};
     }
-    if (t > t0) arrive();  // (the tile before has been read)
-    transfer(prm.K2.row(b, h, t * kWideTile), prm.K2.stride_t, left, piece_k, C::swz_k(C::kMoveRows) << 4, lds0);
-    transfer(prm.V2.row(b, h, t * kWideTile), prm.V2.stride_t, left, piece_v, 0, lds0 + 2 * C::kTileB);
-    arrive();
+  };
+
+  // ---- tiles of the response, in the buffers of even and odd tiles in turn: the next one, and its words, are under way meanwhile
+  const uint32_t* const my_mask = prm.mask + ((int64_t)b * prm.n_resp + query % prm.n_resp) * prm.words;
+  const int resp_end = min(t1, resp_tiles), begin = max(t0 - resp_tiles, 0), tiles = t1 - resp_tiles;  // those of the cache: counted from its first one
+  auto bring_resp = [&](int t, uint32_t odd) __attribute__((always_inline)) {
+    const int left = prm.n_resp - t * kWideTile;
+    transfer(prm.K2.row(b, h, t * kWideTile), prm.K2.stride_t, left, piece_k, C::swz_k(C::kMoveRows) << 4, lds0 + odd * C::kTileB);
+    transfer(prm.V2.row(b, h, t * kWideTile), prm.V2.stride_t, left, piece_v, 0, lds0 + (2 + odd) * C::kTileB);
+  };
+  uint32_t ahead[2] = {0, 0};
+  auto words_of = [&](int t) __attribute__((always_inline)) {
+    const int left = prm.n_resp - t * kWideTile;
+    ahead[0] = my_mask[2 * t];
+    ahead[1] = 2 * t + 1 < prm.words ? my_mask[2 * t + 1] : 0;
+    if (left < 32) ahead[0] &= (1u << left) - 1;
+    if (left > 32 && left < 64) ahead[1] &= (1u << (left - 32)) - 1;
+  };
+  if (t0 < resp_end) {
+    words_of(t0);
+    bring_resp(t0, 0);
+  }
+  for (int t = t0; t < resp_end; ++t) {
+    const uint32_t odd_tile = (t - t0) & 1, k_off = odd_tile * C::kTileB, v0 = lds0 + (2 + odd_tile) * C::kTileB;
+    const uint32_t word[2] = {ahead[0], ahead[1]};
+    arrive();  // (and the tile before has been read)
+    if (t + 1 < resp_end) {
+      words_of(t + 1);
+      bring_resp(t + 1, 1 - odd_tile);
+    }
     if (!__any((word[0] | word[1]) != 0)) continue;  // (none of the wave's queries sees any of it)
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      even[kb] = f32x16{};
+    for (int n = 0; n < kAhead; ++n) fetch(n, odd_tile, odd_tile);
 #pragma unroll
-      for (int i = 0; i < C::kSteps; ++i) {
-        const u32x4 f = *in_lds<const u32x4>(k_at[i], kb * 32 * C::kRowB);
-        mfma_step<bf16_t>(f, qf[i], even[kb]);
-      }
+    for (int n = 0; n < kQK; ++n) {
+      if (n + kAhead < kQK) fetch(n + kAhead, odd_tile, odd_tile);
+      if (n < 2) even[n] = f32x16{};
+      mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], even[n % 2]);
+    }
+    u32x4 most = {};  // of the values, without signs, as pairs of 16 bits
+#pragma unroll
+    for (int j = 0; j < C::kTileB / 1024; ++j) {
+      const u32x4 w = *in_lds<const u32x4>(v0 + j * 1024 + lane * 16);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) most[x] = max_pairs(most[x], w[x] & 0x7FFF7FFFu);
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
       const uint32_t own = word[kb] >> (4 * g);
 #pragma unroll
       for (int i = 0; i < 16; ++i) even[kb][i] = own >> (8 * (i / 4) + i % 4) & 1 ? even[kb][i] : -INFINITY;
@@ -502,16 +549,8 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
       even[i / 16][i % 16] = p;
       l += p;
     }
-    bool any = false;
-#pragma unroll 4
-    for (int j = 0; j < C::kTileB / 1024; ++j) {
-      const u32x4 w = *in_lds<const u32x4>(lds0 + 2 * C::kTileB + j * 1024 + lane * 16);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const uint32_t bits = w[x];
-        any |= (bits & 0x7F800000u) == 0x7F800000u || (bits & 0x7F80u) == 0x7F80u;
-      }
-    }
+    const uint32_t m01 = max_pairs(most[0], most[1]), m23 = max_pairs(most[2], most[3]), all = max_pairs(m01, m23);
+    const bool any = all >= 0x7F800000u || (all & 0xFFFFu) >= 0x7F80u;
     if (__any(any)) {  // (see attend_tree_kernel: key by key, of those that the lane's query sees)
       const uint32_t own = lds0 + C::kProbs + wave * kTile * kTile * 4;
 #pragma unroll
@@ -530,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const uint32_t e = 32 * db + 8 * q + 4 * g;
-              const u32x2 w = *in_lds<const u32x2>(lds0 + 2 * C::kTileB + row * C::kRowB + ((e / 8 ^ v_swizzle<D>(row) << 1) << 4) + e % 8 * 2);
+              const u32x2 w = *in_lds<const u32x2>(v0 + row * C::kRowB + ((e / 8 ^ v_swizzle<D>(row) << 1) << 4) + e % 8 * 2);
               const uint32_t w0 = w[0], w1 = w[1];
               const float v[4] = {as_f32(w0 << 16), as_f32(w0 & 0xFFFF0000u), as_f32(w1 << 16), as_f32(w1 & 0xFFFF0000u)};
 #pragma unroll
@@ -539,41 +578,26 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
         }
       }
     } else {
+      u32x4 pf[4];
 #pragma unroll
-      for (int tp = 0; tp < 4; ++tp) {
-        u32x4 pf;
+      for (int i = 0; i < 32; i += 2) pf[i / 8][i % 8 / 2] = pack_bf16x2(even[i / 16][i % 16], even[i / 16][i % 16 + 1]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) pf[w] = pack_bf16x2(even[tp / 2][tp % 2 * 8 + 2 * w], even[tp / 2][tp % 2 * 8 + 2 * w + 1]);
+      for (int n = kQK; n < kQK + kAhead; ++n) fetch(n, odd_tile, odd_tile);
 #pragma unroll
-        for (int db = 0; db < C::kDB; ++db) {
-          const u32x2 lo = read_transposed(v_at[db], tp * 16 * C::kRowB), hi = read_transposed(v_at[db], (tp * 16 + 8) * C::kRowB);
-          mfma_step<bf16_t>(u32x4{lo[0], lo[1], hi[0], hi[1]}, pf, o[db]);
-        }
+      for (int n = kQK; n < kQK + kPV; ++n) {
+        if (n + kAhead < kQK + kPV) fetch(n + kAhead, odd_tile, odd_tile);
+        mfma_step<bf16_t>(fr[n % (kAhead + 1)], pf[(n - kQK) / C::kDB], o[(n - kQK) % C::kDB]);
       }
     }
   }
 
-  // ---- tiles of the cache: from `begin` on, counted from its first one
-  const int begin = max(t0 - resp_tiles, 0), tiles = t1 - resp_tiles;
+  // ---- tiles of the cache
   if (begin < tiles) {
     if (t0 < resp_tiles) arrive();  // (the response's last tile has been read)
     bring_k(begin, 0);
     bring_v(begin, 0);
     if (begin + 1 < tiles) bring_k(begin + 1, 1);
     arrive();
-    // Fragment n of a tile: 0 .. kQK-1 of its keys (two chains of products, one for 32 keys each), from kQK on of the values of the tile before.
-    constexpr int kQK = 2 * C::kSteps, kPV = 4 * C::kDB, kAhead = 2;
-    u32x4 fr[kAhead + 1];
-    auto fetch = [&](int n, uint32_t odd_k) __attribute__((always_inline)) {
-      u32x4& f = fr[n % (kAhead + 1)];
-      if (n < kQK) {
-        f = *in_lds<const u32x4>(k_at[n / 2], odd_k * C::kTileB + n % 2 * 32 * C::kRowB);
-      } else {
-        const int i = n - kQK, imm = (1 - odd_k) * C::kTileB + i / C::kDB * 16 * C::kRowB;
-        const u32x2 lo = read_transposed(v_at[i % C::kDB], imm), hi = read_transposed(v_at[i % C::kDB], imm + 8 * C::kRowB);
-        f = u32x4{lo[0], lo[1], hi[0], hi[1]};
-      }
-    };
     auto mask = [&](int t, f32x16 (&s)[2]) __attribute__((always_inline)) {  // keys behind the last one
       const int left = cached - t * kWideTile;
       if (left >= kWideTile) return;
@@ -586,7 +610,7 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
     };
 #pragma unroll
     for (int n = 0; n < kQK; ++n) {
-      fetch(n, 0);
+      fetch(n, 0, 0);
       if (n < 2) even[n] = f32x16{};
       mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], even[n % 2]);
     }
@@ -617,11 +641,11 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
       };
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int n = 0; n < kAhead; ++n) fetch(kFrom + n, 1 - kOdd);
+      for (int n = 0; n < kAhead; ++n) fetch(kFrom + n, 1 - kOdd, kOdd);
       if constexpr (kMore) {
 #pragma unroll
         for (int n = 0; n < kQK; ++n) {
-          fetch(n + kAhead, 1 - kOdd);
+          fetch(n + kAhead, 1 - kOdd, kOdd);
           if (n < 2) next[n] = f32x16{};
           mfma_step<bf16_t>(fr[n % (kAhead + 1)], qf[n / 2], next[n % 2]);
 #pragma unroll
@@ -637,7 +661,7 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int n = kQK; n < kQK + kPV; ++n) {
-        if (n + kAhead < kQK + kPV) fetch(n + kAhead, 1 - kOdd);
+        if (n + kAhead < kQK + kPV) fetch(n + kAhead, 1 - kOdd, kOdd);
         mfma_step<bf16_t>(fr[n % (kAhead + 1)], pf[(n - kQK) / C::kDB], o[(n - kQK) % C::kDB]);
         if constexpr (kMore) {
 #pragma unroll
@@ -808,45 +832,83 @@ struct Deal {
   int tile_rows, qtiles, part_rows;
   int chunk;      // tiles of a unit, or 0: a unit per head
   int64_t units;  // at most
-  int64_t most_units;  // more than there are heads: what any capacity up to this one may have
 };
 constexpr int kSharedUnits = 16;  // units of a head on average above which a query row's partial results are read by a whole workgroup
-constexpr int kWideFrom = 64;     // query rows above which a workgroup has 128
+
+// What a launch of each kernel takes, in us: start + round * rounds + steps * step, from launches of 2 ... 64 heads, 48 ... 1792 query rows and 200 ... 32000
+// rows a head.  Both sides: 32 heads x 160 rows x 1000, whole 17, dealt out 27; 4 heads x 256 rows x 4000 16.6 by 32 rows a
+// workgroup, 26 by 128; 4 heads of seven x 64 rows x 32000 84 and 49; 64 heads of seven x 256 x 200 128 and 49.
+struct Form {
+  int tile_rows, keys;  // query rows of a workgroup, keys of a tile
+  int tiles;            // that its waves take in one step
+  int least;            // tiles of a unit
+  int at_once;          // workgroups of a compute unit
+  float start, round;   // the launch; the first loads, the merging and the last stores of each round of workgroups
+  float step;           // of a workgroup alone on its compute unit
+  float beside;         // ... of one that shares it: so many times that, for each
+};
+constexpr float kJoin = 4.f, kPart = 0.15f;  // the second kernel, and a million bytes of partial results, written and read
+
+Form form_of(const maskkv_desc* d, bool wide) {
+  const bool small = d->d == 64;
+  if (wide) return {kWideQueries, kWideTile, 1, 4, 2, 8.f, 0.f, small ? 0.85f : 1.3f, 0.8f};
+  if (d->dtype == MASKKV_BF16) return {kTile, kTile, 8, 8, small ? 2 : 1, 3.f, 6.f, small ? 0.9f : 1.45f, 0.8f};
+  return {kTile, kTile, small ? 8 : 4, small ? 8 : 4, 1, 2.f, 4.f, small ? 4.f : 5.5f, 1.f};
+}
+// Units that a launch is dealt out into, at most: of any capacity.
+int64_t most_units(const Form& f, int qtiles, int64_t BH) {
+  const int64_t wanted = f.at_once * kUnits / qtiles + 1;
+  return (wanted > BH ? wanted : BH) + BH;
+}
+// Tiles that a head has, at most.
+int64_t longest_of(const maskkv_desc* d, const Form& f, int64_t capacity) {
+  return (d->P_max < capacity ? d->P_max : capacity) / f.keys + 1 + (d->n_resp + f.keys - 1) / f.keys;
+}
 
 Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   const int n_q = query_heads_per_kv(d) * d->n_resp;
   const int64_t BH = (int64_t)d->B * d->H;
-  const bool bf16 = d->dtype == MASKKV_BF16;
-  Deal x;
-  x.wide = bf16 && n_q > kWideFrom;
-  x.tile_rows = x.wide ? kWideQueries : kTile;
-  x.qtiles = (n_q + x.tile_rows - 1) / x.tile_rows;
-  x.part_rows = n_q < x.tile_rows ? n_q : x.tile_rows;
-  const int keys = x.wide ? kWideTile : kTile, once = x.wide ? 1 : kWaves;  // keys of a tile, tiles of a workgroup at once
-  const int64_t least = x.wide ? 4 : 2 * kWaves;                             // tiles of a unit
-  const int64_t resp = (d->n_resp + keys - 1) / keys;
-  const int64_t places = (bf16 ? 2 : 1) * kUnits;
-  const int64_t wanted = (places + x.qtiles - 1) / x.qtiles;
-  // whole heads where they fill the chip as they are, or none has more tiles than a unit
-  const int64_t longest = (d->P_max < capacity ? d->P_max : capacity) / keys + 1 + resp;
-  x.chunk = 0;
-  x.units = x.most_units = BH;
-  if (BH * x.qtiles >= places || longest <= least) return x;
-  x.most_units = wanted + BH;  // (of this capacity and of smaller ones)
-  const int64_t tiles = capacity / keys + BH * (resp + 1);
-  int64_t chunk = (tiles + wanted - 1) / wanted;
-  if (chunk < least) chunk = least;
-  chunk = (chunk + once - 1) / once * once;
-  if (longest <= chunk) return x;
-  x.chunk = (int)chunk;
-  x.units = tiles / chunk + BH;
-  return x;
+  Deal best;
+  float best_cost = -1.f;
+  for (int wide = 0; wide < (d->dtype == MASKKV_BF16 && n_q > kWideQueries / 2 ? 2 : 1); ++wide) {
+    const Form f = form_of(d, wide);
+    const int qtiles = (n_q + f.tile_rows - 1) / f.tile_rows;
+    const int64_t resp = (d->n_resp + f.keys - 1) / f.keys, longest = longest_of(d, f, capacity);
+    const float tiles = (float)(BH * resp + capacity / f.keys) + 0.5f * BH, mean = tiles / BH;  // (half a tile of a head is empty, on average)
+    auto cost = [&](float units, float steps) {
+      const float wgs = units * qtiles, rounds = ceilf(wgs / (f.at_once * kUnits));
+      const float step = wgs <= kUnits ? f.step : f.step * f.beside * f.at_once;
+      return f.start + rounds * (f.round + ceilf(steps) * step);
+    };
+    auto take = [&](float us, int64_t chunk) {
+      if (best_cost >= 0.f && us >= best_cost) return;
+      best_cost = us;
+      best = {wide != 0, f.tile_rows, qtiles, n_q < f.tile_rows ? n_q : f.tile_rows, (int)chunk, BH};
+      if (chunk) best.units = (capacity / f.keys + BH * (resp + 1)) / chunk + BH;
+    };
+    // A whole head: the host does not know their lengths, but that none is longer than the longest prompt.
+    const float whole = fminf((float)longest, fmaxf(1.25f * mean, 0.25f * longest));
+    take(cost((float)BH, whole / f.tiles), 0);
+    auto dealt = [&](float wanted) {
+      int64_t chunk = (int64_t)fmaxf(ceilf(wanted), (float)f.least);
+      chunk = (chunk + f.tiles - 1) / f.tiles * f.tiles;
+      if (chunk >= longest || (capacity / f.keys + BH * (resp + 1)) / chunk + BH > most_units(f, qtiles, BH)) return;
+      const float units = fmaxf(tiles / chunk + 0.5f * BH, BH * ceilf(mean / chunk));
+      take(cost(units, fminf((float)chunk, mean) / f.tiles) + kJoin + kPart * units * n_q * d->d * 4e-6f, chunk);
+    };
+    for (int k = 1; k <= f.at_once; ++k) {  // a unit for every compute unit, or for every place in them:
+      const float places = (float)(k * kUnits) / qtiles;
+      dealt(tiles / fmaxf(places - 0.5f * BH, 0.5f * BH));  // for heads of any length, of which half a unit is empty,
+      dealt(mean / fmaxf(floorf(places / BH), 1.f));        // and for heads of one length
+    }
+  }
+  return best;
 }
 
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
-size_t bytes_of(const maskkv_desc* d, const Deal& x, int64_t units) {
-  const size_t rows = (size_t)units * x.qtiles * x.part_rows;
+size_t bytes_of(const maskkv_desc* d, int64_t units, int qtiles, int part_rows) {
+  const size_t rows = (size_t)units * qtiles * part_rows;
   return pad256(rows * d->d * 4) + pad256(rows * 8) + pad256((size_t)d->B * d->H * 8);
 }
 
@@ -854,15 +916,16 @@ template <typename T, int D>
 int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
   static_assert(TreeCfg<T, D>::kLds <= 160 * 1024, "a workgroup's LDS");
   auto kernel = &attend_tree_kernel<T, D>;
-  int lds = TreeCfg<T, D>::kLds;
+  int lds = TreeCfg<T, D>::kLds, threads = TreeCfg<T, D>::kThreads;
   if constexpr (sizeof(T) == 2) {
     if (deal.wide) {
       kernel = &attend_tree_wide_kernel<D>;
       lds = WideCfg<D>::kLds;
+      threads = 256;
     }
   }
   const int64_t groups = deal.units * deal.qtiles;
-  if (groups * kWaves * 64 > 0xFFFFFFFF) {  // (threads of a launch along a dimension)
+  if (groups * threads > 0xFFFFFFFF) {  // (threads of a launch along a dimension)
     set_error("attend_tree: %lld workgroups are more than a launch can have", (long long)groups);
     return MASKKV_ESHAPE;
   }
@@ -872,7 +935,7 @@ int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
     (void)hipGetLastError();
     return MASKKV_EHIP;
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(kWaves * 64), lds, stream, prm);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, stream, prm);
   if (int e = check_launch("attend_tree")) return e;
   if (!deal.chunk) return MASKKV_OK;
   if (deal.units > (int64_t)kSharedUnits * prm.BH)
@@ -887,12 +950,21 @@ int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
 
 size_t attend_tree_needs(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
-  return x.chunk ? bytes_of(d, x, x.units) : 0;
+  return x.chunk ? bytes_of(d, x.units, x.qtiles, x.part_rows) : 0;
 }
 
+// (No unit is dealt out where no head has more tiles than the least of a unit.)
 size_t attend_tree_workspace_bytes(const maskkv_desc* d, int64_t capacity) {
-  const Deal x = deal_of(d, capacity);
-  return x.most_units > (int64_t)d->B * d->H ? bytes_of(d, x, x.most_units) : 0;
+  const int n_q = query_heads_per_kv(d) * d->n_resp;
+  size_t most = 0;
+  for (int wide = 0; wide < (d->dtype == MASKKV_BF16 && n_q > kWideQueries / 2 ? 2 : 1); ++wide) {
+    const Form f = form_of(d, wide);
+    const int qtiles = (n_q + f.tile_rows - 1) / f.tile_rows;
+    if (longest_of(d, f, capacity) <= f.least) continue;
+    const size_t bytes = bytes_of(d, most_units(f, qtiles, (int64_t)d->B * d->H), qtiles, n_q < f.tile_rows ? n_q : f.tile_rows);
+    most = bytes > most ? bytes : most;
+  }
+  return most;
 }
 
 int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, const void* Vc, const int32_t* cu_budget, int64_t capacity,

@@ -116,7 +116,7 @@ class Case:
             off = np.where(np.isinf(want[some]) & (got[some] == want[some]), 0.0, off)
             assert np.array_equal(np.isnan(got[some]), np.isnan(want[some])), f"head {i}: NaN"
             assert off.max() <= 1.0, f"head {i}: an output is {off.max():.2f} times its bound off"
-            far = np.abs(gl - norm)[some].max()
+            far = np.abs(gl[some] - norm[some]).max()
             assert far <= 2 * e + (n + 40) * U, f"head {i}: a normaliser is {far:.3e} off"
 
 
