@@ -1,9 +1,14 @@
 // Rotary positions: pairs of a row's elements turned by position * frequency.
 //
-// A workgroup takes up to eight tokens and some of their heads.  The sines and cosines of its tokens are formed once, by all threads together, and
+// A workgroup takes 8 to 32 tokens and some of their heads.  The sines and cosines of its tokens are formed once, by all threads together, and
 // kept in LDS; a thread then has one place of a token's rows - as many pairs as two pieces of 16 bytes hold - and turns them in one head after the other.
 // The angle is reduced in 64 bits: in whole turns, position * (frequency / 2 pi), of which the fraction is exact; what is left is
-// rounded to 32 bits, off by 2^-25 turns at most, for every position that 32 bits hold.
+// rounded to 32 bits, off by 2^-26 turns at most, for every position that 32 bits hold.
+//
+// Bound by the memory: 32768 tokens of 32 + 32 heads (1.07 GB) 196 us, 5.5 TB/s, as fast as a copy; 8192 tokens of 32 + 8 heads, a token's heads together,
+// 29; 256 tokens of 32 + 32 heads 5.1, one token 4.7, of which the launch is most.
+#include <type_traits>
+
 #include "kernels.hpp"
 
 namespace maskkv {
@@ -11,7 +16,7 @@ namespace maskkv {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 8;   // of a workgroup, at most
+constexpr int kTokens = 32;  // of a workgroup, at most
 constexpr int kAtOnce = 4;   // heads whose rows a thread asks for before it turns the first
 
 struct RotateParams {
@@ -34,15 +39,21 @@ struct Piece {
   static constexpr int kBytes = V * (int)sizeof(T);
   typedef uint32_t Words __attribute__((ext_vector_type(kBytes < 4 ? 1 : kBytes / 4)));
   Words w;
+  template <bool PAST>
   __device__ __forceinline__ void load(const char* from) {
     if constexpr (kBytes == 2)
       w[0] = *reinterpret_cast<const uint16_t*>(from);
+    else if constexpr (PAST)
+      w = __builtin_nontemporal_load(reinterpret_cast<const Words*>(from));
     else
       w = *reinterpret_cast<const Words*>(from);
   }
+  template <bool PAST>
   __device__ __forceinline__ void store(char* to) const {
     if constexpr (kBytes == 2)
       *reinterpret_cast<uint16_t*>(to) = (uint16_t)w[0];
+    else if constexpr (PAST)
+      __builtin_nontemporal_store(w, reinterpret_cast<Words*>(to));
     else
       *reinterpret_cast<Words*>(to) = w;
   }
@@ -64,7 +75,8 @@ struct Piece {
   }
 };
 
-template <typename T, int V, bool PAIRS>
+// PAST: rows are written (1), or read and written (2), past the memory-side cache.
+template <typename T, int V, bool PAIRS, int PAST>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams prm) {
   __shared__ float2 turned[kTokens * 64];  // [token][pair]
   const int b = blockIdx.z, tokens = 1 << prm.tokens_log2, t0 = blockIdx.x << prm.tokens_log2;
@@ -86,8 +98,8 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams prm
       const int h = h0 + u * step;
       if (h >= end || !mine) continue;
       const char* row = h < prm.hq ? prm.q.row(b, h, t) : prm.k.row(b, h - prm.hq, t);
-      x[u].load(row + first);
-      y[u].load(row + second);
+      x[u].template load<PAST == 2>(row + first);
+      y[u].template load<PAST == 2>(row + second);
     }
   };
   int h0 = blockIdx.y * prm.per + (slot >> prm.tokens_log2);
@@ -138,20 +150,25 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams prm
         x[u].set(p);
         y[u].set(q);
       }
-      x[u].store(row + first);
-      y[u].store(row + second);
+      x[u].template store<PAST != 0>(row + first);
+      y[u].template store<PAST != 0>(row + second);
     }
     fetch(h0 + kAtOnce * step);
   }
 }
 
-template <typename T, int V>
+template <typename T, int V, int PAST>
 void launch_pieces(const RotateParams& prm, bool pairs, dim3 grid, hipStream_t stream) {
   if (pairs)
-    hipLaunchKernelGGL((rotate_kernel<T, V, true>), grid, dim3(kThreads), 0, stream, prm);
+    hipLaunchKernelGGL((rotate_kernel<T, V, true, PAST>), grid, dim3(kThreads), 0, stream, prm);
   else
-    hipLaunchKernelGGL((rotate_kernel<T, V, false>), grid, dim3(kThreads), 0, stream, prm);
+    hipLaunchKernelGGL((rotate_kernel<T, V, false, PAST>), grid, dim3(kThreads), 0, stream, prm);
 }
+
+// What is read and written, in bytes, from which on it goes past the memory-side cache, which holds 256 MB (out of it, a step finds what the one before has
+// left): stores from 128 MB on, 8192 tokens of 32 + 8 heads (168 MB) 38.9 us with stores that stay and 29.1 past it, 2 x 3000
+// tokens of 12 + 12 heads in fp32 (74 MB) 14.9 and 21.0; loads too from 512 MB on, a 32k prompt 202 with stores alone, 196.
+constexpr int64_t kStoresPast = (int64_t)128 << 20, kAllPast = (int64_t)512 << 20;
 
 }  // namespace
 
@@ -179,8 +196,13 @@ int launch_rotate(const maskkv_desc* d, const maskkv_rotary* rotary, const int32
   int V = bf16 ? 8 : 4;
   while (prm.half % V) V /= 2;
   while (1 << prm.items_log2 < d->d / (2 * V)) ++prm.items_log2;
-  while (1 << prm.tokens_log2 < kTokens && 1 << prm.tokens_log2 < longest && kThreads >> prm.items_log2 >> prm.tokens_log2 > 1) ++prm.tokens_log2;
-  const int tokens = 1 << prm.tokens_log2, step = kThreads >> prm.items_log2 >> prm.tokens_log2;
+  // as many tokens as still leave a workgroup or two for each compute unit: a head's rows of 32 tokens lie in one stretch of memory, of 8 in four
+  // (32k prompt, 64 heads: 8 tokens 246 us, 16 232, 32 202; 256 tokens of 64 heads 5.1, 8.1, 12.7)
+  const int slots = kThreads >> prm.items_log2;
+  int most_tokens = 8;
+  while (most_tokens < kTokens && (int64_t)d->B * longest / (2 * most_tokens) >= 448) most_tokens *= 2;
+  while (1 << prm.tokens_log2 < most_tokens && 1 << prm.tokens_log2 < longest && 1 << prm.tokens_log2 < slots) ++prm.tokens_log2;
+  const int tokens = 1 << prm.tokens_log2, step = slots >> prm.tokens_log2;
   const int tiles = (longest + tokens - 1) / tokens;
   // heads to several workgroups as long as these do not fill the chip
   const int64_t groups = (int64_t)tiles * d->B, most = (prm.heads + step - 1) / step;
@@ -188,16 +210,29 @@ int launch_rotate(const maskkv_desc* d, const maskkv_rotary* rotary, const int32
   parts = parts < most ? parts : most;
   prm.per = (int)((most + parts - 1) / parts) * step;
   const dim3 grid((unsigned)tiles, (unsigned)((prm.heads + prm.per - 1) / prm.per), (unsigned)d->B);
+  const int64_t bytes = 2 * (int64_t)d->B * longest * prm.heads * d->d * (bf16 ? 2 : 4);
   const bool pairs = rotary->layout == MASKKV_ROTARY_PAIRS;
-  if (bf16) {
-    if (V == 8) launch_pieces<bf16_t, 8>(prm, pairs, grid, stream);
-    if (V == 4) launch_pieces<bf16_t, 4>(prm, pairs, grid, stream);
-    if (V == 2) launch_pieces<bf16_t, 2>(prm, pairs, grid, stream);
-    if (V == 1) launch_pieces<bf16_t, 1>(prm, pairs, grid, stream);
+  auto whole = [&](auto past) {  // (halves of whole pieces)
+    constexpr int kPast = decltype(past)::value;
+    if (bf16)
+      launch_pieces<bf16_t, 8, kPast>(prm, pairs, grid, stream);
+    else
+      launch_pieces<float, 4, kPast>(prm, pairs, grid, stream);
+  };
+  if (V == (bf16 ? 8 : 4)) {
+    if (bytes >= kAllPast)
+      whole(std::integral_constant<int, 2>());
+    else if (bytes >= kStoresPast)
+      whole(std::integral_constant<int, 1>());
+    else
+      whole(std::integral_constant<int, 0>());
+  } else if (bf16) {
+    if (V == 4) launch_pieces<bf16_t, 4, 0>(prm, pairs, grid, stream);
+    if (V == 2) launch_pieces<bf16_t, 2, 0>(prm, pairs, grid, stream);
+    if (V == 1) launch_pieces<bf16_t, 1, 0>(prm, pairs, grid, stream);
   } else {
-    if (V == 4) launch_pieces<float, 4>(prm, pairs, grid, stream);
-    if (V == 2) launch_pieces<float, 2>(prm, pairs, grid, stream);
-    if (V == 1) launch_pieces<float, 1>(prm, pairs, grid, stream);
+    if (V == 2) launch_pieces<float, 2, 0>(prm, pairs, grid, stream);
+    if (V == 1) launch_pieces<float, 1, 0>(prm, pairs, grid, stream);
   }
   return check_launch("rotate");
 }
