@@ -795,34 +795,53 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_tree_join_kernel(c
 }
 
 // ---- who sees whom in drafted trees: a thread a row, which walks up from it.  The rows above have ever smaller numbers, so the words are
-// finished one after the other, the last one first.
-__global__ __launch_bounds__(256) void tree_mask_kernel(const int32_t* parents, int n, int words, uint32_t* mask) {
-  const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const int32_t* const up = parents + (int64_t)b * n;
-  uint32_t* const to = mask + ((int64_t)b * n + i) * words;
-  int p = up[i], at = words - 1, node = i;
-  uint32_t bits = 0;
-  auto put = [&](int j) {
-    for (; at > j / 32; --at) {
+// finished one after the other, the last one first.  Trees of up to kTreeRows rows lie in LDS, parents and words, so that a step of the walk waits for LDS
+// and the words leave in order (64 trees of 512: 9.3 us with both in memory, 7.9 in LDS).
+constexpr int kTreeRows = 1024;
+constexpr int kMaskThreads = 256;
+template <bool LDS>
+__global__ __launch_bounds__(kMaskThreads) void tree_mask_kernel(const int32_t* parents, int n, int words, uint32_t* mask) {
+  __shared__ int32_t own_parents[LDS ? kTreeRows : 1];
+  __shared__ uint32_t own_words[LDS ? kMaskThreads * (kTreeRows / 32 + 1) : 1];
+  const int b = blockIdx.y, first = blockIdx.x * kMaskThreads, i = first + threadIdx.x;
+  const int32_t* up = parents + (int64_t)b * n;
+  if constexpr (LDS) {
+    for (int j = threadIdx.x; j < min(n, first + kMaskThreads); j += kMaskThreads) own_parents[j] = up[j];
+    __syncthreads();
+    up = own_parents;
+  }
+  if (i < n) {
+    const int pitch = words | 1;  // (neighbouring rows on different banks)
+    uint32_t* const to = LDS ? own_words + threadIdx.x * pitch : mask + ((int64_t)b * n + i) * words;
+    int p = up[i], at = words - 1, node = i;
+    uint32_t bits = 0;
+    auto put = [&](int j) {
+      for (; at > j / 32; --at) {
+        to[at] = bits;
+        bits = 0;
+      }
+      bits |= 1u << (j % 32);
+    };
+    if (p >= -1) {
+      put(i);
+      while (p >= 0 && p < node) {
+        const int above = up[p];
+        if (above < -1) break;  // (there is no such row)
+        put(p);
+        node = p;
+        p = above;
+      }
+    }
+    for (; at >= 0; --at) {
       to[at] = bits;
       bits = 0;
     }
-    bits |= 1u << (j % 32);
-  };
-  if (p >= -1) {
-    put(i);
-    while (p >= 0 && p < node) {
-      const int above = up[p];
-      if (above < -1) break;  // (there is no such row)
-      put(p);
-      node = p;
-      p = above;
-    }
   }
-  for (; at >= 0; --at) {
-    to[at] = bits;
-    bits = 0;
+  if constexpr (LDS) {
+    __syncthreads();
+    uint32_t* const to = mask + ((int64_t)b * n + first) * words;
+    const int count = min(n - first, kMaskThreads) * words, pitch = words | 1;
+    for (int j = threadIdx.x; j < count; j += kMaskThreads) to[j] = own_words[j / words * pitch + j % words];
   }
 }
 
@@ -1005,7 +1024,9 @@ int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, cons
 }
 
 int launch_tree_mask(const int32_t* parents, int B, int n, uint32_t* mask, hipStream_t stream) {
-  hipLaunchKernelGGL(tree_mask_kernel, dim3((unsigned)((n + 255) / 256), (unsigned)B), dim3(256), 0, stream, parents, n, (n + 31) / 32, mask);
+  const auto kernel = n <= kTreeRows ? &tree_mask_kernel<true> : &tree_mask_kernel<false>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((n + kMaskThreads - 1) / kMaskThreads), (unsigned)B), dim3(kMaskThreads), 0, stream, parents, n,
+                     (n + 31) / 32, mask);
   return check_launch("tree_mask");
 }
 

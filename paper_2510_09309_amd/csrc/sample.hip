@@ -1048,50 +1048,48 @@ struct Drawer {
     // the parts' sure masses, and the tokens between: a stretch of the list for each part
     double sure = 0.0;
     each_part([&](int i, auto take_part) {
-      double sum = 0.0;
-      int many = 0;
-      // (of 64 blocks, those that stay for sure are put together first: few do, but some in every 64)
+      double sum = 0.0, two = 0.0;
+      int between = 0;
+      // (of 64 blocks, those that stay for sure are put together first: their masses take most of the time; those between are few)
+      constexpr int kOwnList = kFewGroups / 2 / kWaves;
       float* const sure_ones = reinterpret_cast<float*>(s.wide) + ask.wave() * (kWide / kWaves);
+      uint2* const own_list = reinterpret_cast<uint2*>(s.groups) + ask.wave() * kOwnList;
       static_assert(kWide / kWaves >= 64 * E, "room for all of 64 blocks");
-      take_part([&](int, const float (&x)[E]) {
+      auto rank = [](uint64_t in) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0)); };
+      take_part([&](int block, const float (&x)[E]) {
         int n = 0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float at = (ref - x[e]) * to_bin;
-          const uint64_t in = __ballot(at < (float)begin);
-          if (at < (float)begin) sure_ones[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0))] = x[e];
-          n += __popcll(in);
-          many += at >= (float)begin && at < (float)(end + 1);
+          const bool sure = at < (float)begin, in = !sure && at < (float)(end + 1);
+          const uint64_t all_sure = __ballot(sure), all_in = __ballot(in);
+          if (sure) sure_ones[n + rank(all_sure)] = x[e];
+          n += __popcll(all_sure);
+          if (all_in) {
+            const int to = between + rank(all_in);
+            if (in && to < kOwnList) own_list[to] = make_uint2(as_u32(x[e]), (uint32_t)(row.number(block) + e));
+            between += __popcll(all_in);
+          }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        double two = 0.0;
         for (int j = ask.lane(); j < n; j += 128) {
           const float l = sure_ones[j], o = j + 64 < n ? sure_ones[j + 64] : -INFINITY;
           sum += mass(l);
           two += mass(o);
         }
-        sum += two;
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       });
-      sum = sum_wave(sum);
-      const int upto = upto_lane(many), all_of = __builtin_amdgcn_readlane(upto, 63);
+      sum = sum_wave(sum + two);
+      const int all_of = between;
       int to = 0;
-      if (ask.lane() == 0) to = atomicAdd(&s.taken, all_of);
+      if (ask.lane() == 0) to = atomicAdd(&s.taken, all_of <= kOwnList ? all_of : kList + 1);
       to = __builtin_amdgcn_readfirstlane(to);
-      if (all_of && to + all_of <= kList) {
-        int at_list = to + upto - many;
-        take_part([&](int block, const float (&x)[E]) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float at = (ref - x[e]) * to_bin;
-            if (at >= (float)begin && at < (float)(end + 1)) {
-              s.logit[at_list] = x[e];
-              s.number[at_list] = row.number(block) + e;
-              ++at_list;
-            }
-          }
-        });
-      }
+      if (all_of <= kOwnList && to + all_of <= kList)
+        for (int j = ask.lane(); j < all_of; j += 64) {
+          const uint2 one = own_list[j];
+          s.logit[to + j] = as_f32(one.x);
+          s.number[to + j] = (int)one.y;
+        }
       if (ask.lane() == 0) part[i] = Part(sum, 0.0, to, all_of);
     });
     __syncthreads();
