@@ -110,6 +110,27 @@ def test_nearly_flat_rows_of_many_tokens(dtype, limits):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,V", [(16, 30000), (40, 9001), (290, 5000)])
+def test_many_rows_of_which_most_are_nearly_flat(dtype, rows, V):
+    """Among them some of equal logits, some with a few
+    values, and some with other limits; each gives the bits that it gives alone."""
+    rng = np.random.default_rng(rows)
+    l = rng.standard_normal((rows, V)) * np.where(rng.random((rows, 1)) < 0.5, 0.3, 2.0)
+    l[3::11] = 1.25
+    l[4::11] = rng.integers(0, 4, (len(l[4::11]), V))
+    l[5::11, ::7] = -np.inf
+    l[6::11, 17] += 30.0
+    p = np.where(rng.random(rows) < 0.9, 0.2 + 0.79 * rng.random(rows), 1.0)
+    for other in (dict(), dict(k=np.where(rng.random(rows) < 0.2, 40, 0), m=np.where(rng.random(rows) < 0.2, 0.01, 0.0))):
+        c = Case(l, dtype, T=0.8 + rng.random(rows), p=p, seed=rows, **other).run().check()
+        want = c.token.clone(), c.prob.clone()
+        for r in range(0, rows, 5):
+            one = Case(l[r:r + 1], dtype, T=c.T[r], p=c.p[r], u=c.u[r], **{n: v[r] for n, v in other.items()}).run()
+            torch.cuda.synchronize()
+            assert int(one.token[0]) == int(want[0][r]) and float(one.prob[0]) == float(want[1][r])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [5, 300, 10007])
 def test_ties(dtype, V):
     rng = np.random.default_rng(9)
@@ -207,7 +228,7 @@ def test_many_parts():
         Case(l, "bf16", T=0.7, u=0.77, **limits).run().check()
 
 
-@pytest.mark.parametrize("limits", [dict(), dict(k=50, p=0.9), dict(p=0.97)], ids=str)
+@pytest.mark.parametrize("limits", [dict(), dict(k=50, p=0.9), dict(p=0.97), dict(p=0.9, T=1.5)], ids=str)
 def test_captured_replayed_and_equal_bits(limits):
     rng = np.random.default_rng(22)
     c = Case(rows_of(rng, 30, 20000, sharp=False), "bf16", seed=23, **limits).run()
