@@ -829,7 +829,7 @@ int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const in
     return MASKKV_EINVAL;
   }
   if (int e = check_rotary_shape("rotate", rotary->width, desc->d, rotary->layout)) return e;
-  bool finite = isfinite(rotary->amplitude);
+  bool finite = isfinite((float)rotary->amplitude);
   for (int i = 0; i < rotary->width / 2; ++i) finite = finite && isfinite(rotary->freq[i]);
   if (!finite) {
     set_error("rotate: a frequency or the amplitude is not a finite number");

@@ -45,6 +45,12 @@ struct TreeParams {
   int2* parts;      // [BH] a head's first unit, and how many it has
 };
 
+__device__ __forceinline__ void fetch_tree_arguments() {
+  typedef TreeParams A;
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, Q), MASKKV_VIEW_ARGUMENTS(A, K2), MASKKV_VIEW_ARGUMENTS(A, V2), MASKKV_VIEW_ARGUMENTS(A, O),
+                   MASKKV_ARGUMENT(A, Kc), MASKKV_ARGUMENT(A, H), (uint32_t)(offsetof(A, parts) + 4)});
+}
+
 template <typename T, int D>
 struct TreeCfg {
   static constexpr int kWaves = D * (int)sizeof(T) == 512 ? 4 : 8;  // as many as LDS has room for, up to two a SIMD
@@ -85,6 +91,7 @@ __global__ __launch_bounds__((TreeCfg<T, D>::kThreads), (TreeCfg<T, D>::kWaves /
   constexpr int kWaves = C::kWaves;
   constexpr bool F32 = sizeof(T) == 4;
   extern __shared__ __attribute__((aligned(1024))) char tree_lds[];
+  fetch_tree_arguments();
   const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
   const int unit = place.unit, qtile = place.qtile;
   const int resp_tiles = (prm.n_resp + kTile - 1) / kTile;
@@ -393,6 +400,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreeParams prm) {
   using C = WideCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char tree_lds[];
+  fetch_tree_arguments();
   const Place place = place_of(blockIdx.x, prm.units, prm.qtiles);
   const int unit = place.unit, qtile = place.qtile;
   const int resp_tiles = (prm.n_resp + kWideTile - 1) / kWideTile;
@@ -732,6 +740,7 @@ __global__ __launch_bounds__(kJoinGroups * D / 4) void attend_tree_join_kernel(c
   constexpr int kPer = D / 4, kAtOnce = 8, kStep = SHARED ? kJoinGroups : 1;
   __shared__ float4 sums[kJoinGroups][kPer];
   __shared__ float2 tops[kJoinGroups];
+  fetch_tree_arguments();
   const int grp = threadIdx.x / kPer, at = threadIdx.x % kPer, bh = blockIdx.y;
   const int q = SHARED ? blockIdx.x : blockIdx.x * kJoinGroups + grp;
   const int first = prm.parts[bh].x, units = prm.parts[bh].y;

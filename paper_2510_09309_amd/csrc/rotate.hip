@@ -79,6 +79,9 @@ struct Piece {
 template <typename T, int V, bool PAIRS, int PAST>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const RotateParams prm) {
   __shared__ float2 turned[kTokens * 64];  // [token][pair]
+  typedef RotateParams A;
+  fetch_arguments({MASKKV_VIEW_ARGUMENTS(A, q), MASKKV_VIEW_ARGUMENTS(A, k), MASKKV_VIEW_ARGUMENTS(A, q_out), MASKKV_VIEW_ARGUMENTS(A, k_out),
+                   MASKKV_ARGUMENT(A, turns), MASKKV_ARGUMENT(A, len), MASKKV_ARGUMENT(A, positions), MASKKV_ARGUMENT(A, amplitude)});
   const int b = blockIdx.z, tokens = 1 << prm.tokens_log2, t0 = blockIdx.x << prm.tokens_log2;
   const int len = prm.len[b];
   if (t0 >= len) return;

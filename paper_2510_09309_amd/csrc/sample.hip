@@ -387,12 +387,17 @@ struct Ask {
   }
 };
 
-// A logit's place in the order of all, as a whole number.
+// A logit's place in the order of all, as a whole number (of bf16 16 bits are enough).
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t u = as_u32(l);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = as_u32(l), key = u & 0x80000000u ? ~u : u | 0x80000000u;
+  return sizeof(T) == 2 ? key >> 16 : key;
 }
-__device__ __forceinline__ float logit_of(uint32_t key) { return as_f32(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+template <typename T>
+__device__ __forceinline__ float logit_of(uint32_t key) {
+  const uint32_t k = sizeof(T) == 4 ? key : key & 0x8000u ? key << 16 : key << 16 | 0xFFFFu;
+  return as_f32(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
+}
 
 // kDraw threads draw the token of a row.
 template <typename T, int kDraw, typename Shared>
@@ -796,25 +801,40 @@ struct Drawer {
     return true;
   }
 
-  // The last token in rank that stays when the first `goal` tokens do (by_mass: those before which less than `goal_mass` lies), found eleven bits of
-  // its logit's place at a time: that logit, and how many tokens and how much mass lie above it, and how many are its equals.
-  // Of the n tokens of the list, or of all of the row where n is negative; `above` and `mass_above` lie above all of these.
+  // The last token in rank that stays when the first `goal` tokens do (by_mass: those before which less than `goal_mass` lies), found up to eleven bits at a time
+  // of how far its logit's place is behind the first one's: that logit, and how many tokens and how much mass lie above it, and how many are
+  // its equals.  Of the n tokens of the list, or of all of the row where n is negative; `above` and `mass_above` lie above all of these.
   struct Last {
     float logit;
     int above, equal;
     double mass_above;
   };
-  __device__ __forceinline__ Last last_of(int n, bool by_mass, int goal, double goal_mass, int above, double mass_above) {
+  struct Span {  // the first one's place, and in how many bits the others' distances from it fit
+    uint32_t first;
+    int bits;
+  };
+  __device__ __forceinline__ Span span_of(int n) {
+    if (n < 0) return {key_of<T>(ref), 8 * (int)sizeof(T)};
+    float high = -INFINITY, low = -INFINITY;
+    for (int i = threadIdx.x; i < n; i += kDraw) {
+      high = fmaxf(high, s.logit[i]);
+      low = fmaxf(low, -s.logit[i]);
+    }
+    ask.most(high, low);
+    const uint32_t first = key_of<T>(high + 0.f), far = first - key_of<T>(-low + 0.f);
+    return {first, 32 - __builtin_clz(far | 1)};
+  }
+  __device__ __forceinline__ Last last_of(int n, const Span& span, bool by_mass, int goal, double goal_mass, int above, double mass_above) {
     // masses as whole numbers: of so many units, so that those of all tokens fit
     const double unit = ldexp(1.0, 62 - (32 - __builtin_clz((unsigned)prm.V)));
     unsigned long long whole_above = (unsigned long long)rint(mass_above * unit);
     const unsigned long long whole_goal = by_mass ? (unsigned long long)fmin(ceil(goal_mass * unit), 0x1p62) : 0;
     const bool need_mass = lim.p < 1.f;
-    uint32_t key = 0;
+    uint32_t far = 0;  // as much as is known of the distance
     int equal = 0;
 #pragma unroll 1
-    for (int level = 0; level < (sizeof(T) == 2 ? 2 : 3); ++level) {
-      const int shift = level == 0 ? 21 : level == 1 ? 10 : 0, bits = level == 2 ? 10 : 11;
+    for (int left = span.bits; left > 0;) {
+      const int bits = min(left, 11), shift = left - bits;
       __syncthreads();
       for (int i = threadIdx.x; i < kDigits; i += kDraw) {
         s.digits.count[i] = 0;
@@ -822,9 +842,10 @@ struct Drawer {
       }
       __syncthreads();
       auto take = [&](float l) {
-        const uint32_t k = key_of(l);
-        if (l == -INFINITY || (level && k >> (shift + bits) != key >> (shift + bits))) return;
-        const int digit = k >> shift & ((1 << bits) - 1);
+        if (l == -INFINITY) return;
+        const uint32_t z = span.first - key_of<T>(l);
+        if (left < 32 && z >> left != far >> left) return;
+        const int digit = z >> shift & ((1 << bits) - 1);
         atomicAdd(&s.digits.count[digit], 1u);
         if (need_mass) atomicAdd(&s.digits.mass[digit], (unsigned long long)rint(mass(l) * unit));
       };
@@ -834,13 +855,13 @@ struct Drawer {
         each_logit(take);
       }
       __syncthreads();
-      // some digits a thread, the largest first
+      // some digits a thread
       constexpr int kOwn = kDigits / kDraw;
       int many[kOwn], sum = 0, all;
       unsigned long long whole[kOwn], whole_sum = 0, whole_upto = 0, whole_all;
 #pragma unroll
       for (int q = 0; q < kOwn; ++q) {
-        const int digit = kDigits - 1 - (threadIdx.x * kOwn + q);
+        const int digit = threadIdx.x * kOwn + q;
         sum += many[q] = s.digits.count[digit];
         whole_sum += whole[q] = s.digits.mass[digit];
       }
@@ -867,19 +888,19 @@ struct Drawer {
         at = last, at_above = last_above, at_many = last_many, at_whole = last_whole;
       }
       if (who == (int)threadIdx.x) {
-        s.key = key | (uint32_t)(kDigits - 1 - at) << shift;
+        s.key = far | (uint32_t)at << shift;
         s.found = at_above;
         s.count = at_many;
         s.whole = at_whole;
       }
       __syncthreads();
-      key = s.key;
+      far = s.key;
       above = s.found;
       equal = s.count;
       whole_above = s.whole;
+      left = shift;
     }
-    if (sizeof(T) == 2 && !(key & 0x80000000u)) key |= (1u << 10) - 1;  // (of bf16 the low bits are all alike)
-    return {logit_of(key), above, equal, (double)whole_above / unit};
+    return {logit_of<T>(span.first - far), above, equal, (double)whole_above / unit};
   }
 
   // Which tokens stay: those above `last`, and the first `left` of its equals.
@@ -890,10 +911,11 @@ struct Drawer {
   __device__ __forceinline__ Border border_of(int n, int above, double mass_above) {
     Border x = {-INFINITY, 0};
     double all = masses;
+    const Span span = span_of(n);
 #pragma unroll 1
     for (int by_mass = lim.k ? 0 : 1; by_mass < (lim.p < 1.f ? 2 : 1); ++by_mass) {
       const double goal = (double)lim.p * all;
-      const Last y = last_of(n, by_mass, lim.k, goal, above, mass_above);
+      const Last y = last_of(n, span, by_mass, lim.k, goal, above, mass_above);
       if (!by_mass) {
         x = {y.logit, min(lim.k - y.above, y.equal)};
         all = y.mass_above + x.left * mass(x.last);
@@ -996,6 +1018,33 @@ struct Drawer {
       f(i, [&](auto g) { take(at(i), 64, now, g); });
       now = next;
     }
+  }
+
+  // Where the token is, once each part's mass above the last token that stays is known, and how many of its tokens are that one's equals.
+  __device__ __forceinline__ Where where_of(const Border& x) {
+    const int from = from_part(), to = to_part();
+    int same = 0, unused;
+    for (int i = from; i < to; ++i) same += part[i].many;
+    const int same_before = ask.before(same, unused);
+    double each = x.last > -INFINITY ? mass(x.last) : 0.0;
+    if (!(each >= (double)lim.m)) each = 0.0;
+    int nth = same_before;
+    auto mass_in = [&](int j) {
+      const Part y = part[j];
+      const int stay = min(max(x.left - nth, 0), y.many);
+      nth += y.many;
+      return y.mass + stay * each;
+    };
+    double own = 0.0, total;
+    for (int i = from; i < to; ++i) own += mass_in(i);
+    const double base = ask.before(own, total), target = u * total;
+    nth = same_before;
+    double base_of_part;
+    const int i = part_with(target, own, base, mass_in, base_of_part);
+    int equal = 0, equal_all;  // in the parts before
+    for (int j = threadIdx.x; j < i; j += kDraw) equal += part[j].many;
+    ask.before(equal, equal_all);
+    return {i, base_of_part, target, total, x.last, equal_all, x.left};
   }
 
   // With a top-p alone: the last token that stays is looked for among those of a few bins.  A token of less than the share (1 - p) / V of all mass never stays (all of them together have
@@ -1101,15 +1150,7 @@ struct Drawer {
     ask.before(sure, sure_all);
     // (in the first place that is not before all of them there is one token at least above: `above` counts as one where any mass lies above)
     const Border x = border_of(n, begin > 0 && sure_all > 0.0 ? 1 : 0, sure_all);
-    const double each = mass(x.last);
-    int same = 0, unused;
-    for (int i = from; i < to; ++i) {
-      const Part y = part[i];
-      for (int j = 0; j < y.many; ++j) same += s.logit[y.first + j] == x.last;
-    }
-    int nth = ask.before(same, unused);
-    const int same_before = nth;
-    auto mass_in = [&](int i) {
+    for (int i = from; i < to; ++i) {  // the parts with those of their tokens that were between
       const Part y = part[i];
       double sum = y.mass;
       int equal = 0;
@@ -1118,20 +1159,10 @@ struct Drawer {
         equal += l == x.last;
         if (l > x.last) sum += mass(l);
       }
-      sum += min(max(x.left - nth, 0), equal) * each;
-      nth += equal;
-      return sum;
-    };
-    double own = 0.0, total;
-    for (int i = from; i < to; ++i) own += mass_in(i);
-    const double base = ask.before(own, total), target = u * total;
-    nth = same_before;
-    double base_of_part;
-    const int i = part_with(target, own, base, mass_in, base_of_part);
-    int equal = 0, equal_all;  // in the parts before
-    for (int j = threadIdx.x; j < n; j += kDraw) equal += s.logit[j] == x.last && s.number[j] < row.number(i * kPartBlocks);
-    ask.before(equal, equal_all);
-    where = {i, base_of_part, target, total, x.last, equal_all, x.left};
+      part[i] = Part(sum, 0.0, 0, equal);
+    }
+    __syncthreads();
+    where = where_of(x);
     return true;
   }
 
@@ -1158,29 +1189,7 @@ struct Drawer {
       if (ask.lane() == 63) part[i] = Part(sum, 0.0, 0, same);
     });
     __syncthreads();
-    const int from = from_part(), to = to_part();
-    int same = 0, unused;
-    for (int i = from; i < to; ++i) same += part[i].many;
-    const int same_before = ask.before(same, unused);
-    double each = x.last > -INFINITY ? mass(x.last) : 0.0;
-    if (!(each >= (double)lim.m)) each = 0.0;
-    int nth = same_before;
-    auto mass_in = [&](int j) {
-      const Part y = part[j];
-      const int stay = min(max(x.left - nth, 0), y.many);
-      nth += y.many;
-      return y.mass + stay * each;
-    };
-    double own = 0.0, total;
-    for (int i = from; i < to; ++i) own += mass_in(i);
-    const double base = ask.before(own, total), target = u * total;
-    nth = same_before;
-    double base_of_part;
-    const int i = part_with(target, own, base, mass_in, base_of_part);
-    int equal = 0, equal_all;  // in the parts before
-    for (int j = threadIdx.x; j < i; j += kDraw) equal += part[j].many;
-    ask.before(equal, equal_all);
-    return {i, base_of_part, target, total, x.last, equal_all, x.left};
+    return where_of(x);
   }
 
   __device__ __forceinline__ bool draw_few() {

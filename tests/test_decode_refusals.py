@@ -52,7 +52,8 @@ def test_rotate_refuses(mk):
     bad = mk.maskkv_rotary_frequencies(64)
     bad.freq[31] = math.nan
     assert rotate(mk, rotary=bad) == 1 and "finite" in error(mk)
-    assert rotate(mk, rotary=mk.Rotary(width=64, layout=0, amplitude=math.inf)) == 1
+    for amplitude in (math.inf, math.nan, 1e39):                                 # (the last: beyond 32 bits)
+        assert rotate(mk, rotary=mk.Rotary(width=64, layout=0, amplitude=amplitude)) == 1 and "finite" in error(mk)
     assert rotate(mk, positions=None) == 1 and "positions" in error(mk)
     assert rotate(mk, n=-1) == 1 and rotate(mk, n=(1 << 25) + 1) == 1 and "n_tokens" in error(mk)
     assert rotate(mk, lens=[9]) == 1 and rotate(mk, lens=[-1]) == 1 and "token_len" in error(mk)
