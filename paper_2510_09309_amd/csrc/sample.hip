@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleParams pr
 
 // ---- a token for every row
 constexpr int kBins = 1024;      // of the groups' largest logits
-constexpr int kWide = 4096;      // bins of a row's logits
+constexpr int kWide = 2048;      // bins of a row's logits
 constexpr int kFewGroups = 4096; // that are looked into, at most
 constexpr int kRounds = 4;       // groups of a thread that are asked for at once
 constexpr int kFew = 2048;       // tokens that are ranked, at most
@@ -270,7 +270,7 @@ struct DrawShared : AskShared<N> {
       uint32_t count[kBins];
       unsigned long long mass[kBins];
     } bins;
-    uint32_t wide[kWide];
+    unsigned long long wide[kWide];  // how many there are (from kCountAt on), and the sum of how far they lie in the bin, in 2^-15
     struct {
       uint32_t count[kDigits];
       unsigned long long mass[kDigits];
@@ -1047,11 +1047,13 @@ struct Drawer {
     return {i, base_of_part, target, total, x.last, equal_all, x.left};
   }
 
-  // With a top-p alone: the last token that stays is looked for among those of a few bins.  A token of less than the share (1 - p) / V of all mass never stays (all of them together have
-  // less than 1 - p); from there to the largest logit the row's logits are counted in kWide bins, and from how many are in a bin follows of
-  // how much mass they are at least and at most.  Those above the bins in which the limit can lie stay for sure: their mass is added up part by
-  // part.  False: too many are in those bins.
-  __device__ __forceinline__ bool draw_between(Where& where) {
+  // With a top-p and no top-k: the last token that stays is looked for among those of a few bins.  A token of less than the share (1 - p) / V of all mass never
+  // stays (all of them together have less than 1 - p); from there to the largest logit the row's logits are counted in kWide bins, and how far they lie in their bin
+  // is added up.  The masses of a bin are at least those of as many tokens at the mean place, and at most what the bin's ends would have if
+  // that were the mean place of tokens at them (the exponential is convex): that is within 10^-4 of each other, so the limit lies in one bin or two.  Those above these
+  // stay for sure: their mass is added up part by part.  False: too many are in those bins.
+  static constexpr int kCountAt = 39;
+  __device__ __forceinline__ bool draw_between(Border& border) {
     const float depth = -(float)log((1.0 - (double)lim.p) * masses / prm.V) * lim.T;  // (of the smallest that can stay)
     const float range = depth * 1.0001f + 1e-4f * (fabsf(ref) + lim.T);
     if (!(range > 0.f) || !(range < 1e30f)) return false;
@@ -1062,18 +1064,22 @@ struct Drawer {
     __syncthreads();
     each_logit([&](float l) {
       const float at = (ref - l) * to_bin;
-      if (at < (float)kWide) atomicAdd(&s.wide[(int)at], 1u);
+      if (at < (float)kWide) atomicAdd(&s.wide[(int)at], (1ull << kCountAt) + (uint32_t)((at - (float)(int)at) * 0x1p15f));
     });
     __syncthreads();
     constexpr int kOwn = kWide / kDraw;
     const double step = -(double)range / kWide * c, goal = (double)lim.p * masses;
+    const double ratio = exp2_64(step);  // of the masses at a bin's ends
     double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0, all;
 #pragma unroll
     for (int q = 0; q < kOwn; ++q) {
       const int bin = threadIdx.x * kOwn + q;
-      const double n = s.wide[bin];  // (bins are told apart in 32 bits: their ends are off by 2^-11 of a bin at most)
-      most_sum += most[q] = n * exp2_64((bin - 0.01) * step < 0.0 ? (bin - 0.01) * step : 0.0);
-      least_sum += least[q] = n * exp2_64((bin + 1.01) * step);
+      const unsigned long long w = s.wide[bin];
+      // (places are known in 32 bits, to 2^-10 of a bin, and are cut to 2^-15)
+      const double n = (double)(w >> kCountAt), mean = n > 0.0 ? (double)(w & ((1ull << kCountAt) - 1)) * 0x1p-15 / n : 0.0;
+      const double begin = exp2_64(fmin((bin - 0.002) * step, 0.0));
+      most_sum += most[q] = n * begin * (1.0 + (ratio - 1.0) * fmax(mean - 0.002, 0.0));
+      least_sum += least[q] = n * exp2_64((bin + mean + 0.002) * step);
     }
     double most_upto = ask.before(most_sum, all), least_upto = ask.before(least_sum, all);
     int begin = kWide, end = kWide;  // the limit lies in no bin before `begin`, and no token behind `end` stays
@@ -1101,9 +1107,10 @@ struct Drawer {
       int between = 0;
       // (of 64 blocks, those that stay for sure are put together first: their masses take most of the time; those between are few)
       constexpr int kOwnList = kFewGroups / 2 / kWaves;
-      float* const sure_ones = reinterpret_cast<float*>(s.wide) + ask.wave() * (kWide / kWaves);
+      constexpr int kOwnSure = 2 * kWide / kWaves;
+      float* const sure_ones = reinterpret_cast<float*>(s.wide) + ask.wave() * kOwnSure;
       uint2* const own_list = reinterpret_cast<uint2*>(s.groups) + ask.wave() * kOwnList;
-      static_assert(kWide / kWaves >= 64 * E, "room for all of 64 blocks");
+      static_assert(kOwnSure >= 64 * E, "room for all of 64 blocks");
       auto rank = [](uint64_t in) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, 0)); };
       take_part([&](int block, const float (&x)[E]) {
         int n = 0;
@@ -1149,28 +1156,24 @@ struct Drawer {
     double sure_all;
     ask.before(sure, sure_all);
     // (in the first place that is not before all of them there is one token at least above: `above` counts as one where any mass lies above)
-    const Border x = border_of(n, begin > 0 && sure_all > 0.0 ? 1 : 0, sure_all);
+    border = border_of(n, begin > 0 && sure_all > 0.0 ? 1 : 0, sure_all);
     for (int i = from; i < to; ++i) {  // the parts with those of their tokens that were between
       const Part y = part[i];
       double sum = y.mass;
       int equal = 0;
       for (int j = 0; j < y.many; ++j) {
         const float l = s.logit[y.first + j];
-        equal += l == x.last;
-        if (l > x.last) sum += mass(l);
+        equal += l == border.last;
+        if (l > border.last) sum += mass(l);
       }
       part[i] = Part(sum, 0.0, 0, equal);
     }
     __syncthreads();
-    where = where_of(x);
     return true;
   }
 
-  __device__ __forceinline__ Where draw_any() {
-    Border x = {-INFINITY, 0};
-    if (lim.k || lim.p < 1.f) x = border_of(-1, 0, 0.0);
-    __syncthreads();
-    // the mass of each part that stays for sure, and how many of its tokens are equal to the last one
+  // The mass of each part above the last token that stays, and how many of its tokens are that one's equals.
+  __device__ __forceinline__ void add_up(const Border& x) {
     each_part([&](int i, auto take_part) {
       double sum = 0.0;
       int same = 0;
@@ -1189,7 +1192,6 @@ struct Drawer {
       if (ask.lane() == 63) part[i] = Part(sum, 0.0, 0, same);
     });
     __syncthreads();
-    return where_of(x);
   }
 
   __device__ __forceinline__ bool draw_few() {
@@ -1217,12 +1219,19 @@ struct Drawer {
         drawn = draw_few();
         if (!drawn) {
           __syncthreads();
-          bool found = false;
-          if (lim.p < 1.f && !lim.k && !(lim.m > 0.f)) found = draw_between(where);
-          if (!found) {
+          Border x = {-INFINITY, 0};
+          bool found = lim.p < 1.f && !lim.k && draw_between(x);
+          if (!found && (lim.k || lim.p < 1.f)) {
             __syncthreads();
-            where = draw_any();
+            x = border_of(-1, 0, 0.0);
           }
+          if (found && !(mass(x.last) >= (double)lim.m)) {  // min_p is what ends them
+            x = {-INFINITY, 0};
+            found = false;
+          }
+          __syncthreads();
+          if (!found) add_up(x);
+          where = where_of(x);
         }
       }
       if (!drawn) draw_in(where);

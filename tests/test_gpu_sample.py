@@ -101,7 +101,7 @@ def test_temperatures(dtype, T):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("limits", [dict(), dict(p=0.7), dict(k=70000), dict(k=3000, p=0.9), dict(m=0.01), dict(p=0.99, m=0.3)], ids=str)
+@pytest.mark.parametrize("limits", [dict(), dict(p=0.7), dict(p=0.995), dict(p=0.9, m=1e-5), dict(k=70000), dict(k=3000, p=0.9), dict(m=0.01), dict(p=0.99, m=0.3)], ids=str)
 def test_nearly_flat_rows_of_many_tokens(dtype, limits):
     rng = np.random.default_rng(7)
     V = 126464 if dtype == "bf16" else 80001
