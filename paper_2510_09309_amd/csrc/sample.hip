@@ -4,13 +4,19 @@
 // at the row's temperature and at temperature 1, and, where the row has limits, the largest logit of each group of 128 bytes.  The second
 // has a workgroup a row: it adds up the parts and, without limits, reads the one part again in which the wanted mass is reached.  With limits,
 // the groups' largest logits say how small a token that stays can be (`floor_of`): few groups reach that, and the tokens of these that do are ranked in
-// LDS (`draw_few`).  Where too many do - nearly flat rows, no limit but a small min-p - the last token that stays is found by histograms over the bits of the logits'
-// order, and the row is read part by part again (`draw_any`).
+// LDS (`draw_few`).  Where too many do, a top-p's last token is looked for between two bounds of the row's masses (`draw_between`); what is left - a top-k of
+// thousands, thousands of equal logits - takes histograms over all bits of the logits' order (`border_of`), and the row is read part by part again.
 //
 // Which token is drawn must not depend on roundings: in a flat row of 10^5 tokens an error of 10^-7 of the mass is a hundredth of a token.
 // Masses are therefore 64 bits wide from the exponential on: 2^f on [-1/2, 1/2] as 1 + f q(f), q the polynomial of degree 8 through
 // (2^f - 1)/f at nine Chebyshev points, off by 4e-14, on a vector unit that does 64-bit operations at the rate of 32-bit ones.
 // Histograms add up whole numbers, so that the order in which threads come to them has no part in the result.
+//
+// Bound by the vector pipe where all masses are needed: 256 rows of 126464 (65 MB, 12.7 us at a copy's rate) 36 + 5.7 us, the pipe busy all the time of the
+// first kernel, with 17 operations in 64 bits a logit and another 10 for the confidence's sum.  By latency where they are not: one row of 32001 with
+// top-k and top-p 4.7 + 9.6 us, of which 3 are the list's two waits for memory and its scans.  By one compute unit in a nearly flat row with a top-p: 152064 tokens 95 us,
+// of which 25 are the counting (atomics of LDS) and 50 the masses that stay for sure.  (Dealt to the whole chip by three launches more, 64 rows of which
+// eight were flat took 94 instead of 129 us, but 64 rows of which all were 115 instead of 120, and those where none was 5 to 6 us longer.)
 #include <type_traits>
 
 #include "kernels.hpp"
@@ -72,31 +78,37 @@ struct Limits {
     some = !greedy && (k || p < 1.f || m > 0.f);
     masses = !greedy && !k && (p < 1.f || !(m > 0.f));
   }
-  __device__ __forceinline__ double c() const { return 1.4426950408889634074 / (double)T; }
+  // (at an infinite temperature all finite logits have one mass, and -infinity none)
+  __device__ __forceinline__ double c() const { return fmax(1.4426950408889634074 / (double)T, 1e-290); }
 };
 
-// 2^t, t <= 0 (what is below 2^-1000, or NaN, is 2^-1000; 2^0 is 1 exactly).  A sum with 1.5 * 2^52 rounds t to a whole number, which is the low word of the
-// sum; it is added to the exponent as it is.  (rint, a conversion to an integer and ldexp took as long, but were exact below.)
-__device__ __forceinline__ double exp2_64(double t) {
-  constexpr double kRound = 0x1.8p52;
-  double kFirst = 1.0203121070622722e-07;
-  asm("" : "+v"(kFirst));  // (two constants are more than an instruction takes: this one in registers, once)
-  t = fmax(t, -1000.0);
-  const double n = t + kRound, f = t - (n - kRound);
-  double q = kFirst;
-  q = fma(q, f, 1.325522487501112e-06);
-  q = fma(q, f, 1.5252686846270554e-05);
-  q = fma(q, f, 0.00015403455852469646);
-  q = fma(q, f, 0.0013333558179043094);
-  q = fma(q, f, 0.00961812915940254);
-  q = fma(q, f, 0.055504108664760424);
-  q = fma(q, f, 0.2402265069581299);
-  q = fma(q, f, 0.6931471805599453);
-  const double m = fma(q, f, 1.0);
-  return __hiloint2double(__double2hiint(m) + (__double2loint(n) << 20), __double2loint(m));
-}
-// Mass of a logit relative to the largest one.  (That of -infinity is 2^-1000, which is nothing beside the largest one's 1.)
-__device__ __forceinline__ double mass_of(float l, float top, double c) { return exp2_64(((double)l - (double)top) * c); }
+// 2^t for t = d * c, t <= 0, d >= -1000 / c: what is below 2^-1000, or NaN, is 2^-1000, which is nothing beside the largest one's 1; 2^0 is 1 exactly.
+// A sum with 1.5 * 2^52 rounds t to a whole number, which is the low word of the sum; it is added to the exponent as it is.
+struct Power {
+  double c, least, first;  // first: of the polynomial's coefficients
+  __device__ __forceinline__ explicit Power(double by) : c(by), least(-1000.0 / by), first(1.0203121070622722e-07) {
+    asm("" : "+v"(first));  // (two constants are more than an instruction takes: this one in registers, once)
+  }
+  __device__ __forceinline__ double operator()(double d) const {
+    constexpr double kRound = 0x1.8p52;
+    d = fmax(d, least);
+    const double n = fma(d, c, kRound), f = fma(d, c, kRound - n);
+    double q = first;
+    q = fma(q, f, 1.325522487501112e-06);
+    q = fma(q, f, 1.5252686846270554e-05);
+    q = fma(q, f, 0.00015403455852469646);
+    q = fma(q, f, 0.0013333558179043094);
+    q = fma(q, f, 0.00961812915940254);
+    q = fma(q, f, 0.055504108664760424);
+    q = fma(q, f, 0.2402265069581299);
+    q = fma(q, f, 0.6931471805599453);
+    const double m = fma(q, f, 1.0);
+    return __hiloint2double(__double2hiint(m) + (__double2loint(n) << 20), __double2loint(m));
+  }
+  // The mass of a logit relative to the largest one.
+  __device__ __forceinline__ double of(float l, float top) const { return (*this)((double)l - (double)top); }
+};
+constexpr double kLog2e64 = 1.4426950408889634074;
 
 // A row in blocks of 16 bytes that begin at multiples of 16 bytes: its first and last one may be another row's in part.
 template <typename T>
@@ -224,19 +236,20 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleParams pr
   double mass = 0.0, plain = 0.0;
   if (ref > -INFINITY) {
     if (prm.logprob) {
+      const Power plainly(kLog2e64);
       // (of bf16 the differences are exact but for logits below 2^-12 or so; of fp32 they are not)
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          plain += sizeof(T) == 2 ? (double)fast_exp2((x[j][e] - ref) * kLog2e) : mass_of(x[j][e], ref, 1.4426950408889634074);
+          plain += sizeof(T) == 2 ? (double)fast_exp2((x[j][e] - ref) * kLog2e) : plainly.of(x[j][e], ref);
     }
     if (lim.masses) {
-      const double c = lim.c();
+      const Power power(lim.c());
 #pragma unroll
       for (int j = 0; j < kLoads; ++j)
 #pragma unroll
-        for (int e = 0; e < E; ++e) mass += mass_of(x[j][e], ref, c);
+        for (int e = 0; e < E; ++e) mass += power.of(x[j][e], ref);
     }
   }
   if (prm.logprob) plain = sum_wave(plain);
@@ -417,7 +430,8 @@ struct Drawer {
   float4 first_groups;                        // the first of a thread
   float top = 0.f, ref = 0.f;                 // the largest logit, and what masses are relative to
   float least = 0.f;                          // the smallest of the groups' largest
-  double c = 0.0, u = 0.0;
+  const Power power;           // with the temperature
+  double u = 0.0;
   double masses = 0.0, plain = 0.0;  // of all tokens
   double mine = 0.0;                 // of this thread's parts, and before them
   double before = 0.0;
@@ -427,7 +441,7 @@ struct Drawer {
   __device__ __forceinline__ Drawer(const SampleParams& p, Shared& shared, int number)
       : prm(p), s(shared), ask(shared), row(p, number), lim(p, number), r(number), part(p.part + (int64_t)number * p.parts),
         group(p.group + (int64_t)number * p.parts * kGroups), groups((row.blocks + kGroupBlocks - 1) / kGroupBlocks),
-        groups_each((groups + 4 * kDraw - 1) / (4 * kDraw) * 4), parts_each((p.parts + kDraw - 1) / kDraw) {}
+        groups_each((groups + 4 * kDraw - 1) / (4 * kDraw) * 4), parts_each((p.parts + kDraw - 1) / kDraw), power(lim.greedy ? 1.0 : lim.c()) {}
 
   __device__ __forceinline__ float seen(float l) const { return top == INFINITY ? finite_top(l) : l; }
   __device__ __forceinline__ void read(int block, float (&x)[E]) const {
@@ -439,9 +453,9 @@ struct Drawer {
   }
   // (What is about 2^-1000 is nothing: a part of which no token has a mass is none that is drawn from.)
   static __device__ __forceinline__ double or_nothing(double m, double least) { return m > least ? m : 0.0; }
-  __device__ __forceinline__ double mass(float l) const { return or_nothing(mass_of(l, ref, c), 0x1p-999); }
-  __device__ __forceinline__ double part_unit(float part_top, double by) const {
-    return part_top == top ? 1.0 : top == INFINITY ? 0.0 : or_nothing(exp2_64(((double)part_top - (double)ref) * by), 0x1p-990);
+  __device__ __forceinline__ double mass(float l) const { return or_nothing(power.of(l, ref), 0x1p-999); }
+  __device__ __forceinline__ double part_unit(float part_top, const Power& by) const {
+    return part_top == top ? 1.0 : top == INFINITY ? 0.0 : or_nothing(by.of(part_top, ref), 0x1p-990);
   }
   // This thread's parts, and its groups' largest logits in their order (f(logit, group)).
   __device__ __forceinline__ int from_part() const { return min((int)threadIdx.x * parts_each, prm.parts); }
@@ -488,10 +502,11 @@ struct Drawer {
     ref = top == INFINITY ? 0.f : top;
     least = top == INFINITY ? 0.f : -low;
     double own = 0.0;
+    const Power plainly(kLog2e64);
     for (int i = from; i < to; ++i) {
       const Part x = i == from ? one : part[i];
-      if (lim.masses) mine += x.mass * part_unit(x.top, c);
-      if (prm.logprob) own += x.plain * part_unit(x.top, 1.4426950408889634074);
+      if (lim.masses) mine += x.mass * part_unit(x.top, power);
+      if (prm.logprob) own += x.plain * part_unit(x.top, plainly);
     }
     if (prm.logprob) ask.before(own, plain);
     if (lim.masses) before = ask.before(mine, masses);
@@ -606,7 +621,7 @@ struct Drawer {
   __device__ __forceinline__ Where draw_all() {
     double base;
     const double target = u * masses;
-    const int i = part_with(target, mine, before, [&](int j) { return part[j].mass * part_unit(part[j].top, c); }, base);
+    const int i = part_with(target, mine, before, [&](int j) { return part[j].mass * part_unit(part[j].top, power); }, base);
     return {i, base, target, masses, -INFINITY, 0, 0};
   }
 
@@ -1068,8 +1083,8 @@ struct Drawer {
     });
     __syncthreads();
     constexpr int kOwn = kWide / kDraw;
-    const double step = -(double)range / kWide * c, goal = (double)lim.p * masses;
-    const double ratio = exp2_64(step);  // of the masses at a bin's ends
+    const double step = -(double)range / kWide, goal = (double)lim.p * masses;
+    const double ratio = power(step);  // of the masses at a bin's ends
     double least[kOwn], most[kOwn], least_sum = 0.0, most_sum = 0.0, all;
 #pragma unroll
     for (int q = 0; q < kOwn; ++q) {
@@ -1077,9 +1092,9 @@ struct Drawer {
       const unsigned long long w = s.wide[bin];
       // (places are known in 32 bits, to 2^-10 of a bin, and are cut to 2^-15)
       const double n = (double)(w >> kCountAt), mean = n > 0.0 ? (double)(w & ((1ull << kCountAt) - 1)) * 0x1p-15 / n : 0.0;
-      const double begin = exp2_64(fmin((bin - 0.002) * step, 0.0));
+      const double begin = power(fmin((bin - 0.002) * step, 0.0));
       most_sum += most[q] = n * begin * (1.0 + (ratio - 1.0) * fmax(mean - 0.002, 0.0));
-      least_sum += least[q] = n * exp2_64((bin + mean + 0.002) * step);
+      least_sum += least[q] = n * power((bin + mean + 0.002) * step);
     }
     double most_upto = ask.before(most_sum, all), least_upto = ask.before(least_sum, all);
     int begin = kWide, end = kWide;  // the limit lies in no bin before `begin`, and no token behind `end` stays
@@ -1252,7 +1267,6 @@ __global__ __launch_bounds__(LIMITS ? kLimited : kFree) void sample_draw_kernel(
   float u = prm.uniform[r];
   u = u >= 0.f ? fminf(u, 1.f - 0x1p-24f) : u < 0.f ? 0.f : 1.f - 0x1p-24f;
   d.u = (double)u;
-  d.c = d.lim.greedy ? 0.0 : d.lim.c();
   d.template draw<LIMITS>();
 }
 
