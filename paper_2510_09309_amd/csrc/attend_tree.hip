@@ -15,11 +15,12 @@
 // Sums, maxima and outputs are fp32; probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product: fp32 operands have a
 // sixteenth of its rate.  The sum that divides them is of the unrounded ones.
 //
-// Bound by the memory and by what precedes and follows it where few rows meet a long cache: 64 rows of 32 heads x 4096 (69 MB) 16.8 us, 4.1 TB/s, and 4 for
-// the joining launch; 8 rows over 32 x 8192 (134 MB) 31 together.  By latency where there is little: 256 heads x 32 rows x 64 ... 1024 14.4 (54 MB), four
-// heads of 8 fp32 rows 6.9.  With many rows (the second kernel) by matrix and softmax phases and the clock that the board's power leaves: 4 heads
-// of 336 rows x 30011 33.6 us, 700 TFLOP/s with the padding to 384 rows, both pipes busy 40 % of the time.
-// Eight waves a workgroup and one of these a compute unit, not two of four waves: ragged batch 18.7 and 14.7 us, single token of 7 heads x 30k rows 17.8 and 16.7.
+// By latency and memory where few rows meet a long cache: 64 rows of 32 heads x 4096 (69 MB) 17.7 us, 3.9 TB/s, waves waiting 41 % of their cycles, and 4.0 for
+// the joining launch; 8 rows over 32 x 8192 (134 MB) 31 together.  By latency where there is little: 256 heads x 32 rows x 64 ... 1024 14.5 (54 MB), four
+// heads of 8 fp32 rows 7.0.  With many rows (the second kernel) by matrix and softmax phases: 4 heads of 336 rows x 30011 34.1 us, 690 TFLOP/s with
+// the padding to 384 rows, both pipes busy 40 % of the time; joining 7.4.
+// Eight waves a workgroup and one of these a compute unit, not two of four waves (both sides in their own best number of units): ragged batch 18.7 and 15.1 us, single token
+// of 7 heads x 30k rows 17.8 and 17.2, 64 rows over 4096 21.0 and 20.9.
 #include <cmath>
 #include <type_traits>
 

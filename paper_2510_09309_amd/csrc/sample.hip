@@ -12,11 +12,13 @@
 // (2^f - 1)/f at nine Chebyshev points, off by 4e-14, on a vector unit that does 64-bit operations at the rate of 32-bit ones.
 // Histograms add up whole numbers, so that the order in which threads come to them has no part in the result.
 //
-// Bound by the vector pipe where all masses are needed: 256 rows of 126464 (65 MB, 12.7 us at a copy's rate) 36 + 5.7 us, the pipe busy all the time of the
-// first kernel, with 17 operations in 64 bits a logit and another 10 for the confidence's sum.  By latency where they are not: one row of 32001 with
-// top-k and top-p 4.7 + 9.6 us, of which 3 are the list's two waits for memory and its scans.  By one compute unit in a nearly flat row with a top-p: 152064 tokens 95 us,
-// of which 25 are the counting (atomics of LDS) and 50 the masses that stay for sure.  (Dealt to the whole chip by three launches more, 64 rows of which
-// eight were flat took 94 instead of 129 us, but 64 rows of which all were 115 instead of 120, and those where none was 5 to 6 us longer.)
+// The one exception is the confidence of bf16 rows, whose terms are fp32 exponentials added up in 64 bits: nothing is drawn by them.
+//
+// Bound by the vector pipe where all masses are needed: 256 rows of 126464 (65 MB, 12.7 us at a copy's rate) 35.7 + 5.8 us, the pipe busy all of the
+// first kernel's time: a mass is 16 operations in 64 bits.  By latency where they are not: one row of 32001 with top-k and top-p 4.6 + 10.0 us.
+// By one compute unit in a nearly flat row with a top-p: 64 rows of 152064 with mixed limits 32 us a call where no row is, 94 to 117 where one is.
+// (Such rows dealt to the whole chip by three launches more: 64 rows with mixed limits 129 -> 94 us and 64 rows with a top-p at temperature 1.4 120 -> 115, but
+// sharp ones 27.5 -> 32.5, 256 of 126464 48.8 -> 55.3, 100 of 50000 with a top-k 16.7 -> 22.5.)
 #include <type_traits>
 
 #include "kernels.hpp"
