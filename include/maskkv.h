@@ -450,7 +450,8 @@ int maskkv_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t dtype, si
  * as 0, one of 1 and more (or NaN) as the largest below 1; limits that are NaN are none.
  * logits: DEVICE [rows, vocab] in `dtype` (a maskkv_dtype), rows row_stride >= vocab elements apart, aligned to an element; vocab 1 .. 2^24; 0 <= rows <= 2^20.
  * token: DEVICE int32 [rows]; prob, logprob: DEVICE float [rows], or NULL.  Masses are held in 64 bits and summed up in a fixed order (or as whole
- * numbers): equal calls give equal bits, and the tokens are those of the definition in 64 bits.
+ * numbers): equal calls give equal bits, and a token is the definition's unless the random number or a limit lies within 1e-10 of the mass of where
+ * another one would be.  (The terms of logprob's sum are 32-bit exponentials where the logits are bf16; the sum has 64 bits.)
  */
 int maskkv_sample(const void* logits, int64_t rows, int32_t vocab, int32_t dtype, int64_t row_stride,
                   const maskkv_sampling* sampling, int32_t* token, float* prob, float* logprob, void* workspace,

@@ -818,9 +818,18 @@ struct Drawer {
     return true;
   }
 
+  // The tokens of a list, or all of the row where n is negative.
+  template <typename F>
+  __device__ __forceinline__ void each_of(int n, F f) const {
+    if (n < 0) return each_logit(f);
+    for (int i = threadIdx.x; i < n; i += kDraw) f(s.logit[i]);
+  }
+
   // The last token in rank that stays when the first `goal` tokens do (by_mass: those before which less than `goal_mass` lies), found up to eleven bits at a time
-  // of how far its logit's place is behind the first one's: that logit, and how many tokens and how much mass lie above it, and how many are
-  // its equals.  Of the n tokens of the list, or of all of the row where n is negative; `above` and `mass_above` lie above all of these.
+  // of how far its logit's place is behind the first one's: that logit, and how many tokens and (by_mass) how much mass lie above it, and how many are
+  // its equals.  Of the n tokens of the list, or of all of the row where n is negative, down to the logit `low`; `above` and `mass_above` lie above all of these.
+  // Masses are added up as whole numbers, in units of at most 2^-61 of `held`, which is the mass of all that are looked at: each is off by half a unit,
+  // 2^24 of them by 2^-38 of `held`.
   struct Last {
     float logit;
     int above, equal;
@@ -841,12 +850,10 @@ struct Drawer {
     const uint32_t first = key_of<T>(high + 0.f), far = first - key_of<T>(-low + 0.f);
     return {first, 32 - __builtin_clz(far | 1)};
   }
-  __device__ __forceinline__ Last last_of(int n, const Span& span, bool by_mass, int goal, double goal_mass, int above, double mass_above) {
-    // masses as whole numbers: of so many units, so that those of all tokens fit
-    const double unit = ldexp(1.0, 62 - (32 - __builtin_clz((unsigned)prm.V)));
-    unsigned long long whole_above = (unsigned long long)rint(mass_above * unit);
-    const unsigned long long whole_goal = by_mass ? (unsigned long long)fmin(ceil(goal_mass * unit), 0x1p62) : 0;
-    const bool need_mass = lim.p < 1.f;
+  __device__ __forceinline__ Last last_of(int n, const Span& span, float low, double held, bool by_mass, int goal, double goal_mass, int above, double mass_above) {
+    const double unit = ldexp(1.0, 61 - ilogb(held));
+    unsigned long long whole_above = by_mass ? (unsigned long long)rint(mass_above * unit) : 0;
+    const unsigned long long whole_goal = by_mass ? (unsigned long long)fmin(fmax(ceil(goal_mass * unit), 0.0), 0x1p62) : 0;
     uint32_t far = 0;  // as much as is known of the distance
     int equal = 0;
 #pragma unroll 1
@@ -859,18 +866,14 @@ struct Drawer {
       }
       __syncthreads();
       auto take = [&](float l) {
-        if (l == -INFINITY) return;
+        if (l == -INFINITY || l < low) return;
         const uint32_t z = span.first - key_of<T>(l);
         if (left < 32 && z >> left != far >> left) return;
         const int digit = z >> shift & ((1 << bits) - 1);
         atomicAdd(&s.digits.count[digit], 1u);
-        if (need_mass) atomicAdd(&s.digits.mass[digit], (unsigned long long)rint(mass(l) * unit));
+        if (by_mass) atomicAdd(&s.digits.mass[digit], (unsigned long long)rint(mass(l) * unit));
       };
-      if (n >= 0) {
-        for (int i = threadIdx.x; i < n; i += kDraw) take(s.logit[i]);
-      } else {
-        each_logit(take);
-      }
+      each_of(n, take);
       __syncthreads();
       // some digits a thread
       constexpr int kOwn = kDigits / kDraw;
@@ -883,7 +886,7 @@ struct Drawer {
         whole_sum += whole[q] = s.digits.mass[digit];
       }
       int upto = above + ask.before(sum, all);
-      if (need_mass) whole_upto = whole_above + ask.before(whole_sum, whole_all);
+      if (by_mass) whole_upto = whole_above + ask.before(whole_sum, whole_all);
       // the first one with which the goal is reached; or the last one there is
       int at = -1, last = -1, at_above = 0, last_above = 0, at_many = 0, last_many = 0;
       unsigned long long at_whole = 0, last_whole = 0;
@@ -927,15 +930,22 @@ struct Drawer {
   };
   __device__ __forceinline__ Border border_of(int n, int above, double mass_above) {
     Border x = {-INFINITY, 0};
-    double all = masses;
+    double all = masses, held = masses;  // of what top-k leaves; of that and of all equals of its last one
     const Span span = span_of(n);
 #pragma unroll 1
     for (int by_mass = lim.k ? 0 : 1; by_mass < (lim.p < 1.f ? 2 : 1); ++by_mass) {
       const double goal = (double)lim.p * all;
-      const Last y = last_of(n, span, by_mass, lim.k, goal, above, mass_above);
+      const Last y = last_of(n, span, x.last, by_mass ? held : 1.0, by_mass, lim.k, goal, above, mass_above);
       if (!by_mass) {
         x = {y.logit, min(lim.k - y.above, y.equal)};
-        all = y.mass_above + x.left * mass(x.last);
+        if (!(lim.p < 1.f)) break;
+        // (`held` is at most 1 + equals / k times `all`, for the least of k masses is at most a k-th of them: in `all` the limit is
+        // known to (k + equals) 2^-62, 2^-37 at most)
+        double own = 0.0;
+        each_of(n, [&](float l) { own += l > x.last ? mass(l) : 0.0; });
+        ask.before(own, held);
+        all = held + x.left * mass(x.last);
+        held += y.equal * mass(x.last);
         continue;
       }
       const double room = ceil((goal - y.mass_above) / mass(y.logit));
