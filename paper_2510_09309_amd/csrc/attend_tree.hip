@@ -10,7 +10,7 @@
 //
 // What a row does not see must not reach it, be it infinite or NaN: a product of the matrix pipe would turn a probability of 0 times such
 // a value into NaN.  Tiles of the response are looked through for them, and one that has any takes the product key by key (`add_seen`).  Cached rows
-// are seen by all queries of their head, and a tile's places behind the last row hold that row again.
+// are seen by all queries of their head; a tile's places behind the last row hold that row again, as a key that is masked, and zeros as a value.
 //
 // Sums, maxima and outputs are fp32; probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product: fp32 operands have a
 // sixteenth of its rate.  The sum that divides them is of the unrounded ones.
@@ -278,6 +278,10 @@ __global__ __launch_bounds__((TreeCfg<T, D>::kThreads), (TreeCfg<T, D>::kWaves /
       wait_moves<C::kMoves>();
     } else {
       wait_moves<0>();
+    }
+    if (!kResp && left < kTile) {  // (places behind the last row: 0 times an infinite value would be NaN)
+      for (int at = left * C::kRowB + lane * 16; at < C::kTileB; at += 1024) *reinterpret_cast<u32x4*>(v_lds + at) = u32x4{};
+      lds_is_read();
     }
     if (plain) {
       if constexpr (!F32) {
@@ -645,6 +649,9 @@ __global__ __launch_bounds__(256, 2) void attend_tree_wide_kernel(const TreePara
       if constexpr (kMore) {
         if (t + 2 < tiles) bring_k(t + 2, kOdd);
         bring_v(t + 1, 1 - kOdd);
+      } else if (const int left = cached - t * kWideTile; left < kWideTile) {  // (places behind the last row: 0 times an infinite value would be NaN)
+        for (int at = left * C::kRowB + threadIdx.x * 16; at < C::kTileB; at += 256 * 16) *in_lds<u32x4>(lds0 + (2 + kOdd) * C::kTileB + at) = u32x4{};
+        arrive();
       }
       raise();
       u32x4 pf[4];
