@@ -262,7 +262,7 @@ typedef struct maskkv_rotary {
   int32_t width;    /* even, 2 .. head_dim */
   int32_t layout;   /* a maskkv_rotary_layout */
   double amplitude; /* 1, or what a scaling for long contexts asks for */
-  double freq[64];  /* radians a position, entries 0 .. width/2 - 1 */
+  double freq[64];  /* radians a position, entries 0 .. width/2 - 1; 2^31 times each of them is finite */
 } maskkv_rotary;
 
 /* How frequencies are scaled for contexts `factor` times as long as the `trained` one (with f_i = base^(-2i/width)):

@@ -163,6 +163,9 @@ int check_mx(const char* what, const char* name, const maskkv_mx_cache* c, int64
 
 constexpr int kMostTokens = 1 << 25;  // of a sequence, in maskkv_rotate (a launch has fewer than 2^32 threads along a dimension)
 
+// The angle of the farthest position has to be a number.
+bool is_frequency(double f) { return isfinite(f * 2147483648.0); }
+
 int check_rotary_shape(const char* what, int32_t width, int32_t most, int32_t layout) {
   if (width < 2 || width > most || (width & 1)) {
     set_error("%s: width %d must be even and in 2..%d", what, width, most);
@@ -791,7 +794,7 @@ int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_
       const double keep = fmin(fmax((turns - slow) / (fast - slow), 0.0), 1.0);
       f *= keep + (1.0 - keep) / factor;
     }
-    if (!isfinite(f)) {
+    if (!is_frequency(f)) {
       set_error("rotary_frequencies: base %g is beyond the range of frequencies", base);
       return MASKKV_EINVAL;
     }
@@ -830,9 +833,9 @@ int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const in
   }
   if (int e = check_rotary_shape("rotate", rotary->width, desc->d, rotary->layout)) return e;
   bool finite = isfinite((float)rotary->amplitude);
-  for (int i = 0; i < rotary->width / 2; ++i) finite = finite && isfinite(rotary->freq[i]);
+  for (int i = 0; i < rotary->width / 2; ++i) finite = finite && is_frequency(rotary->freq[i]);
   if (!finite) {
-    set_error("rotate: a frequency or the amplitude is not a finite number");
+    set_error("rotate: a frequency times 2^31 or the amplitude is not a finite number");
     return MASKKV_EINVAL;
   }
   if (n_tokens < 0 || n_tokens > kMostTokens) {
