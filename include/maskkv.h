@@ -422,7 +422,7 @@ int maskkv_attend_tree(const maskkv_desc* desc, const maskkv_tensor* Q_resp, con
                        const uint32_t* mask, float scale, const maskkv_tensor* O, float* lse, void* workspace,
                        size_t workspace_bytes, void* stream);
 
-/* What maskkv_sample draws from: DEVICE arrays with an entry a row, or NULL. */
+/* What maskkv_sample draws from: DEVICE arrays with an entry a row, 4-byte aligned (as token, prob and logprob), or NULL. */
 typedef struct maskkv_sampling {
   const float* temperature; /* NULL: 1 each */
   const int32_t* top_k;     /* NULL, or an entry of 0 or less: no limit */

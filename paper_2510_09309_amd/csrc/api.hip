@@ -759,6 +759,13 @@ int maskkv_sample(const void* logits, int64_t rows, int32_t vocab, int32_t dtype
     set_error("sample: logits must be aligned to an element");
     return MASKKV_EINVAL;
   }
+  // (an entry a row is read by scalar loads, which leave out the lowest bits of an address)
+  for (const void* p : {(const void*)sampling->temperature, (const void*)sampling->top_k, (const void*)sampling->top_p, (const void*)sampling->min_p,
+                        (const void*)sampling->uniform, (const void*)token, (const void*)prob, (const void*)logprob})
+    if ((uintptr_t)p & 3) {
+      set_error("sample: the arrays of an entry a row must be 4-byte aligned");
+      return MASKKV_EINVAL;
+    }
   if (int e = check_workspace("sample", workspace, workspace_bytes, sample_workspace_bytes(rows, vocab, dtype))) return e;
   return launch_sample(logits, rows, vocab, dtype, row_stride * eb, sampling, token, prob, logprob, workspace,
                        reinterpret_cast<hipStream_t>(stream));
@@ -854,8 +861,8 @@ int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const in
       return MASKKV_EINVAL;
     }
   if (n_tokens == 0) return MASKKV_OK;
-  if (!positions) {
-    set_error("rotate: positions is NULL");
+  if (!positions || ((uintptr_t)positions & 3)) {
+    set_error("rotate: positions is NULL or not 4-byte aligned");
     return MASKKV_EINVAL;
   }
   return launch_rotate(desc, rotary, positions, n_tokens, token_len, Q ? &q : nullptr, &qo, K ? &k : nullptr, &ko,
