@@ -811,8 +811,8 @@ int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_
   return MASKKV_OK;
 }
 
-// One of maskkv_rotate's inputs with its output: both views, or neither.
-static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const maskkv_tensor* out, const char* name, View* from, View* to) {
+// One of maskkv_rotate's inputs with its output, of so many heads and tokens: both views, or neither.
+static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const maskkv_tensor* out, const char* name, int heads, int n_tokens, View* from, View* to) {
   if (!in != !out) {
     set_error("rotate: only one of %s and %s_out is NULL", name, name);
     return MASKKV_EINVAL;
@@ -821,7 +821,8 @@ static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const 
   if (int e = make_view(desc, in, name, from)) return e;
   if (int e = make_view(desc, out, name, to)) return e;
   if (from->ptr != to->ptr) return MASKKV_OK;
-  bool same = from->stride_t == to->stride_t && from->stride_h == to->stride_h;
+  // (a stride that no element is behind says nothing)
+  bool same = (from->stride_t == to->stride_t || n_tokens <= 1) && (from->stride_h == to->stride_h || heads == 1);
   for (int b = 0; b < desc->B; ++b) same = same && from->boff[b] == to->boff[b];
   if (same) return MASKKV_OK;
   set_error("rotate: %s_out begins where %s does and is not the same view", name, name);
@@ -853,8 +854,8 @@ int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const in
     set_error("rotate: neither Q nor K is given");
     return MASKKV_EINVAL;
   }
-  if (int e = check_turned(desc, Q, Q_out, "Q", &q, &qo)) return e;
-  if (int e = check_turned(desc, K, K_out, "K", &k, &ko)) return e;
+  if (int e = check_turned(desc, Q, Q_out, "Q", desc->H * query_heads_per_kv(desc), n_tokens, &q, &qo)) return e;
+  if (int e = check_turned(desc, K, K_out, "K", desc->H, n_tokens, &k, &ko)) return e;
   for (int b = 0; token_len && b < desc->B; ++b)
     if (token_len[b] < 0 || token_len[b] > n_tokens) {
       set_error("rotate: token_len[%d] = %d outside 0..n_tokens = %d", b, token_len[b], n_tokens);

@@ -26,3 +26,16 @@ def test_frequencies_that_are_given_out_are_taken(mk):
         assert rotate(mk, rotary=r, lens=[0]) == 0
     with pytest.raises(mk.MaskKVError):
         mk.maskkv_rotary_frequencies(64, mk.ROTARY_HALVES, 1e-318)
+
+
+def test_a_view_of_one_token_or_one_head_is_itself_whatever_its_stride(mk):
+    """In place, a row a head: the stride between tokens that there are not says nothing, and likewise that between heads."""
+    def strides(h, t):
+        v = view(mk)
+        v.stride_h, v.stride_t = h, t
+        return v
+
+    assert rotate(mk, n=1, lens=[0], Q=strides(64, 64), Q_out=strides(64, 128)) == 0
+    assert rotate(mk, desc(mk, H=1), n=8, lens=[0], Q=strides(512, 64), Q_out=strides(4096, 64)) == 0
+    assert rotate(mk, n=2, lens=[0], Q=strides(64, 64), Q_out=strides(64, 128)) == 1 and "same view" in error(mk)
+    assert rotate(mk, desc(mk, q_per_kv=2, H=1), n=1, lens=[0], Q=strides(512, 64), Q_out=strides(4096, 64)) == 1 and "same view" in error(mk)
