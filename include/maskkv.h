@@ -291,7 +291,8 @@ int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_
  * Rotates the rows of queries, of keys, or of both in one launch.  For b < B and t < token_len[b]:
  *   Q_out[b,h,t,:] = Q[b,h,t,:] turned by the position positions[b*n_tokens + t],  h < H*g;  K_out from K likewise, h < H.
  * Q, Q_out: views [B, H*g, n_tokens, d]; K, K_out: views [B, H, n_tokens, d]; a pair of them may be NULL, an output may be its own
- * input (the same view: in place), and outputs share no element with another view of the call.  positions: DEVICE int32 [B, n_tokens],
+ * input (the same view: in place), and outputs share no element with another view of the call (one that shares some with its own input is refused
+ * where both have the same strides, or begin at the same row).  positions: DEVICE int32 [B, n_tokens],
  * any sign: rows turned by p and then by -p are (to rounding, with amplitude 1) what they were, so the rows of a cache can be moved to other
  * positions.  (A packed cache is a view of one sequence and one head.)  token_len: HOST int32 [B], 0 .. n_tokens, or NULL: n_tokens each; rows from token_len[b] on are left untouched.
  * 0 <= n_tokens <= 2^25.  Of the description B, H, d, dtype and q_per_kv count.  Angles are formed and reduced in 64 bits, sines and cosines and the

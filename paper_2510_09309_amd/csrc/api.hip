@@ -811,8 +811,38 @@ int maskkv_rotary_frequencies(int32_t width, int32_t layout, double base, int32_
   return MASKKV_OK;
 }
 
+// Whether rows of two views with the same strides share bytes: of all their heads, and of the first n[b] tokens of each sequence.
+static bool rows_meet(const maskkv_desc* desc, const View& x, const View& y, int heads, const int32_t* n) {
+  const int64_t row = (int64_t)desc->d * elem_bytes(desc), sh = x.stride_h, st = x.stride_t;
+  auto end = [&](int b) { return (heads - 1) * sh + (n[b] - 1) * st + row; };  // of a sequence's rows, from its first one's begin
+  int64_t lo[2] = {INT64_MAX, INT64_MAX}, hi[2] = {INT64_MIN, INT64_MIN};
+  for (int v = 0; v < 2; ++v)
+    for (int b = 0; b < desc->B; ++b) {
+      if (n[b] < 1) continue;
+      const int64_t at = (int64_t)(uintptr_t)(v ? y : x).ptr + (v ? y : x).boff[b];
+      lo[v] = at < lo[v] ? at : lo[v];
+      hi[v] = at + end(b) > hi[v] ? at + end(b) : hi[v];
+    }
+  if (lo[0] >= hi[1] || lo[1] >= hi[0]) return false;
+  for (int a = 0; a < desc->B; ++a)
+    for (int b = 0; b < desc->B; ++b) {
+      if (n[a] < 1 || n[b] < 1) continue;
+      const int64_t far = (int64_t)(uintptr_t)x.ptr + x.boff[a] - (int64_t)(uintptr_t)y.ptr - y.boff[b];
+      if (far >= end(b) || -far >= end(a)) continue;
+      for (int64_t dh = 1 - heads; dh < heads; ++dh) {  // (of two heads so far apart: the tokens whose rows begin nearest to each other)
+        const int64_t x0 = far + dh * sh, least = 1 - n[b], most = n[a] - 1;
+        int64_t dt = -x0 / st;
+        for (dt -= 1; dt * st + x0 <= -row; ++dt) {}
+        dt = dt < least ? least : dt;
+        if (dt <= most && x0 + dt * st > -row && x0 + dt * st < row) return true;
+      }
+    }
+  return false;
+}
+
 // One of maskkv_rotate's inputs with its output, of so many heads and tokens: both views, or neither.
-static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const maskkv_tensor* out, const char* name, int heads, int n_tokens, View* from, View* to) {
+static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const maskkv_tensor* out, const char* name, int heads, int n_tokens, const int32_t* token_len,
+                        View* from, View* to) {
   if (!in != !out) {
     set_error("rotate: only one of %s and %s_out is NULL", name, name);
     return MASKKV_EINVAL;
@@ -820,12 +850,18 @@ static int check_turned(const maskkv_desc* desc, const maskkv_tensor* in, const 
   if (!in) return MASKKV_OK;
   if (int e = make_view(desc, in, name, from)) return e;
   if (int e = make_view(desc, out, name, to)) return e;
-  if (from->ptr != to->ptr) return MASKKV_OK;
   // (a stride that no element is behind says nothing)
-  bool same = (from->stride_t == to->stride_t || n_tokens <= 1) && (from->stride_h == to->stride_h || heads == 1);
-  for (int b = 0; b < desc->B; ++b) same = same && from->boff[b] == to->boff[b];
-  if (same) return MASKKV_OK;
-  set_error("rotate: %s_out begins where %s does and is not the same view", name, name);
+  const bool strides = (from->stride_t == to->stride_t || n_tokens <= 1) && (from->stride_h == to->stride_h || heads == 1);
+  bool same = strides, begin = false;
+  int32_t n[MASKKV_MAX_BATCH];
+  for (int b = 0; b < desc->B; ++b) {
+    n[b] = token_len ? token_len[b] : n_tokens;
+    const bool there = from->ptr + from->boff[b] == to->ptr + to->boff[b];
+    same = same && there;
+    begin = begin || (there && n[b] > 0);
+  }
+  if (same || !(strides ? rows_meet(desc, *from, *to, heads, n) : begin)) return MASKKV_OK;
+  set_error("rotate: %s_out overlaps %s and is not the same view", name, name);
   return MASKKV_EINVAL;
 }
 
@@ -854,13 +890,13 @@ int maskkv_rotate(const maskkv_desc* desc, const maskkv_rotary* rotary, const in
     set_error("rotate: neither Q nor K is given");
     return MASKKV_EINVAL;
   }
-  if (int e = check_turned(desc, Q, Q_out, "Q", desc->H * query_heads_per_kv(desc), n_tokens, &q, &qo)) return e;
-  if (int e = check_turned(desc, K, K_out, "K", desc->H, n_tokens, &k, &ko)) return e;
   for (int b = 0; token_len && b < desc->B; ++b)
     if (token_len[b] < 0 || token_len[b] > n_tokens) {
       set_error("rotate: token_len[%d] = %d outside 0..n_tokens = %d", b, token_len[b], n_tokens);
       return MASKKV_EINVAL;
     }
+  if (int e = check_turned(desc, Q, Q_out, "Q", desc->H * query_heads_per_kv(desc), n_tokens, token_len, &q, &qo)) return e;
+  if (int e = check_turned(desc, K, K_out, "K", desc->H, n_tokens, token_len, &k, &ko)) return e;
   if (n_tokens == 0) return MASKKV_OK;
   if (!positions || ((uintptr_t)positions & 3)) {
     set_error("rotate: positions is NULL or not 4-byte aligned");

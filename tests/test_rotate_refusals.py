@@ -1,6 +1,8 @@
 """What maskkv_rotate and maskkv_rotary_frequencies refuse or take at the edges of their arguments (CPU: the pointers are fake, and no call has rows to turn)."""
+import ctypes as ct
 import math
 
+import numpy as np
 import pytest
 
 from tests.test_decode_refusals import F, desc, error, mk, rotate, view  # noqa: F401  (mk: a fixture)
@@ -37,5 +39,40 @@ def test_a_view_of_one_token_or_one_head_is_itself_whatever_its_stride(mk):
 
     assert rotate(mk, n=1, lens=[0], Q=strides(64, 64), Q_out=strides(64, 128)) == 0
     assert rotate(mk, desc(mk, H=1), n=8, lens=[0], Q=strides(512, 64), Q_out=strides(4096, 64)) == 0
-    assert rotate(mk, n=2, lens=[0], Q=strides(64, 64), Q_out=strides(64, 128)) == 1 and "same view" in error(mk)
-    assert rotate(mk, desc(mk, q_per_kv=2, H=1), n=1, lens=[0], Q=strides(512, 64), Q_out=strides(4096, 64)) == 1 and "same view" in error(mk)
+    assert rotate(mk, n=2, lens=[1], Q=strides(64, 64), Q_out=strides(64, 128)) == 1 and "same view" in error(mk)
+    assert rotate(mk, desc(mk, q_per_kv=2, H=1), n=1, lens=[1], Q=strides(512, 64), Q_out=strides(4096, 64)) == 1 and "same view" in error(mk)
+
+
+def views(mk, rng, B, base, sb, sh, st, lens):
+    v = mk._CTensor(base, sb, sh, st, None)
+    if rng.random() < 0.3:
+        v.seq_start = (ct.c_int32 * B)(*[int(x) for x in rng.integers(0, 12, B)])
+    return v
+
+
+def test_an_output_that_overlaps_its_input(mk):
+    """Random views of one buffer with the same strides, against the rows' bytes written out.  A call that is not refused fails to be launched here (there is no GPU)
+    or has no rows."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the pointers are fake: calls that are taken would run")
+    rng = np.random.default_rng(0)
+    refused = taken = 0
+    for _ in range(1500):
+        B, H, g, n = (int(rng.integers(1, hi)) for hi in (4, 4, 3, 8))
+        st = 64 * int(rng.integers(1, 5))
+        sh = int(rng.choice([64, 64 * n, st * n, st * 9, 8 * int(rng.integers(0, 40))]))
+        sb = int(rng.choice([sh * H * g, st * n, 64 * 100, 0]))
+        lens = [int(x) for x in rng.integers(0, n + 1, B)]
+        v, o = (views(mk, rng, B, 0x100000 + 16 * int(rng.integers(0, 1500)) * int(rng.random() < 0.8), sb, sh, st, lens) for _ in range(2))
+
+        def rows(t):
+            return {(t.ptr + 2 * (b * sb + h * sh + (i + (t.seq_start[b] if t.seq_start else 0)) * st)) // 16 + e
+                    for b in range(B) for h in range(H * g) for i in range(lens[b]) for e in range(8)}
+
+        start = lambda t: [t.ptr + 2 * (b * sb + (t.seq_start[b] if t.seq_start else 0) * st) for b in range(B)]
+        meet = start(v) != start(o) and bool(rows(v) & rows(o))
+        got = rotate(mk, desc(mk, B=B, H=H, q_per_kv=0 if g == 1 else g), n=n, lens=lens, Q=v, Q_out=o)
+        assert (got == 1) == meet, (B, H, g, n, st, sh, sb, lens, got, error(mk))
+        refused, taken = refused + meet, taken + (not meet)
+    assert refused > 200 and taken > 200
