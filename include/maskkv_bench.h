@@ -97,6 +97,15 @@ int maskkv_bench_score_split(const maskkv_desc* desc, int32_t* split);
  */
 int maskkv_bench_attend_mx_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan);
 
+/*
+ * How maskkv_attend_tree would deal out a description and capacity.  plan: HOST array of 6:
+ *   [0] query rows of a workgroup: 32 or 128, a kernel each; [1] workgroups of a unit; [2] tiles of keys (64 at 128 rows, else 32) of a unit,
+ *   or 0: a unit is a head; [3] units, at most; [4] 1: the partial results of a query row are joined by a workgroup of its own; [5] bytes of
+ *   workspace that the call needs.
+ * Enqueues nothing.  Errors are reported through maskkv_last_error() of libmaskkv.so.
+ */
+int maskkv_bench_attend_tree_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan);
+
 #ifdef __cplusplus
 }
 #endif

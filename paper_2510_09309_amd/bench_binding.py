@@ -13,7 +13,7 @@ from . import binding as _b
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MASKKV_BENCH_LIB_PATH", os.path.join(_HERE, "libmaskkv_bench.so"))
 SYMBOLS = ["maskkv_bench_last_error", "maskkv_bench_probe", "maskkv_bench_score_marked", "maskkv_bench_hold_sweep",
-           "maskkv_bench_score_plan", "maskkv_bench_score_split", "maskkv_bench_attend_mx_plan"]
+           "maskkv_bench_score_plan", "maskkv_bench_score_split", "maskkv_bench_attend_mx_plan", "maskkv_bench_attend_tree_plan"]
 
 
 def _load() -> ct.CDLL:
@@ -106,6 +106,22 @@ def maskkv_bench_attend_mx_plan(desc: "_b.Desc", capacity: int) -> AttendMxPlan:
     plan = (ct.c_int64 * 8)()
     _b._check(_lib.maskkv_bench_attend_mx_plan(ct.byref(desc.c()), ct.c_int64(capacity), plan), "maskkv_bench_attend_mx_plan")
     return AttendMxPlan(*plan)
+
+
+class AttendTreePlan(NamedTuple):
+    """How maskkv_attend_tree would deal out a description and capacity (see maskkv_bench.h)."""
+    tile_rows: int
+    qtiles: int
+    chunk: int
+    units: int
+    shared: int
+    needs: int
+
+
+def maskkv_bench_attend_tree_plan(desc: "_b.Desc", capacity: int) -> AttendTreePlan:
+    plan = (ct.c_int64 * 6)()
+    _b._check(_lib.maskkv_bench_attend_tree_plan(ct.byref(desc.c()), ct.c_int64(capacity), plan), "maskkv_bench_attend_tree_plan")
+    return AttendTreePlan(*plan)
 
 
 def raw_library() -> ct.CDLL:

@@ -252,6 +252,14 @@ int attend_mx_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendMxPlan
   return MASKKV_OK;
 }
 
+int attend_tree_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendTreePlan* plan) {
+  Lens lens;
+  if (int e = check_desc(desc, &lens)) return e;
+  if (int e = check_capacity("attend_tree", "capacity", capacity)) return e;
+  *plan = attend_tree_plan(desc, capacity);
+  return MASKKV_OK;
+}
+
 }  // namespace maskkv
 
 using namespace maskkv;

@@ -948,6 +948,8 @@ Deal deal_of(const maskkv_desc* d, int64_t capacity) {
   return best;
 }
 
+bool shared_rows(const Deal& x, int64_t BH) { return x.chunk && x.units > kSharedUnits * BH; }
+
 size_t pad256(size_t n) { return (n + 255) / 256 * 256; }
 
 size_t bytes_of(const maskkv_desc* d, int64_t units, int qtiles, int part_rows) {
@@ -981,7 +983,7 @@ int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
   hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), lds, stream, prm);
   if (int e = check_launch("attend_tree")) return e;
   if (!deal.chunk) return MASKKV_OK;
-  if (deal.units > (int64_t)kSharedUnits * prm.BH)
+  if (shared_rows(deal, prm.BH))
     hipLaunchKernelGGL((attend_tree_join_kernel<T, D, true>), dim3((unsigned)prm.n_q, (unsigned)prm.BH), dim3(kJoinGroups * D / 4), 0, stream, prm);
   else
     hipLaunchKernelGGL((attend_tree_join_kernel<T, D, false>), dim3((unsigned)(prm.n_q + kJoinGroups - 1) / kJoinGroups, (unsigned)prm.BH),
@@ -994,6 +996,11 @@ int launch_one(const TreeParams& prm, const Deal& deal, hipStream_t stream) {
 size_t attend_tree_needs(const maskkv_desc* d, int64_t capacity) {
   const Deal x = deal_of(d, capacity);
   return x.chunk ? bytes_of(d, x.units, x.qtiles, x.part_rows) : 0;
+}
+
+AttendTreePlan attend_tree_plan(const maskkv_desc* d, int64_t capacity) {
+  const Deal x = deal_of(d, capacity);
+  return {x.tile_rows, x.qtiles, x.chunk, x.units, shared_rows(x, (int64_t)d->B * d->H), attend_tree_needs(d, capacity)};
 }
 
 // (No unit is dealt out where no head has more tiles than the least of a unit.)

@@ -6,7 +6,8 @@
 //   maskkv_bench_hold_sweep    makes maskkv_score take its fallback.
 //   maskkv_bench_score_plan    how maskkv_score would score a description;
 //   maskkv_bench_score_split   whether it would deal out rows and keys of a short fp32 prompt;
-//   maskkv_bench_attend_mx_plan   how maskkv_attend_mx would deal a cache out.
+//   maskkv_bench_attend_mx_plan   how maskkv_attend_mx would deal a cache out;
+//   maskkv_bench_attend_tree_plan   how maskkv_attend_tree would.
 #include <stdio.h>
 
 #include "../kernels.hpp"
@@ -372,6 +373,14 @@ int maskkv_bench_attend_mx_plan(const maskkv_desc* desc, int64_t capacity, int64
   if (int e = attend_mx_plan_entry(desc, capacity, &p)) return e;
   const int64_t v[8] = {p.tile_rows, p.qtiles, p.chunk, p.units, p.ranked, p.shared, p.extras, p.cut};
   for (int i = 0; i < 8; ++i) plan[i] = v[i];
+  return MASKKV_OK;
+}
+
+int maskkv_bench_attend_tree_plan(const maskkv_desc* desc, int64_t capacity, int64_t* plan) {
+  AttendTreePlan p;
+  if (int e = attend_tree_plan_entry(desc, capacity, &p)) return e;
+  const int64_t v[6] = {p.tile_rows, p.qtiles, p.chunk, p.units, p.shared, (int64_t)p.needs};
+  for (int i = 0; i < 6; ++i) plan[i] = v[i];
   return MASKKV_OK;
 }
 

@@ -120,6 +120,15 @@ int launch_attend_mx(const maskkv_desc* d, const View& Q, const MxCache& cache, 
                      const View& V2, float scale, const View& O, float* lse, void* workspace, hipStream_t stream);
 
 // attend_tree.hip
+struct AttendTreePlan {
+  int tile_rows;  // query rows of a workgroup: 32 or 128, which of the kernels
+  int qtiles;     // workgroups of a unit
+  int chunk;      // tiles of a unit, or 0: a unit is a head
+  int64_t units;  // at most
+  bool shared;    // partial results of a row are joined by a whole workgroup
+  size_t needs;   // bytes of workspace
+};
+AttendTreePlan attend_tree_plan(const maskkv_desc* d, int64_t capacity);
 size_t attend_tree_workspace_bytes(const maskkv_desc* d, int64_t capacity);  // of this capacity and of all smaller ones
 size_t attend_tree_needs(const maskkv_desc* d, int64_t capacity);            // of this one
 int launch_attend_tree(const maskkv_desc* d, const View& Q, const void* Kc, const void* Vc, const int32_t* cu_budget, int64_t capacity,
@@ -167,5 +176,6 @@ int score_entry(const maskkv_desc* desc, const maskkv_tensor* Q_mask, const mask
 // The plan that it makes for a description, and whether it deals out rows and keys instead.
 int score_plan(const maskkv_desc* desc, SweepPlan* plan, RowsSplit* split);
 int attend_mx_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendMxPlan* plan);
+int attend_tree_plan_entry(const maskkv_desc* desc, int64_t capacity, AttendTreePlan* plan);
 
 }  // namespace maskkv
