@@ -271,7 +271,9 @@ typedef struct maskkv_rotary {
  *   BASE    the same with base * factor^(width / (width - 2)) for base (width 2: as PLAIN): the fastest pair keeps its frequency, the slowest is divided by factor
  *   BANDS   by how often a pair turns within the trained length, r = trained * f_i / (2 pi): f_i where r >= fast, f_i / factor where
  *           r <= slow, and between them f_i * (w + (1 - w) / factor) with w = (r - slow) / (fast - slow);
- *           amplitude 1 + 0.1 ln(factor), for queries and for keys. */
+ *           amplitude 1 + 0.1 ln(factor), for queries and for keys.
+ * (The bands' ramp goes over how often a pair turns, not over the pair's number, and always comes with its amplitude.  A model that was trained with another
+ * ramp, or with none but the frequencies, has its entries of maskkv_rotary set by the caller.) */
 typedef enum maskkv_rotary_scaling {
   MASKKV_ROTARY_PLAIN = 0,
   MASKKV_ROTARY_LINEAR = 1,
@@ -416,7 +418,8 @@ int maskkv_attend_tree_workspace_bytes(const maskkv_desc* desc, int64_t capacity
  * mask: DEVICE uint32 [B, n_resp, (n_resp + 31) / 32], the same for all heads; bits from n_resp on are not looked at.  What a row does not see has no
  * part in its result, be it infinite or NaN.  A row that sees nothing (no bit, and no cached row) gets O = 0 and lse = -infinity.
  * The keys of a head are dealt to several workgroups where its query rows are few: single tokens and small trees over long caches.
- * capacity <= MASKKV_MX_MAX_ROWS.  Everything else as in maskkv_attend.
+ * capacity <= MASKKV_MX_MAX_ROWS.  A call that would launch 2^32 threads or more is MASKKV_ESHAPE: none of up to 2^27 query rows (B*H*g*n_resp) does.
+ * Everything else as in maskkv_attend.
  */
 int maskkv_attend_tree(const maskkv_desc* desc, const maskkv_tensor* Q_resp, const void* Kc, const void* Vc,
                        const int32_t* cu_budget, int64_t capacity, const maskkv_tensor* K_resp, const maskkv_tensor* V_resp,
@@ -449,7 +452,8 @@ int maskkv_sample_workspace_bytes(int64_t rows, int32_t vocab, int32_t dtype, si
  * A temperature of 0 or less (or NaN) takes the first of the largest logits, prob 1.  A NaN logit counts as -infinity; where +infinity occurs, its tokens share
  * all mass evenly.  A row without a finite or infinite logit above -infinity has token -1, prob 0 and logprob -infinity.  A random number below 0 counts
  * as 0, one of 1 and more (or NaN) as the largest below 1; limits that are NaN are none.
- * logits: DEVICE [rows, vocab] in `dtype` (a maskkv_dtype), rows row_stride >= vocab elements apart, aligned to an element; vocab 1 .. 2^24; 0 <= rows <= 2^20.
+ * logits: DEVICE [rows, vocab] in `dtype` (a maskkv_dtype), rows row_stride >= vocab elements apart, aligned to an element; vocab 1 .. 2^24; 0 <= rows <= 2^20
+ * (and rows times the stretches of 4 KB that a row, beginning anywhere in 16 bytes, may take fewer than 2^26 - 4, else MASKKV_ESHAPE).
  * token: DEVICE int32 [rows]; prob, logprob: DEVICE float [rows], or NULL.  Masses are held in 64 bits and summed up in a fixed order (or as whole
  * numbers): equal calls give equal bits, and a token is the definition's unless the random number or a limit lies within 1e-10 of the mass of where
  * another one would be.  (The terms of logprob's sum are 32-bit exponentials where the logits are bf16; the sum has 64 bits.)
