@@ -4,7 +4,8 @@
 // A workgroup has eight waves (fp32 at head_dim 128: four) and serves 32 query rows of a head.  Logits are formed transposed (keys on the matrix instruction's row axis), so that a
 // lane owns one query, its word of the mask covers a tile of 32 response rows, and its probabilities are the B operand of
 // O^T = V^T P^T as they stand.  The waves take tiles of 32 keys in turn, each through LDS of its own and without a barrier: K and V come by direct
-// transfers, K of the next tile while this one's softmax runs, V of the next behind this one's product.  The waves are merged at the end.
+// transfers, K of the next tile while this one's softmax runs, V of the next behind this one's product.  (The compiler waits for the query's fragments in front of the
+// first product of every turn, not of the first one only, and so for all transfers: the logits of a tile wait for its V too.)  The waves are merged at the end.
 //
 // The keys of a head go to several workgroups where the launch would not fill the chip (`deal_of`), and a second kernel joins the partial results.
 //
@@ -15,10 +16,10 @@
 // Sums, maxima and outputs are fp32; probabilities are rounded to bf16, by at most 2^-8 of each, as the operand of the second product: fp32 operands have a
 // sixteenth of its rate.  The sum that divides them is of the unrounded ones.
 //
-// By latency and memory where few rows meet a long cache: 64 rows of 32 heads x 4096 (69 MB) 17.7 us, 3.9 TB/s, waves waiting 41 % of their cycles, and 4.0 for
-// the joining launch; 8 rows over 32 x 8192 (134 MB) 31 together.  By latency where there is little: 256 heads x 32 rows x 64 ... 1024 14.5 (54 MB), four
-// heads of 8 fp32 rows 7.0.  With many rows (the second kernel) by matrix and softmax phases: 4 heads of 336 rows x 30011 34.1 us, 690 TFLOP/s with
-// the padding to 384 rows, both pipes busy 40 % of the time; joining 7.4.
+// By latency (of that wait, too) and memory where few rows meet a long cache: 64 rows of 32 heads x 4096 (69 MB) 17.3 us, 4.0 TB/s, waves waiting 42 % of their
+// cycles, and 3.9 to 4.7 for the joining launch; 8 rows over 32 x 8192 (134 MB) 31 together.  By latency where there is little: 256 heads x 32 rows x 64 ... 1024
+// 14.8 (54 MB), four heads of 8 fp32 rows 6.8.  With many rows (the second kernel) by matrix and softmax phases: 4 heads of 336 rows x 30011 33.8 us, 700 TFLOP/s
+// with the padding to 384 rows, both pipes busy 40 % of the time; joining 7.4.
 // Eight waves a workgroup and one of these a compute unit, not two of four waves (both sides in their own best number of units): ragged batch 18.7 and 15.1 us, single token
 // of 7 heads x 30k rows 17.8 and 17.2, 64 rows over 4096 21.0 and 20.9.
 #include <cmath>

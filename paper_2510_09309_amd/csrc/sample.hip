@@ -14,9 +14,11 @@
 //
 // The one exception is the confidence of bf16 rows, whose terms are fp32 exponentials added up in 64 bits: nothing is drawn by them.
 //
-// Bound by the vector pipe where all masses are needed: 256 rows of 126464 (65 MB, 12.7 us at a copy's rate) 35.7 + 5.8 us, the pipe busy all of the
-// first kernel's time: a mass is 16 operations in 64 bits.  By latency where they are not: one row of 32001 with top-k and top-p 4.6 + 10.0 us.
-// By one compute unit in a nearly flat row with a top-p: 64 rows of 152064 with mixed limits 32 us a call where no row is, 94 to 117 where one is.
+// Bound by the vector pipe where all masses are needed: 256 rows of 126464 (65 MB, 12.7 us at a copy's rate) 36.0 + 5.7 us, the pipe busy all of the
+// first kernel's time with 34 instructions a logit: 17 for its mass (16 of them in 64 bits), the others for its term of the confidence, the largest logits and
+// what a logit is read with.  By latency where masses are not needed: one row of 32001 with top-k and top-p 4.5 + 10.4 us.
+// By one compute unit in a nearly flat row with a top-p: 64 rows of 152064 with mixed limits 33 us a call where no row is, 96 to 117 where one is; and in a row
+// that is searched whole, 64 of 152064 with a top-k of 50000 and a top-p 340.
 // (Such rows dealt to the whole chip by three launches more: 64 rows with mixed limits 129 -> 94 us and 64 rows with a top-p at temperature 1.4 120 -> 115, but
 // sharp ones 27.5 -> 32.5, 256 of 126464 48.8 -> 55.3, 100 of 50000 with a top-k 16.7 -> 22.5.)
 #include <type_traits>
