@@ -837,6 +837,12 @@ static bool rows_meet(const maskkv_desc* desc, const View& x, const View& y, int
       if (n[a] < 1 || n[b] < 1) continue;
       const int64_t far = (int64_t)(uintptr_t)x.ptr + x.boff[a] - (int64_t)(uintptr_t)y.ptr - y.boff[b];
       if (far >= end(b) || -far >= end(a)) continue;
+      // (a token's heads side by side with other rows, or each head with other heads: where the first rows lie tells)
+      auto apart = [&](int64_t period, int64_t bytes) {
+        const int64_t m = (far % period + period) % period;
+        return m >= bytes && m + bytes <= period;
+      };
+      if (apart(st, (heads - 1) * sh + row) || (sh > 0 && st % sh == 0 && apart(sh, row))) continue;
       for (int64_t dh = 1 - heads; dh < heads; ++dh) {  // (of two heads so far apart: the tokens whose rows begin nearest to each other)
         const int64_t x0 = far + dh * sh, least = 1 - n[b], most = n[a] - 1;
         int64_t dt = -x0 / st;

@@ -76,3 +76,32 @@ def test_an_output_that_overlaps_its_input(mk):
         assert (got == 1) == meet, (B, H, g, n, st, sh, sb, lens, got, error(mk))
         refused, taken = refused + meet, taken + (not meet)
     assert refused > 200 and taken > 200
+
+
+def test_views_that_take_turns_in_one_buffer(mk):
+    """Several views' heads of a token behind each other, and head by head in turn, as fused projections leave them: against the rows' bytes written out."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("the pointers are fake: calls that are taken would run")
+    rng = np.random.default_rng(1)
+    refused = taken = 0
+    for _ in range(1500):
+        B, H, n, parts = (int(rng.integers(1, hi)) for hi in (4, 5, 8, 4))
+        d = 64
+        st = d * H * parts + int(rng.choice([0, 8, 64]))
+        sh = d if rng.random() < 0.5 else d * parts
+        sb = st * n * int(rng.integers(0, 2)) + 8 * int(rng.integers(0, 3))
+        lens = [int(x) for x in rng.integers(0, n + 1, B)]
+        at = lambda: 0x100000 + 2 * int(rng.choice([d, H * d, 8])) * int(rng.integers(0, 2 * parts + 1)) + 2 * st * int(rng.integers(0, 3))
+        v, o = (views(mk, rng, B, at(), sb, sh, st, lens) for _ in range(2))
+
+        def rows(t):
+            return {(t.ptr + 2 * (b * sb + h * sh + (i + (t.seq_start[b] if t.seq_start else 0)) * st)) // 16 + e
+                    for b in range(B) for h in range(H) for i in range(lens[b]) for e in range(8)}
+
+        start = lambda t: [t.ptr + 2 * (b * sb + (t.seq_start[b] if t.seq_start else 0) * st) for b in range(B)]
+        meet = start(v) != start(o) and bool(rows(v) & rows(o))
+        got = rotate(mk, desc(mk, B=B, H=H), n=n, lens=lens, Q=v, Q_out=o)
+        assert (got == 1) == meet, (B, H, n, parts, st, sh, sb, lens, got, error(mk))
+        refused, taken = refused + meet, taken + (not meet)
+    assert refused > 200 and taken > 200
